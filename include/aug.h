@@ -20,6 +20,7 @@
  *   aug_attn_plan     host: validates a formed batch and writes the work list
  *   aug_plan_upload   pinned host -> device: the work list, on the launch stream
  *   aug_kv_append     device: the step's new K/V rows into their paged slots
+ *   aug_kv_read       device: rows of the paged cache back out, dequantised
  *   aug_attn_mixed    device: one launch of paged, causal, grouped-query
  *                     attention over every chunked-prefill row and decode row
  *                     of the batch (plus a merge launch for split prefill tiles)
@@ -57,7 +58,7 @@ typedef enum {
   AUG_ERR_HIP = -4           /* the HIP runtime reported an error */
 } aug_status;
 
-typedef enum { AUG_F32 = 0, AUG_BF16 = 1, AUG_FP8_E4M3FN = 2 } aug_dtype;
+typedef enum { AUG_F32 = 0, AUG_BF16 = 1, AUG_FP8_E4M3FN = 2, AUG_MXFP4 = 3 } aug_dtype;
 
 /* Request queues of Algorithm 1: running, swapped, waiting, paused. */
 typedef enum { AUG_WAITING = 0, AUG_RUNNING = 1, AUG_SWAPPED = 2, AUG_PAUSED = 3 } aug_state;
@@ -82,9 +83,20 @@ typedef enum { AUG_ORDER_THETA = 0, AUG_ORDER_FCFS = 1, AUG_ORDER_SSJF = 2 } aug
  *   h / (num_q_heads / num_kv_heads) (grouped-query attention).
  *   head_dim: 64 or 128.  block_size: 16 (tokens per KV block).
  *   Supported dtype sets (q, kv, out): (F32, F32, F32), (BF16, BF16, BF16),
- *   (BF16, FP8_E4M3FN, BF16).
+ *   (BF16, FP8_E4M3FN, BF16), (BF16, MXFP4, BF16); the last two with head_dim 128.
  *   softmax_scale: multiplies q.k before the softmax (typically 1/sqrt(head_dim));
- *   finite and > 0. */
+ *   finite and > 0.
+ *
+ * MXFP4 caches hold 4.25 bits per element: E2M1 codes (sign, then the index
+ * into 0, 0.5, 1, 1.5, 2, 3, 4, 6) in groups of 32 dims of one token, each with
+ * a power-of-two scale X as one byte X + 127 (the OCP microscaling format);
+ * value = code * 2^X. A pool is [num_pool_blocks][num_kv_heads * 1088] bytes,
+ * 16-byte aligned: of every block, first the codes of all heads, 1024 bytes
+ * each, then their scales, 64 bytes each. No k_scale and v_scale arrays.
+ *   K: codes [16 tokens][128 dims], scales [16 tokens][4 groups]
+ *   V: codes [4 token quads][16 octets of dims][4 tokens][8 dims],
+ *      scales [4 groups][16 tokens]
+ * The first of two codes in a byte is the low nibble. */
 typedef struct {
   int32_t num_q_heads;
   int32_t num_kv_heads;
@@ -156,7 +168,8 @@ typedef struct {
  * products on 16x16 bf16 MFMAs; every other shape runs on the vector ALUs.
  * AUTO takes MFMA for groups of eight and for groups of four over fp8 KV
  * (the vector ALUs cannot keep up with the KV stream there) and VALU
- * otherwise; four-head groups over bf16 KV run on MFMA only when asked for. */
+ * otherwise; four-head groups over bf16 KV run on MFMA only when asked for.
+ * Every group over MXFP4 KV runs on MFMA, and only there. */
 typedef enum { AUG_ROWS_AUTO = 0, AUG_ROWS_VALU = 1, AUG_ROWS_MFMA = 2 } aug_row_path;
 
 /* Arithmetic of the prefill tiles' products S = Q K^T and O = P V. BF16: Q,
@@ -209,7 +222,7 @@ aug_status aug_attn_plan(const aug_attn_shape* shape, const aug_batch_desc* batc
  * row items run on and the arithmetic of the prefill tiles (info->row_path
  * and info->tile_path record the resolved choices, which aug_attn_mixed
  * follows). Same image layout and errors, plus AUG_ERR_UNSUPPORTED for
- * AUG_ROWS_MFMA, AUG_TILES_FP8_QK or AUG_TILES_FP8 on a shape without that path and
+ * AUG_ROWS_MFMA, AUG_ROWS_VALU, AUG_TILES_FP8_QK or AUG_TILES_FP8 on a shape without that path and
  * AUG_ERR_INVALID for an unknown path or a non-zero reserved field. */
 aug_status aug_attn_plan_opts(const aug_attn_shape* shape, const aug_batch_desc* batch,
                               const aug_plan_options* opts, void* plan_host, size_t plan_cap,
@@ -248,7 +261,7 @@ aug_status aug_plan_upload(const void* host_src, void* dev_dst, size_t bytes, vo
  *              again; calls that overlap on one copy race
  *   q          [total_rows][num_q_heads][head_dim], q_dtype
  *   k_cache,   [num_pool_blocks][num_kv_heads][block_size][head_dim], kv_dtype
- *   v_cache
+ *   v_cache    (MXFP4: see aug_attn_shape)
  *   k_scale,   [num_pool_blocks][num_kv_heads] float32, dequantisation scale of
  *   v_scale    each fp8 block (value = code * scale); NULL unless kv is fp8
  *   block_ids  the block table (CSR payload of aug_batch_desc)
@@ -304,7 +317,7 @@ aug_status aug_attn_mixed_noalloc(const aug_attn_shape* shape, const aug_attn_pl
  * block_size], for every KV head. Device memory:
  *   plan_dev   the plan image of aug_attn_plan for this batch (read only)
  *   k_new,     [total_rows][num_kv_heads][head_dim]: float32 for f32 caches,
- *   v_new      bf16 for bf16 and fp8 caches; finite values
+ *   v_new      bf16 for every other; finite values
  *   k_cache, v_cache, k_scale, v_scale, block_ids  as for aug_attn_mixed;
  *              written in place
  * f32 and bf16 caches receive the rows unchanged. fp8 E4M3FN caches (one
@@ -315,6 +328,11 @@ aug_status aug_attn_mixed_noalloc(const aug_attn_shape* shape, const aug_attn_pl
  * re-encoded as enc(dec(code) * old / new); new tokens are enc(x / scale)
  * (0 if the scale is 0). enc rounds to nearest even and saturates at +-448;
  * products and quotients are single float32 operations in that order.
+ * MXFP4 caches: a token's group of 32 dims with largest magnitude a in
+ * [1.75 * 2^(E-1), 1.75 * 2^E) gets X = E - 2, at least -125 and at most 125
+ * (a = 0: -125), and its codes are x / 2^X rounded to the nearest level, ties
+ * to the even code, saturating at 6. Tokens are independent: nothing that the
+ * block held before changes.
  * A block id outside the pool is skipped. The blocks that receive tokens
  * must be distinct across the batch (aug_attn_plan checks this when it is
  * given the host block table); two requests appending into one block would
@@ -328,6 +346,25 @@ aug_status aug_kv_append(const aug_attn_shape* shape, const aug_attn_plan_info* 
                          void* v_cache, float* k_scale, float* v_scale, const int32_t* block_ids,
                          int32_t num_pool_blocks, void* stream);
 
+/* Read rows back: row i of k_out and v_out ([n][num_kv_heads][head_dim], float32
+ * for f32 caches, bf16 for every other) receives the K and V of the token in
+ * slot slots[i] % block_size of block slots[i] / block_size, for every KV head,
+ * in any order and any number of times. f32 and bf16 caches return their bits,
+ * MXFP4 caches their values, which bf16 holds exactly, fp8 caches code * scale
+ * rounded to bf16 (nearest even). These are the rows that aug_kv_append takes,
+ * so a request moves from one cache format to another through them. Rows of
+ * slots outside the pool (negative ones too) become zero; k_out and v_out must
+ * not overlap the cache. Device memory:
+ *   slots      int64 [n]
+ * and the caches as for aug_attn_mixed; outputs 16-byte aligned. Enqueued on
+ * `stream` as one kernel launch (none for n = 0); no allocation.
+ * Errors: AUG_ERR_INVALID (shape, NULL or misaligned pointers, n < 0, missing
+ * scales for fp8), AUG_ERR_UNSUPPORTED (dtype set; n * num_kv_heads of 2^31 and
+ * more), AUG_ERR_HIP (launch). */
+aug_status aug_kv_read(const aug_attn_shape* shape, const void* k_cache, const void* v_cache,
+                       const float* k_scale, const float* v_scale, const int64_t* slots, int64_t n,
+                       int32_t num_pool_blocks, void* k_out, void* v_out, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Park / resume (Swap policy: swap-out during an external call, swap-in     */
 /* when it returns; Appendix B, Algorithm 1 step (2))                         */
@@ -335,7 +372,7 @@ aug_status aug_kv_append(const aug_attn_shape* shape, const aug_attn_plan_info* 
 
 /* Bytes of one parked block record: K[block] then V[block]
  * (num_kv_heads * block_size * head_dim elements each, the pool's own bit
- * patterns), then, for fp8 caches, k_scale[block] and v_scale[block]
+ * patterns; MXFP4: num_kv_heads * 1088 bytes each), then, for fp8 caches, k_scale[block] and v_scale[block]
  * (num_kv_heads float32 each). Returns 0 for an invalid shape. */
 size_t aug_kv_record_bytes(const aug_attn_shape* shape);
 

@@ -16,8 +16,8 @@ the batch:
 The paged cache is first materialised into contiguous per-request K/V by
 walking the request's block table, then truncated to ctx_r tokens, so slots
 past the context never take part. Inputs are decoded exactly to float64 (fp8
-codes times their per-(block, KV head) float32 scale) and all arithmetic is
-float64.
+codes times their per-(block, KV head) float32 scale, 4-bit codes times their
+group's power of two) and all arithmetic is float64.
 """
 
 from __future__ import annotations
@@ -26,17 +26,20 @@ from typing import Iterable, Optional
 
 import numpy as np
 
-from .codecs import e4m3fn_bits_to_f64, e4m3fn_encode, storage_to_f64
+from .codecs import e4m3fn_bits_to_f64, e4m3fn_encode, mxfp4_blocks_to_f64, storage_to_f64
 
 BLOCK = 16
 
 
 def materialise_kv(cache: np.ndarray, scale: Optional[np.ndarray], kv_dtype: str,
-                   blocks: np.ndarray, ctx: int) -> np.ndarray:
+                   blocks: np.ndarray, ctx: int, is_v: bool = False) -> np.ndarray:
     """Contiguous [ctx, H_kv, D] float64 K or V of one request."""
     nblk = -(-ctx // BLOCK)
     blocks = np.asarray(blocks[:nblk], dtype=np.int64)
-    raw = storage_to_f64(cache[blocks], kv_dtype)            # [nblk, H_kv, 16, D]
+    if kv_dtype == "fp4":                                    # the only format whose K and V are laid out apart
+        raw = mxfp4_blocks_to_f64(cache[blocks], is_v)
+    else:
+        raw = storage_to_f64(cache[blocks], kv_dtype)        # [nblk, H_kv, 16, D]
     if kv_dtype == "fp8":
         raw = raw * scale[blocks].astype(np.float64)[:, :, None, None]
     h_kv, d = raw.shape[1], raw.shape[3]
@@ -61,6 +64,34 @@ def attend_request(q_rows: np.ndarray, k: np.ndarray, v: np.ndarray, num_q_heads
         p /= p.sum(axis=1, keepdims=True)
         out[:, h, :] = p @ v[:, g, :]
     return out
+
+
+def request_weights(q_rows: np.ndarray, k: np.ndarray, head: int, num_q_heads: int, num_kv_heads: int,
+                    softmax_scale: float, softcap: float = 0.0, slopes=None, first=None, end=None) -> np.ndarray:
+    """Attention weights [q, ctx] of one query head of one request with modified
+    scores. Row j at position i = ctx - q_len + j sees keys first[j] <= t <
+    end[j] (defaults 0 and i + 1):
+
+        s_t = scale <q, k_t>;  s_t = c tanh(s_t / c)  (softcap c > 0);
+        s_t = s_t - slopes[head] |i - t|;  softmax over the keys seen.
+
+    A row that sees no key has no weights (all zero)."""
+    q_len, ctx = q_rows.shape[0], k.shape[0]
+    pos = ctx - q_len + np.arange(q_len)
+    t = np.arange(ctx)
+    s = (q_rows[:, head, :] @ k[:, head // (num_q_heads // num_kv_heads), :].T) * softmax_scale
+    if softcap > 0:
+        s = softcap * np.tanh(s / softcap)
+    if slopes is not None:
+        s = s - float(slopes[head]) * np.abs(pos[:, None] - t[None, :])
+    lo = np.zeros(q_len, np.int64) if first is None else np.asarray(first)
+    hi = pos + 1 if end is None else np.asarray(end)
+    seen = (t[None, :] >= lo[:, None]) & (t[None, :] < hi[:, None])
+    s = np.where(seen, s, -np.inf)
+    top = s.max(axis=1, keepdims=True, initial=-np.inf)
+    p = np.exp(s - np.where(np.isfinite(top), top, 0.0))
+    total = p.sum(axis=1, keepdims=True)
+    return p / np.where(total > 0, total, 1.0)
 
 
 def round_query_rows_e4m3(q_rows: np.ndarray) -> np.ndarray:
@@ -103,7 +134,7 @@ def paged_attention(q, q_dtype, k_cache, v_cache, k_scale, v_scale, kv_dtype,
         ctx = int(ctx_len[r])
         blocks = block_ids[int(bt_start[r]):int(bt_start[r + 1])]
         k = materialise_kv(k_cache, k_scale, kv_dtype, blocks, ctx)
-        v = materialise_kv(v_cache, v_scale, kv_dtype, blocks, ctx)
+        v = materialise_kv(v_cache, v_scale, kv_dtype, blocks, ctx, is_v=True)
         q_rows = storage_to_f64(q[q0:q1], q_dtype)
         if fp8_chunk_queries and q1 - q0 > 1:
             q_rows = round_query_rows_e4m3(q_rows)

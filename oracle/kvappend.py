@@ -24,7 +24,11 @@ The paper fixes no cache format; the reading taken here:
       of the block is re-encoded: code <- enc((dec(code) * s_old) / s);
     - new tokens: code = enc(x / s), or 0 when s == 0;
     - the block's scale becomes s.
-  enc is round-to-nearest-even to E4M3FN saturating at +-448
+* MXFP4 caches: every token and KV head by itself, groups of 32 dims with a
+  power-of-two scale (``codecs.mxfp4_encode``), K and V in the layouts of
+  ``codecs.mxfp4_places``.
+
+  For fp8, enc is round-to-nearest-even to E4M3FN saturating at +-448
   (``codecs.e4m3fn_encode``); every product and quotient above is one IEEE
   float32 operation, in the order written.
 """
@@ -33,7 +37,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from .codecs import E4M3FN_TABLE, bf16_bits_to_f64, e4m3fn_encode
+from .codecs import CELL, E4M3FN_TABLE, bf16_bits_to_f64, e4m3fn_encode, mxfp4_encode, mxfp4_places
 
 BLOCK = 16
 FP8_MAX = np.float32(448.0)
@@ -78,6 +82,19 @@ def _append_fp8(cache, scale, new_bits, segs, bt_start, block_ids, h_kv):
             scale[b, h] = s
 
 
+def _append_fp4(cache, new_bits, segs, bt_start, block_ids, is_v):
+    h_kv = cache.shape[1] // CELL
+    for r, blk, row0, n, slot0 in segs:
+        b = int(block_ids[int(bt_start[r]) + blk])
+        for i in range(n):
+            codes, scales = mxfp4_encode(bf16_bits_to_f64(new_bits[row0 + i]))
+            for h in range(h_kv):
+                byte, nib, at = mxfp4_places(h_kv, h, slot0 + i, is_v)
+                cache[b, byte[0::2]] = codes[h, 0::2] | (codes[h, 1::2] << 4)
+                assert not nib[0::2].any() and nib[1::2].all() and (byte[0::2] == byte[1::2]).all()
+                cache[b, at] = scales[h]
+
+
 def append(k_cache, v_cache, k_scale, v_scale, kv_dtype, k_new, v_new, q_start, ctx_len, bt_start,
            block_ids):
     """Return copies of (k_cache, v_cache, k_scale, v_scale) after appending
@@ -87,6 +104,10 @@ def append(k_cache, v_cache, k_scale, v_scale, kv_dtype, k_new, v_new, q_start, 
     ks = None if k_scale is None else k_scale.copy()
     vs = None if v_scale is None else v_scale.copy()
     segs = append_segments(q_start, ctx_len, bt_start)
+    if kv_dtype == "fp4":
+        _append_fp4(k, np.asarray(k_new, np.uint16), segs, bt_start, block_ids, False)
+        _append_fp4(v, np.asarray(v_new, np.uint16), segs, bt_start, block_ids, True)
+        return k, v, ks, vs
     h_kv = k.shape[1]
     if kv_dtype == "fp8":
         _append_fp8(k, ks, np.asarray(k_new, np.uint16), segs, bt_start, block_ids, h_kv)

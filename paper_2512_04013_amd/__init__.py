@@ -28,18 +28,19 @@ LIB_PATH = os.path.join(_HERE, "libaug.so")
 _HOST_ONLY_LIB = os.environ.get("AUG_HOST_ONLY_LIB")
 
 AUG_OK, AUG_ERR_INVALID, AUG_ERR_UNSUPPORTED, AUG_ERR_NO_SPACE, AUG_ERR_HIP = 0, -1, -2, -3, -4
-AUG_F32, AUG_BF16, AUG_FP8_E4M3FN = 0, 1, 2
+AUG_F32, AUG_BF16, AUG_FP8_E4M3FN, AUG_MXFP4 = 0, 1, 2, 3
 AUG_WAITING, AUG_RUNNING, AUG_SWAPPED, AUG_PAUSED = 0, 1, 2, 3
 AUG_POL_NONE, AUG_PRESERVE, AUG_DISCARD, AUG_SWAP = 0, 1, 2, 3
 AUG_ROWS_AUTO, AUG_ROWS_VALU, AUG_ROWS_MFMA = 0, 1, 2
 AUG_TILES_AUTO, AUG_TILES_BF16, AUG_TILES_FP8_QK, AUG_TILES_FP8 = 0, 1, 2, 3
 
-DTYPE_CODES = {"f32": AUG_F32, "bf16": AUG_BF16, "fp8": AUG_FP8_E4M3FN}
+DTYPE_CODES = {"f32": AUG_F32, "bf16": AUG_BF16, "fp8": AUG_FP8_E4M3FN, "fp4": AUG_MXFP4}
+MXFP4_CELL_BYTES = 1088    # of one (block, KV head) of a 4-bit pool: uint8 [blocks][kv heads * 1088]
 
 EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_attn_plan_opts",
             "aug_attn_workspace_size",
             "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_noalloc",
-            "aug_kv_append", "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
+            "aug_kv_append", "aug_kv_read", "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
             "aug_status_string", "aug_last_error", "aug_abi_version"]
 
 
@@ -143,6 +144,7 @@ def lib():
                                          P, P, P, C.c_int32, P, P]
     L.aug_kv_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_attn_plan_info), P, P, P, P, P,
                                 P, P, P, C.c_int32, P]
+    L.aug_kv_read.argtypes = [C.POINTER(aug_attn_shape), P, P, P, P, P, C.c_int64, C.c_int32, P, P, P]
     L.aug_plan_upload.argtypes = [P, P, C.c_size_t, P]
     L.aug_kv_record_bytes.argtypes = [C.POINTER(aug_attn_shape)]
     L.aug_kv_record_bytes.restype = C.c_size_t
@@ -155,7 +157,7 @@ def lib():
     L.aug_request_arrive.argtypes = [P, C.c_int64, C.c_double, C.c_int32, C.c_int32, C.c_double, C.c_int32]
     L.aug_request_return.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_double, C.c_int32]
     for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
-              "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_park", "aug_kv_resume",
+              "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
               "aug_form_batch", "aug_request_arrive", "aug_request_return"):
         getattr(L, f).restype = C.c_int
     L.aug_status_string.argtypes = [C.c_int]
@@ -363,6 +365,15 @@ def aug_kv_append(shape: aug_attn_shape, info: aug_attn_plan_info, plan_dev, k_n
     _check(lib().aug_kv_append(C.byref(shape), C.byref(info), _ptr(plan_dev), _ptr(k_new), _ptr(v_new),
                                _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
                                _ptr(block_ids), int(num_pool_blocks), st), "aug_kv_append")
+
+
+def aug_kv_read(shape: aug_attn_shape, k_cache, v_cache, k_scale, v_scale, slots, n: int, num_pool_blocks: int,
+                k_out, v_out, stream=None):
+    """Enqueue the read of the rows in ``slots`` (int64: block * 16 + slot) of
+    the pool into ``k_out`` and ``v_out``, dequantised."""
+    st = _stream(stream, k_out, k_cache)
+    _check(lib().aug_kv_read(C.byref(shape), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                             _ptr(slots), int(n), int(num_pool_blocks), _ptr(k_out), _ptr(v_out), st), "aug_kv_read")
 
 
 # ---- park / resume -------------------------------------------------------------------

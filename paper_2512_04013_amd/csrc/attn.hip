@@ -74,7 +74,7 @@ constexpr float kRescaleSlack = 8.0f;
 constexpr int kThreads = 256;
 
 
-enum : int { KV_F32 = 0, KV_BF16 = 1, KV_FP8 = 2 };
+enum : int { KV_F32 = 0, KV_BF16 = 1, KV_FP8 = 2, KV_FP4 = 3 };
 
 struct AttnArgs {
   const WorkItem* items;
@@ -123,6 +123,20 @@ template <bool HI>
 __device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
+
+// Eight E2M1 codes (the low nibble of a byte first) times a power of two -> eight
+// bf16 values in order, exactly.
+__device__ __forceinline__ uint4 fp4x8_to_bf16x8(uint32_t w, float scale) {
+  uint4 o;
+  o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  return o;
+}
+
+// The power of two of byte k of a word of scale bytes (exponent + 127).
+__device__ __forceinline__ float fp4_scale(uint32_t w, int k) { return __uint_as_float(((w >> (8 * k)) & 0xFFu) << 23); }
 
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
@@ -892,9 +906,39 @@ template <> struct MfmaRowKv<KV_FP8> {
   }
 };
 
+template <> struct MfmaRowKv<KV_FP4> {
+  struct K { uint4 w; uint32_t s; };   // token l % 16, dims 32g .. + 31, and their scale byte
+  struct V { uint4 w; uint32_t s; };   // word t: token 4g + t, dims 8m .. + 7; byte t: its scale
+  static constexpr int EB = 0;         // not a whole number of bytes: cells, see load_block
+  __device__ static constexpr int k_dim(int s, int g) { return 32 * g + 8 * s; }
+  template <bool S>
+  __device__ static void load_k(const char* codes, const char* scales, int j, int g, K& k) {
+    k.w = load_kv<S, uint4>(codes + 64 * j + 16 * g);
+    k.s = *reinterpret_cast<const uint8_t*>(scales + 4 * j + g);
+  }
+  template <bool S>
+  __device__ static void load_v(const char* codes, const char* scales, int j, int g, V& v) {
+    v.w = load_kv<S, uint4>(codes + 256 * g + 16 * j);
+    v.s = *reinterpret_cast<const uint32_t*>(scales + 16 * (j >> 2) + 4 * g);
+  }
+  __device__ static uint4 k_operand(const K& k, int s) {
+    const uint32_t w[4] = {k.w.x, k.w.y, k.w.z, k.w.w};
+    return fp4x8_to_bf16x8(w[s], fp4_scale(k.s, 0));
+  }
+  __device__ static void zero_v(V& v, int t) {   // the scale byte too: 255 stands for NaN
+    (t == 0 ? v.w.x : t == 1 ? v.w.y : t == 2 ? v.w.z : v.w.w) = 0u;
+    v.s &= ~(0xFFu << (8 * t));
+  }
+  __device__ static void v_operands(const V& v, uint2 (&op)[8]) {
+    const MfmaRowKv<KV_BF16>::V b = {{fp4x8_to_bf16x8(v.w.x, fp4_scale(v.s, 0)), fp4x8_to_bf16x8(v.w.y, fp4_scale(v.s, 1)),
+                                      fp4x8_to_bf16x8(v.w.z, fp4_scale(v.s, 2)), fp4x8_to_bf16x8(v.w.w, fp4_scale(v.s, 3))}};
+    MfmaRowKv<KV_BF16>::v_operands(b, op);
+  }
+};
+
 template <int KVT, int OT, int NW, int G, bool STREAM>
 __device__ void row_item_mfma(const WorkItem& it, const AttnArgs& a, float* lds) {
-  static_assert(G == 8 || G == 4, "one 16-column MFMA holds the group's heads");
+  static_assert(G <= 8, "one 16-column MFMA holds the group's heads");
   constexpr int D = 128;
   constexpr bool FP8 = KVT == KV_FP8;
   constexpr bool REST = FP8 && G == 4;   // columns 4 .. 7: the rest of the probabilities
@@ -938,9 +982,17 @@ __device__ void row_item_mfma(const WorkItem& it, const AttnArgs& a, float* lds)
   struct Scales { float k, v; };
   auto load_block = [&](int bid, typename KV::K& k, typename KV::V& v, Scales& sc2) {
     if (static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks)) {
-      const int64_t base = (static_cast<int64_t>(bid) * a.hkv + kvh) * kHead;
-      KV::template load_k<STREAM>(kc + base + k_lane, k);
-      KV::template load_v<STREAM>(vc + base + v_lane, kRow, v);
+      if constexpr (KVT == KV_FP4) {
+        const int64_t block = static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
+        const int64_t codes = block + kvh * aug::kMxCodes, scales = block + a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
+        KV::template load_k<STREAM>(kc + codes, kc + scales, j, g, k);
+        KV::template load_v<STREAM>(vc + codes, vc + scales, j, g, v);
+        return;
+      } else {
+        const int64_t base = (static_cast<int64_t>(bid) * a.hkv + kvh) * kHead;
+        KV::template load_k<STREAM>(kc + base + k_lane, k);
+        KV::template load_v<STREAM>(vc + base + v_lane, kRow, v);
+      }
       if constexpr (FP8) {
         sc2.k = load_uniform(a.k_scale + static_cast<int64_t>(bid) * a.hkv + kvh);
         sc2.v = load_uniform(a.v_scale + static_cast<int64_t>(bid) * a.hkv + kvh);
@@ -1094,7 +1146,7 @@ struct TileLds {
   // bf16 keys and values, and fp8 keys that stay codes (fp8 score products),
   // come by direct loads, rows of D elements without padding (see tile_chunk);
   // other fp8 ones through registers, converted and padded. K, then V.
-  static constexpr bool DMA = KVT != KV_FP8;
+  static constexpr bool DMA = KVT == KV_BF16;
   static constexpr bool K8 = F8 >= 1;
   static_assert(!K8 || (KVT == KV_FP8 && D == 128), "fp8 score products need fp8 keys and head_dim 128");
   static constexpr int ROW = K8 ? D : D * 2;              // bytes of an unpadded row
@@ -1168,7 +1220,7 @@ template <int KVT, int D, int G, int OT, int F8>
 __device__ void tile_item(const WorkItem& it, const AttnArgs& a, unsigned char* smem) {
   using raw_t = uint2;                // eight codes, converted (exactly) to bf16 on the way into LDS
   using Codes = RowMath<KV_FP8, AUG_BF16>;
-  constexpr bool FP8 = KVT == KV_FP8;
+  constexpr bool FP8 = KVT == KV_FP8, FP4 = KVT == KV_FP4;
   using L = TileLds<KVT, D, F8>;
   constexpr bool DMA = L::DMA;        // bf16 K/V go straight to LDS
   // Without a request the score products over fp8 keys are bf16 too: the keys
@@ -1329,6 +1381,11 @@ __device__ void tile_item(const WorkItem& it, const AttnArgs& a, unsigned char* 
   // fp8 through registers (bf16 takes none of this): a thread stages KPT
   // consecutive keys of one block (KPT divides 16)
   raw_t kr[KPT], vr[KPT];
+  // 4-bit: a thread stages 32 dims of one key and four keys of eight dims of the
+  // values, 16 bytes of codes each, with their scale bytes
+  const int key4 = threadIdx.x / 4, grp4 = threadIdx.x % 4, quad4 = threadIdx.x / 16, oct4 = threadIdx.x % 16;
+  uint4 kw4, vw4;
+  uint32_t ks4 = 0, vs4 = 0;
   float sc_reg = 1.f;   // fp8: thread t < 8 carries scale t of the tile (k0..3, v0..3)
   float vsc_reg = 1.f;  // fp8 values: the V scale of the block this thread stages
   // KPT consecutive key rows (dims 8 tcx .. 8 tcx + 7) of `src`, zero where
@@ -1347,8 +1404,40 @@ __device__ void tile_item(const WorkItem& it, const AttnArgs& a, unsigned char* 
                                                   : raw_t{};
     return ok ? bid : -1;
   };
+  auto load_tile4 = [&](int k0, auto full_tag) {
+    constexpr bool FULL = decltype(full_tag)::value;
+    kw4 = vw4 = uint4{0, 0, 0, 0};
+    ks4 = vs4 = 0;
+    const auto block_of = [&](int tok) {
+      const int bid = FULL || tok < key_end ? ids[(tok >> 4) - blk_first] : -1;
+      return static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks) ? bid : -1;
+    };
+    const int64_t scales = static_cast<int64_t>(a.hkv) * aug::kMxCodes + kvh * aug::kMxScales;
+    const int ktok = k0 + key4, vtok = k0 + 4 * quad4;
+    if (const int bid = block_of(ktok); FULL || bid >= 0) {
+      const char* block = kc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
+      kw4 = *reinterpret_cast<const uint4*>(block + kvh * aug::kMxCodes + 64 * (ktok & 15) + 16 * grp4);
+      ks4 = *reinterpret_cast<const uint8_t*>(block + scales + 4 * (ktok & 15) + grp4);
+    }
+    if (const int bid = block_of(vtok); FULL || bid >= 0) {
+      const char* block = vc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
+      vw4 = *reinterpret_cast<const uint4*>(block + kvh * aug::kMxCodes + 64 * (vtok & 15) + 16 * oct4);
+      vs4 = *reinterpret_cast<const uint32_t*>(block + scales + 16 * (oct4 >> 2) + (vtok & 15));
+      if constexpr (!FULL) {   // past the span: value and scale (255 stands for NaN) zero
+        const int n = key_end - vtok;
+        if (n < 4) vw4.w = 0u;
+        if (n < 3) vw4.z = 0u;
+        if (n < 2) vw4.y = 0u;
+        vs4 = n < 4 ? vs4 & ((1u << (8 * n)) - 1u) : vs4;
+      }
+    }
+  };
   auto load_tile = [&](int k0, auto full_tag) {
     constexpr bool FULL = decltype(full_tag)::value;
+    if constexpr (FP4) {
+      load_tile4(k0, full_tag);
+      return;
+    }
     const int tok0 = k0 + tk * KPT;
     const int slot = (tok0 >> 4) - blk_first;
     if constexpr (QK8) {
@@ -1391,6 +1480,15 @@ __device__ void tile_item(const WorkItem& it, const AttnArgs& a, unsigned char* 
   auto store_tile = [&](int stage) {
     uint16_t* ks = reinterpret_cast<uint16_t*>(smem + stage * L::STAGE);
     uint16_t* vs = ks + L::KBYTES / 2;
+    if constexpr (FP4) {
+      const uint32_t kw[4] = {kw4.x, kw4.y, kw4.z, kw4.w}, vw[4] = {vw4.x, vw4.y, vw4.z, vw4.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        *reinterpret_cast<uint4*>(ks + key4 * L::KS + 32 * grp4 + 8 * u) = fp4x8_to_bf16x8(kw[u], fp4_scale(ks4, 0));
+        *reinterpret_cast<uint4*>(vs + (4 * quad4 + u) * L::VS + 8 * oct4) = fp4x8_to_bf16x8(vw[u], fp4_scale(vs4, u));
+      }
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < KPT; ++u) {
       if constexpr (!QK8) *reinterpret_cast<uint4*>(ks + (tk * KPT + u) * L::KS + 8 * tc) = Codes::prep(kr[u]);
@@ -1812,7 +1910,7 @@ constexpr int row_lds_bytes() { return NW * G * row_lds_stride(D) * 4; }
 // path (eight or four query heads per KV head, head_dim 128, bf16 or fp8 KV).
 template <int KVT, int D, int G, int QT>
 constexpr bool row_mfma_capable() {
-  return (G == 8 || G == 4) && D == 128 && (KVT == KV_BF16 || KVT == KV_FP8) && QT == AUG_BF16;
+  return KVT == KV_FP4 || ((G == 8 || G == 4) && D == 128 && (KVT == KV_BF16 || KVT == KV_FP8) && QT == AUG_BF16);
 }
 
 // The workgroup's item through scalar loads (the address is the same for all
@@ -1930,7 +2028,7 @@ __global__ __launch_bounds__(kThreads) void tile_merge_kernel(AttnArgs a) {
 template <int KVT, int D, int G, int QT, int OT, bool ROW_MFMA>
 aug_status launch_rows(const AttnArgs& a, const aug_attn_plan_info& info, hipStream_t st) {
   if (info.num_prefill_items > 0) {
-    if constexpr ((KVT == KV_BF16 || KVT == KV_FP8) && QT == AUG_BF16) {
+    if constexpr (KVT != KV_F32) {
       if (info.tile_path == AUG_TILES_FP8_QK || info.tile_path == AUG_TILES_FP8) {
         if constexpr (KVT == KV_FP8 && D == 128) {
           if (info.tile_path == AUG_TILES_FP8)
@@ -1966,7 +2064,9 @@ template <int KVT, int D, int G, int QT, int OT>
 aug_status launch(const AttnArgs& a, const aug_attn_plan_info& info, hipStream_t st) {
   if (info.num_items > 0) {
     aug_status rs;
-    if constexpr (row_mfma_capable<KVT, D, G, QT>()) {
+    if constexpr (KVT == KV_FP4) {
+      rs = launch_rows<KVT, D, G, QT, OT, true>(a, info, st);   // the only row path
+    } else if constexpr (row_mfma_capable<KVT, D, G, QT>()) {
       rs = info.row_path == AUG_ROWS_VALU ? launch_rows<KVT, D, G, QT, OT, false>(a, info, st)
                                           : launch_rows<KVT, D, G, QT, OT, true>(a, info, st);
     } else {
@@ -1989,7 +2089,7 @@ aug_status dispatch_dg(int d, int g, const AttnArgs& a, const aug_attn_plan_info
                        hipStream_t st) {
 #define AUG_CASE(DD, GG) \
   if (d == DD && g == GG) return launch<KVT, DD, GG, QT, OT>(a, info, st);
-  if constexpr (KVT != KV_FP8) {
+  if constexpr (KVT != KV_FP8 && KVT != KV_FP4) {
     AUG_CASE(64, 1) AUG_CASE(64, 2) AUG_CASE(64, 4) AUG_CASE(64, 8)
   }
   AUG_CASE(128, 1) AUG_CASE(128, 2) AUG_CASE(128, 4) AUG_CASE(128, 8)
@@ -2008,6 +2108,8 @@ aug_status check_call(const char* who, const aug_attn_shape* s, const aug_attn_p
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   if (s->kv_dtype == AUG_FP8_E4M3FN && (!k_scale || !v_scale))
     return aug::fail(AUG_ERR_INVALID, "%s: fp8 KV needs k_scale and v_scale", who);
+  if (s->kv_dtype == AUG_MXFP4 && ((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 15))
+    return aug::fail(AUG_ERR_INVALID, "%s: MXFP4 pools must be 16-byte aligned", who);
   if (num_pool_blocks < 1) return aug::fail(AUG_ERR_INVALID, "%s: empty pool", who);
   return AUG_OK;
 }
@@ -2039,6 +2141,7 @@ aug_status enqueue(const aug_attn_shape* s, const aug_attn_plan_info* info, void
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (s->kv_dtype == AUG_F32) return dispatch_dg<KV_F32, AUG_F32, AUG_F32>(s->head_dim, g, a, *info, st);
   if (s->kv_dtype == AUG_BF16) return dispatch_dg<KV_BF16, AUG_BF16, AUG_BF16>(s->head_dim, g, a, *info, st);
+  if (s->kv_dtype == AUG_MXFP4) return dispatch_dg<KV_FP4, AUG_BF16, AUG_BF16>(s->head_dim, g, a, *info, st);
   return dispatch_dg<KV_FP8, AUG_BF16, AUG_BF16>(s->head_dim, g, a, *info, st);
 }
 

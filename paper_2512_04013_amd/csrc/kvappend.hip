@@ -10,7 +10,8 @@
 // consecutive slots of the block. For fp8 caches the wave also reduces the
 // rows' largest magnitude, derives the block's new scale from it and the old
 // one, re-encodes the block's earlier codes when the scale grows, and encodes
-// the new rows (round to nearest even, saturating at +-448).
+// the new rows (round to nearest even, saturating at +-448). In 4-bit caches
+// every 32 dims of a row have their own scale (append_fp4_kernel).
 //
 // HBM-bound and tiny next to attention: bytes per new token and KV head are
 // the input row (D * 2 or 4) plus the cache row (D * 1, 2 or 4), for K and V.
@@ -216,6 +217,51 @@ __global__ __launch_bounds__(kThreads) void append_fp8_kernel(AppendArgs a) {
   if (lane == 0) *scale = s;
 }
 
+// MXFP4 caches (head_dim 128): bf16 rows in, codes and a scale byte for every 32
+// dims out. A lane takes eight dims of a row, so a group of 32 is a quad of lanes:
+// its maximum is two quad permutations away. The scale is a power of two (from
+// the maximum's exponent field, one higher from 1.75 * 2^k on, where the largest
+// element would otherwise lose more than an eighth to saturation), so dividing
+// by it is exact and the only rounding is the conversion's, to nearest even.
+// Rows are independent: a block's earlier tokens are left alone.
+__global__ __launch_bounds__(kThreads) void append_fp4_kernel(AppendArgs a) {
+  constexpr int D = 128;
+  constexpr int LPR = D / 8, RPP = 64 / LPR;
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= static_cast<int64_t>(a.num_items) * a.hkv * 2) return;
+  const AppendItem it = load_item(a.items, unit / (2 * a.hkv));
+  const int kvh = static_cast<int>((unit >> 1) % a.hkv);
+  const bool is_v = unit & 1;
+  const int32_t bid = a.block_ids[it.bt_index];
+  if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) return;
+  const uint16_t* src = reinterpret_cast<const uint16_t*>(is_v ? a.v_new : a.k_new);
+  char* block = (is_v ? a.v_cache : a.k_cache) + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
+  char* codes = block + kvh * aug::kMxCodes;
+  char* scales = block + a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
+  const int oct = lane % LPR;
+  for (int r = lane / LPR; r < it.n_rows; r += RPP) {
+    const uint4 w = *reinterpret_cast<const uint4*>(src + ((static_cast<int64_t>(it.q_row0) + r) * a.hkv + kvh) * D + 8 * oct);
+    const float x[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y),
+                        bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+    amax = max_with<0x4E>(max_with<0xB1>(amax));       // over the quad: lanes ^ 1, ^ 2
+    const int field = static_cast<int>((__float_as_uint(amax) + (1u << 21)) >> 23);
+    const int byte = min(max(field - 2, 2), 252);
+    const float s = __uint_as_float(static_cast<uint32_t>(byte) << 23);
+    uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+    const int slot = it.slot0 + r, group = oct >> 2;
+    const int at = is_v ? 256 * (slot >> 2) + 16 * oct + 4 * (slot & 3) : 64 * slot + 4 * oct;
+    *reinterpret_cast<uint32_t*>(codes + at) = c;
+    if ((oct & 3) == 0) scales[is_v ? 16 * group + slot : 4 * slot + group] = static_cast<char>(byte);
+  }
+}
+
 }  // namespace
 
 extern "C" aug_status aug_kv_append(const aug_attn_shape* s, const aug_attn_plan_info* info,
@@ -231,6 +277,8 @@ extern "C" aug_status aug_kv_append(const aug_attn_shape* s, const aug_attn_plan
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   const bool fp8 = s->kv_dtype == AUG_FP8_E4M3FN;
   if (fp8 && (!k_scale || !v_scale)) return aug::fail(AUG_ERR_INVALID, "%s: fp8 cache without scales", who);
+  if (s->kv_dtype == AUG_MXFP4 && ((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 15))
+    return aug::fail(AUG_ERR_INVALID, "%s: MXFP4 pools must be 16-byte aligned", who);
   if (num_pool_blocks < 1) return aug::fail(AUG_ERR_INVALID, "%s: empty pool", who);
 
   AppendArgs a{};
@@ -251,6 +299,8 @@ extern "C" aug_status aug_kv_append(const aug_attn_shape* s, const aug_attn_plan
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (fp8) {
     hipLaunchKernelGGL(append_fp8_kernel, dim3(grid), dim3(kThreads), 0, st, a);
+  } else if (s->kv_dtype == AUG_MXFP4) {
+    hipLaunchKernelGGL(append_fp4_kernel, dim3(grid), dim3(kThreads), 0, st, a);
   } else if (s->kv_dtype == AUG_BF16) {
     if (s->head_dim == 64) hipLaunchKernelGGL((append_copy_kernel<2, 64>), dim3(grid), dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((append_copy_kernel<2, 128>), dim3(grid), dim3(kThreads), 0, st, a);

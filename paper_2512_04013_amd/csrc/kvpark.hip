@@ -3,7 +3,8 @@
 // Appendix B; the swapped queue of Algorithm 1, step (2)).
 //
 // One (block, all KV heads) of the pool is contiguous: K[block] is
-// num_kv_heads * 16 * head_dim elements, likewise V[block]. A parked record
+// num_kv_heads * 16 * head_dim elements (with their scales, in a 4-bit cache),
+// likewise V[block]. A parked record
 // is K[block] | V[block] | k_scale[block] | v_scale[block] (scales for fp8
 // caches only). Park gathers the listed blocks' records into a contiguous
 // device staging buffer with one kernel (16-byte loads and stores, four
@@ -23,6 +24,7 @@
 
 #include "aug.h"
 #include "checks.h"
+#include "plan_format.h"
 #include "status.h"
 
 namespace {
@@ -40,9 +42,8 @@ struct RecordGeom {
 };
 
 RecordGeom geom(const aug_attn_shape& s) {
-  const int64_t elem = s.kv_dtype == AUG_F32 ? 4 : s.kv_dtype == AUG_BF16 ? 2 : 1;
   RecordGeom g{};
-  g.kv_bytes = static_cast<int64_t>(s.num_kv_heads) * s.block_size * s.head_dim * elem;
+  g.kv_bytes = s.num_kv_heads * aug::cell_bytes(s.kv_dtype, s.head_dim);
   g.scale_bytes = s.kv_dtype == AUG_FP8_E4M3FN ? static_cast<int64_t>(s.num_kv_heads) * 4 : 0;
   g.rec_bytes = 2 * g.kv_bytes + 2 * g.scale_bytes;
   return g;

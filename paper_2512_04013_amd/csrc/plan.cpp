@@ -29,16 +29,20 @@ bool dtype_set_supported(const aug_attn_shape& s) {
   if (s.q_dtype == AUG_F32 && s.kv_dtype == AUG_F32 && s.out_dtype == AUG_F32) return true;
   if (s.q_dtype == AUG_BF16 && s.kv_dtype == AUG_BF16 && s.out_dtype == AUG_BF16) return true;
   if (s.q_dtype == AUG_BF16 && s.kv_dtype == AUG_FP8_E4M3FN && s.out_dtype == AUG_BF16) return true;
+  if (s.q_dtype == AUG_BF16 && s.kv_dtype == AUG_MXFP4 && s.out_dtype == AUG_BF16) return true;
   return false;
 }
 
 bool row_mfma_supported(const aug_attn_shape& s) {
+  if (s.kv_dtype == AUG_MXFP4) return true;
   return (s.num_q_heads == 8 * s.num_kv_heads || s.num_q_heads == 4 * s.num_kv_heads) && s.head_dim == 128 && s.q_dtype == AUG_BF16 &&
          (s.kv_dtype == AUG_BF16 || s.kv_dtype == AUG_FP8_E4M3FN);
 }
 
+bool row_valu_supported(const aug_attn_shape& s) { return s.kv_dtype != AUG_MXFP4; }
+
 bool tiles_supported(const aug_attn_shape& s) {
-  return s.q_dtype == AUG_BF16 && (s.kv_dtype == AUG_BF16 || s.kv_dtype == AUG_FP8_E4M3FN);
+  return s.q_dtype == AUG_BF16;
 }
 
 // fp8 score products on the tiles: fp8 keys (head_dim 128) and bf16 queries
@@ -65,6 +69,8 @@ aug_status check_shape(const aug_attn_shape* s, const char* who) {
                 s->kv_dtype, s->out_dtype);
   if (s->kv_dtype == AUG_FP8_E4M3FN && s->head_dim != 128)
     return fail(AUG_ERR_UNSUPPORTED, "%s: fp8 KV needs head_dim 128", who);
+  if (s->kv_dtype == AUG_MXFP4 && s->head_dim != 128)
+    return fail(AUG_ERR_UNSUPPORTED, "%s: MXFP4 KV needs head_dim 128", who);
   if (!std::isfinite(s->softmax_scale) || !(s->softmax_scale > 0.f))
     return fail(AUG_ERR_INVALID, "%s: softmax_scale must be finite and positive", who);
   return AUG_OK;
@@ -87,7 +93,7 @@ aug_status check_plan_info(const aug_attn_plan_info* info, const aug_attn_shape*
                 who, info->num_q_heads, info->num_kv_heads, info->head_dim, info->q_dtype, info->kv_dtype,
                 info->out_dtype, s->num_q_heads, s->num_kv_heads, s->head_dim, s->q_dtype, s->kv_dtype,
                 s->out_dtype);
-  if (info->row_path != AUG_ROWS_VALU && !(info->row_path == AUG_ROWS_MFMA && row_mfma_supported(*s)))
+  if (!(info->row_path == AUG_ROWS_VALU && row_valu_supported(*s)) && !(info->row_path == AUG_ROWS_MFMA && row_mfma_supported(*s)))
     return fail(AUG_ERR_INVALID, "%s: info names row path %d, which this shape cannot run", who, info->row_path);
   if (info->tile_path != AUG_TILES_BF16 &&
       !((info->tile_path == AUG_TILES_FP8_QK || info->tile_path == AUG_TILES_FP8) && tile_fp8qk_supported(*s)))
@@ -115,9 +121,7 @@ struct Sized {
 // figures were taken with K/V staged through registers. The row split below has
 // its own, from the direct loads: 4.5 us and 2.0 a step.)
 constexpr int kSlots = 512;
-double row_item_ns(int64_t keys, int32_t head_dim, int32_t kv_bytes) {
-  return static_cast<double>(keys) * head_dim * kv_bytes * 2 / 11.5;
-}
+double row_item_ns(int64_t keys, int64_t key_bytes) { return static_cast<double>(keys * key_bytes) / 11.5; }
 double tile_item_ns(int64_t key_tiles) { return 3000.0 + static_cast<double>(key_tiles) * 2600.0; }
 double merge_ns(int64_t partial_bytes) {
   return partial_bytes > 0 ? 5000.0 + static_cast<double>(partial_bytes) / 1500.0 : 0.0;
@@ -280,7 +284,7 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
   const int32_t waves = wide_rows ? 8 : 4;
   // bf16 rows in eight waves leave room for one workgroup a CU
   const int64_t slots = wide_rows && s.kv_dtype == AUG_BF16 ? kSlots / 2 : kSlots;
-  const int64_t block_bytes = int64_t{2} * kBlock * s.head_dim * (s.kv_dtype == AUG_F32 ? 4 : s.kv_dtype == AUG_BF16 ? 2 : 1);
+  const int64_t block_bytes = 2 * cell_bytes(s.kv_dtype, s.head_dim);
   const int64_t row_kv_bytes = row_kv_keys * block_bytes / kBlock;
   int64_t n_tiles = 0;
   for (const auto& t : tiles) n_tiles += t.second;
@@ -392,6 +396,8 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   if (row_path == AUG_ROWS_MFMA && !row_mfma_supported(*s))
     return fail(AUG_ERR_UNSUPPORTED, "%s: the MFMA row path needs 8 or 4 query heads per KV head, head_dim 128 "
                 "and bf16 or fp8 KV", who);
+  if (row_path == AUG_ROWS_VALU && !row_valu_supported(*s))
+    return fail(AUG_ERR_UNSUPPORTED, "%s: rows over MXFP4 KV run on the MFMA path only", who);
   // AUTO takes the MFMA rows where the vector ALUs cannot keep up with the KV
   // stream: groups of eight heads, and groups of four over fp8 KV (half the
   // bytes for the same arithmetic). Vector ALUs against MFMA for the latter, over
@@ -401,7 +407,7 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   // vector ALUs, which are at the HBM bound there (294 against 289 us for the
   // same 256 decodes), unless asked for.
   if (row_path == AUG_ROWS_AUTO)
-    row_path = row_mfma_supported(*s) && (s->num_q_heads == 8 * s->num_kv_heads || s->kv_dtype == AUG_FP8_E4M3FN)
+    row_path = row_mfma_supported(*s) && (s->num_q_heads == 8 * s->num_kv_heads || s->kv_dtype == AUG_FP8_E4M3FN || s->kv_dtype == AUG_MXFP4)
                    ? AUG_ROWS_MFMA : AUG_ROWS_VALU;
   int32_t tile_path = opts->tile_path;
   if (tile_path != AUG_TILES_AUTO && tile_path != AUG_TILES_BF16 && tile_path != AUG_TILES_FP8_QK &&
@@ -483,14 +489,12 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
       return fail(AUG_ERR_INVALID, "%s: block %d receives new tokens more than once", who, *dup);
   }
 
-  const int32_t kv_elem = s->kv_dtype == AUG_F32 ? 4 : s->kv_dtype == AUG_BF16 ? 2 : 1;
-  const int64_t key_bytes = int64_t{2} * s->head_dim * kv_elem;   // K and V of one key and KV head
+  const int64_t key_bytes = 2 * cell_bytes(s->kv_dtype, s->head_dim) / kBlock;   // K and V of one key and KV head
   const bool stream = streams_kv(*b, hkv, decode_keys, key_bytes);
   // a launch without tiles runs MFMA row items on eight-wave workgroups
   const bool wide_rows = !any_tiled && row_path == AUG_ROWS_MFMA;
   const int32_t split = choose_split(total_row_keys, kv_split_tokens, wide_rows, !any_tiled);
   const int32_t pos_per_tile = kTileRows / g;
-  const int32_t kv_bytes_all = s->kv_dtype == AUG_F32 ? 4 : s->kv_dtype == AUG_BF16 ? 2 : 1;
 
   // Keys per span of a split prefill tile. Splitting evens out the items but
   // costs a partial per row and span and their merge, so each candidate span
@@ -510,9 +514,9 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
       const int32_t nspan = (ctx + split - 1) / split;
       const int32_t span = (((ctx + nspan - 1) / nspan + kBlock - 1) / kBlock) * kBlock;
       const int32_t nsp = (ctx + span - 1) / span;
-      const double t = row_item_ns(std::min(span, ctx), s->head_dim, kv_bytes_all);
+      const double t = row_item_ns(std::min(span, ctx), key_bytes);
       row_longest = std::max(row_longest, t);
-      row_total += row_item_ns(ctx, s->head_dim, kv_bytes_all) * hkv;
+      row_total += row_item_ns(ctx, key_bytes) * hkv;
       if (nsp > 1) row_partial_bytes += static_cast<int64_t>(nsp) * hkv * partial_floats(g, s->head_dim) * 4;
     }
     double best = 0.0;
@@ -578,7 +582,6 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     int32_t r, span, nspan;
     double ns;      // estimated time of one of its items
   };
-  const int32_t kv_bytes = s->kv_dtype == AUG_F32 ? 4 : s->kv_dtype == AUG_BF16 ? 2 : 1;
   std::vector<RowReq> row_reqs;
   std::vector<Sized> tiles;
   std::vector<MergeGroup> tile_groups;
@@ -630,7 +633,7 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     // decodes have one row; rows of an untiled prefill get spans of their own length
     const int32_t keys = ctx;  // the longest row of the request
     const int32_t span = row_span(keys, row_split);
-    row_reqs.push_back({r, span, (keys + span - 1) / span, row_item_ns(span, s->head_dim, kv_bytes)});
+    row_reqs.push_back({r, span, (keys + span - 1) / span, row_item_ns(span, key_bytes)});
     for (int32_t j = 0; j < q; ++j) {
       const int32_t k = ctx - q + j + 1;
       const int64_t ns = (k + span - 1) / span;

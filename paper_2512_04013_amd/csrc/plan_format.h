@@ -4,11 +4,18 @@
 
 #include <cstdint>
 
+#include "aug.h"
+
 namespace aug {
 
 constexpr int32_t kPlanMagic = 0x4E4C5041;  // "APLN"
 constexpr int32_t kPlanVersion = 4;
 constexpr int32_t kBlock = 16;              // tokens per KV block
+// MXFP4 pools: bytes of one (block, KV head): 16 tokens x 128 dims of 4-bit
+// codes, then (after all heads' codes) a scale byte for every 32 dims of a token.
+// All heads' scales stand together behind their codes, so that the codes start on
+// whole 128-byte lines; the (block, head) is what one wave reads of a cache.
+constexpr int32_t kMxCodes = 1024, kMxScales = 64, kMxCell = kMxCodes + kMxScales;
 constexpr int32_t kKeyTile = 64;            // keys per MFMA tile (4 blocks)
 constexpr int32_t kTileRows = 128;          // query rows (positions x group heads) per MFMA tile
 constexpr int32_t kTileSpanMin = 256;       // a tile is never split into spans shorter than this
@@ -126,6 +133,12 @@ constexpr int64_t plan_image_bytes(int64_t num_items, int64_t num_groups, int64_
 // a multiple of 4 floats so every slot starts 16-byte aligned.
 constexpr int64_t partial_floats(int32_t group, int32_t head_dim) {
   return ((static_cast<int64_t>(group) * (head_dim + 2) + 3) / 4) * 4;
+}
+
+// Bytes of K (or V) of one (block, KV head).
+constexpr int64_t cell_bytes(int32_t kv_dtype, int32_t head_dim) {
+  return kv_dtype == AUG_MXFP4 ? kMxCell
+                               : int64_t{kBlock} * head_dim * (kv_dtype == AUG_F32 ? 4 : kv_dtype == AUG_BF16 ? 2 : 1);
 }
 
 }  // namespace aug

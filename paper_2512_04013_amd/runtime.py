@@ -12,17 +12,17 @@ import time
 import numpy as np
 import torch
 
-from . import (aug_attn_mixed, aug_attn_plan, aug_kv_append, aug_kv_park, aug_kv_record_bytes, aug_kv_resume,
-               aug_plan_upload, make_shape)
+from . import (AUG_MXFP4, MXFP4_CELL_BYTES, aug_attn_mixed, aug_attn_plan, aug_kv_append, aug_kv_park, aug_kv_read,
+               aug_kv_record_bytes, aug_kv_resume, aug_plan_upload, make_shape)
 
-_TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8}
+_TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8, "fp4": torch.uint8}
 
 
 def to_device_array(x: np.ndarray, dtype: str, device) -> torch.Tensor:
-    """Host bit patterns (float32 / uint16 bf16 / uint8 fp8) -> device tensor."""
+    """Host bit patterns (float32 / uint16 bf16 / uint8 fp8 and 4-bit pools) -> device tensor."""
     if dtype == "bf16":
         return torch.from_numpy(np.ascontiguousarray(x).view(np.int16)).view(torch.bfloat16).to(device)
-    if dtype == "fp8":
+    if dtype in ("fp8", "fp4"):
         return torch.from_numpy(np.ascontiguousarray(x, dtype=np.uint8)).to(device)
     return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(device)
 
@@ -39,6 +39,11 @@ class PagedKV:
         self.k_cache, self.v_cache = k_cache, v_cache
         self.k_scale, self.v_scale = k_scale, v_scale
         self.num_pool_blocks = int(k_cache.shape[0])
+        if shape.kv_dtype == AUG_MXFP4:
+            want = (self.num_pool_blocks, shape.num_kv_heads * MXFP4_CELL_BYTES)
+            for t in (k_cache, v_cache):
+                if tuple(t.shape) != want or t.dtype != torch.uint8:
+                    raise ValueError(f"a 4-bit pool is uint8 of shape {want}, got {t.dtype} {tuple(t.shape)}")
         self.record_bytes = aug_kv_record_bytes(shape)
         staging_bytes = max(self.record_bytes, (staging_bytes // self.record_bytes) * self.record_bytes)
         self.staging = torch.empty(staging_bytes, dtype=torch.uint8, device=k_cache.device)
@@ -55,6 +60,26 @@ class PagedKV:
         aug_kv_resume(self.shape, self.k_cache, self.v_cache, self.k_scale, self.v_scale, blocks_dev,
                       len(blocks_host), self.num_pool_blocks, host_src, self.staging,
                       block_ids_host=blocks_host, stream=stream)
+
+    def read(self, slots: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
+        """The K and V rows ([n][H_kv][D], float32 for f32 pools, else bf16) of
+        the tokens in ``slots`` (int64, block * 16 + slot): what ``append`` takes,
+        so a request moves to a pool of another format. Returns (k, v)."""
+        if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
+            raise ValueError(f"slots must be a contiguous int64 vector, got {slots.dtype} {tuple(slots.shape)}")
+        if slots.device != self.k_cache.device:
+            raise ValueError(f"slots on {slots.device}, the pool on {self.k_cache.device}")
+        want = (slots.numel(), self.shape.num_kv_heads, self.shape.head_dim)
+        dtype = torch.float32 if self.shape.kv_dtype == 0 else torch.bfloat16
+        k_out = torch.empty(want, dtype=dtype, device=slots.device) if k_out is None else k_out
+        v_out = torch.empty(want, dtype=dtype, device=slots.device) if v_out is None else v_out
+        for t in (k_out, v_out):
+            if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.device != slots.device:
+                raise ValueError(f"K/V rows must be contiguous {dtype} of shape {want} on {slots.device}, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
+        aug_kv_read(self.shape, self.k_cache, self.v_cache, self.k_scale, self.v_scale, slots, slots.numel(),
+                    self.num_pool_blocks, k_out, v_out, stream=stream)
+        return k_out, v_out
 
 
 class MixedAttention:

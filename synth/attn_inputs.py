@@ -4,7 +4,7 @@ Layout of every batch (one attention layer):
 
 * ``q``        [sum_q, H_q, D]            query rows of all requests, request after request
 * ``k_cache``  [n_blocks, H_kv, 16, D]    pool of 16-token blocks, head-major inside a block
-* ``v_cache``  same as ``k_cache``
+* ``v_cache``  same as ``k_cache``; 4-bit pools are [n_blocks, H_kv * 1088] bytes (codes, then scales)
 * ``k_scale``, ``v_scale`` [n_blocks, H_kv] float32, only for fp8 caches
 * ``q_start``  [R+1] int32  row offsets of each request into ``q``
 * ``ctx_len``  [R]   int32  keys of each request, counting this step's query tokens
@@ -62,7 +62,7 @@ class AttnBatch:
     num_kv_heads: int
     head_dim: int
     q_dtype: str          # "f32" | "bf16"
-    kv_dtype: str         # "f32" | "bf16" | "fp8"
+    kv_dtype: str         # "f32" | "bf16" | "fp8" | "fp4"
     out_dtype: str        # "f32" | "bf16"
     softmax_scale: float
     q: np.ndarray
@@ -132,12 +132,28 @@ def encode_e4m3fn_bits(y: np.ndarray) -> np.ndarray:
     return (code | (sign.astype(np.int64) << 7)).astype(np.uint8)
 
 
+def encode_mxfp4(x: np.ndarray):
+    """float32 rows [..., 128] -> E2M1 codes [..., 128] and scale bytes [..., 4]
+    (groups of 32 dims, scale 2^(byte - 127)), round to nearest even, saturating."""
+    g = np.asarray(x, dtype=np.float32).reshape(*x.shape[:-1], 4, 32)
+    a = np.abs(g).max(axis=-1)
+    byte = np.clip(((a.view(np.uint32) + np.uint32(1 << 21)) >> np.uint32(23)).astype(np.int64) - 2, 2, 252)
+    y = np.abs(np.ldexp(g, (127 - byte)[..., None].astype(np.int32)))
+    code = np.zeros(y.shape, np.uint8)
+    for i, mid in enumerate((0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)):
+        code += (y >= mid) if i % 2 else (y > mid)          # a midpoint goes to the even code
+    code |= np.signbit(g).astype(np.uint8) << 3
+    return code.reshape(x.shape), byte.astype(np.uint8)
+
+
 # ---------------------------------------------------------------------------
 # pool filling
 # ---------------------------------------------------------------------------
 
 def _empty_pool(n_blocks, h_kv, d, kv_dtype):
     shape = (n_blocks, h_kv, BLOCK, d)
+    if kv_dtype == "fp4":
+        return np.full((n_blocks, h_kv * 1088), 255, dtype=np.uint8)     # every scale NaN
     if kv_dtype == "f32":
         return np.full(shape, F32_NAN, dtype=np.float32)
     if kv_dtype == "bf16":
@@ -155,13 +171,30 @@ def _to_storage(x: np.ndarray, dtype: str) -> np.ndarray:
     raise ValueError(dtype)
 
 
-def _write_tokens(pool, scale, vals, blocks, ctx, kv_dtype):
+def _write_tokens(pool, scale, vals, blocks, ctx, kv_dtype, is_v=False):
     """Write ``vals`` [ctx, H_kv, D] (float32) into ``pool`` at ``blocks``; the
     slots past ``ctx`` in the last block keep their NaN poison."""
     nblk = -(-ctx // BLOCK)
     h_kv, d = vals.shape[1], vals.shape[2]
     blocks = np.asarray(blocks[:nblk], dtype=np.int64)
     full = ctx // BLOCK
+    if kv_dtype == "fp4":
+        code, byte = encode_mxfp4(vals)                          # [ctx, H_kv, 128], [ctx, H_kv, 4]
+        packed = code[..., 0::2] | (code[..., 1::2] << 4)
+        at = np.arange(ctx)
+        blk, t = at // BLOCK, at % BLOCK
+        codes = pool[blocks, :h_kv * 1024].reshape(nblk, h_kv, 1024)      # copies of these blocks
+        scales = pool[blocks, h_kv * 1024:].reshape(nblk, h_kv, 64)
+        for h in range(h_kv):
+            if is_v:
+                codes.reshape(-1, h_kv, 4, 16, 4, 4)[blk, h, t // 4, :, t % 4] = packed[:, h].reshape(ctx, 16, 4)
+                scales.reshape(-1, h_kv, 4, 16)[blk, h, :, t] = byte[:, h]
+            else:
+                codes.reshape(-1, h_kv, 16, 64)[blk, h, t] = packed[:, h]
+                scales.reshape(-1, h_kv, 16, 4)[blk, h, t] = byte[:, h]
+        pool[blocks, :h_kv * 1024] = codes.reshape(nblk, -1)
+        pool[blocks, h_kv * 1024:] = scales.reshape(nblk, -1)
+        return
     if kv_dtype == "fp8":
         pad = np.zeros((nblk * BLOCK, h_kv, d), dtype=np.float32)
         pad[:ctx] = vals
@@ -261,10 +294,10 @@ def make_batch_from_lengths(
     def fill(job):
         key, ctx, where = job
         g = np.random.default_rng([seed, 7, key])
-        for cache, scale in ((k_cache, k_scale), (v_cache, v_scale)):
+        for cache, scale, is_v in ((k_cache, k_scale, False), (v_cache, v_scale, True)):
             x = g.standard_normal((ctx, num_kv_heads, head_dim), dtype=np.float32)
             x *= kv_std32
-            _write_tokens(cache, scale, x, where, ctx, kv_dtype)
+            _write_tokens(cache, scale, x, where, ctx, kv_dtype, is_v)
 
     workers = min(16, os.cpu_count() or 1)
     if workers > 1 and len(jobs) > 1:
@@ -336,8 +369,19 @@ def poison_new_slots(batch: AttnBatch, copy: bool = True) -> AttnBatch:
     the step's K/V exist. Scales are left as they are."""
     out = dataclasses.replace(batch, k_cache=batch.k_cache.copy(), v_cache=batch.v_cache.copy()) \
         if copy else batch
-    nan = {"f32": F32_NAN, "bf16": BF16_NAN, "fp8": FP8_NAN}[batch.kv_dtype]
     q_len = batch.q_len
+    if batch.kv_dtype == "fp4":
+        h = batch.num_kv_heads
+        k_scales = out.k_cache[:, h * 1024:].reshape(-1, h, 16, 4)
+        v_scales = out.v_cache[:, h * 1024:].reshape(-1, h, 4, 16)
+        for r in range(batch.num_reqs):
+            p = np.arange(int(batch.ctx_len[r]) - int(q_len[r]), int(batch.ctx_len[r]))
+            k_scales[batch.blocks_of(r)[p // BLOCK], :, p % BLOCK] = 255
+            v_scales[batch.blocks_of(r)[p // BLOCK], :, :, p % BLOCK] = 255
+        out.k_cache[:, h * 1024:] = k_scales.reshape(-1, h * 64)
+        out.v_cache[:, h * 1024:] = v_scales.reshape(-1, h * 64)
+        return out
+    nan = {"f32": F32_NAN, "bf16": BF16_NAN, "fp8": FP8_NAN}[batch.kv_dtype]
     for r in range(batch.num_reqs):
         blocks = batch.blocks_of(r)
         for p in range(int(batch.ctx_len[r]) - int(q_len[r]), int(batch.ctx_len[r])):
