@@ -24,6 +24,9 @@
  *   aug_attn_mixed    device: one launch of paged, causal, grouped-query
  *                     attention over every chunked-prefill row and decode row
  *                     of the batch (plus a merge launch for split prefill tiles)
+ *   aug_attn_plan_masked, aug_attn_mixed_scored
+ *                     the same with a span of keys for every row, and with
+ *                     capped or distance-biased scores
  *   aug_kv_park       device -> pinned host: swap-out of KV blocks
  *   aug_kv_resume     pinned host -> device: swap-in into (new) KV blocks
  *
@@ -228,6 +231,30 @@ aug_status aug_attn_plan_opts(const aug_attn_shape* shape, const aug_batch_desc*
                               const aug_plan_options* opts, void* plan_host, size_t plan_cap,
                               aug_attn_plan_info* info);
 
+/* A span of keys for every row, in HOST memory: row i (of the batch's
+ * total_rows) sees keys row_first[i] <= t < row_end[i] of its request, whatever
+ * its position. NULL stands for 0 and for the row's position + 1, so both NULL is
+ * the causal mask. Spans make sliding windows (row_first), documents packed into
+ * one request (row_first at the start of the row's document), prefixes attended
+ * from both sides (row_end at least the prefix's length, whose keys must be in
+ * the cache by then) and any mixture of them; a row with row_end <= row_first
+ * sees nothing. 0 <= row_first, row_end <= ctx_len of the request. */
+typedef struct {
+  const int32_t* row_first;
+  const int32_t* row_end;
+} aug_row_mask;
+
+/* aug_attn_plan_opts with a mask (NULL: none, the same plan): the work list
+ * covers only keys that some row of an item sees, and the image ends with the
+ * spans (8 bytes a row). The plan is launched as any other, by aug_attn_mixed,
+ * aug_attn_mixed_noalloc or aug_attn_mixed_scored, and aug_kv_append takes it.
+ * Rows that see no key give zeros.
+ * Errors: those of aug_attn_plan_opts, AUG_ERR_INVALID for a span outside the
+ * row's context, AUG_ERR_UNSUPPORTED for a mask with fp8 tile products. */
+aug_status aug_attn_plan_masked(const aug_attn_shape* shape, const aug_batch_desc* batch,
+                                const aug_plan_options* opts, const aug_row_mask* mask, void* plan_host,
+                                size_t plan_cap, aug_attn_plan_info* info);
+
 /* Device workspace (split-K partials, in bytes) that aug_attn_mixed needs for
  * this batch with this split: the planner's size query, the same validation
  * as aug_attn_plan, nothing written but *bytes. The batch is the formed batch
@@ -281,6 +308,33 @@ aug_status aug_attn_mixed(const aug_attn_shape* shape, const aug_attn_plan_info*
                           const void* v_cache, const float* k_scale, const float* v_scale,
                           const int32_t* block_ids, int32_t num_pool_blocks, void* out,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Modified scores. With s = softmax_scale * q.k of query head h, position i and
+ * key t:
+ *   softcap > 0:   s = softcap * tanh(s / softcap); between AUG_SOFTCAP_MIN and
+ *                  AUG_SOFTCAP_MAX, since s is then off by softcap * 2^-20. 0: no cap
+ *   slopes:        s = s - slopes[h] * |i - t|, after the cap; device float32
+ *                  [num_q_heads], finite, read when the kernel runs. NULL: no bias
+ *   reserved       zero */
+#define AUG_SOFTCAP_MIN 0.0009765625f
+#define AUG_SOFTCAP_MAX 4096.0f
+typedef struct {
+  float softcap;
+  int32_t reserved;
+  const float* slopes;
+} aug_score_options;
+
+/* aug_attn_mixed with modified scores, for every cache format, with or without a
+ * mask in the plan. Without a cap, slopes and a mask it computes what aug_attn_mixed
+ * computes.
+ * Errors: those of aug_attn_mixed, AUG_ERR_INVALID for NULL options, a softcap
+ * outside its range or a non-zero reserved field, AUG_ERR_UNSUPPORTED for a plan
+ * with fp8 tile products. */
+aug_status aug_attn_mixed_scored(const aug_attn_shape* shape, const aug_attn_plan_info* info,
+                                 const aug_score_options* score, void* plan_dev, const void* q,
+                                 const void* k_cache, const void* v_cache, const float* k_scale,
+                                 const float* v_scale, const int32_t* block_ids, int32_t num_pool_blocks,
+                                 void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of the library's own device array for split-K partials, used by
  * aug_attn_mixed_noalloc (64 MiB per GPU the library runs on). */

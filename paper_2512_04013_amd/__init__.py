@@ -37,9 +37,9 @@ AUG_TILES_AUTO, AUG_TILES_BF16, AUG_TILES_FP8_QK, AUG_TILES_FP8 = 0, 1, 2, 3
 DTYPE_CODES = {"f32": AUG_F32, "bf16": AUG_BF16, "fp8": AUG_FP8_E4M3FN, "fp4": AUG_MXFP4}
 MXFP4_CELL_BYTES = 1088    # of one (block, KV head) of a 4-bit pool: uint8 [blocks][kv heads * 1088]
 
-EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_attn_plan_opts",
+EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked",
             "aug_attn_workspace_size",
-            "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_noalloc",
+            "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_scored", "aug_attn_mixed_noalloc",
             "aug_kv_append", "aug_kv_read", "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
             "aug_status_string", "aug_last_error", "aug_abi_version"]
 
@@ -78,6 +78,14 @@ class aug_attn_plan_info(C.Structure):
 class aug_plan_options(C.Structure):
     _fields_ = [("kv_split_tokens", C.c_int32), ("row_path", C.c_int32), ("tile_path", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class aug_row_mask(C.Structure):
+    _fields_ = [("row_first", C.c_void_p), ("row_end", C.c_void_p)]
+
+
+class aug_score_options(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("reserved", C.c_int32), ("slopes", C.c_void_p)]
 
 
 class aug_request(C.Structure):
@@ -136,6 +144,12 @@ def lib():
                                 C.c_size_t, C.POINTER(aug_attn_plan_info)]
     L.aug_attn_plan_opts.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_batch_desc),
                                      C.POINTER(aug_plan_options), P, C.c_size_t, C.POINTER(aug_attn_plan_info)]
+    L.aug_attn_plan_masked.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_batch_desc),
+                                       C.POINTER(aug_plan_options), C.POINTER(aug_row_mask), P, C.c_size_t,
+                                       C.POINTER(aug_attn_plan_info)]
+    L.aug_attn_mixed_scored.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_attn_plan_info),
+                                        C.POINTER(aug_score_options), P, P, P, P, P, P, P, C.c_int32, P, P,
+                                        C.c_size_t, P]
     L.aug_attn_workspace_size.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_batch_desc), C.c_int32,
                                           C.POINTER(C.c_size_t)]
     L.aug_attn_mixed.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_attn_plan_info), P, P, P, P,
@@ -156,8 +170,8 @@ def lib():
                                  C.POINTER(aug_batch_plan)]
     L.aug_request_arrive.argtypes = [P, C.c_int64, C.c_double, C.c_int32, C.c_int32, C.c_double, C.c_int32]
     L.aug_request_return.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_double, C.c_int32]
-    for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
-              "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
+    for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
+              "aug_attn_mixed_scored", "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
               "aug_form_batch", "aug_request_arrive", "aug_request_return"):
         getattr(L, f).restype = C.c_int
     L.aug_status_string.argtypes = [C.c_int]
@@ -280,11 +294,17 @@ def _batch_desc(q_start, ctx_len, bt_start, num_pool_blocks, block_ids=None):
 
 def aug_attn_plan(shape: aug_attn_shape, q_start, ctx_len, bt_start, num_pool_blocks: int,
                   block_ids=None, kv_split_tokens: int = 0, row_path: int = AUG_ROWS_AUTO,
-                  tile_path: int = AUG_TILES_AUTO):
+                  tile_path: int = AUG_TILES_AUTO, row_first=None, row_end=None):
     """Validate a batch (host arrays) and build its plan image (aug_attn_plan,
-    or aug_attn_plan_opts when a row or tile path is requested). Returns
+    or aug_attn_plan_opts when a row or tile path is requested, or
+    aug_attn_plan_masked when a span of keys is given for every row). Returns
     (info, plan) with plan a numpy uint8 array of info.plan_bytes bytes."""
     L = lib()
+    spans = [None if a is None else _i32(a) for a in (row_first, row_end)]
+    for a in spans:
+        if a is not None and a.shape != (int(q_start[-1]),):
+            raise ValueError(f"one span for each of {int(q_start[-1])} rows, got {a.shape}")
+    mask = aug_row_mask(*(None if a is None else a.ctypes.data for a in spans))
     desc, keep = _batch_desc(q_start, ctx_len, bt_start, num_pool_blocks, block_ids)
     info = aug_attn_plan_info()
     # one scratch image per thread: ctypes releases the GIL during the call
@@ -292,7 +312,11 @@ def aug_attn_plan(shape: aug_attn_shape, q_start, ctx_len, bt_start, num_pool_bl
     if buf is None:
         buf = _plan_scratch.buf = np.zeros(1 << 20, dtype=np.uint8)
     while True:
-        if row_path == AUG_ROWS_AUTO and tile_path == AUG_TILES_AUTO:
+        if row_first is not None or row_end is not None:
+            opts = aug_plan_options(int(kv_split_tokens), int(row_path), int(tile_path))
+            st = L.aug_attn_plan_masked(C.byref(shape), C.byref(desc), C.byref(opts), C.byref(mask), buf.ctypes.data,
+                                        buf.nbytes, C.byref(info))
+        elif row_path == AUG_ROWS_AUTO and tile_path == AUG_TILES_AUTO:
             st = L.aug_attn_plan(C.byref(shape), C.byref(desc), int(kv_split_tokens), buf.ctypes.data,
                                  buf.nbytes, C.byref(info))
         else:
@@ -332,12 +356,21 @@ def aug_plan_upload(host_src, dev_dst, nbytes: Optional[int] = None, stream=None
 
 def aug_attn_mixed(shape: aug_attn_shape, info: aug_attn_plan_info, plan_dev, q, k_cache, v_cache,
                    k_scale, v_scale, block_ids, num_pool_blocks: int, out, workspace,
-                   workspace_bytes: Optional[int] = None, stream=None):
+                   workspace_bytes: Optional[int] = None, stream=None, softcap: float = 0.0, slopes=None):
     """Enqueue the attention of a planned batch (all device arguments are torch
-    tensors or raw device addresses)."""
+    tensors or raw device addresses); with a softcap (tanh cap on the scores) or
+    slopes (float32 [num_q_heads], bias by distance) through
+    aug_attn_mixed_scored."""
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = _stream(stream, q, out)
+    if softcap or slopes is not None:
+        score = aug_score_options(float(softcap), 0, _ptr(slopes))
+        _check(lib().aug_attn_mixed_scored(C.byref(shape), C.byref(info), C.byref(score), _ptr(plan_dev), _ptr(q),
+                                           _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                           _ptr(block_ids), int(num_pool_blocks), _ptr(out), _ptr(workspace),
+                                           int(workspace_bytes), st), "aug_attn_mixed_scored")
+        return
     _check(lib().aug_attn_mixed(C.byref(shape), C.byref(info), _ptr(plan_dev), _ptr(q),
                                 _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
                                 _ptr(block_ids), int(num_pool_blocks), _ptr(out), _ptr(workspace),

@@ -82,7 +82,7 @@ aug_status check_plan_info(const aug_attn_plan_info* info, const aug_attn_shape*
       info->num_tile_merge_groups < 0 || info->num_tile_merge_groups > info->num_merge_groups ||
       info->num_append_items < 0 || info->num_prefill_items < 0 || info->num_prefill_items > info->num_items ||
       info->workspace_bytes < 0 ||
-      info->plan_bytes != plan_image_bytes(info->num_items, info->num_merge_groups, info->num_append_items))
+      info->total_rows < 0 || (info->plan_bytes != spans_offset(*info) && !plan_has_spans(*info)))
     return fail(AUG_ERR_INVALID, "%s: info is not consistent with a plan image", who);
   if (info->num_q_heads != s->num_q_heads || info->num_kv_heads != s->num_kv_heads ||
       info->head_dim != s->head_dim || info->q_dtype != s->q_dtype || info->kv_dtype != s->kv_dtype ||
@@ -192,12 +192,59 @@ double block_latency_ns(const aug_attn_shape& s, bool mfma, bool rows_only) {
 }
 double tile_step_ns(const aug_attn_shape& s) { return s.head_dim == 64 ? 1100 : 2000; }
 
+// The keys that a row sees.
+struct Keys {
+  int32_t lo, hi;
+  bool none() const { return hi <= lo; }
+  int32_t first_block() const { return none() ? 0 : lo / kBlock * kBlock; }   // where its row items start
+  int32_t count() const { return none() ? 0 : hi - first_block(); }          // keys that they read
+};
+
+// Row j of request r under the batch's mask, if it has one.
+struct RowKeys {
+  const aug_batch_desc& b;
+  const int32_t* first;
+  const int32_t* end;
+  bool masked() const { return first || end; }
+  Keys operator()(int32_t r, int32_t j) const {
+    const int32_t row = b.q_start[r] + j;
+    return {first ? first[row] : 0, end ? end[row] : b.ctx_len[r] - (b.q_start[r + 1] - b.q_start[r]) + j + 1};
+  }
+};
+
+// A prefill tile: rows j0 .. j0 + n - 1 of request r and the keys that they read,
+// from a whole key tile on; all of them see every key of [full_lo, full_hi).
+struct TileRows {
+  int32_t r, j0, n, lo, hi, full_lo, full_hi;
+};
+
+TileRows tile_rows(const RowKeys& keys, int32_t r, int32_t j0, int32_t n) {
+  if (!keys.masked()) {
+    const Keys last = keys(r, j0 + n - 1);
+    return {r, j0, n, 0, last.hi, 0, keys(r, j0).hi};
+  }
+  TileRows t{r, j0, n, INT32_MAX, 0, 0, INT32_MAX};
+  for (int32_t j = j0; j < j0 + n; ++j) {
+    const Keys k = keys(r, j);
+    if (k.none()) {
+      t.full_hi = 0;
+      continue;
+    }
+    t.lo = std::min(t.lo, k.lo);
+    t.hi = std::max(t.hi, k.hi);
+    t.full_lo = std::max(t.full_lo, k.lo);
+    t.full_hi = std::min(t.full_hi, k.hi);
+  }
+  t.lo = t.hi > 0 ? t.lo / kKeyTile * kKeyTile : 0;
+  return t;
+}
+
 // Whether the decodes' row items load their K/V past the caches: the launch
 // reads enough of it (kStreamBytes) and, where the block table tells, most of
 // it once. Rows of one chunk read the same keys and never stream. Requests share
 // whole prefixes, so one block in kSample tells (plans of 64 decodes over 96k
 // blocks take 71 us, 65 without this look and 133 with one at every block).
-bool streams_kv(const aug_batch_desc& b, int32_t hkv, int64_t decode_keys, int64_t key_bytes) {
+bool streams_kv(const aug_batch_desc& b, const RowKeys& keys, int32_t hkv, int64_t decode_keys, int64_t key_bytes) {
   if (decode_keys * key_bytes < kStreamBytes) return false;
   if (!b.block_ids) return true;
   std::vector<uint64_t> seen((static_cast<size_t>(b.num_pool_blocks) + 63) / 64);
@@ -206,7 +253,8 @@ bool streams_kv(const aug_batch_desc& b, int32_t hkv, int64_t decode_keys, int64
   for (int32_t r = 0; r < b.num_reqs; ++r) {
     if (b.q_start[r + 1] - b.q_start[r] != 1) continue;
     const int32_t* ids = b.block_ids + b.bt_start[r];
-    for (int32_t i = 0, n = (b.ctx_len[r] + kBlock - 1) / kBlock; i < n; i += kSample) {
+    const Keys k = keys(r, 0);
+    for (int32_t i = k.first_block() / kBlock, n = k.none() ? 0 : (k.hi + kBlock - 1) / kBlock; i < n; i += kSample) {
       uint64_t& word = seen[static_cast<uint32_t>(ids[i]) >> 6];
       const uint64_t bit = uint64_t{1} << (ids[i] & 63);
       again += (word & bit) != 0;
@@ -257,6 +305,7 @@ struct TileSpans {
 
 // Near-equal spans of whole key tiles for a tile item that reads `keys` keys.
 TileSpans tile_spans(int32_t keys, int32_t limit) {
+  if (keys == 0) return {kKeyTile, 1};   // no row sees a key: one item that writes zeros
   const int32_t n = (keys + limit - 1) / limit;
   const int32_t span = (((keys + n - 1) / n + kKeyTile - 1) / kKeyTile) * kKeyTile;
   return {span, (keys + span - 1) / span};
@@ -385,6 +434,12 @@ extern "C" aug_status aug_attn_plan(const aug_attn_shape* s, const aug_batch_des
 extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batch_desc* b,
                                          const aug_plan_options* opts, void* plan_host, size_t plan_cap,
                                          aug_attn_plan_info* info) {
+  return aug_attn_plan_masked(s, b, opts, nullptr, plan_host, plan_cap, info);
+}
+
+extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_batch_desc* b,
+                                           const aug_plan_options* opts, const aug_row_mask* mask, void* plan_host,
+                                           size_t plan_cap, aug_attn_plan_info* info) {
   const char* who = "aug_attn_plan";
   if (aug_status st = check_shape(s, who); st != AUG_OK) return st;
   if (!opts) return fail(AUG_ERR_INVALID, "%s: options are NULL", who);
@@ -415,6 +470,8 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     return fail(AUG_ERR_INVALID, "%s: unknown tile path %d", who, tile_path);
   if ((tile_path == AUG_TILES_FP8_QK || tile_path == AUG_TILES_FP8) && !tile_fp8qk_supported(*s))
     return fail(AUG_ERR_UNSUPPORTED, "%s: fp8 tile products need fp8 KV, bf16 queries and head_dim 128", who);
+  if (mask && tile_path != AUG_TILES_AUTO && tile_path != AUG_TILES_BF16)
+    return fail(AUG_ERR_UNSUPPORTED, "%s: a mask needs bf16 tile products", who);
   if (tile_path == AUG_TILES_AUTO) tile_path = AUG_TILES_BF16;   // fp8 tile products are opt-in
   if (!b || !info) return fail(AUG_ERR_INVALID, "%s: batch or info is NULL", who);
   const int32_t n = b->num_reqs;
@@ -427,6 +484,7 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   if (n > 0 && b->q_start[0] != 0) return fail(AUG_ERR_INVALID, "%s: q_start[0] != 0", who);
   const int32_t hkv = s->num_kv_heads;
   const int32_t g = s->num_q_heads / hkv;
+  const RowKeys keys{*b, mask ? mask->row_first : nullptr, mask ? mask->row_end : nullptr};
   int64_t total_row_keys = 0;   // keys that row items read, per KV head read once for each of a request's rows
   int64_t row_kv_keys = 0;      // the same, each request's K/V counted once
   int64_t decode_keys = 0;      // of that, the requests of one row
@@ -456,7 +514,23 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     }
     const bool tiled = q > 1 && tiles_supported(*s);
     any_tiled = any_tiled || tiled;
-    if (!tiled) {
+    if (keys.masked()) {
+      Keys all{INT32_MAX, 0};      // keys that some row of the request reads
+      int64_t sum = 0;
+      for (int32_t j = 0; j < q; ++j) {
+        const Keys k = keys(r, j);
+        if (k.lo < 0 || k.lo > ctx || k.hi < 0 || k.hi > ctx)
+          return fail(AUG_ERR_INVALID, "%s: row %d of request %d sees keys %d .. %d of %lld", who, j, r, k.lo, k.hi,
+                      (long long)ctx);
+        sum += k.count();
+        if (!k.none()) all = {std::min(all.lo, k.lo), std::max(all.hi, k.hi)};
+      }
+      if (!tiled) {
+        total_row_keys += sum * hkv;
+        row_kv_keys += static_cast<int64_t>(all.count()) * hkv;
+        if (q == 1) decode_keys += sum * hkv;
+      }
+    } else if (!tiled) {
       // rows at positions ctx-q .. ctx-1 read pos+1 keys each
       total_row_keys += (q * (2 * ctx - q + 1) / 2) * hkv;
       row_kv_keys += ctx * hkv;
@@ -490,7 +564,7 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   }
 
   const int64_t key_bytes = 2 * cell_bytes(s->kv_dtype, s->head_dim) / kBlock;   // K and V of one key and KV head
-  const bool stream = streams_kv(*b, hkv, decode_keys, key_bytes);
+  const bool stream = streams_kv(*b, keys, hkv, decode_keys, key_bytes);
   // a launch without tiles runs MFMA row items on eight-wave workgroups
   const bool wide_rows = !any_tiled && row_path == AUG_ROWS_MFMA;
   const int32_t split = choose_split(total_row_keys, kv_split_tokens, wide_rows, !any_tiled);
@@ -501,18 +575,24 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   // is priced as the makespan of the whole launch (row items included) plus
   // its merge, and the cheapest wins (ties: the longer span).
   int32_t tile_span = kTileSpanMax;
+  std::vector<TileRows> tile_list;
   int32_t longest_tile = 0;
-  for (int32_t r = 0; r < n && tiles_supported(*s); ++r)
-    if (b->q_start[r + 1] - b->q_start[r] > 1) longest_tile = std::max(longest_tile, b->ctx_len[r]);
+  for (int32_t r = 0; r < n && any_tiled; ++r) {
+    const int32_t q = b->q_start[r + 1] - b->q_start[r];
+    for (int32_t j0 = 0; q > 1 && j0 < q; j0 += pos_per_tile) {
+      tile_list.push_back(tile_rows(keys, r, j0, std::min(pos_per_tile, q - j0)));
+      longest_tile = std::max(longest_tile, tile_list.back().hi - tile_list.back().lo);
+    }
+  }
   if (longest_tile > kTileSpanMin) {
     double row_total = 0.0, row_longest = 0.0;
     int64_t row_partial_bytes = 0;
     for (int32_t r = 0; r < n; ++r) {
       const int32_t q = b->q_start[r + 1] - b->q_start[r];
       if (q > 1) continue;
-      const int32_t ctx = b->ctx_len[r];
-      const int32_t nspan = (ctx + split - 1) / split;
-      const int32_t span = (((ctx + nspan - 1) / nspan + kBlock - 1) / kBlock) * kBlock;
+      const int32_t ctx = keys(r, 0).count();
+      if (ctx == 0) continue;
+      const int32_t span = row_span(ctx, split);
       const int32_t nsp = (ctx + span - 1) / span;
       const double t = row_item_ns(std::min(span, ctx), key_bytes);
       row_longest = std::max(row_longest, t);
@@ -526,20 +606,12 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
       if (have && longest_tile / cand > 1024) continue;   // at most ~1k spans per tile row
       double total = row_total, longest = row_longest;
       int64_t partial_bytes = row_partial_bytes;
-      for (int32_t r = 0; r < n; ++r) {
-        const int32_t q = b->q_start[r + 1] - b->q_start[r];
-        if (q <= 1) continue;
-        const int32_t ctx = b->ctx_len[r];
-        for (int32_t j0 = 0; j0 < q; j0 += pos_per_tile) {
-          const int32_t nr = std::min(pos_per_tile, q - j0);
-          const int32_t key_end = ctx - q + j0 + nr;
-          const int32_t nsplit = (key_end + cand - 1) / cand;
-          const int32_t span = (((key_end + nsplit - 1) / nsplit + kKeyTile - 1) / kKeyTile) * kKeyTile;
-          const int32_t nsp = (key_end + span - 1) / span;
-          longest = std::max(longest, tile_item_ns((std::min(span, key_end) + kKeyTile - 1) / kKeyTile));
-          total += (tile_item_ns(0) * nsp + tile_item_ns((key_end + kKeyTile - 1) / kKeyTile) - tile_item_ns(0)) * hkv;
-          if (nsp > 1) partial_bytes += static_cast<int64_t>(nr) * nsp * hkv * partial_floats(g, s->head_dim) * 4;
-        }
+      for (const TileRows& t : tile_list) {
+        const int32_t count = t.hi - t.lo;
+        const auto [span, nsp] = tile_spans(count, cand);
+        longest = std::max(longest, tile_item_ns((std::min(span, count) + kKeyTile - 1) / kKeyTile));
+        total += (tile_item_ns(0) * nsp + tile_item_ns((count + kKeyTile - 1) / kKeyTile) - tile_item_ns(0)) * hkv;
+        if (nsp > 1) partial_bytes += static_cast<int64_t>(t.n) * nsp * hkv * partial_floats(g, s->head_dim) * 4;
       }
       const double cost = makespan_bound(longest, total) + merge_ns(partial_bytes);
       if (!have || cost < best) {
@@ -558,16 +630,18 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     for (int32_t r = 0; r < n; ++r) {
       const int32_t q = b->q_start[r + 1] - b->q_start[r];
       const int32_t ctx = b->ctx_len[r];
-      if (q == 1 || !tiles_supported(*s)) {
+      if (q > 1 && tiles_supported(*s)) continue;
+      if (!keys.masked()) {
         rows.push_back({q, ctx});
         continue;
       }
-      for (int32_t j0 = 0; j0 < q; j0 += pos_per_tile) {
-        const int32_t nr = std::min(pos_per_tile, q - j0);
-        const TileSpans ts = tile_spans(ctx - q + j0 + nr, tile_span);
-        steps[ts.span / kKeyTile] += static_cast<int64_t>(ts.count) * hkv;
-        if (ts.count > 1) tile_partials += static_cast<int64_t>(nr) * ts.count * hkv;
-      }
+      for (int32_t j = 0; j < q; ++j)
+        if (const int32_t count = keys(r, j).count(); count > 0) rows.push_back({1, count});
+    }
+    for (const TileRows& t : tile_list) {
+      const TileSpans ts = tile_spans(t.hi - t.lo, tile_span);
+      steps[ts.span / kKeyTile] += static_cast<int64_t>(ts.count) * hkv;
+      if (ts.count > 1) tile_partials += static_cast<int64_t>(t.n) * ts.count * hkv;
     }
     Durations tile_items;
     for (size_t i = 1; i < steps.size(); ++i)
@@ -579,7 +653,7 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   // Row items: a request's spans are equal (within one block), so ordering
   // requests by span length orders their items longest first.
   struct RowReq {
-    int32_t r, span, nspan;
+    int32_t r, span;
     double ns;      // estimated time of one of its items
   };
   std::vector<RowReq> row_reqs;
@@ -587,56 +661,58 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
   std::vector<MergeGroup> tile_groups;
   int64_t n_row_items = 0, n_groups = 0, tile_parts = 0, row_parts = 0;
   int64_t order = 0;
+  for (const TileRows& t : tile_list) {
+    // long tiles are split into near-equal spans of whole key tiles; each
+    // row of a split tile then has one partial per span, stored together
+    const auto [span, nsp] = tile_spans(t.hi - t.lo, tile_span);
+    static_assert(kTileSpanMax % kKeyTile == 0 && kTileSpanMin % kKeyTile == 0,
+                  "tile spans are whole key tiles");
+    // span <= tile_span <= kTileSpanMax, so the kernel's per-item block-id buffer suffices
+    for (int32_t h = 0; h < hkv; ++h) {
+      const int32_t g0 = static_cast<int32_t>(tile_groups.size());
+      for (int32_t sidx = 0; sidx < nsp; ++sidx) {
+        WorkItem it{};
+        it.kvh = static_cast<int16_t>(h);
+        it.kind = kTileItem;
+        it.q_row0 = b->q_start[t.r] + t.j0;
+        it.n_rows = static_cast<int16_t>(t.n);
+        it.part_stride = static_cast<int16_t>(nsp);
+        it.key_begin = t.lo + sidx * span;
+        it.key_end = std::min(t.hi, t.lo + (sidx + 1) * span);
+        it.pos0 = b->ctx_len[t.r] - (b->q_start[t.r + 1] - b->q_start[t.r]) + t.j0;
+        it.bt_off = b->bt_start[t.r];
+        it.part = nsp > 1 ? static_cast<int32_t>(tile_parts) + sidx : -1;
+        it.group = nsp > 1 ? g0 : -1;
+        if (keys.masked()) {
+          it.reserved[0] = t.full_lo;
+          it.reserved[1] = t.full_hi;
+        }
+        const int64_t steps = (it.key_end - it.key_begin + kKeyTile - 1) / kKeyTile;
+        tiles.push_back({it, tile_item_ns(steps), order++});
+      }
+      if (nsp > 1) {
+        for (int32_t j = 0; j < t.n; ++j)
+          tile_groups.push_back(MergeGroup{b->q_start[t.r] + t.j0 + j, h,
+                                           static_cast<int32_t>(tile_parts) + j * nsp, nsp});
+        tile_parts += static_cast<int64_t>(t.n) * nsp;
+        n_groups += t.n;
+      }
+    }
+  }
   for (int32_t r = 0; r < n; ++r) {
     const int32_t q = b->q_start[r + 1] - b->q_start[r];
-    const int32_t ctx = b->ctx_len[r];
-    if (q > 1 && tiles_supported(*s)) {
-      for (int32_t j0 = 0; j0 < q; j0 += pos_per_tile) {
-        const int32_t nr = std::min(pos_per_tile, q - j0);
-        const int32_t pos0 = ctx - q + j0;
-        const int32_t key_end = pos0 + nr;
-        // long tiles are split into near-equal spans of whole key tiles; each
-        // row of a split tile then has one partial per span, stored together
-        const auto [span, nsp] = tile_spans(key_end, tile_span);
-        static_assert(kTileSpanMax % kKeyTile == 0 && kTileSpanMin % kKeyTile == 0,
-                      "tile spans are whole key tiles");
-        // span <= tile_span <= kTileSpanMax, so the kernel's per-item block-id buffer suffices
-        for (int32_t h = 0; h < hkv; ++h) {
-          const int32_t g0 = static_cast<int32_t>(tile_groups.size());
-          for (int32_t sidx = 0; sidx < nsp; ++sidx) {
-            WorkItem it{};
-            it.kvh = static_cast<int16_t>(h);
-            it.kind = kTileItem;
-            it.q_row0 = b->q_start[r] + j0;
-            it.n_rows = static_cast<int16_t>(nr);
-            it.part_stride = static_cast<int16_t>(nsp);
-            it.key_begin = sidx * span;
-            it.key_end = std::min(key_end, (sidx + 1) * span);
-            it.pos0 = pos0;
-            it.bt_off = b->bt_start[r];
-            it.part = nsp > 1 ? static_cast<int32_t>(tile_parts) + sidx : -1;
-            it.group = nsp > 1 ? g0 : -1;
-            const int64_t steps = (it.key_end - it.key_begin + kKeyTile - 1) / kKeyTile;
-            tiles.push_back({it, tile_item_ns(steps), order++});
-          }
-          if (nsp > 1) {
-            for (int32_t j = 0; j < nr; ++j)
-              tile_groups.push_back(MergeGroup{b->q_start[r] + j0 + j, h,
-                                               static_cast<int32_t>(tile_parts) + j * nsp, nsp});
-            tile_parts += static_cast<int64_t>(nr) * nsp;
-            n_groups += nr;
-          }
-        }
-      }
-      continue;
-    }
+    if (q > 1 && tiles_supported(*s)) continue;
     // decodes have one row; rows of an untiled prefill get spans of their own length
-    const int32_t keys = ctx;  // the longest row of the request
-    const int32_t span = row_span(keys, row_split);
-    row_reqs.push_back({r, span, (keys + span - 1) / span, row_item_ns(span, key_bytes)});
+    int32_t most = b->ctx_len[r];  // keys of the request's longest row
+    if (keys.masked()) {
+      most = 1;
+      for (int32_t j = 0; j < q; ++j) most = std::max(most, keys(r, j).count());
+    }
+    const int32_t span = row_span(most, row_split);
+    row_reqs.push_back({r, span, row_item_ns(span, key_bytes)});
     for (int32_t j = 0; j < q; ++j) {
-      const int32_t k = ctx - q + j + 1;
-      const int64_t ns = (k + span - 1) / span;
+      const int32_t k = keys(r, j).count();
+      const int64_t ns = std::max(1, (k + span - 1) / span);   // a row without keys is one item, which writes zeros
       n_row_items += ns * hkv;
       if (ns > 1) {
         n_groups += hkv;
@@ -662,7 +738,8 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     return fail(AUG_ERR_UNSUPPORTED, "%s: %lld split-K partials", who, (long long)n_parts);
   const int64_t counters_off = groups_off + n_groups * static_cast<int64_t>(sizeof(MergeGroup));
   const int64_t append_off = append_offset(n_items, n_groups);
-  const int64_t plan_bytes = plan_image_bytes(n_items, n_groups, n_append);
+  const int64_t spans_off = plan_image_bytes(n_items, n_groups, n_append);
+  const int64_t plan_bytes = spans_off + (keys.masked() ? spans_bytes(total_rows) : 0);
   if (plan_bytes > INT32_MAX)
     return fail(AUG_ERR_UNSUPPORTED, "%s: plan image of %lld bytes", who, (long long)plan_bytes);
   const int64_t ws = ((n_parts * partial_floats(g, s->head_dim) * 4 + 255) / 256) * 256;
@@ -735,8 +812,9 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
     const int32_t ctx = b->ctx_len[r];
     for (int32_t j = 0; j < q; ++j) {
       const int32_t pos = ctx - q + j;
-      const int32_t keys = pos + 1;
-      const int32_t nspan = (keys + rr.span - 1) / rr.span;
+      const Keys row = keys(r, j);
+      const int32_t from = row.first_block(), until = row.none() ? 0 : row.hi;
+      const int32_t nspan = std::max(1, (row.count() + rr.span - 1) / rr.span);
       for (int32_t h = 0; h < hkv; ++h) {
         const int32_t part0 = nspan > 1 ? parts : -1;
         const int32_t group = nspan > 1 ? ng : -1;
@@ -751,8 +829,8 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
           it.q_row0 = b->q_start[r] + j;
           it.n_rows = 1;
           it.part_stride = 1;
-          it.key_begin = sidx * rr.span;
-          it.key_end = std::min(keys, (sidx + 1) * rr.span);
+          it.key_begin = from + sidx * rr.span;
+          it.key_end = std::min(until, from + (sidx + 1) * rr.span);
           it.pos0 = pos;
           it.bt_off = b->bt_start[r];
           it.part = nspan > 1 ? part0 + sidx : -1;
@@ -779,6 +857,16 @@ extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batc
                              static_cast<int16_t>(p % kBlock), b->bt_start[r] + blk, 0};
       p = end;
     }
+  }
+  if (keys.masked()) {
+    std::memset(base + spans_off, 0, static_cast<size_t>(plan_bytes - spans_off));
+    auto* spans = reinterpret_cast<int32_t*>(base + spans_off);
+    for (int32_t r = 0; r < n; ++r)
+      for (int32_t j = 0; j < b->q_start[r + 1] - b->q_start[r]; ++j) {
+        const Keys k = keys(r, j);
+        spans[2 * (b->q_start[r] + j)] = k.lo;
+        spans[2 * (b->q_start[r] + j) + 1] = k.hi;
+      }
   }
   return AUG_OK;
 }

@@ -91,6 +91,8 @@ struct WorkItem {            // 48 bytes
   // counter counts finished spans and its n_parts is the number of spans.
   // -1 when not split.
   int32_t group;
+  // plans with row spans, tiles: the last first key and the first end of the rows,
+  // between which every row sees every key
   int32_t reserved[3];
 };
 
@@ -126,6 +128,16 @@ constexpr int64_t append_offset(int64_t num_items, int64_t num_groups) {
 }
 constexpr int64_t plan_image_bytes(int64_t num_items, int64_t num_groups, int64_t num_append) {
   return append_offset(num_items, num_groups) + num_append * static_cast<int64_t>(sizeof(AppendItem));
+}
+
+// Plans with a mask go on with the key span (first, one past the last) of every
+// row, two int32 each, padded to 16 bytes; their size tells them from the others.
+constexpr int64_t spans_bytes(int64_t total_rows) { return (total_rows * 8 + 15) / 16 * 16; }
+inline int64_t spans_offset(const aug_attn_plan_info& i) {
+  return plan_image_bytes(i.num_items, i.num_merge_groups, i.num_append_items);
+}
+inline bool plan_has_spans(const aug_attn_plan_info& i) {
+  return i.total_rows > 0 && i.plan_bytes == spans_offset(i) + spans_bytes(i.total_rows);
 }
 
 // Split-K partial of one (row, KV head, key span): unnormalised o[G][D]

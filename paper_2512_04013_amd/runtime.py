@@ -88,13 +88,16 @@ class MixedAttention:
 
     def __init__(self, shape, kv: PagedKV, q_start, ctx_len, bt_start, block_ids_host,
                  block_ids_dev: torch.Tensor, kv_split_tokens: int = 0, check_blocks: bool = True,
-                 row_path: int = 0, tile_path: int = 0):
+                 row_path: int = 0, tile_path: int = 0, row_first=None, row_end=None):
+        """``row_first`` and ``row_end`` (host, one entry per query row): the
+        keys that each row sees instead of the causal ones (``row_spans`` makes
+        them)."""
         self.shape, self.kv = shape, kv
         device = kv.k_cache.device
         self.info, plan = aug_attn_plan(shape, q_start, ctx_len, bt_start, kv.num_pool_blocks,
                                         block_ids_host if check_blocks else None,
                                         kv_split_tokens=kv_split_tokens, row_path=row_path,
-                                        tile_path=tile_path)
+                                        tile_path=tile_path, row_first=row_first, row_end=row_end)
         # pinned staging kept alive with the batch; the library's copy kernel
         # moves it on the current stream of the cache's device
         self.plan_host = torch.from_numpy(plan.copy()).pin_memory()
@@ -111,15 +114,21 @@ class MixedAttention:
         self._new_dtype = torch.float32 if shape.kv_dtype == 0 else torch.bfloat16
 
     def run(self, q: torch.Tensor, stream=None, kv: "PagedKV" = None, block_ids: torch.Tensor = None,
-            out: torch.Tensor = None):
+            out: torch.Tensor = None, softcap: float = 0.0, slopes: torch.Tensor = None):
         """Enqueue the batch's attention. ``kv``, ``block_ids`` and ``out``
         default to the planned ones; another layer of the same batch passes its
-        own pool, block ids (same table shape) and output, and reuses the plan."""
+        own pool, block ids (same table shape) and output, and reuses the plan.
+        ``softcap``: scores become softcap * tanh(score / softcap); ``slopes``
+        (float32 [num_q_heads]): less slope * |position - key|."""
         kv = self.kv if kv is None else kv
         out = self.out if out is None else out
+        if slopes is not None and (slopes.shape != (self.shape.num_q_heads,) or slopes.dtype != torch.float32 or
+                                   slopes.device != q.device or not slopes.is_contiguous()):
+            raise ValueError(f"slopes must be contiguous float32 of shape ({self.shape.num_q_heads},) on {q.device}, got "
+                             f"{slopes.dtype} {tuple(slopes.shape)} on {slopes.device}")
         aug_attn_mixed(self.shape, self.info, self.plan_dev, q, kv.k_cache, kv.v_cache,
                        kv.k_scale, kv.v_scale, self.block_ids if block_ids is None else block_ids,
-                       kv.num_pool_blocks, out, self.workspace, stream=stream)
+                       kv.num_pool_blocks, out, self.workspace, stream=stream, softcap=softcap, slopes=slopes)
         return out
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, stream=None, kv: "PagedKV" = None,
@@ -135,6 +144,28 @@ class MixedAttention:
         aug_kv_append(self.shape, self.info, self.plan_dev, k_new, v_new, kv.k_cache,
                       kv.v_cache, kv.k_scale, kv.v_scale, self.block_ids if block_ids is None else block_ids,
                       kv.num_pool_blocks, stream=stream)
+
+
+def row_spans(q_start, ctx_len, window: int = 0, prefix_len=None, doc_start=None):
+    """(row_first, row_end) of a batch's query rows, which ``MixedAttention``
+    takes: causal, and
+
+    * ``window`` > 0: the row's own key and the window - 1 before it;
+    * ``prefix_len`` (per request): keys before it are seen by every row of the
+      request, later ones causally;
+    * ``doc_start`` (per row): no key before it, the first of the row's document.
+    """
+    q_start, ctx_len = np.asarray(q_start, np.int64), np.asarray(ctx_len, np.int64)
+    q_len = np.diff(q_start)
+    pos = np.arange(int(q_start[-1])) - np.repeat(q_start[:-1] - (ctx_len - q_len), q_len)
+    first, end = np.zeros_like(pos), pos + 1
+    if window > 0:
+        first = np.maximum(first, end - window)
+    if prefix_len is not None:
+        end = np.maximum(end, np.repeat(np.minimum(prefix_len, ctx_len), q_len))
+    if doc_start is not None:
+        first = np.maximum(first, np.asarray(doc_start, np.int64))
+    return first.astype(np.int32), end.astype(np.int32)
 
 
 def shape_of(batch) -> object:
