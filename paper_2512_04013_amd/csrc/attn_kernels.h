@@ -178,6 +178,40 @@ __device__ __forceinline__ uint4 fp4x8_to_bf16x8(uint32_t w, float scale) {
 // The power of two of byte k of a word of scale bytes (exponent + 127).
 __device__ __forceinline__ float fp4_scale(uint32_t w, int k) { return __uint_as_float(((w >> (8 * k)) & 0xFFu) << 23); }
 
+__device__ __forceinline__ void unpack_bf16x8(const uint4& w, float* f) {
+  f[0] = bf16_lo(w.x); f[1] = bf16_hi(w.x); f[2] = bf16_lo(w.y); f[3] = bf16_hi(w.y);
+  f[4] = bf16_lo(w.z); f[5] = bf16_hi(w.z); f[6] = bf16_lo(w.w); f[7] = bf16_hi(w.w);
+}
+
+// bf16 values of a vector with largest magnitude `amax` as sums of two E4M3 codes:
+// x * 2^(127 - byte) rounded to nearest (its largest magnitude falls in [128, 256)),
+// and the rest times 2^kRestLog2, so that the values are the first codes times
+// 2^(byte - 127) plus the second times 2^(byte - kRestLog2 - 127). A bf16 value has
+// 8 significant bits and a code 4: what the first rounds off has at most 4 bits
+// left, and the second holds it exactly for |x| of 2^-14 amax and more.
+struct TwoCodes {
+  static constexpr int kRestLog2 = 5;
+  int byte;
+  float down;
+  __device__ explicit TwoCodes(float amax)
+      : byte(max(static_cast<int>((__float_as_uint(amax) >> 23) & 0xFFu) - 7, 8)),
+        down(__uint_as_float(static_cast<uint32_t>(254 - byte) << 23)) {}
+  // four values -> the four first codes and the four second ones
+  __device__ __forceinline__ uint2 operator()(const float* x) const {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[e] * down;
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false);
+    const auto b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+    constexpr float up = static_cast<float>(1 << kRestLog2);
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a[0]) * up, (y[1] - a[1]) * up, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - b[0]) * up, (y[3] - b[1]) * up, r, true);
+    return uint2{static_cast<uint32_t>(c), static_cast<uint32_t>(r)};
+  }
+};
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
@@ -966,39 +1000,9 @@ template <> struct MfmaRowKv<KV_FP8> {
   }
 };
 
-template <> struct MfmaRowKv<KV_FP4> {
-  struct K { uint4 w; uint32_t s; };   // token l % 16, dims 32g .. + 31, and their scale byte
-  struct V { uint4 w; uint32_t s; };   // word t: token 4g + t, dims 8m .. + 7; byte t: its scale
-  static constexpr int EB = 0;         // not a whole number of bytes: cells, see load_block
-  __device__ static constexpr int k_dim(int s, int g) { return 32 * g + 8 * s; }
-  template <bool S>
-  __device__ static void load_k(const char* codes, const char* scales, int j, int g, K& k) {
-    k.w = load_kv<S, uint4>(codes + 64 * j + 16 * g);
-    k.s = *reinterpret_cast<const uint8_t*>(scales + 4 * j + g);
-  }
-  template <bool S>
-  __device__ static void load_v(const char* codes, const char* scales, int j, int g, V& v) {
-    v.w = load_kv<S, uint4>(codes + 256 * g + 16 * j);
-    v.s = *reinterpret_cast<const uint32_t*>(scales + 16 * (j >> 2) + 4 * g);
-  }
-  __device__ static uint4 k_operand(const K& k, int s) {
-    const uint32_t w[4] = {k.w.x, k.w.y, k.w.z, k.w.w};
-    return fp4x8_to_bf16x8(w[s], fp4_scale(k.s, 0));
-  }
-  __device__ static void zero_v(V& v, int t) {   // the scale byte too: 255 stands for NaN
-    (t == 0 ? v.w.x : t == 1 ? v.w.y : t == 2 ? v.w.z : v.w.w) = 0u;
-    v.s &= ~(0xFFu << (8 * t));
-  }
-  __device__ static void v_operands(const V& v, uint2 (&op)[8]) {
-    const MfmaRowKv<KV_BF16>::V b = {{fp4x8_to_bf16x8(v.w.x, fp4_scale(v.s, 0)), fp4x8_to_bf16x8(v.w.y, fp4_scale(v.s, 1)),
-                                      fp4x8_to_bf16x8(v.w.z, fp4_scale(v.s, 2)), fp4x8_to_bf16x8(v.w.w, fp4_scale(v.s, 3))}};
-    MfmaRowKv<KV_BF16>::v_operands(b, op);
-  }
-};
-
 template <int KVT, int OT, int NW, int G, bool STREAM, bool MOD>
 __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds) {
-  static_assert(G <= 8, "one 16-column MFMA holds the group's heads");
+  static_assert(G == 8 || G == 4, "one 16-column MFMA holds the group's heads");
   constexpr int D = 128;
   constexpr bool FP8 = KVT == KV_FP8;
   constexpr bool REST = FP8 && G == 4;   // columns 4 .. 7: the rest of the probabilities
@@ -1048,17 +1052,9 @@ __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds
   struct Scales { float k, v; };
   auto load_block = [&](int bid, typename KV::K& k, typename KV::V& v, Scales& sc2) {
     if (static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks)) {
-      if constexpr (KVT == KV_FP4) {
-        const int64_t block = static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
-        const int64_t codes = block + kvh * aug::kMxCodes, scales = block + a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
-        KV::template load_k<STREAM>(kc + codes, kc + scales, j, g, k);
-        KV::template load_v<STREAM>(vc + codes, vc + scales, j, g, v);
-        return;
-      } else {
-        const int64_t base = (static_cast<int64_t>(bid) * a.hkv + kvh) * kHead;
-        KV::template load_k<STREAM>(kc + base + k_lane, k);
-        KV::template load_v<STREAM>(vc + base + v_lane, kRow, v);
-      }
+      const int64_t base = (static_cast<int64_t>(bid) * a.hkv + kvh) * kHead;
+      KV::template load_k<STREAM>(kc + base + k_lane, k);
+      KV::template load_v<STREAM>(vc + base + v_lane, kRow, v);
       if constexpr (FP8) {
         sc2.k = load_uniform(a.k_scale + static_cast<int64_t>(bid) * a.hkv + kvh);
         sc2.v = load_uniform(a.v_scale + static_cast<int64_t>(bid) * a.hkv + kvh);
@@ -1206,6 +1202,249 @@ __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds
 }
 
 // ---------------------------------------------------------------------------
+// row items over 4-bit KV (MFMA)
+// ---------------------------------------------------------------------------
+//
+// One query row and its G (1, 2, 4 or 8) query heads against two 16-token blocks
+// at a time and wave:
+//   S^T[16 keys][16 columns] = K Q^T, one 16x16x128 fp8 x 4-bit MFMA a block. Lane
+//     l brings the 32 dims 32g .. of token l % 16 (g = l / 16) as they lie in the
+//     cache, 16 bytes, and the scale byte of that group, so the keys are never
+//     converted. The queries are two E4M3 codes per element (TwoCodes): columns 0 ..
+//     7 take the first codes of the heads, columns 8 .. 15 the second, and one lane
+//     rotation adds the halves. (The MFMA wants bytes 0 .. 15 of lane group g for
+//     dims 16g .. and bytes 16 .. 31 for dims 64 + 16g ...)
+//   O^T[128 dims][16 columns] += V^T P^T, eight 16x16x32 bf16 MFMAs over the two
+//     blocks' 32 keys: slots 0 .. 3 of lane group g are keys 4g .. 4g + 3 of the
+//     first block, slots 4 .. 7 of the second, as the scores lie; row m of MFMA b is
+//     dim 8m + b. A lane's V is one 16-byte cell a block (four tokens of eight
+//     dims), converted to bf16 with the tokens' scales and paired by tokens.
+// Bound by HBM: a pair of blocks is 4352 bytes, 1670 cycles of a SIMD's share of the
+// card's rate, and about 150 vector instructions.
+struct MxBlock {
+  uint4 k, v;              // codes
+  uint32_t ks, vs;         // scale byte of the lane's keys' group, and of its four tokens' values
+  int bid;
+};
+
+// The row's queries as the lane's operand: the codes of column l % 16 and the
+// exponent byte that goes with them. Made before an item's kind of loads is known;
+// made in both branches, the unconverted values stayed in registers through the
+// first one's loop.
+struct MxQuery {
+  v8i_t codes;
+  int byte;
+};
+template <int G>
+__device__ __forceinline__ MxQuery mx_query(const WorkItem& it, const AttnArgs& a) {
+  constexpr int D = 128;
+  const int j = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3, head = j & 7;
+  const uint16_t* qb = static_cast<const uint16_t*>(a.q) +
+                       (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(it.kvh) * G + head) * D + 16 * g;
+  float x[32];
+  float amax = 0.f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint4 w = head < G ? *reinterpret_cast<const uint4*>(qb + 64 * (c >> 1) + 8 * (c & 1)) : uint4{0, 0, 0, 0};
+    unpack_bf16x8(w, x + 8 * c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[8 * c + e]));
+  }
+  const TwoCodes split(group4_max(amax));
+  MxQuery q;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint2 w = split(x + 4 * i);
+    q.codes[i] = static_cast<int>(j < 8 ? w.x : w.y);
+  }
+  q.byte = j < 8 ? split.byte : split.byte - TwoCodes::kRestLog2;
+  return q;
+}
+
+template <int OT, int NW, int G, bool STREAM, bool MOD>
+__device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, const MxQuery& q, float* lds) {
+  constexpr int D = 128;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = lane & 15;            // column: head j & 7 (of G)
+  const int g = lane >> 4;            // keys 4g .. 4g + 3 of a block
+  const int kvh = it.kvh;
+  const int head = j & 7;
+
+  const float sc = a.scale_log2;
+  const int2 keys = row_keys<MOD>(a, it.q_row0, it.pos0);
+  const float from = distance_from(it.pos0, keys);
+  float slope = 0.f;
+  if constexpr (MOD) {
+    if (a.slopes && head < G) slope = -kLog2e * a.slopes[kvh * G + head];
+  }
+  float m_run = kNegBig, l_run = 0.f;
+  f32x4_t oacc[8];
+#pragma unroll
+  for (int b = 0; b < 8; ++b) oacc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  const int blk0 = it.key_begin / kBlock;
+  const int nblk = (it.key_end - it.key_begin + kBlock - 1) / kBlock;
+  const int32_t* table = a.block_ids + it.bt_off + blk0;
+  const char* kc = static_cast<const char*>(a.k_cache);
+  const char* vc = static_cast<const char*>(a.v_cache);
+  const int64_t block_bytes = static_cast<int64_t>(a.hkv) * aug::kMxCell;
+  const int codes = kvh * aug::kMxCodes, scales = a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
+  const int k_codes = codes + 64 * j + 16 * g, k_scale = scales + 4 * j + g;
+  const int v_codes = codes + 256 * g + 16 * j, v_scale = scales + 16 * (j >> 2) + 4 * g;
+
+  auto load_block = [&](int bid, MxBlock& b) {
+    // A block that is none (past the span, or outside the pool) loads the pool's
+    // first one and counts for nothing: loads under a condition would make the
+    // compiler wait for all of them wherever it cannot count them.
+    b.bid = bid;
+    const int64_t at = static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks) ? bid * block_bytes : 0;
+    const char* kb = kc + at;
+    const char* vb = vc + at;
+    b.k = load_kv<STREAM, uint4>(kb + k_codes);
+    b.v = load_kv<STREAM, uint4>(vb + v_codes);
+    b.ks = *reinterpret_cast<const uint8_t*>(kb + k_scale);
+    b.vs = *reinterpret_cast<const uint32_t*>(vb + v_scale);
+  };
+  // Pairs of blocks in two register sets that take turns; ids one pair ahead.
+  struct Pair { MxBlock b[2]; };
+  int next[2];
+  auto ids = [&](int bi) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) next[i] = bi + i < nblk ? load_uniform(table + bi + i) : -1;
+  };
+  auto fetch = [&](int bi, Pair& p) {
+    __builtin_amdgcn_s_setprio(1);   // loads ahead of the other waves' work, as in row_item_mfma
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_block(next[i], p.b[i]);
+    __builtin_amdgcn_s_setprio(0);
+    ids(bi + 2 * NW);
+  };
+  auto compute = [&](int bi, Pair& p) {
+    const int tok0 = (blk0 + bi) * kBlock;
+    float sv[8];
+    bool full = tok0 + 2 * kBlock <= it.key_end && (!MOD || tok0 >= keys.x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      MxBlock& b = p.b[i];
+      const bool ok = static_cast<uint32_t>(b.bid) < static_cast<uint32_t>(a.num_pool_blocks);
+      full = full && ok;
+      const v8i_t kop = {static_cast<int>(b.k.x), static_cast<int>(b.k.y), static_cast<int>(b.k.z),
+                         static_cast<int>(b.k.w), 0, 0, 0, 0};
+      f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
+      sacc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kop, q.codes, sacc, 4, 0, 0, static_cast<int>(b.ks), 0,
+                                                              q.byte);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sv[4 * i + r] = sacc[r] + lane8_other(sacc[r]);   // both codes of the query
+    }
+    float coef = sc;
+    if constexpr (MOD) {
+      if (a.cap_in != 0.f) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sv[r] = capped<false>(a, sv[r] * sc);
+        coef = 1.f;
+      }
+      if (a.slopes) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float away = fabsf(from - static_cast<float>(tok0 + 16 * (r >> 2) + 4 * g + (r & 3)));
+          sv[r] = fmaf(sv[r], coef, slope * away);
+        }
+        coef = 1.f;
+      }
+    }
+    if (!full) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        MxBlock& b = p.b[r >> 2];
+        const int tok = tok0 + 16 * (r >> 2) + 4 * g + (r & 3);
+        const bool valid = static_cast<uint32_t>(b.bid) < static_cast<uint32_t>(a.num_pool_blocks) && tok < it.key_end &&
+                           (!MOD || tok >= keys.x);
+        sv[r] = valid ? sv[r] : -INFINITY;
+        if (!valid) {   // value and scale (255 stands for NaN) zero, so 0 * value never meets NaN
+          const int t = r & 3;
+          (t == 0 ? b.v.x : t == 1 ? b.v.y : t == 2 ? b.v.z : b.v.w) = 0u;
+          b.vs &= ~(0xFFu << (8 * t));
+        }
+      }
+    }
+    float top = sv[0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) top = fmaxf(top, sv[r]);
+    const float mn = fmaxf(m_run, group4_max(top) * coef);
+    if (__any(mn > m_run + kRescaleSlack)) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= alpha;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) oacc[b] *= alpha;
+      m_run = mn;
+    }
+    uint32_t pp[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      pp[r] = pack_bf16(__builtin_amdgcn_exp2f(fmaf(sv[2 * r], coef, -m_run)),
+                        __builtin_amdgcn_exp2f(fmaf(sv[2 * r + 1], coef, -m_run)));
+      l_run = dot2_bf16(pp[r], kBf16PairOne, l_run);        // exactly the packed probabilities
+    }
+    const bf16x8_t pop = as_bf16x8(uint4{pp[0], pp[1], pp[2], pp[3]});
+    float vsc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) vsc[i][t] = fp4_scale(p.b[i].vs, t);
+    // dims 8m + 2e and + 1: a byte of each token's word gives both, paired by tokens
+    // they are the operands of two MFMAs
+    auto dims = [&](auto sel) {
+      constexpr int E = decltype(sel)::value;
+      uint32_t x[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t w[4] = {p.b[i].v.x, p.b[i].v.y, p.b[i].v.z, p.b[i].v.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          x[i][t] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], vsc[i][t], E));
+      }
+      const auto pair = [&](uint32_t which) {
+        return as_bf16x8(uint4{__builtin_amdgcn_perm(x[0][1], x[0][0], which), __builtin_amdgcn_perm(x[0][3], x[0][2], which),
+                               __builtin_amdgcn_perm(x[1][1], x[1][0], which), __builtin_amdgcn_perm(x[1][3], x[1][2], which)});
+      };
+      oacc[2 * E] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pair(0x05040100u), pop, oacc[2 * E], 0, 0, 0);
+      oacc[2 * E + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pair(0x07060302u), pop, oacc[2 * E + 1], 0, 0, 0);
+    };
+    dims(std::integral_constant<int, 0>{});
+    dims(std::integral_constant<int, 1>{});
+    dims(std::integral_constant<int, 2>{});
+    dims(std::integral_constant<int, 3>{});
+  };
+  Pair p0, p1;
+  int bi = 2 * wave;
+  ids(bi);
+  fetch(bi, p0);
+  for (; bi < nblk; bi += 4 * NW) {
+    fetch(bi + 2 * NW, p1);
+    compute(bi, p0);
+    fetch(bi + 4 * NW, p0);
+    compute(bi + 2 * NW, p1);
+  }
+
+  // this wave's result for head j: dims 32g + 8r + b from oacc[b][r]
+  constexpr int ROW = row_lds_stride(D);
+  const float l_tot = group4_sum(l_run);
+  if (j < G) {
+    float* dst = lds + (wave * G + j) * ROW;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int b = 0; b < 8; ++b) dst[32 * g + 8 * r + b] = oacc[b][r];
+    if (g == 0) {
+      dst[D] = m_run;
+      dst[D + 1] = l_tot;
+    }
+  }
+  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds);
+}
+
+// ---------------------------------------------------------------------------
 // tile items (bf16 MFMA)
 // ---------------------------------------------------------------------------
 
@@ -1223,9 +1462,10 @@ struct TileLds {
   // other fp8 ones through registers, converted and padded. K, then V.
   static constexpr bool DMA = KVT == KV_BF16;
   static constexpr bool K8 = F8 >= 1;
+  static constexpr bool K4 = KVT == KV_FP4;      // 4-bit keys stay codes too, with their scales behind them
   static_assert(!K8 || (KVT == KV_FP8 && D == 128), "fp8 score products need fp8 keys and head_dim 128");
-  static constexpr int ROW = K8 ? D : D * 2;              // bytes of an unpadded row
-  static constexpr int KBYTES = DMA || K8 ? 64 * ROW : 64 * KS * 2;
+  static constexpr int ROW = K4 ? D / 2 : K8 ? D : D * 2;   // bytes of an unpadded row
+  static constexpr int KBYTES = DMA || K8 ? 64 * ROW : K4 ? 64 * (ROW + 4) : 64 * KS * 2;
   static constexpr int STAGE = KBYTES + (DMA ? 64 * ROW : 64 * VS * 2);   // bytes of one K + V stage
   static constexpr int IDS = aug::kTileSpanMax / kBlock + 8; // block ids of one item's key span
   // fp8, per stage and block of the tile: the K scale times the softmax
@@ -1234,7 +1474,7 @@ struct TileLds {
   static constexpr int SCALES = 2 * NSC * 4;
   static constexpr int BYTES = 2 * STAGE + IDS * 4 + SCALES;
   static_assert(D * VT8 <= 64 * VS * 2, "transposed fp8 values fit the V region of a stage");
-  static_assert(!(DMA || K8) || 2 * STAGE <= 65536, "direct loads address a stage with 16 bits");
+  static_assert(!(DMA || K8 || K4) || 2 * STAGE <= 65536, "direct loads address a stage with 16 bits");
 };
 
 // Direct loads fill LDS in order (lane l of an instruction writes bytes 16 l ..
@@ -1242,10 +1482,12 @@ struct TileLds {
 // 16-byte chunk c of row r sits at chunk c ^ tile_chunk(r) of its row, and the
 // loads permute which chunk each lane fetches. Sixteen rows at one column (the
 // K operands) and four rows at four neighbouring columns (the transposing V
-// reads) then fall on distinct banks; so do sixteen 128-byte rows of key codes.
-template <int D, bool K8>
+// reads) then fall on distinct banks; so do sixteen 128-byte rows of fp8 key codes
+// and sixteen 64-byte rows of 4-bit ones.
+template <int D, int ROW>
 __device__ __forceinline__ int tile_chunk(int r) {
-  if constexpr (K8) return (r >> 1) & 7;
+  if constexpr (ROW == 64) return (r >> 2) & 3;
+  if constexpr (ROW == 128 && D == 128) return (r >> 1) & 7;
   return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
@@ -1304,6 +1546,13 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   // product, saved 4 % on 16 chunks of 512 rows, 64/8 heads, but elements below
   // 2^-22 of their row's largest magnitude were lost.)
   constexpr bool QK8 = L::K8;
+  // Over 4-bit keys they run on the fp8 x 4-bit MFMAs, which take the codes and
+  // their scales as they are: 16 bytes of a key for 32 dims from LDS instead of 64.
+  // A query element has 8 significant bits and goes in as the sum of two E4M3 codes
+  // of 4 bits (its value rounded, and 32 times the rest), which is exact down to
+  // 2^-14 of its vector's largest magnitude, and 2^-21 of that off below.
+  constexpr bool QK4 = L::K4;
+  constexpr bool KDMA = DMA || QK8 || QK4;   // the keys, at least, come by direct loads
   constexpr bool PV8 = F8 >= 2;
   // fp8 probabilities: a lane's P values are stored as E4M3 codes of
   // p * (vs_b / vref) * 2^kPv8Log2, with vs_b the block's V scale and vref the
@@ -1346,12 +1595,37 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   // fp8 scores: the row rounded to E4M3 after division by its scale qscale
   // (largest magnitude / 448), as the B operands of the two 64-dim k-steps:
   // lane half hh holds dims 64h + 32hh .. + 31 of k-step h.
-  uint4 qreg[QK8 ? 1 : KSTEPS];
-  v8i_t q8[2];
+  uint4 qreg[QK8 || QK4 ? 1 : KSTEPS];
+  v8i_t q8[2], q8rest[2];
   float qscale = 1.f;
+  int q4exp = 0;              // 4-bit keys: the query's exponent byte
   {
     const int64_t qoff = (static_cast<int64_t>(it.q_row0 + p) * a.hq + static_cast<int64_t>(kvh) * G + gh) * D;
-    if constexpr (!QK8) {
+    if constexpr (QK4) {
+      // the lane's bytes of k-step h: dims 64h + 16hh .. + 15, then 64h + 32 + 16hh .. + 15
+      float x[2][32];
+      float amax = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c4 = 0; c4 < 4; ++c4) {
+          const int dim = 64 * h + 32 * (c4 >> 1) + 16 * hh + 8 * (c4 & 1);
+          const uint4 w = row_ok ? *reinterpret_cast<const uint4*>(qb + qoff + dim) : uint4{0, 0, 0, 0};
+          unpack_bf16x8(w, x[h] + 8 * c4);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[h][8 * c4 + e]));
+        }
+      const TwoCodes split(max_across_halves(amax));
+      q4exp = split.byte;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint2 w = split(x[h] + 4 * i);
+          q8[h][i] = static_cast<int>(w.x);
+          q8rest[h][i] = static_cast<int>(w.y);
+        }
+    } else if constexpr (!QK8) {
 #pragma unroll
       for (int s = 0; s < KSTEPS; ++s)
         qreg[s] = row_ok ? *reinterpret_cast<const uint4*>(qb + qoff + 16 * s + 8 * hh) : uint4{0, 0, 0, 0};
@@ -1474,10 +1748,10 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   // fp8 through registers (bf16 takes none of this): a thread stages KPT
   // consecutive keys of one block (KPT divides 16)
   raw_t kr[KPT], vr[KPT];
-  // 4-bit: a thread stages 32 dims of one key and four keys of eight dims of the
-  // values, 16 bytes of codes each, with their scale bytes
-  const int key4 = threadIdx.x / 4, grp4 = threadIdx.x % 4, quad4 = threadIdx.x / 16, oct4 = threadIdx.x % 16;
-  uint4 kw4, vw4;
+  // 4-bit: a thread stages four keys of eight dims of the values, 16 bytes of codes
+  // with their scale bytes, and the first 64 a key's four scale bytes
+  const int quad4 = threadIdx.x / 16, oct4 = threadIdx.x % 16;
+  uint4 vw4;
   uint32_t ks4 = 0, vs4 = 0;
   float sc_reg = 1.f;   // fp8: thread t < 8 carries scale t of the tile (k0..3, v0..3)
   float vsc_reg = 1.f;  // fp8 values: the V scale of the block this thread stages
@@ -1499,19 +1773,19 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   };
   auto load_tile4 = [&](int k0, auto full_tag) {
     constexpr bool FULL = decltype(full_tag)::value;
-    kw4 = vw4 = uint4{0, 0, 0, 0};
+    vw4 = uint4{0, 0, 0, 0};
     ks4 = vs4 = 0;
     const auto block_of = [&](int tok) {
       const int bid = FULL || tok < key_end ? ids[(tok >> 4) - blk_first] : -1;
       return static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks) ? bid : -1;
     };
     const int64_t scales = static_cast<int64_t>(a.hkv) * aug::kMxCodes + kvh * aug::kMxScales;
-    const int ktok = k0 + key4, vtok = k0 + 4 * quad4;
-    if (const int bid = block_of(ktok); FULL || bid >= 0) {
-      const char* block = kc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
-      kw4 = *reinterpret_cast<const uint4*>(block + kvh * aug::kMxCodes + 64 * (ktok & 15) + 16 * grp4);
-      ks4 = *reinterpret_cast<const uint8_t*>(block + scales + 4 * (ktok & 15) + grp4);
+    if (threadIdx.x < 64) {
+      const int ktok = k0 + threadIdx.x;
+      if (const int bid = block_of(ktok); FULL || bid >= 0)
+        ks4 = *reinterpret_cast<const uint32_t*>(kc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell + scales + 4 * (ktok & 15));
     }
+    const int vtok = k0 + 4 * quad4;
     if (const int bid = block_of(vtok); FULL || bid >= 0) {
       const char* block = vc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
       vw4 = *reinterpret_cast<const uint4*>(block + kvh * aug::kMxCodes + 64 * (vtok & 15) + 16 * oct4);
@@ -1574,12 +1848,11 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     uint16_t* ks = reinterpret_cast<uint16_t*>(smem + stage * L::STAGE);
     uint16_t* vs = ks + L::KBYTES / 2;
     if constexpr (FP4) {
-      const uint32_t kw[4] = {kw4.x, kw4.y, kw4.z, kw4.w}, vw[4] = {vw4.x, vw4.y, vw4.z, vw4.w};
+      const uint32_t vw[4] = {vw4.x, vw4.y, vw4.z, vw4.w};
+      if (threadIdx.x < 64) *reinterpret_cast<uint32_t*>(smem + stage * L::STAGE + 64 * L::ROW + 4 * threadIdx.x) = ks4;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        *reinterpret_cast<uint4*>(ks + key4 * L::KS + 32 * grp4 + 8 * u) = fp4x8_to_bf16x8(kw[u], fp4_scale(ks4, 0));
+      for (int u = 0; u < 4; ++u)
         *reinterpret_cast<uint4*>(vs + (4 * quad4 + u) * L::VS + 8 * oct4) = fp4x8_to_bf16x8(vw[u], fp4_scale(vs4, u));
-      }
       return;
     }
 #pragma unroll
@@ -1629,12 +1902,12 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     }
   };
 
-  // direct loads (fp8: of the keys only): wave w fetches block w of a key tile,
+  // direct loads (fp8 and 4 bits: of the keys only): wave w fetches block w of a key tile,
   // RPI rows an instruction
   constexpr int RPI = 1024 / L::ROW;
   const int dma_wave = __builtin_amdgcn_readfirstlane(wave);
   const int dma_row = lane * 16 / L::ROW;            // row within an instruction
-  const uint32_t dma_off = dma_row * L::ROW + (((lane & (L::ROW / 16 - 1)) ^ tile_chunk<D, QK8>(dma_row)) << 4);
+  const uint32_t dma_off = dma_row * L::ROW + (((lane & (L::ROW / 16 - 1)) ^ tile_chunk<D, L::ROW>(dma_row)) << 4);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) unsigned char*)(smem)));
   // pools that are not 16-byte aligned (a caller's own offsets) go through registers
@@ -1645,16 +1918,17 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     const int bid = __builtin_amdgcn_readfirstlane(tok0 < key_end ? ids[(tok0 >> 4) - blk_first] : -1);
     dma_bid = static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks) ? bid : -1;
     if (dma_bid < 0) return;
-    const int64_t base = (static_cast<int64_t>(bid) * a.hkv + kvh) * head_stride * EB;
+    const int64_t base = FP4 ? static_cast<int64_t>(bid) * a.hkv * aug::kMxCell + kvh * aug::kMxCodes
+                             : (static_cast<int64_t>(bid) * a.hkv + kvh) * head_stride * EB;
     const uint32_t dst = lds0 + stage * L::STAGE + dma_wave * 16 * L::ROW;
-    if (odd_pool) {
+    if (!FP4 && odd_pool) {
       // opaque, or the loop's addresses are kept in registers throughout the item
       uint32_t from = dma_off, to = lane * 16;
       asm volatile("" : "+v"(from), "+v"(to));
       unsigned char* block = smem + stage * L::STAGE + dma_wave * 16 * L::ROW;
 #pragma unroll 1
       for (int i = 0; i < 16 / RPI; ++i) {
-        const uint32_t off = i * 1024 + (from ^ (tile_chunk<D, QK8>(RPI * i) << 4));
+        const uint32_t off = i * 1024 + (from ^ (tile_chunk<D, L::ROW>(RPI * i) << 4));
         uint4 x;
         __builtin_memcpy(&x, kc + base + off, 16);
         *reinterpret_cast<uint4*>(block + i * 1024 + to) = x;
@@ -1668,7 +1942,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
 #pragma unroll
     for (int i = 0; i < 16 / RPI; ++i) {
       // rows RPI i ..: the chunk permutation of row dma_row, with i's own bits
-      const uint32_t off = i * 1024 + (dma_off ^ (tile_chunk<D, QK8>(RPI * i) << 4));
+      const uint32_t off = i * 1024 + (dma_off ^ (tile_chunk<D, L::ROW>(RPI * i) << 4));
       load_to_lds16(kc + base, off, dst + i * 1024);
       if constexpr (DMA) load_to_lds16(vc + base, off, dst + L::KBYTES + i * 1024);
     }
@@ -1689,19 +1963,19 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         }
     }
   };
-  // operand addresses of the direct layout in a stage: chunk hh (codes: 2hh) of
+  // operand addresses of the direct layout in a stage: chunk hh (fp8 codes: 2hh) of
   // K row n (rows n and n + 32 share a permutation), and the row and columns of
   // v_lane_off in V; the other chunks are exclusive-ors away
-  const uint32_t k_lane = n * L::ROW + (((QK8 ? 2 * hh : hh) ^ tile_chunk<D, QK8>(n)) << 4);
+  const uint32_t k_lane = n * L::ROW + (((QK8 ? 2 * hh : hh) ^ tile_chunk<D, L::ROW>(n)) << 4);
   const int v_row = 4 * hh + (lane & 15) / 4;
   const uint32_t v_lane = L::KBYTES + v_row * L::ROW +
-                          (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ tile_chunk<D, QK8>(v_row)) << 4) + 8 * (lane & 1);
+                          (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ tile_chunk<D, L::ROW>(v_row)) << 4) + 8 * (lane & 1);
 
   auto step = [&](int t, auto mask_tag) {
     constexpr bool MASK = decltype(mask_tag)::value;
     const int k0 = t * 64;
     const int stage = (t - t0) & 1;
-    if constexpr (DMA || QK8) settle_tile(t, stage);
+    if constexpr (KDMA) settle_tile(t, stage);
     __syncthreads();   // stage `stage` is written; the other stage's readers are done
     if (t + 1 < t1) {
       if constexpr (!DMA) {
@@ -1715,7 +1989,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       // compiler waits for every load before it, and would for these (two
       // 4096-row chunks, 64/8 heads, both products fp8: 1107 -> 1052 us, fp8
       // scores alone 943 -> 930).
-      if constexpr (DMA || QK8) issue_tile(t + 1, stage ^ 1);
+      if constexpr (KDMA) issue_tile(t + 1, stage ^ 1);
     }
     const uint32_t k_base = k_lane + stage * L::STAGE, v_base = v_lane + stage * L::STAGE;
     const uint16_t* ks = reinterpret_cast<const uint16_t*>(smem + stage * L::STAGE);
@@ -1748,6 +2022,36 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         for (int h = 0; h < 2; ++h)
           sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][h], q8[h], sacc[mb], 0, 0, 0, 127, 0, 127);
       }
+    } else if constexpr (QK4) {
+      // 4 bits: K rows of 64 bytes and their scale bytes against the query's two
+      // codes, two 64-dim k-steps per 32 keys; of a k-step the halves take the first
+      // and the second 32 dims, whose scale is byte 2h + hh of the key's word
+      v8i_t kop[2][2];
+      int ksc[2];
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 w = *reinterpret_cast<const uint4*>(smem + (k_base ^ (32 * h)) + 32 * mb * L::ROW);
+          kop[mb][h] = v8i_t{static_cast<int>(w.x), static_cast<int>(w.y), static_cast<int>(w.z), static_cast<int>(w.w),
+                             0, 0, 0, 0};
+        }
+        ksc[mb] = static_cast<int>(*reinterpret_cast<const uint32_t*>(smem + stage * L::STAGE + 64 * L::ROW + 4 * (32 * mb + n)) >>
+                                   (8 * hh));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sacc[mb][e] = 0.f;
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8[0], sacc[mb], 4, 0, 0, ksc[mb], 0, q4exp);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8[1], sacc[mb], 4, 0, 2, ksc[mb], 0, q4exp);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8rest[0], sacc[mb], 4, 0, 0, ksc[mb], 0,
+                                                                   q4exp - TwoCodes::kRestLog2);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8rest[1], sacc[mb], 4, 0, 2, ksc[mb], 0,
+                                                                   q4exp - TwoCodes::kRestLog2);
+      }
     } else {
       uint4 kop[2][KSTEPS];
 #pragma unroll
@@ -1774,7 +2078,20 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     // lanes i/4, 4 + i/4, 8 + i/4 and 12 + i/4 of its group, so addressing
     // row (lane % 16) / 4 at column 4 (lane % 4) hands each lane four
     // consecutive keys of one dimension: the operand layout of V^T.
-    uint4 vop[PV8 ? 1 : 4][PV8 ? 1 : DB];
+    // With modified scores a step of them is read when it is multiplied: the scores
+    // take the registers.
+    const auto v_operand = [&](int s, int db) {
+      const uint16_t* v0 = vs + (16 * s) * L::VS + 32 * db + v_lane_off;
+      const uint16_t* v1 = v0 + 8 * L::VS;
+      if constexpr (DMA) {
+        v0 = reinterpret_cast<const uint16_t*>(smem + (v_base ^ (64 * db)) + 16 * s * L::ROW);
+        v1 = reinterpret_cast<const uint16_t*>(smem + (v_base ^ (64 * db + 32)) + (16 * s + 8) * L::ROW);
+      }
+      const uint2 lo = ds_read_tr16(v0);
+      const uint2 hi = ds_read_tr16(v1);
+      return uint4{lo.x, lo.y, hi.x, hi.y};
+    };
+    uint4 vop[PV8 || MOD ? 1 : 4][PV8 ? 1 : DB];
     // fp8 values: lane (dimension n of a 32-dim block, half hh) takes the 32
     // codes of its dimension for the keys whose bit 2 is hh
     v8i_t vop8[PV8 ? DB : 1];
@@ -1789,21 +2106,11 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
                          static_cast<int>(lo.w), static_cast<int>(hi.x), static_cast<int>(hi.y),
                          static_cast<int>(hi.z), static_cast<int>(hi.w)};
       }
-    } else {
+    } else if constexpr (!MOD) {
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const uint16_t* v0 = vs + (16 * s) * L::VS + 32 * db + v_lane_off;
-          const uint16_t* v1 = v0 + 8 * L::VS;
-          if constexpr (DMA) {
-            v0 = reinterpret_cast<const uint16_t*>(smem + (v_base ^ (64 * db)) + 16 * s * L::ROW);
-            v1 = reinterpret_cast<const uint16_t*>(smem + (v_base ^ (64 * db + 32)) + (16 * s + 8) * L::ROW);
-          }
-          const uint2 lo = ds_read_tr16(v0);
-          const uint2 hi = ds_read_tr16(v1);
-          vop[s][db] = uint4{lo.x, lo.y, hi.x, hi.y};
-        }
+        for (int db = 0; db < DB; ++db) vop[s][db] = v_operand(s, db);
     }
 
     // Entry (mb, i, j) of this lane is key k0 + 32mb + 8i + 4hh + j, which
@@ -1819,13 +2126,14 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       if constexpr (MOD) return !MASK || static_cast<uint32_t>(k - lo) < len;
       else return !MASK || k <= lim;
     };
-    if constexpr (MASK && !MOD) {
+    const auto mask = [&] {
 #pragma unroll
       for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (!live(mb, e)) sacc[mb][e] = -INFINITY;
-    }
+    };
+    if constexpr (MASK && !MOD) mask();
     // log2-domain coefficient of the raw score, per block (fp8: K scale folded in)
     float coef[4], vlog[4], vinv[4];
 #pragma unroll
@@ -1834,6 +2142,36 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       vlog[b] = FP8 ? stage_scales[stage * L::NSC + 4 + b] : 0.f;
       vinv[b] = FP8 ? stage_scales[stage * L::NSC + 8 + b] : 1.f;
     }
+    if constexpr (MOD) {
+      // the cap leaves -1 / (1 + 2^(..)) in the place of the raw score, with one
+      // positive coefficient; the bias leaves the score itself
+      if (a.cap_in != 0.f) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const float in = coef[b] * a.cap_in;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int mb = b >> 1, i = 8 * (b & 1) + e;
+            sacc[mb][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(sacc[mb][i] * in));
+          }
+          coef[b] = -a.cap_out;
+        }
+      }
+      if (a.slopes) {
+        const float off = static_cast<float>(k0 + 4 * hh) - from;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int mb = b >> 1, i = 8 * (b & 1) + e;
+            const float away = fabsf(off + static_cast<float>(16 * b + 8 * (e >> 2) + (e & 3)));
+            sacc[mb][i] = fmaf(sacc[mb][i], coef[b], slope * away);
+          }
+          coef[b] = 1.f;
+        }
+      }
+      if constexpr (MASK) mask();
+    }
     // row maximum of the scaled scores: block maxima of the raw scores times
     // the (non-negative) block coefficients. The raw scores are finite or
     // -inf (masked), so the NaN-propagating maximum (three operands per
@@ -1841,37 +2179,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     // fp8 blocks combine with fmaxf, which drops the NaN of a masked block
     // under a zero key scale.
     float smax;
-    if constexpr (MOD) {
-      // the scores themselves, in the log2 domain, take the place of the raw ones
-#pragma unroll
-      for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sacc[mb][e] *= coef[2 * mb + (e >> 3)];
-      if (a.cap_in != 0.f) {
-#pragma unroll
-        for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sacc[mb][e] = capped<false>(a, sacc[mb][e]);
-      }
-      if (a.slopes) {
-        const float off = static_cast<float>(k0 + 4 * hh) - from;
-#pragma unroll
-        for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            sacc[mb][e] = fmaf(slope, fabsf(off + static_cast<float>(32 * mb + 8 * (e >> 2) + (e & 3))), sacc[mb][e]);
-      }
-      smax = -INFINITY;
-#pragma unroll
-      for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (!live(mb, e)) sacc[mb][e] = -INFINITY;
-          smax = __builtin_elementwise_maximum(smax, sacc[mb][e]);
-        }
-#pragma unroll
-      for (int b = 0; b < 4; ++b) coef[b] = 1.f;
-    } else if constexpr (FP8) {
+    if constexpr (FP8) {
       smax = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
@@ -1886,7 +2194,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       smax = sacc[0][0];
 #pragma unroll
       for (int e = 1; e < 32; ++e) smax = __builtin_elementwise_maximum(smax, sacc[e >> 4][e & 15]);
-      smax *= c;
+      smax *= MOD ? coef[0] : c;
     }
     smax = max_across_halves(smax);
     const float mn = fmaxf(m_run, smax);
@@ -1959,9 +2267,13 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
                          dot2_bf16(pw.y, kBf16PairOne, dot2_bf16(pw.x, kBf16PairOne, FP8 ? 0.f : l_run))));
       l_run = FP8 ? fmaf(bsum, vinv[s], l_run) : bsum;
       const bf16x8_t pop = as_bf16x8(pw);
+      if constexpr (MOD) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) vop[0][db] = v_operand(s, db);
+      }
 #pragma unroll
       for (int db = 0; db < DB; ++db)
-        acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[s][db]), pop, acc_o[db], 0, 0, 0);
+        acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[MOD ? 0 : s][db]), pop, acc_o[db], 0, 0, 0);
     }
     }
     // From here to the next tile's score MFMAs (barrier, staging of the tile
@@ -1973,7 +2285,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   };
 
   int t = t0;
-  if constexpr (DMA || QK8) issue_tile(t0, 0);
+  if constexpr (KDMA) issue_tile(t0, 0);
   if constexpr (!DMA) {
     if (t0 < t_load) load_tile(t0 * 64, bool_tag<true>{});
     else load_tile(t0 * 64, bool_tag<false>{});
@@ -2078,9 +2390,12 @@ __device__ __forceinline__ void attn_body(const Args<MOD>& a) {
   // row items always fetch a wave's next block while the current one is
   // computed: short spans (small batches) are latency bound otherwise
   float* lds = reinterpret_cast<float*>(smem);
+  MxQuery query;
+  if constexpr (KVT == KV_FP4) query = mx_query<G>(it, a);
   auto row = [&](auto stream_tag) {
     constexpr bool S = decltype(stream_tag)::value;
-    if constexpr (ROW_MFMA && row_mfma_capable<KVT, D, G, QT>()) row_item_mfma<KVT, OT, NW, G, S, MOD>(it, a, lds);
+    if constexpr (KVT == KV_FP4) row_item_mx<OT, NW, G, S, MOD>(it, a, query, lds);
+    else if constexpr (ROW_MFMA && row_mfma_capable<KVT, D, G, QT>()) row_item_mfma<KVT, OT, NW, G, S, MOD>(it, a, lds);
     else row_item<KVT, D, G, QT, OT, true, NW, S, MOD>(it, a, lds);
   };
   if (it.stream) row(bool_tag<true>{});
@@ -2091,6 +2406,14 @@ __device__ __forceinline__ void attn_body(const Args<MOD>& a) {
 template <int KVT, int D, int G, int QT, int OT, bool ROW_MFMA, int NW, bool MOD>
 __global__ __launch_bounds__(64 * NW) void attn_rows_kernel(Args<MOD> a) {
   attn_body<KVT, D, G, QT, OT, false, ROW_MFMA, NW, 0, MOD>(a);
+}
+
+// 4-bit rows: four waves a SIMD, two workgroups a compute unit, so at most 128
+// registers. HBM needs that many loads in flight: with one workgroup (172
+// registers) 512 decodes over 1.7M keys, 64/8 heads, took 351 us, with two XXX.
+template <int G, int NW, bool MOD>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4, 4))) void attn_rows_mx_kernel(Args<MOD> a) {
+  attn_body<KV_FP4, 128, G, AUG_BF16, AUG_BF16, false, true, NW, 0, MOD>(a);
 }
 
 // Mixed batches: MFMA tiles and row items in one launch. The tile path's
@@ -2191,8 +2514,11 @@ aug_status launch_rows(const Args<MOD>& a, const aug_attn_plan_info& info, hipSt
     // merged through partials. The VALU row path keeps four waves: its
     // register use would leave a compute unit a single eight-wave workgroup.
     constexpr int NW = ROW_MFMA && row_mfma_capable<KVT, D, G, QT>() ? 8 : 4;
-    hipLaunchKernelGGL((attn_rows_kernel<KVT, D, G, QT, OT, ROW_MFMA, NW, MOD>), dim3(info.num_items), dim3(64 * NW), 0,
-                       st, a);
+    if constexpr (KVT == KV_FP4)
+      hipLaunchKernelGGL((attn_rows_mx_kernel<G, NW, MOD>), dim3(info.num_items), dim3(64 * NW), 0, st, a);
+    else
+      hipLaunchKernelGGL((attn_rows_kernel<KVT, D, G, QT, OT, ROW_MFMA, NW, MOD>), dim3(info.num_items), dim3(64 * NW),
+                         0, st, a);
   }
   return AUG_OK;
 }
