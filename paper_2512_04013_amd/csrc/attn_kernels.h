@@ -1227,42 +1227,8 @@ struct MxBlock {
   int bid;
 };
 
-// The row's queries as the lane's operand: the codes of column l % 16 and the
-// exponent byte that goes with them. Made before an item's kind of loads is known;
-// made in both branches, the unconverted values stayed in registers through the
-// first one's loop.
-struct MxQuery {
-  v8i_t codes;
-  int byte;
-};
-template <int G>
-__device__ __forceinline__ MxQuery mx_query(const WorkItem& it, const AttnArgs& a) {
-  constexpr int D = 128;
-  const int j = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3, head = j & 7;
-  const uint16_t* qb = static_cast<const uint16_t*>(a.q) +
-                       (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(it.kvh) * G + head) * D + 16 * g;
-  float x[32];
-  float amax = 0.f;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const uint4 w = head < G ? *reinterpret_cast<const uint4*>(qb + 64 * (c >> 1) + 8 * (c & 1)) : uint4{0, 0, 0, 0};
-    unpack_bf16x8(w, x + 8 * c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[8 * c + e]));
-  }
-  const TwoCodes split(group4_max(amax));
-  MxQuery q;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint2 w = split(x + 4 * i);
-    q.codes[i] = static_cast<int>(j < 8 ? w.x : w.y);
-  }
-  q.byte = j < 8 ? split.byte : split.byte - TwoCodes::kRestLog2;
-  return q;
-}
-
 template <int OT, int NW, int G, bool STREAM, bool MOD>
-__device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, const MxQuery& q, float* lds) {
+__device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) {
   constexpr int D = 128;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1271,6 +1237,18 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, const MxQuer
   const int kvh = it.kvh;
   const int head = j & 7;
 
+  // The queries (dims 16g .. + 15 and 64 + 16g .. + 15 of the column's head) are on
+  // their way while the first blocks are asked for, and converted behind that.
+  uint4 raw[4];
+  {
+    const uint16_t* qb = static_cast<const uint16_t*>(a.q) +
+                         (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(kvh) * G + head) * D + 16 * g;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      raw[c] = head < G ? *reinterpret_cast<const uint4*>(qb + 64 * (c >> 1) + 8 * (c & 1)) : uint4{0, 0, 0, 0};
+  }
+  v8i_t qop;
+  int qbyte;
   const float sc = a.scale_log2;
   const int2 keys = row_keys<MOD>(a, it.q_row0, it.pos0);
   const float from = distance_from(it.pos0, keys);
@@ -1332,8 +1310,7 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, const MxQuer
       const v8i_t kop = {static_cast<int>(b.k.x), static_cast<int>(b.k.y), static_cast<int>(b.k.z),
                          static_cast<int>(b.k.w), 0, 0, 0, 0};
       f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
-      sacc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kop, q.codes, sacc, 4, 0, 0, static_cast<int>(b.ks), 0,
-                                                              q.byte);
+      sacc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kop, qop, sacc, 4, 0, 0, static_cast<int>(b.ks), 0, qbyte);
 #pragma unroll
       for (int r = 0; r < 4; ++r) sv[4 * i + r] = sacc[r] + lane8_other(sacc[r]);   // both codes of the query
     }
@@ -1420,6 +1397,26 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, const MxQuer
   int bi = 2 * wave;
   ids(bi);
   fetch(bi, p0);
+  {
+    float x[32];
+    float amax = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      // opaque: both kinds of loads convert them, and values that one kind shares
+      // with the other stay in registers through its loop
+      asm volatile("" : "+v"(raw[c].x), "+v"(raw[c].y), "+v"(raw[c].z), "+v"(raw[c].w));
+      unpack_bf16x8(raw[c], x + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[8 * c + e]));
+    }
+    const TwoCodes split(group4_max(amax));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint2 w = split(x + 4 * i);
+      qop[i] = static_cast<int>(j < 8 ? w.x : w.y);
+    }
+    qbyte = j < 8 ? split.byte : split.byte - TwoCodes::kRestLog2;
+  }
   for (; bi < nblk; bi += 4 * NW) {
     fetch(bi + 2 * NW, p1);
     compute(bi, p0);
@@ -2390,11 +2387,9 @@ __device__ __forceinline__ void attn_body(const Args<MOD>& a) {
   // row items always fetch a wave's next block while the current one is
   // computed: short spans (small batches) are latency bound otherwise
   float* lds = reinterpret_cast<float*>(smem);
-  MxQuery query;
-  if constexpr (KVT == KV_FP4) query = mx_query<G>(it, a);
   auto row = [&](auto stream_tag) {
     constexpr bool S = decltype(stream_tag)::value;
-    if constexpr (KVT == KV_FP4) row_item_mx<OT, NW, G, S, MOD>(it, a, query, lds);
+    if constexpr (KVT == KV_FP4) row_item_mx<OT, NW, G, S, MOD>(it, a, lds);
     else if constexpr (ROW_MFMA && row_mfma_capable<KVT, D, G, QT>()) row_item_mfma<KVT, OT, NW, G, S, MOD>(it, a, lds);
     else row_item<KVT, D, G, QT, OT, true, NW, S, MOD>(it, a, lds);
   };
@@ -2408,9 +2403,14 @@ __global__ __launch_bounds__(64 * NW) void attn_rows_kernel(Args<MOD> a) {
   attn_body<KVT, D, G, QT, OT, false, ROW_MFMA, NW, 0, MOD>(a);
 }
 
-// 4-bit rows: four waves a SIMD, two workgroups a compute unit, so at most 128
-// registers. HBM needs that many loads in flight: with one workgroup (172
-// registers) 512 decodes over 1.7M keys, 64/8 heads, took 351 us, with two XXX.
+// 4-bit rows: four waves a SIMD, so at most 128 registers; HBM needs that many loads
+// in flight (512 decodes over 1.7M keys, 64/8 heads: 351 us with two waves a SIMD,
+// 320 with four). Workgroups of eight waves make an item end sooner, of four waves
+// let a compute unit overlap the ends and starts of four items: eight / four waves
+// take 49.0 / 48.6 us for 512 items of 4000 keys, 10.4 / 8.7 for 512 of 300, 18.0 /
+// 13.6 for 1024 of 300, 315 / 309 for the 512 decodes, but 19.3 for 256 items of 4000
+// keys where four waves a CU would leave half of it empty.
+constexpr int kMxItems = 512;   // items from which workgroups have four waves
 template <int G, int NW, bool MOD>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4, 4))) void attn_rows_mx_kernel(Args<MOD> a) {
   attn_body<KV_FP4, 128, G, AUG_BF16, AUG_BF16, false, true, NW, 0, MOD>(a);
@@ -2514,8 +2514,12 @@ aug_status launch_rows(const Args<MOD>& a, const aug_attn_plan_info& info, hipSt
     // merged through partials. The VALU row path keeps four waves: its
     // register use would leave a compute unit a single eight-wave workgroup.
     constexpr int NW = ROW_MFMA && row_mfma_capable<KVT, D, G, QT>() ? 8 : 4;
-    if constexpr (KVT == KV_FP4)
-      hipLaunchKernelGGL((attn_rows_mx_kernel<G, NW, MOD>), dim3(info.num_items), dim3(64 * NW), 0, st, a);
+    if constexpr (KVT == KV_FP4) {
+      if (info.num_items >= kMxItems)
+        hipLaunchKernelGGL((attn_rows_mx_kernel<G, 4, MOD>), dim3(info.num_items), dim3(64 * 4), 0, st, a);
+      else
+        hipLaunchKernelGGL((attn_rows_mx_kernel<G, 8, MOD>), dim3(info.num_items), dim3(64 * 8), 0, st, a);
+    }
     else
       hipLaunchKernelGGL((attn_rows_kernel<KVT, D, G, QT, OT, ROW_MFMA, NW, MOD>), dim3(info.num_items), dim3(64 * NW),
                          0, st, a);

@@ -131,7 +131,7 @@ double merge_ns(int64_t partial_bytes) {
 // its total work spread evenly.
 double makespan_bound(double longest, double total) { return std::max(longest, total / kSlots); }
 
-int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, bool rows_only) {
+int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, bool rows_only, bool four_bits) {
   if (requested > 0) return ((requested + kBlock - 1) / kBlock) * kBlock;   // requested <= kMaxSplit
   // About four row items per compute unit (256 CUs), but never spans under
   // 512 keys (on small batches an item's fixed latency, query load, state
@@ -141,11 +141,13 @@ int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, 
   // Eight-wave row items (MFMA rows without tiles) take spans twice as long,
   // so that each wave streams as many keys as in a four-wave item. Four-wave
   // row items of a launch without tiles go up to 6144 keys (measured 3.5 %
-  // faster on 64 decodes over 16k-32k keys; beside tiles 4096 stays best).
+  // faster on 64 decodes over 16k-32k keys; beside tiles 4096 stays best). Rows over
+  // 4-bit KV stream twice as many keys in the same time and go up to 16384 (64
+  // decodes over 16k-32k keys, 32/8 heads, 297 -> 279 us).
   const int32_t f = wide_rows ? 2 : 1;
   int64_t s = (total_row_keys + 1024 / f - 1) / (1024 / f);
   s = std::max<int64_t>(s, 512 * f);
-  s = std::min<int64_t>(s, wide_rows ? 8192 : rows_only ? 6144 : 4096);
+  s = std::min<int64_t>(s, wide_rows ? (four_bits ? 16384 : 8192) : rows_only ? 6144 : 4096);
   return static_cast<int32_t>(((s + kBlock - 1) / kBlock) * kBlock);
 }
 
@@ -177,12 +179,18 @@ constexpr Prices kRowsAlone = {400, 3900, 1.4, 350, 0.35, 11000, 11000};
 // and middle mixed batches of every layer shape (with the prices above 64 decodes
 // beside two chunks at head_dim 64 took 31.2 instead of 29.4 us).
 constexpr Prices kBesideTiles = {2500, 1600, 4, 0, 0, 9000, 6400};
+// Rows alone over 4-bit KV, whose blocks go in pairs: fitted to 170 batches (4
+// layer shapes, 1 to 128 equal or lognormal decodes of 300 to 16000 keys) at up to
+// 15 splits each. The pick is within 2 % of the best one in the mean, 8 % with the
+// prices of the other rows (16 decodes of 1000 keys 12.7 -> 7.6 us).
+constexpr Prices kMxAlone = {530, 4800, 3.2, 350, 0.41, 5900, 6500};
 constexpr double kTileFixed = 4500;                                     // ns
 constexpr int32_t kSplits[] = {128, 192, 256, 384, 512, 768, 1024, 1280, 1536, 2048, 3072, 4096, 6144, 8192};
 constexpr int32_t kMaxIters = 8192 / kBlock;
 
 double block_latency_ns(const aug_attn_shape& s, bool mfma, bool rows_only) {
   const bool f32 = s.kv_dtype == AUG_F32, bf16 = s.kv_dtype == AUG_BF16;
+  if (s.kv_dtype == AUG_MXFP4) return rows_only ? 570 : 400;
   if (!rows_only) return s.head_dim == 64 ? (f32 ? 400 : 550) : f32 ? 1700 : bf16 ? 950 : mfma ? 630 : 1000;
   const int32_t g = s.num_q_heads / s.num_kv_heads;
   if (s.head_dim == 64) return g == 8 ? 1500 : f32 ? 750 : 840;
@@ -359,7 +367,7 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
   const int64_t part_bytes = partial_floats(g, s.head_dim) * 4;
   const int64_t max_parts =
       std::max<int64_t>(parts_before, static_cast<int64_t>(AUG_NOALLOC_SCRATCH_BYTES) / part_bytes - tile_partials - 1);
-  const Prices& price_of = rows_only ? kRowsAlone : kBesideTiles;
+  const Prices& price_of = !rows_only ? kBesideTiles : s.kv_dtype == AUG_MXFP4 ? kMxAlone : kRowsAlone;
   const double rate = row_kv_bytes >= kStreamBytes ? price_of.memory_rate : price_of.cached_rate;
   const double latency = block_latency_ns(s, mfma, rows_only);
   int32_t longest = 0;
@@ -567,7 +575,7 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
   const bool stream = streams_kv(*b, keys, hkv, decode_keys, key_bytes);
   // a launch without tiles runs MFMA row items on eight-wave workgroups
   const bool wide_rows = !any_tiled && row_path == AUG_ROWS_MFMA;
-  const int32_t split = choose_split(total_row_keys, kv_split_tokens, wide_rows, !any_tiled);
+  const int32_t split = choose_split(total_row_keys, kv_split_tokens, wide_rows, !any_tiled, s->kv_dtype == AUG_MXFP4);
   const int32_t pos_per_tile = kTileRows / g;
 
   // Keys per span of a split prefill tile. Splitting evens out the items but
