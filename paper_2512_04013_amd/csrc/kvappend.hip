@@ -233,17 +233,29 @@ __global__ __launch_bounds__(kThreads) void append_fp4_kernel(AppendArgs a) {
   const AppendItem it = load_item(a.items, unit / (2 * a.hkv));
   const int kvh = static_cast<int>((unit >> 1) % a.hkv);
   const bool is_v = unit & 1;
+  // the block id and the rows (a block has at most four for a lane) are on their
+  // way together
   const int32_t bid = a.block_ids[it.bt_index];
-  if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) return;
   const uint16_t* src = reinterpret_cast<const uint16_t*>(is_v ? a.v_new : a.k_new);
+  const int oct = lane % LPR, r0 = lane / LPR;
+  uint4 w[kBlock / RPP];
+#pragma unroll
+  for (int p = 0; p < kBlock / RPP; ++p) {
+    const int r = r0 + p * RPP;
+    w[p] = uint4{0u, 0u, 0u, 0u};
+    if (r < it.n_rows)
+      w[p] = *reinterpret_cast<const uint4*>(src + ((static_cast<int64_t>(it.q_row0) + r) * a.hkv + kvh) * D + 8 * oct);
+  }
+  if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) return;
   char* block = (is_v ? a.v_cache : a.k_cache) + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
   char* codes = block + kvh * aug::kMxCodes;
   char* scales = block + a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
-  const int oct = lane % LPR;
-  for (int r = lane / LPR; r < it.n_rows; r += RPP) {
-    const uint4 w = *reinterpret_cast<const uint4*>(src + ((static_cast<int64_t>(it.q_row0) + r) * a.hkv + kvh) * D + 8 * oct);
-    const float x[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y),
-                        bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
+#pragma unroll
+  for (int p = 0; p < kBlock / RPP; ++p) {
+    const int r = r0 + p * RPP;
+    if (r >= it.n_rows) break;
+    const float x[8] = {bf16_lo(w[p].x), bf16_hi(w[p].x), bf16_lo(w[p].y), bf16_hi(w[p].y),
+                        bf16_lo(w[p].z), bf16_hi(w[p].z), bf16_lo(w[p].w), bf16_hi(w[p].w)};
     float amax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));

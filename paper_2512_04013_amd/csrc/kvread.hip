@@ -36,43 +36,72 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
 }
 
+// Pieces that a lane makes, a workgroup's width apart: their slots, then their
+// cache words, are on their way together.
+constexpr int kPieces = 4;
+
 template <int KV, int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
   constexpr int PPR = D * (KV == AUG_F32 ? 4 : 2) / 16;      // pieces of one row and head
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= a.pieces) return;
   const int is_v = blockIdx.y;
-  const int piece = static_cast<int>(i % PPR);
-  const int64_t head_row = i / PPR;
-  const int kvh = static_cast<int>(head_row % a.hkv);
-  const int64_t slot = a.slots[head_row / a.hkv];
-  uint4 o{0u, 0u, 0u, 0u};
-  if (static_cast<uint64_t>(slot) < static_cast<uint64_t>(a.num_slots)) {
-    const int64_t block = slot / kBlock;
-    const int t = static_cast<int>(slot % kBlock);
-    const char* cache = a.cache[is_v];
-    if constexpr (KV == AUG_MXFP4) {
-      const char* base = cache + block * a.hkv * aug::kMxCell;
-      const char* codes = base + kvh * aug::kMxCodes + (is_v ? 256 * (t >> 2) + 16 * piece + 4 * (t & 3) : 64 * t + 4 * piece);
-      const char* scales = base + a.hkv * aug::kMxCodes + kvh * aug::kMxScales + (is_v ? 4 * (piece & ~3) + t : 4 * t + (piece >> 2));
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(codes);
-      const float s = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint8_t*>(scales)) << 23);
-      o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-      o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
-      o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-      o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
-    } else if constexpr (KV == AUG_FP8_E4M3FN) {
-      const uint2 w = *reinterpret_cast<const uint2*>(cache + (((block * a.hkv + kvh) * kBlock + t) * D + 8 * piece));
-      const float s = a.scale[is_v][block * a.hkv + kvh];
-      const auto p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, true);
-      const auto p2 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, false), p3 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, true);
-      o = uint4{bf16_pair(p0[0] * s, p0[1] * s), bf16_pair(p1[0] * s, p1[1] * s), bf16_pair(p2[0] * s, p2[1] * s),
-                bf16_pair(p3[0] * s, p3[1] * s)};
-    } else {
-      o = *reinterpret_cast<const uint4*>(cache + ((((block * a.hkv + kvh) * kBlock + t) * PPR + piece) << 4));
+  const char* cache = a.cache[is_v];
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads * kPieces) + threadIdx.x;
+  int64_t slot[kPieces];
+  int kvh[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u) {
+    const int64_t i = first + u * kThreads;
+    slot[u] = -1;
+    if (i < a.pieces) {
+      const uint32_t head_row = static_cast<uint32_t>(i / PPR);     // below 2^31
+      kvh[u] = static_cast<int>(head_row % a.hkv);
+      slot[u] = a.slots[head_row / a.hkv];
     }
   }
-  *reinterpret_cast<uint4*>(a.out[is_v] + (i << 4)) = o;
+  uint4 w[kPieces];
+  float scale[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u) {
+    w[u] = uint4{0u, 0u, 0u, 0u};
+    scale[u] = 0.f;
+    if (static_cast<uint64_t>(slot[u]) >= static_cast<uint64_t>(a.num_slots)) continue;
+    const int64_t block = slot[u] / kBlock;
+    const int t = static_cast<int>(slot[u] % kBlock);
+    const int piece = static_cast<int>((first + u * kThreads) % PPR);
+    if constexpr (KV == AUG_MXFP4) {
+      const char* base = cache + block * a.hkv * aug::kMxCell;
+      const char* codes = base + kvh[u] * aug::kMxCodes + (is_v ? 256 * (t >> 2) + 16 * piece + 4 * (t & 3) : 64 * t + 4 * piece);
+      const char* scales = base + a.hkv * aug::kMxCodes + kvh[u] * aug::kMxScales + (is_v ? 4 * (piece & ~3) + t : 4 * t + (piece >> 2));
+      w[u].x = *reinterpret_cast<const uint32_t*>(codes);
+      scale[u] = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint8_t*>(scales)) << 23);
+    } else if constexpr (KV == AUG_FP8_E4M3FN) {
+      const uint2 c = *reinterpret_cast<const uint2*>(cache + (((block * a.hkv + kvh[u]) * kBlock + t) * D + 8 * piece));
+      w[u].x = c.x;
+      w[u].y = c.y;
+      scale[u] = a.scale[is_v][block * a.hkv + kvh[u]];
+    } else {
+      w[u] = *reinterpret_cast<const uint4*>(cache + ((((block * a.hkv + kvh[u]) * kBlock + t) * PPR + piece) << 4));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u) {
+    const int64_t i = first + u * kThreads;
+    if (i >= a.pieces) return;
+    uint4 o = w[u];
+    const float s = scale[u];
+    if constexpr (KV == AUG_MXFP4) {
+      o = uint4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u].x, s, 0)),
+                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u].x, s, 1)),
+                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u].x, s, 2)),
+                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u].x, s, 3))};
+    } else if constexpr (KV == AUG_FP8_E4M3FN) {
+      const auto p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[u].x, false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[u].x, true);
+      const auto p2 = __builtin_amdgcn_cvt_pk_f32_fp8(w[u].y, false), p3 = __builtin_amdgcn_cvt_pk_f32_fp8(w[u].y, true);
+      o = uint4{bf16_pair(p0[0] * s, p0[1] * s), bf16_pair(p1[0] * s, p1[1] * s), bf16_pair(p2[0] * s, p2[1] * s),
+                bf16_pair(p3[0] * s, p3[1] * s)};
+    }
+    *reinterpret_cast<uint4*>(a.out[is_v] + (i << 4)) = o;
+  }
 }
 
 }  // namespace
@@ -105,7 +134,7 @@ extern "C" aug_status aug_kv_read(const aug_attn_shape* s, const void* k_cache, 
   a.pieces = n * s->num_kv_heads * (s->head_dim * (s->kv_dtype == AUG_F32 ? 4 : 2) / 16);
   a.num_slots = static_cast<int64_t>(num_pool_blocks) * kBlock;
   a.hkv = s->num_kv_heads;
-  const dim3 grid(static_cast<uint32_t>((a.pieces + kThreads - 1) / kThreads), 2);
+  const dim3 grid(static_cast<uint32_t>((a.pieces + kThreads * kPieces - 1) / (kThreads * kPieces)), 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
 #define AUG_READ(KV, D) hipLaunchKernelGGL((read_kernel<KV, D>), grid, dim3(kThreads), 0, st, a)
   if (s->kv_dtype == AUG_MXFP4) AUG_READ(AUG_MXFP4, 128);
