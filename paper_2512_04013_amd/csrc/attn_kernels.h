@@ -2049,6 +2049,23 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8rest[1], sacc[mb], 4, 0, 2, ksc[mb], 0,
                                                                    q4exp - TwoCodes::kRestLog2);
       }
+    } else if constexpr (MOD && FP8) {
+      // half the K operands at a time: with the staged codes of the next tile and
+      // the rows' spans there are no registers for all of them
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+        uint4 kop[KSTEPS];
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s)
+          kop[s] = *reinterpret_cast<const uint4*>(ks + (32 * mb + n) * L::KS + 16 * s + 8 * hh);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sacc[mb][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s)
+          sacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[s]), as_bf16x8(qreg[s]), sacc[mb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
       uint4 kop[2][KSTEPS];
 #pragma unroll
@@ -2140,6 +2157,9 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       vinv[b] = FP8 ? stage_scales[stage * L::NSC + 8 + b] : 1.f;
     }
     if constexpr (MOD) {
+      // a zero key scale is taken as 2^-100, or it would make NaN of masked scores
+#pragma unroll
+      for (int b = 0; b < 4; ++b) coef[b] = FP8 ? fmaxf(coef[b], 0x1p-100f) : coef[b];
       // the cap leaves -1 / (1 + 2^(..)) in the place of the raw score, with one
       // positive coefficient; the bias leaves the score itself
       if (a.cap_in != 0.f) {
@@ -2251,7 +2271,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = __builtin_amdgcn_exp2f(fmaf(sacc[mb][e0 + e], coef[s], bias));
-        pv[e] = live(mb, e0 + e) ? x : 0.f;
+        pv[e] = MOD || live(mb, e0 + e) ? x : 0.f;   // MOD: 2^-inf is zero, as no coefficient is
       }
       uint4 pw;
       pw.x = pack_bf16(pv[0], pv[1]);
@@ -2265,6 +2285,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       l_run = FP8 ? fmaf(bsum, vinv[s], l_run) : bsum;
       const bf16x8_t pop = as_bf16x8(pw);
       if constexpr (MOD) {
+        __builtin_amdgcn_sched_barrier(0);   // or they are all read ahead, into spilled registers
 #pragma unroll
         for (int db = 0; db < DB; ++db) vop[0][db] = v_operand(s, db);
       }
@@ -2293,9 +2314,11 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     }
   }
   if constexpr (MOD) {
-    for (; t < t1; ++t) {
-      if (t >= t_from && t < t_full) step(t, bool_tag<false>{});
-      else step(t, bool_tag<true>{});
+    // masked, whole, masked again: two loops in turn, since a choice within one loop
+    // copies the accumulators wherever its sides meet
+    for (int masked = min(t_from, t1); t < t1; masked = t1) {
+      for (; t < masked; ++t) step(t, bool_tag<true>{});
+      for (; t < t_full; ++t) step(t, bool_tag<false>{});
     }
   } else {
     for (; t < t_full; ++t) step(t, bool_tag<false>{});

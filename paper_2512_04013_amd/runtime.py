@@ -12,7 +12,7 @@ import time
 import numpy as np
 import torch
 
-from . import (AUG_MXFP4, MXFP4_CELL_BYTES, aug_attn_mixed, aug_attn_plan, aug_kv_append, aug_kv_park, aug_kv_read,
+from . import (AUG_F32, AUG_MXFP4, MXFP4_CELL_BYTES, aug_attn_mixed, aug_attn_plan, aug_kv_append, aug_kv_park, aug_kv_read,
                aug_kv_record_bytes, aug_kv_resume, aug_plan_upload, make_shape)
 
 _TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8, "fp4": torch.uint8}
@@ -44,6 +44,10 @@ class PagedKV:
             for t in (k_cache, v_cache):
                 if tuple(t.shape) != want or t.dtype != torch.uint8:
                     raise ValueError(f"a 4-bit pool is uint8 of shape {want}, got {t.dtype} {tuple(t.shape)}")
+        # what read() gives out, and where
+        self._row = (shape.num_kv_heads, shape.head_dim)
+        self._row_dtype = torch.float32 if shape.kv_dtype == AUG_F32 else torch.bfloat16
+        self._device = k_cache.get_device()
         self.record_bytes = aug_kv_record_bytes(shape)
         staging_bytes = max(self.record_bytes, (staging_bytes // self.record_bytes) * self.record_bytes)
         self.staging = torch.empty(staging_bytes, dtype=torch.uint8, device=k_cache.device)
@@ -65,19 +69,19 @@ class PagedKV:
         """The K and V rows ([n][H_kv][D], float32 for f32 pools, else bf16) of
         the tokens in ``slots`` (int64, block * 16 + slot): what ``append`` takes,
         so a request moves to a pool of another format. Returns (k, v)."""
-        if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
-            raise ValueError(f"slots must be a contiguous int64 vector, got {slots.dtype} {tuple(slots.shape)}")
-        if slots.device != self.k_cache.device:
-            raise ValueError(f"slots on {slots.device}, the pool on {self.k_cache.device}")
-        want = (slots.numel(), self.shape.num_kv_heads, self.shape.head_dim)
-        dtype = torch.float32 if self.shape.kv_dtype == 0 else torch.bfloat16
+        if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous() or \
+                slots.get_device() != self._device:
+            raise ValueError(f"slots must be a contiguous int64 vector on {self.k_cache.device}, got {slots.dtype} "
+                             f"{tuple(slots.shape)} on {slots.device}")
+        n = len(slots)
+        want, dtype = (n, *self._row), self._row_dtype
         k_out = torch.empty(want, dtype=dtype, device=slots.device) if k_out is None else k_out
         v_out = torch.empty(want, dtype=dtype, device=slots.device) if v_out is None else v_out
         for t in (k_out, v_out):
-            if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.device != slots.device:
+            if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.get_device() != self._device:
                 raise ValueError(f"K/V rows must be contiguous {dtype} of shape {want} on {slots.device}, got "
                                  f"{t.dtype} {tuple(t.shape)} on {t.device}")
-        aug_kv_read(self.shape, self.k_cache, self.v_cache, self.k_scale, self.v_scale, slots, slots.numel(),
+        aug_kv_read(self.shape, self.k_cache, self.v_cache, self.k_scale, self.v_scale, slots, n,
                     self.num_pool_blocks, k_out, v_out, stream=stream)
         return k_out, v_out
 
