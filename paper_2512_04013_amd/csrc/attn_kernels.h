@@ -2049,23 +2049,6 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8rest[1], sacc[mb], 4, 0, 2, ksc[mb], 0,
                                                                    q4exp - TwoCodes::kRestLog2);
       }
-    } else if constexpr (MOD && FP8) {
-      // half the K operands at a time: with the staged codes of the next tile and
-      // the rows' spans there are no registers for all of them
-      __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-      for (int mb = 0; mb < 2; ++mb) {
-        uint4 kop[KSTEPS];
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s)
-          kop[s] = *reinterpret_cast<const uint4*>(ks + (32 * mb + n) * L::KS + 16 * s + 8 * hh);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sacc[mb][e] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s)
-          sacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[s]), as_bf16x8(qreg[s]), sacc[mb], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
     } else {
       uint4 kop[2][KSTEPS];
 #pragma unroll
@@ -2285,7 +2268,6 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       l_run = FP8 ? fmaf(bsum, vinv[s], l_run) : bsum;
       const bf16x8_t pop = as_bf16x8(pw);
       if constexpr (MOD) {
-        __builtin_amdgcn_sched_barrier(0);   // or they are all read ahead, into spilled registers
 #pragma unroll
         for (int db = 0; db < DB; ++db) vop[0][db] = v_operand(s, db);
       }
