@@ -382,10 +382,10 @@ __device__ __forceinline__ float2 load_partial2(const float* p) {
 // since the partials come from other workgroups of this launch).
 template <int D, int G, int OT, int NT, bool MOD>
 __device__ __forceinline__ void merge_group_direct(const MergeGroup& g, const float* partials, void* out,
-                                                   int32_t hq) {
+                                                   int32_t hq, uint32_t tid) {
   const int64_t pf = aug::partial_floats(G, D);
   const float* base = partials + static_cast<int64_t>(g.part0) * pf;
-  for (int c = threadIdx.x; c < G * D / 4; c += NT) {
+  for (int c = tid; c < G * D / 4; c += NT) {
     const int h = (4 * c) / D;
     float mx = kNegBig, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
     int s = 0;
@@ -433,11 +433,11 @@ __device__ __forceinline__ void merge_group_direct(const MergeGroup& g, const fl
 // returns the counter to zero, so the plan image can be launched again.
 // `lds` needs one int and must be free when this is called.
 template <int D, int G, int OT, int NT, bool MOD>
-__device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n_rows, float* lds) {
+__device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n_rows, float* lds, uint32_t tid) {
   __builtin_amdgcn_s_waitcnt(0);   // this thread's partial stores have completed
   __syncthreads();
   int* flag = reinterpret_cast<int*>(lds);
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     const int done = __hip_atomic_fetch_add(a.counters + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool last = done == a.groups[group].n_parts - 1;
     if (last) __hip_atomic_store(a.counters + group, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -445,7 +445,8 @@ __device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n
   }
   __syncthreads();
   if (!*flag) return;
-  for (int r = 0; r < n_rows; ++r) merge_group_direct<D, G, OT, NT, MOD>(a.groups[group + r], a.partials, a.out, a.hq);
+  for (int r = 0; r < n_rows; ++r) 
+    merge_group_direct<D, G, OT, NT, MOD>(a.groups[group + r], a.partials, a.out, a.hq, tid);
 }
 
 // A value at a wave-uniform address that no kernel of the launch writes: a
@@ -470,12 +471,12 @@ constexpr int row_lds_stride(int d) { return d + 4; }
 // so that a group of eight heads is one pass over the workgroup with the
 // statistics read once, and partials leave in 8-byte stores.
 template <int D, int G, int OT, int NW, bool MOD>
-__device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnArgs& a, float* lds) {
+__device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnArgs& a, float* lds, uint32_t tid) {
   constexpr int ROW = row_lds_stride(D);
   constexpr int W = G * D >= 4 * 64 * NW ? 4 : 2;   // dims per thread
   const int kvh = it.kvh;
   __syncthreads();
-  for (int idx = threadIdx.x; idx < G * D / W; idx += 64 * NW) {
+  for (int idx = tid; idx < G * D / W; idx += 64 * NW) {
     const int h = idx * W / D;
     const int d = idx * W % D;
     float mw[NW];
@@ -510,7 +511,7 @@ __device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnAr
       }
     }
   }
-  if (it.part >= 0) finish_split<D, G, OT, 64 * NW, MOD>(a, it.group, 1, lds);
+  if (it.part >= 0) finish_split<D, G, OT, 64 * NW, MOD>(a, it.group, 1, lds, tid);
 }
 
 // Reduction of a row item's lane groups (lanes with equal `dl`; they differ
@@ -869,7 +870,7 @@ __device__ void row_item(const WorkItem& it, const Args<MOD>& a, float* lds) {
 #pragma unroll
     for (int h = 0; h < G; ++h) lds[(wave * G + h) * ROW + D] = mg[h];
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds);
+  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -1198,7 +1199,7 @@ __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds
       dst[D + 1] = l_tot;
     }
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds);
+  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -1241,8 +1242,12 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
   // their way while the first blocks are asked for, and converted behind that.
   uint4 raw[4];
   {
+    // opaque, and different for the two kinds of loads: what both have in common is
+    // made once before them, and then stays in registers through the first one's loop
+    int dim = 16 * g;
+    asm volatile("; queries, kind of loads %1" : "+v"(dim) : "n"(STREAM ? 1 : 0));
     const uint16_t* qb = static_cast<const uint16_t*>(a.q) +
-                         (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(kvh) * G + head) * D + 16 * g;
+                         (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(kvh) * G + head) * D + dim;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       raw[c] = head < G ? *reinterpret_cast<const uint4*>(qb + 64 * (c >> 1) + 8 * (c & 1)) : uint4{0, 0, 0, 0};
@@ -1256,6 +1261,9 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
   if constexpr (MOD) {
     if (a.slopes && head < G) slope = -kLog2e * a.slopes[kvh * G + head];
   }
+  // columns 8 .. 15 of P take what the rounding of columns 0 .. 7 to bf16 left over;
+  // the end adds them up
+  const float rest = j & 8 ? 1.f : 0.f;
   float m_run = kNegBig, l_run = 0.f;
   f32x4_t oacc[8];
 #pragma unroll
@@ -1359,8 +1367,10 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
     uint32_t pp[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      pp[r] = pack_bf16(__builtin_amdgcn_exp2f(fmaf(sv[2 * r], coef, -m_run)),
-                        __builtin_amdgcn_exp2f(fmaf(sv[2 * r + 1], coef, -m_run)));
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[2 * r], coef, -m_run));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(sv[2 * r + 1], coef, -m_run));
+      const uint32_t w = pack_bf16(e0, e1);
+      pp[r] = pack_bf16(fmaf(-bf16_lo(w), rest, e0), fmaf(-bf16_hi(w), rest, e1));
       l_run = dot2_bf16(pp[r], kBf16PairOne, l_run);        // exactly the packed probabilities
     }
     const bf16x8_t pop = as_bf16x8(uint4{pp[0], pp[1], pp[2], pp[3]});
@@ -1402,9 +1412,6 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
     float amax = 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      // opaque: both kinds of loads convert them, and values that one kind shares
-      // with the other stay in registers through its loop
-      asm volatile("" : "+v"(raw[c].x), "+v"(raw[c].y), "+v"(raw[c].z), "+v"(raw[c].w));
       unpack_bf16x8(raw[c], x + 8 * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[8 * c + e]));
@@ -1426,19 +1433,27 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
 
   // this wave's result for head j: dims 32g + 8r + b from oacc[b][r]
   constexpr int ROW = row_lds_stride(D);
-  const float l_tot = group4_sum(l_run);
-  if (j < G) {
-    float* dst = lds + (wave * G + j) * ROW;
+  float l_tot = group4_sum(l_run);
+  l_tot += lane8_other(l_tot);
+#pragma unroll
+  for (int b = 0; b < 8; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) oacc[b][r] += lane8_other(oacc[b][r]);
+  // the lane's number again, rather than registers that hold it through the loop
+  const int lane_end = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  const int je = lane_end & 15, ge = lane_end >> 4;
+  if (je < G) {
+    float* dst = lds + (wave * G + je) * ROW;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int b = 0; b < 8; ++b) dst[32 * g + 8 * r + b] = oacc[b][r];
-    if (g == 0) {
+      for (int b = 0; b < 8; ++b) dst[32 * ge + 8 * r + b] = oacc[b][r];
+    if (ge == 0) {
       dst[D] = m_run;
       dst[D + 1] = l_tot;
     }
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds);
+  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, 64 * wave + lane_end);
 }
 
 // ---------------------------------------------------------------------------
