@@ -94,7 +94,7 @@ typedef enum { AUG_ORDER_THETA = 0, AUG_ORDER_FCFS = 1, AUG_ORDER_SSJF = 2 } aug
  * into 0, 0.5, 1, 1.5, 2, 3, 4, 6) in groups of 32 dims of one token, each with
  * a power-of-two scale X as one byte X + 127 (the OCP microscaling format);
  * value = code * 2^X. A pool is [num_pool_blocks][num_kv_heads * 1088] bytes,
- * 16-byte aligned: of every block, first the codes of all heads, 1024 bytes
+ * 16-byte aligned (queries over them are finite): of every block, first the codes of all heads, 1024 bytes
  * each, then their scales, 64 bytes each. No k_scale and v_scale arrays.
  *   K: codes [16 tokens][128 dims], scales [16 tokens][4 groups]
  *   V: codes [4 token quads][16 octets of dims][4 tokens][8 dims],
@@ -238,7 +238,9 @@ aug_status aug_attn_plan_opts(const aug_attn_shape* shape, const aug_batch_desc*
  * one request (row_first at the start of the row's document), prefixes attended
  * from both sides (row_end at least the prefix's length, whose keys must be in
  * the cache by then) and any mixture of them; a row with row_end <= row_first
- * sees nothing. 0 <= row_first, row_end <= ctx_len of the request. */
+ * sees nothing. 0 <= row_first, row_end <= ctx_len of the request. Keys that no row
+ * of the request sees may hold anything, NaN too; keys that some row sees are
+ * finite, also for the other rows. */
 typedef struct {
   const int32_t* row_first;
   const int32_t* row_end;
@@ -314,7 +316,8 @@ aug_status aug_attn_mixed(const aug_attn_shape* shape, const aug_attn_plan_info*
  *   softcap > 0:   s = softcap * tanh(s / softcap); between AUG_SOFTCAP_MIN and
  *                  AUG_SOFTCAP_MAX, since s is then off by softcap * 2^-20. 0: no cap
  *   slopes:        s = s - slopes[h] * |i - t|, after the cap; device float32
- *                  [num_q_heads], finite, read when the kernel runs. NULL: no bias
+ *                  [num_q_heads], magnitudes below 2^100, read when the kernel runs.
+ *                  NULL: no bias
  *   reserved       zero */
 #define AUG_SOFTCAP_MIN 0.0009765625f
 #define AUG_SOFTCAP_MAX 4096.0f

@@ -301,9 +301,9 @@ def aug_attn_plan(shape: aug_attn_shape, q_start, ctx_len, bt_start, num_pool_bl
     (info, plan) with plan a numpy uint8 array of info.plan_bytes bytes."""
     L = lib()
     spans = [None if a is None else _i32(a) for a in (row_first, row_end)]
-    for a in spans:
-        if a is not None and a.shape != (int(q_start[-1]),):
-            raise ValueError(f"one span for each of {int(q_start[-1])} rows, got {a.shape}")
+    for a, given in zip(spans, (row_first, row_end)):
+        if a is not None and (a.shape != (int(q_start[-1]),) or (a != given).any()):
+            raise ValueError(f"one 32-bit span for each of {int(q_start[-1])} rows, got {a.shape}")
     mask = aug_row_mask(*(None if a is None else a.ctypes.data for a in spans))
     desc, keep = _batch_desc(q_start, ctx_len, bt_start, num_pool_blocks, block_ids)
     info = aug_attn_plan_info()

@@ -1747,11 +1747,14 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   }
   // MOD: tiles t_from .. t_full - 1 lie between the last first key and the first
   // end of the tile's rows, as the planner noted them
-  int t_from = t0, until = it.pos0 + 1;
+  // and no row sees a key before key_first, which may hold anything: the values (and
+  // scales) there are staged as zeros, as those past key_end are.
+  int t_from = t0, until = it.pos0 + 1, key_first = 0;
   if constexpr (MOD) {
     if (a.row_span) {
       t_from = (it.reserved[0] + 63) / 64;
       until = it.reserved[1];
+      key_first = it.reserved[2];
     }
   }
   const int t_full = bad && !DMA ? t0 : max(t0, min(t1, min(until, key_end) / 64));
@@ -1808,6 +1811,13 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         if (n < 3) vw4.z = 0u;
         if (n < 2) vw4.y = 0u;
         vs4 = n < 4 ? vs4 & ((1u << (8 * n)) - 1u) : vs4;
+        if (const int m = key_first - vtok; MOD && m > 0) {
+          vw4.x = 0u;
+          if (m > 1) vw4.y = 0u;
+          if (m > 2) vw4.z = 0u;
+          if (m > 3) vw4.w = 0u;
+          vs4 = m < 4 ? vs4 & ~((1u << (8 * m)) - 1u) : 0u;
+        }
       }
     }
   };
@@ -1837,7 +1847,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
                             static_cast<int64_t>(tok0 & 15) * D + 8 * tc) * EB;
 #pragma unroll
       for (int u = 0; u < KPT; ++u) {
-        if (ok && tok0 + u < key_end) {
+        if (ok && tok0 + u < key_end && (!MOD || tok0 + u >= key_first)) {
           kr[u] = *reinterpret_cast<const raw_t*>(kc + base + static_cast<int64_t>(u) * D * EB);
           vr[u] = *reinterpret_cast<const raw_t*>(vc + base + static_cast<int64_t>(u) * D * EB);
         } else {
@@ -1849,7 +1859,8 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     if constexpr (FP8) {
       if (threadIdx.x < 8) {
         const int b = (k0 >> 4) + (threadIdx.x & 3) - blk_first;
-        const int sb = (k0 + 16 * (threadIdx.x & 3)) < key_end ? ids[b] : -1;
+        const int block0 = k0 + 16 * (threadIdx.x & 3);
+        const int sb = block0 < key_end && (!MOD || block0 + 16 > key_first) ? ids[b] : -1;
         const float* sa = threadIdx.x < 4 ? a.k_scale : a.v_scale;
         sc_reg = static_cast<uint32_t>(sb) < static_cast<uint32_t>(a.num_pool_blocks)
                      ? sa[static_cast<int64_t>(sb) * a.hkv + kvh] : 1.f;
@@ -1964,12 +1975,12 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   auto settle_tile = [&](int t, int stage) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int tok0 = t * 64 + 16 * dma_wave;
-    if (dma_bid < 0 || tok0 + 16 > key_end) {
+    if (dma_bid < 0 || tok0 + 16 > key_end || (MOD && tok0 < key_first)) {
       const int first = dma_bid < 0 ? 0 : key_end - tok0;
       unsigned char* dst = smem + stage * L::STAGE + dma_wave * 16 * L::ROW;
 #pragma unroll
       for (int i = 0; i < 16 / RPI; ++i)
-        if (RPI * i + dma_row >= first) {
+        if (RPI * i + dma_row >= first || (MOD && tok0 + RPI * i + dma_row < key_first)) {
           *reinterpret_cast<uint4*>(dst + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
           if constexpr (DMA) *reinterpret_cast<uint4*>(dst + L::KBYTES + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
         }
@@ -2302,7 +2313,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   int t = t0;
   if constexpr (KDMA) issue_tile(t0, 0);
   if constexpr (!DMA) {
-    if (t0 < t_load) load_tile(t0 * 64, bool_tag<true>{});
+    if (t0 < t_load && (!MOD || t0 * 64 >= key_first)) load_tile(t0 * 64, bool_tag<true>{});
     else load_tile(t0 * 64, bool_tag<false>{});
     store_tile(0);
     if (t0 + 1 < t1) {

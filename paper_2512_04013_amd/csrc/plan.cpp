@@ -220,30 +220,40 @@ struct RowKeys {
   }
 };
 
-// A prefill tile: rows j0 .. j0 + n - 1 of request r and the keys that they read,
-// from a whole key tile on; all of them see every key of [full_lo, full_hi).
+// A prefill tile: rows j0 .. j0 + n - 1 of request r, the keys [first, hi) that they
+// see, read from `lo`, a whole key tile, on; all rows see every key of [full_lo,
+// full_hi).
 struct TileRows {
-  int32_t r, j0, n, lo, hi, full_lo, full_hi;
+  int32_t r, j0, n, lo, hi, first, full_lo, full_hi;
 };
 
+// The tile of rows j0 .. of request r, at most n of them. Under a mask it ends where
+// the rows' keys would leave a gap: every key between its first and its last one is
+// then seen by some row, so keys that no row sees (which may hold anything) are
+// never multiplied, and no key tile is read for nothing.
 TileRows tile_rows(const RowKeys& keys, int32_t r, int32_t j0, int32_t n) {
   if (!keys.masked()) {
     const Keys last = keys(r, j0 + n - 1);
-    return {r, j0, n, 0, last.hi, 0, keys(r, j0).hi};
+    return {r, j0, n, 0, last.hi, 0, 0, keys(r, j0).hi};
   }
-  TileRows t{r, j0, n, INT32_MAX, 0, 0, INT32_MAX};
-  for (int32_t j = j0; j < j0 + n; ++j) {
-    const Keys k = keys(r, j);
+  TileRows t{r, j0, 0, 0, 0, 0, 0, INT32_MAX};
+  for (; t.n < n; ++t.n) {
+    const Keys k = keys(r, j0 + t.n);
     if (k.none()) {
       t.full_hi = 0;
       continue;
     }
-    t.lo = std::min(t.lo, k.lo);
+    if (t.hi == 0) {
+      t.first = k.lo;
+    } else if (k.lo > t.hi || k.hi < t.first) {
+      break;
+    }
+    t.first = std::min(t.first, k.lo);
     t.hi = std::max(t.hi, k.hi);
     t.full_lo = std::max(t.full_lo, k.lo);
     t.full_hi = std::min(t.full_hi, k.hi);
   }
-  t.lo = t.hi > 0 ? t.lo / kKeyTile * kKeyTile : 0;
+  t.lo = t.first / kKeyTile * kKeyTile;
   return t;
 }
 
@@ -478,7 +488,7 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
     return fail(AUG_ERR_INVALID, "%s: unknown tile path %d", who, tile_path);
   if ((tile_path == AUG_TILES_FP8_QK || tile_path == AUG_TILES_FP8) && !tile_fp8qk_supported(*s))
     return fail(AUG_ERR_UNSUPPORTED, "%s: fp8 tile products need fp8 KV, bf16 queries and head_dim 128", who);
-  if (mask && tile_path != AUG_TILES_AUTO && tile_path != AUG_TILES_BF16)
+  if (mask && (mask->row_first || mask->row_end) && tile_path != AUG_TILES_AUTO && tile_path != AUG_TILES_BF16)
     return fail(AUG_ERR_UNSUPPORTED, "%s: a mask needs bf16 tile products", who);
   if (tile_path == AUG_TILES_AUTO) tile_path = AUG_TILES_BF16;   // fp8 tile products are opt-in
   if (!b || !info) return fail(AUG_ERR_INVALID, "%s: batch or info is NULL", who);
@@ -522,27 +532,29 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
     }
     const bool tiled = q > 1 && tiles_supported(*s);
     any_tiled = any_tiled || tiled;
-    if (keys.masked()) {
-      Keys all{INT32_MAX, 0};      // keys that some row of the request reads
-      int64_t sum = 0;
-      for (int32_t j = 0; j < q; ++j) {
-        const Keys k = keys(r, j);
-        if (k.lo < 0 || k.lo > ctx || k.hi < 0 || k.hi > ctx)
-          return fail(AUG_ERR_INVALID, "%s: row %d of request %d sees keys %d .. %d of %lld", who, j, r, k.lo, k.hi,
-                      (long long)ctx);
-        sum += k.count();
-        if (!k.none()) all = {std::min(all.lo, k.lo), std::max(all.hi, k.hi)};
-      }
-      if (!tiled) {
-        total_row_keys += sum * hkv;
-        row_kv_keys += static_cast<int64_t>(all.count()) * hkv;
-        if (q == 1) decode_keys += sum * hkv;
-      }
-    } else if (!tiled) {
+    if (!tiled && !keys.masked()) {
       // rows at positions ctx-q .. ctx-1 read pos+1 keys each
       total_row_keys += (q * (2 * ctx - q + 1) / 2) * hkv;
       row_kv_keys += ctx * hkv;
       if (q == 1) decode_keys += ctx * hkv;
+    }
+  }
+  // the rows' spans, once q_start is known to count them
+  for (int32_t r = 0; r < n && keys.masked(); ++r) {
+    const int32_t q = b->q_start[r + 1] - b->q_start[r], ctx = b->ctx_len[r];
+    Keys all{INT32_MAX, 0};      // keys that some row of the request reads
+    int64_t sum = 0;
+    for (int32_t j = 0; j < q; ++j) {
+      const Keys k = keys(r, j);
+      if (k.lo < 0 || k.lo > ctx || k.hi < 0 || k.hi > ctx)
+        return fail(AUG_ERR_INVALID, "%s: row %d of request %d sees keys %d .. %d of %d", who, j, r, k.lo, k.hi, ctx);
+      sum += k.count();
+      if (!k.none()) all = {std::min(all.lo, k.lo), std::max(all.hi, k.hi)};
+    }
+    if (q == 1 || !tiles_supported(*s)) {
+      total_row_keys += sum * hkv;
+      row_kv_keys += static_cast<int64_t>(all.count()) * hkv;
+      if (q == 1) decode_keys += sum * hkv;
     }
   }
   const int64_t total_rows = n > 0 ? b->q_start[n] : 0;
@@ -587,7 +599,7 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
   int32_t longest_tile = 0;
   for (int32_t r = 0; r < n && any_tiled; ++r) {
     const int32_t q = b->q_start[r + 1] - b->q_start[r];
-    for (int32_t j0 = 0; q > 1 && j0 < q; j0 += pos_per_tile) {
+    for (int32_t j0 = 0; q > 1 && j0 < q; j0 += tile_list.back().n) {
       tile_list.push_back(tile_rows(keys, r, j0, std::min(pos_per_tile, q - j0)));
       longest_tile = std::max(longest_tile, tile_list.back().hi - tile_list.back().lo);
     }
@@ -699,6 +711,7 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
         if (keys.masked()) {
           it.reserved[0] = t.full_lo;
           it.reserved[1] = t.full_hi;
+          it.reserved[2] = t.first;
         }
         const int64_t steps = (it.key_end - it.key_begin + kKeyTile - 1) / kKeyTile;
         tiles.push_back({it, tile_item_ns(steps), order++});

@@ -92,7 +92,7 @@ struct WorkItem {            // 48 bytes
   // -1 when not split.
   int32_t group;
   // plans with row spans, tiles: the last first key and the first end of the rows,
-  // between which every row sees every key
+  // between which every row sees every key, and the first key that any row sees
   int32_t reserved[3];
 };
 

@@ -239,3 +239,53 @@ def test_a_step_with_modified_scores_in_a_graph(layer):
     torch.cuda.synchronize()
     want, bound = reference(b, k, v, ks, vs, softcap=30.0, row_first=first, row_end=end)
     within(rt.to_host_f64(att.out), want, bound, "new slopes")
+
+
+@pytest.mark.parametrize("layer", ["f32-4x4-d64", "bf16-16x8-d64", "bf16-32x8-d128", "fp8-16x2-d128", "fp4-8x2-d128"])
+@pytest.mark.parametrize("mask", ["window", "padding", "far"])
+def test_keys_that_no_row_sees_may_hold_anything(layer, mask):
+    """NaN keys, values and scales wherever no row of the request looks: before a
+    window, between documents, behind a prefix. The results are those without."""
+    from paper_2512_04013_amd import runtime as rt
+    say(f"[scored NaN] {layer} {mask}")
+    b = _batch(layer, [1, 1, 140, 60, 2], [300, 77, 500, 333, 100], seed=16)
+    first, end = [], []
+    for r in range(b.num_reqs):
+        q, ctx = int(b.q_len[r]), int(b.ctx_len[r])
+        pos = np.arange(ctx - q, ctx)
+        lo, hi = np.zeros(q, int), pos + 1
+        if mask == "window":
+            lo = np.maximum(0, pos - 37)
+        elif mask == "padding":
+            lo = np.where(pos % 70 < 50, pos // 70 * 70, ctx)             # documents of 50 rows, 20 of padding
+            hi = np.where(pos % 70 < 50, pos + 1, 0)
+        else:
+            lo, hi = np.full(q, ctx // 3), np.full(q, ctx // 2)
+        first.append(lo)
+        end.append(hi)
+    first, end = np.concatenate(first).astype(np.int32), np.concatenate(end).astype(np.int32)
+    slopes = _slopes(b)
+    want, bound = reference(b, softcap=20.0, slopes=slopes, row_first=first, row_end=end)
+    h = b.num_kv_heads
+    for r in range(b.num_reqs):
+        seen = np.zeros(int(b.ctx_len[r]), bool)
+        for row in range(int(b.q_start[r]), int(b.q_start[r + 1])):
+            seen[first[row]:end[row]] = True
+        for t in np.nonzero(~seen)[0]:
+            blk, slot = b.blocks_of(r)[t // 16], t % 16
+            if b.kv_dtype == "fp4":
+                b.k_cache[blk, h * 1024:].reshape(h, 16, 4)[:, slot] = 255
+                b.v_cache[blk, h * 1024:].reshape(h, 4, 16)[:, :, slot] = 255
+            else:
+                nan = {"f32": np.float32(np.nan), "bf16": np.uint16(0x7FC0), "fp8": np.uint8(0x7F)}[b.kv_dtype]
+                b.k_cache[blk, :, slot] = nan
+                b.v_cache[blk, :, slot] = nan
+                if b.kv_dtype == "fp8" and not seen[t // 16 * 16:t // 16 * 16 + 16].any():
+                    b.k_scale[blk] = b.v_scale[blk] = np.nan
+    shape, kv, q, bids = rt.upload_batch(b)
+    for split in (0, 64):
+        att = rt.MixedAttention(shape, kv, b.q_start, b.ctx_len, b.bt_start, b.block_ids, bids, kv_split_tokens=split,
+                                row_first=first, row_end=end)
+        got = rt.to_host_f64(att.run(q, softcap=20.0, slopes=torch.from_numpy(slopes).cuda()))
+        torch.cuda.synchronize()
+        within(got, want, bound, f"{layer} {mask} split {split}")

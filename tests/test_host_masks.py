@@ -183,3 +183,34 @@ def test_row_spans():
     assert first.tolist() == [0, 0, 0, 0] and end.tolist() == [4, 4, 5, 9]
     first, end = row_spans(q_start, ctx, window=3, doc_start=[2, 2, 4, 0])
     assert first.tolist() == [2, 2, 4, 6] and end.tolist() == [3, 4, 5, 9]
+
+
+def test_tiles_end_where_no_row_sees_a_key():
+    """Rows of two documents with padding between them do not share a tile, and the
+    tiles' notes name the first key that a row sees."""
+    s = _shape()
+    ctx = 400
+    pos = np.arange(ctx)
+    first, end = np.where(pos < 110, 0, 150), pos + 1
+    end[110:150] = 0                                    # padding sees nothing, and nobody sees it
+    info, plan = aug.aug_attn_plan(s, [0, ctx], [ctx], [0, 25], 25, row_first=first, row_end=end)
+    items, _, _ = _items(plan, info)
+    for it in items[items["kvh"] == 0]:
+        rows = np.arange(it["q_row0"], it["q_row0"] + it["n_rows"])
+        live = rows[end[rows] > first[rows]]
+        if len(live):
+            assert (live < 110).all() or (live >= 150).all()
+            assert it["res2"][2] == first[live].min() and it["kb"] == it["res2"][2] // 64 * 64
+
+
+def test_malformed_batches_are_refused_before_their_spans_are_read():
+    """q_start that does not rise is refused, although spans of its last entry's
+    length were given: no span beyond them is looked at."""
+    s = _shape()
+    spans = np.zeros(5, np.int32)
+    for q_start in ([0, 1000000, 5], [0, 5, 5], [0, 7, 5]):
+        with pytest.raises(AugError) as e:
+            aug.aug_attn_plan(s, q_start, [1000000, 40], [0, 62500, 62503], 62503, row_first=spans, row_end=spans)
+        assert e.value.status == aug.AUG_ERR_INVALID and "rows" in str(e.value)
+    with pytest.raises(ValueError):
+        aug.aug_attn_plan(s, [0, 1], [40], [0, 3], 3, row_first=np.array([2 ** 32 + 1]))
