@@ -27,6 +27,11 @@
 //    lane-local plus one exchange between the two lane halves, and
 //    O^T = V^T P^T takes P straight from the S^T accumulators.
 //
+// 4-bit KV has row items of its own (row_item_mx), for every group size, and its
+// tiles multiply the key codes as they are. Modified scores (tanh cap, bias by
+// distance, a span of keys for every row: MOD) are instantiations beside the plain
+// ones, which have none of their arguments or registers.
+//
 // Keys past a request's context (tail of its last block) and blocks it does
 // not list never reach the arithmetic: their loads are skipped (zero-filled)
 // and their scores masked, so NaN or garbage in unused slots cannot leak.
@@ -101,6 +106,12 @@ struct AttnArgs {
 // log2 domain the cap is -2 cap log2(e) / (1 + 2^(2 s log2(e) / cap)): tanh(x) = 1 -
 // 2 / (1 + e^2x), less the constant cap that every key of a row shares. It is off
 // by about cap * 2^-21 (one exp2 and one reciprocal of a value in 0 .. 1).
+//
+// What bounds them: rows stay bound by their K/V (256 decodes with a window of 1024
+// keys and a cap, 32/8 heads, bf16: 174 us, 6.1 TB/s). Tiles are bound by their vector
+// instructions, which hardly overlap with the MFMAs at two waves a SIMD: a cap adds
+// two quarter-rate instructions to the one of the softmax, per score (fp8, 64/8
+// heads, a step of two workgroups on a compute unit: 2.3 us plain, 3.4 capped).
 struct ScoreArgs : AttnArgs {
   const int2* row_span;   // first and one past the last key of every row; NULL: causal
   const float* slopes;    // per query head; NULL: no bias
@@ -445,7 +456,7 @@ __device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n
   }
   __syncthreads();
   if (!*flag) return;
-  for (int r = 0; r < n_rows; ++r) 
+  for (int r = 0; r < n_rows; ++r)
     merge_group_direct<D, G, OT, NT, MOD>(a.groups[group + r], a.partials, a.out, a.hq, tid);
 }
 
@@ -1221,7 +1232,10 @@ __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds
 //     dim 8m + b. A lane's V is one 16-byte cell a block (four tokens of eight
 //     dims), converted to bf16 with the tokens' scales and paired by tokens.
 // Bound by HBM: a pair of blocks is 4352 bytes, 1670 cycles of a SIMD's share of the
-// card's rate, and about 150 vector instructions.
+// card's rate, and about 170 vector instructions. 512 decodes over 1.7M keys, 64/8
+// heads: 310 us, 6.2 TB/s, where bare loads of the same cells reach 6.7; what is left
+// is the start and end of 4096 items. One block at a time, with the keys converted
+// for four 16x16x32 MFMAs, took 320 us and had no room for the rest columns.
 struct MxBlock {
   uint4 k, v;              // codes
   uint32_t ks, vs;         // scale byte of the lane's keys' group, and of its four tokens' values
@@ -1318,7 +1332,8 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
       const v8i_t kop = {static_cast<int>(b.k.x), static_cast<int>(b.k.y), static_cast<int>(b.k.z),
                          static_cast<int>(b.k.w), 0, 0, 0, 0};
       f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
-      sacc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kop, qop, sacc, 4, 0, 0, static_cast<int>(b.ks), 0, qbyte);
+      sacc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kop, qop, sacc, 4, 0, 0, static_cast<int>(b.ks), 0,
+                                                              qbyte);
 #pragma unroll
       for (int r = 0; r < 4; ++r) sv[4 * i + r] = sacc[r] + lane8_other(sacc[r]);   // both codes of the query
     }
@@ -1562,7 +1577,9 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   // their scales as they are: 16 bytes of a key for 32 dims from LDS instead of 64.
   // A query element has 8 significant bits and goes in as the sum of two E4M3 codes
   // of 4 bits (its value rounded, and 32 times the rest), which is exact down to
-  // 2^-14 of its vector's largest magnitude, and 2^-21 of that off below.
+  // 2^-14 of its vector's largest magnitude, and 2^-21 of that off below. 16 chunks of
+  // 512 rows, 64/8 heads: 402 us with the keys converted to bf16 on their way into
+  // LDS, 383 so (971 TFLOP/s; a large bf16 matrix product reaches 1227 on the card).
   constexpr bool QK4 = L::K4;
   constexpr bool KDMA = DMA || QK8 || QK4;   // the keys, at least, come by direct loads
   constexpr bool PV8 = F8 >= 2;
@@ -1798,7 +1815,8 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     if (threadIdx.x < 64) {
       const int ktok = k0 + threadIdx.x;
       if (const int bid = block_of(ktok); FULL || bid >= 0)
-        ks4 = *reinterpret_cast<const uint32_t*>(kc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell + scales + 4 * (ktok & 15));
+        ks4 = *reinterpret_cast<const uint32_t*>(kc + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell + scales +
+                                                 4 * (ktok & 15));
     }
     const int vtok = k0 + 4 * quad4;
     if (const int bid = block_of(vtok); FULL || bid >= 0) {
@@ -2059,8 +2077,8 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
           kop[mb][h] = v8i_t{static_cast<int>(w.x), static_cast<int>(w.y), static_cast<int>(w.z), static_cast<int>(w.w),
                              0, 0, 0, 0};
         }
-        ksc[mb] = static_cast<int>(*reinterpret_cast<const uint32_t*>(smem + stage * L::STAGE + 64 * L::ROW + 4 * (32 * mb + n)) >>
-                                   (8 * hh));
+        const auto* words = reinterpret_cast<const uint32_t*>(smem + stage * L::STAGE + 64 * L::ROW);
+        ksc[mb] = static_cast<int>(words[32 * mb + n] >> (8 * hh));
       }
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(0);
@@ -2068,12 +2086,15 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       for (int mb = 0; mb < 2; ++mb) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sacc[mb][e] = 0.f;
-        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8[0], sacc[mb], 4, 0, 0, ksc[mb], 0, q4exp);
-        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8[1], sacc[mb], 4, 0, 2, ksc[mb], 0, q4exp);
-        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8rest[0], sacc[mb], 4, 0, 0, ksc[mb], 0,
-                                                                   q4exp - TwoCodes::kRestLog2);
-        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8rest[1], sacc[mb], 4, 0, 2, ksc[mb], 0,
-                                                                   q4exp - TwoCodes::kRestLog2);
+        const int rest = q4exp - TwoCodes::kRestLog2;
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8[0], sacc[mb], 4, 0, 0, ksc[mb], 0,
+                                                                   q4exp);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8[1], sacc[mb], 4, 0, 2, ksc[mb], 0,
+                                                                   q4exp);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][0], q8rest[0], sacc[mb], 4, 0, 0, ksc[mb],
+                                                                   0, rest);
+        sacc[mb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop[mb][1], q8rest[1], sacc[mb], 4, 0, 2, ksc[mb],
+                                                                   0, rest);
       }
     } else {
       uint4 kop[2][KSTEPS];

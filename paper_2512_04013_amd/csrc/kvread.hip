@@ -4,7 +4,8 @@
 // A lane makes 16 bytes of one output row (8 bf16 or 4 floats); lanes of a wave
 // cover consecutive pieces of consecutive rows, so stores are whole lines. A
 // row's slot is one 8-byte load, the same for the lanes of the row. HBM-bound:
-// the cache row in, the decoded row out.
+// the cache row in, the decoded row out. 16 fp8 requests, 31k rows of 64/8 heads:
+// 38.6 us, 5.0 TB/s in and out (a large copy reaches 4.8), 52.7 with one piece a lane.
 
 #include <hip/hip_runtime.h>
 
@@ -70,8 +71,10 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
     const int piece = static_cast<int>((first + u * kThreads) % PPR);
     if constexpr (KV == AUG_MXFP4) {
       const char* base = cache + block * a.hkv * aug::kMxCell;
-      const char* codes = base + kvh[u] * aug::kMxCodes + (is_v ? 256 * (t >> 2) + 16 * piece + 4 * (t & 3) : 64 * t + 4 * piece);
-      const char* scales = base + a.hkv * aug::kMxCodes + kvh[u] * aug::kMxScales + (is_v ? 4 * (piece & ~3) + t : 4 * t + (piece >> 2));
+      const char* codes = base + kvh[u] * aug::kMxCodes;
+      const char* scales = base + a.hkv * aug::kMxCodes + kvh[u] * aug::kMxScales;
+      codes += is_v ? 256 * (t >> 2) + 16 * piece + 4 * (t & 3) : 64 * t + 4 * piece;
+      scales += is_v ? 4 * (piece & ~3) + t : 4 * t + (piece >> 2);      // group piece / 4
       w[u].x = *reinterpret_cast<const uint32_t*>(codes);
       scale[u] = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint8_t*>(scales)) << 23);
     } else if constexpr (KV == AUG_FP8_E4M3FN) {
