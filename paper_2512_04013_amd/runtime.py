@@ -7,6 +7,7 @@ the device memory and the stream); the arithmetic runs in libaug.so.
 
 from __future__ import annotations
 
+import contextlib
 import time
 
 import numpy as np
@@ -29,6 +30,16 @@ def to_device_array(x: np.ndarray, dtype: str, device) -> torch.Tensor:
 
 def to_host_f64(t: torch.Tensor) -> np.ndarray:
     return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _allocating_on(stream, device):
+    """Context in which torch allocates from ``stream`` (a torch stream, a raw
+    handle, or None for the current one)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 class PagedKV:
@@ -68,15 +79,21 @@ class PagedKV:
     def read(self, slots: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
         """The K and V rows ([n][H_kv][D], float32 for f32 pools, else bf16) of
         the tokens in ``slots`` (int64, block * 16 + slot): what ``append`` takes,
-        so a request moves to a pool of another format. Returns (k, v)."""
+        so a request moves to a pool of another format. Returns (k, v). Rows that
+        are allocated here belong to ``stream``, as if it were torch's current
+        one: another stream waits for it before it reads them."""
         if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous() or \
                 slots.get_device() != self._device:
             raise ValueError(f"slots must be a contiguous int64 vector on {self.k_cache.device}, got {slots.dtype} "
                              f"{tuple(slots.shape)} on {slots.device}")
         n = len(slots)
         want, dtype = (n, *self._row), self._row_dtype
-        k_out = torch.empty(want, dtype=dtype, device=slots.device) if k_out is None else k_out
-        v_out = torch.empty(want, dtype=dtype, device=slots.device) if v_out is None else v_out
+        if k_out is None or v_out is None:
+            # on the stream that writes them: memory that the current stream gave
+            # back may still be in use there
+            with _allocating_on(stream, slots.device):
+                k_out = torch.empty(want, dtype=dtype, device=slots.device) if k_out is None else k_out
+                v_out = torch.empty(want, dtype=dtype, device=slots.device) if v_out is None else v_out
         for t in (k_out, v_out):
             if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.get_device() != self._device:
                 raise ValueError(f"K/V rows must be contiguous {dtype} of shape {want} on {slots.device}, got "
