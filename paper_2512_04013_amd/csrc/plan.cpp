@@ -131,6 +131,8 @@ double merge_ns(int64_t partial_bytes) {
 // its total work spread evenly.
 double makespan_bound(double longest, double total) { return std::max(longest, total / kSlots); }
 
+constexpr int32_t kBesideTilesMax = 4096;   // longest row span of the split by size beside tiles
+
 int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, bool rows_only, bool four_bits) {
   if (requested > 0) return ((requested + kBlock - 1) / kBlock) * kBlock;   // requested <= kMaxSplit
   // About four row items per compute unit (256 CUs), but never spans under
@@ -147,7 +149,7 @@ int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, 
   const int32_t f = wide_rows ? 2 : 1;
   int64_t s = (total_row_keys + 1024 / f - 1) / (1024 / f);
   s = std::max<int64_t>(s, 512 * f);
-  s = std::min<int64_t>(s, wide_rows ? (four_bits ? 16384 : 8192) : rows_only ? 6144 : 4096);
+  s = std::min<int64_t>(s, wide_rows ? (four_bits ? 16384 : 8192) : rows_only ? 6144 : kBesideTilesMax);
   return static_cast<int32_t>(((s + kBlock - 1) / kBlock) * kBlock);
 }
 
@@ -335,7 +337,7 @@ struct RowLoad {           // rows that become row items
 
 // The split of the row items when the caller leaves it to the planner. `before`
 // is the split by size that prefill tiles were cut against and `tiles` their
-// items. Launches of many items keep it: their rounds even out (spans of one
+// items. Launches of many row items keep it: their rounds even out (spans of one
 // resident workgroup's share of all keys, twice as long, were no faster with
 // head_dim 128 and up to 14 % slower with 64: 300 decodes over 393k keys, 8/8
 // heads, 132 -> 150 us).
@@ -369,9 +371,20 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
     }
     return n;
   };
-  const int64_t n_before = count(before);
+  int64_t n_before = count(before);
   const int64_t parts_before = parts;
   constexpr int64_t kManyItems = 4 * kSlots;
+  // The split by size wants four row items per compute unit, tiles or not. Where both
+  // together are many, the rows go in the longest spans that it knows beside tiles: 64
+  // decodes beside 2048 tiles (fp8, 64/8 heads) 173 -> 161 us, beside 880 (bf16, 32/8)
+  // 237 -> 229, 250 beside 128 (head_dim 64, 16/8) 119 -> 115; with masks and caps alike.
+  // Of 12 such batches, plain, capped and masked, the worst lost 3 % (48 decodes beside
+  // 1152 tiles of prefixes, head_dim 64: 144 -> 148), most gained 2-8. Below the limit
+  // every split is priced.
+  if (!rows_only && n_before >= kManyItems) {
+    before = std::max(before, kBesideTilesMax);
+    n_before = count(before);
+  }
   if (n_before >= kManyItems) return before;
   // a batch that fits the library's own scratch array keeps fitting it
   const int64_t part_bytes = partial_floats(g, s.head_dim) * 4;
@@ -604,11 +617,6 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
       longest_tile = std::max(longest_tile, tile_list.back().hi - tile_list.back().lo);
     }
   }
-  // Tiles that fill the GPU twice over leave nothing to gain from many short row
-  // items (64 decodes over 180k keys beside 2048 capped tiles, fp8, 64/8 heads: 274 us
-  // cut by size, 259 in spans of 4096). Plans without a mask keep their cut.
-  if (keys.masked() && kv_split_tokens <= 0 && static_cast<int64_t>(tile_list.size()) * hkv >= 2 * kSlots)
-    split = std::max(split, 4096);
   if (longest_tile > kTileSpanMin) {
     double row_total = 0.0, row_longest = 0.0;
     int64_t row_partial_bytes = 0;
