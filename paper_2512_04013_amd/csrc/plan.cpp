@@ -144,8 +144,8 @@ int32_t choose_split(int64_t total_row_keys, int32_t requested, bool wide_rows, 
   // so that each wave streams as many keys as in a four-wave item. Four-wave
   // row items of a launch without tiles go up to 6144 keys (measured 3.5 %
   // faster on 64 decodes over 16k-32k keys; beside tiles 4096 stays best). Rows over
-  // 4-bit KV stream twice as many keys in the same time and go up to 16384 (64
-  // decodes over 16k-32k keys, 32/8 heads, 297 -> 279 us).
+  // 4-bit KV stream twice as many keys in the same time and go up to 16384 (32/8
+  // heads: 64 decodes of 32768 keys 375 -> 362 us, 128 of 16k-32k 553 -> 545).
   const int32_t f = wide_rows ? 2 : 1;
   int64_t s = (total_row_keys + 1024 / f - 1) / (1024 / f);
   s = std::max<int64_t>(s, 512 * f);
@@ -447,6 +447,7 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
     price(split);
     if (split >= longest) break;                 // nothing splits from here on
   }
+  if (!priced_before && before > kSplits[std::size(kSplits) - 1]) price(before);   // 4-bit rows (64 decodes of 16k-32k keys 298 -> 288 us)
   return best;
 }
 

@@ -1,5 +1,5 @@
 """What the planner cuts its row items by: the same beside many tiles with a mask
-as without one."""
+as without one, and by its prices wherever it prices."""
 
 import os
 
@@ -41,3 +41,16 @@ def test_causal_spans_cut_the_rows_as_no_spans_do(layer, chunks, rows, prior, de
     for f in FIELDS.names[:-1]:
         assert np.array_equal(a[f], b[f]), f
     assert info.num_partials == minfo.num_partials and info.kv_split_tokens == minfo.kv_split_tokens
+
+def test_long_four_bit_contexts_are_cut_by_price_too():
+    """Spans over 8192 keys are among the priced ones: 64 contexts of 16384 keys stay
+    whole (181 us; two spans of 8192 each: 187), those of 16k to 32k keys go in
+    halves (288 and 298 us)."""
+    for hq in (8, 32, 64):
+        shape = aug.make_shape(hq, 8, 128, "bf16", "fp4", "bf16", 0.1)
+        info, items = _plan(shape, [1] * 64, [16384] * 64)
+        assert info.num_items == 512 and info.num_partials == 0
+        ctx = np.random.default_rng(1).integers(16385, 32769, 64)
+        info, items = _plan(shape, [1] * 64, ctx)
+        span = items["ke"] - items["kb"]
+        assert info.num_items == 1024 and (span > 8192).all() and (span <= 16384).all()
