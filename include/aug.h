@@ -299,7 +299,9 @@ aug_status aug_plan_upload(const void* host_src, void* dev_dst, size_t bytes, vo
  *   workspace  >= info->workspace_bytes bytes (split-K partials); contents on
  *              entry do not matter
  * Slots past a request's context and blocks it does not list never influence
- * its output, whatever they hold. Enqueued on `stream` as one kernel launch:
+ * its output, whatever they hold. Keys of a block id outside the pool (in a table
+ * that the planner has not checked) count for nothing, and a row that has no other
+ * gives zeros. Enqueued on `stream` as one kernel launch:
  * split decode rows are merged in it by the workgroup that finishes each
  * row's last span; split prefill tiles are merged by a second small launch
  * when info->num_tile_merge_groups > 0.

@@ -35,7 +35,8 @@
 // Keys past a request's context (tail of its last block) and blocks it does
 // not list never reach the arithmetic: their loads are skipped (zero-filled)
 // and their scores masked, so NaN or garbage in unused slots cannot leak.
-// Block ids outside the pool are treated the same way (never dereferenced).
+// Block ids outside the pool are treated the same way (never dereferenced); a row
+// that they leave without keys gives zeros.
 //
 // Split-K: an item whose keys were split writes an unnormalised partial
 // (o, m, l) per row to the workspace. A decode row's span then counts itself
@@ -143,7 +144,8 @@ __device__ __forceinline__ float capped(const ScoreArgs& a, float x) {
   else return a.cap_out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a.cap_in * x));
 }
 
-__device__ __forceinline__ float over_sum(float o, float l, bool mod) { return mod && l == 0.f ? 0.f : o / l; }
+// A row that no key is left to (its mask, or blocks outside the pool) gives zeros.
+__device__ __forceinline__ float over_sum(float o, float l) { return l == 0.f ? 0.f : o / l; }
 
 // ---------------------------------------------------------------------------
 // small helpers
@@ -391,7 +393,7 @@ __device__ __forceinline__ float2 load_partial2(const float* p) {
 // folds four output dims of one head over all spans online, its loads of
 // (m, l) and of the partial values all independent (device-scope loads,
 // since the partials come from other workgroups of this launch).
-template <int D, int G, int OT, int NT, bool MOD>
+template <int D, int G, int OT, int NT>
 __device__ __forceinline__ void merge_group_direct(const MergeGroup& g, const float* partials, void* out,
                                                    int32_t hq, uint32_t tid) {
   const int64_t pf = aug::partial_floats(G, D);
@@ -429,7 +431,7 @@ __device__ __forceinline__ void merge_group_direct(const MergeGroup& g, const fl
       fold(load_partial(p + G * D + h), load_partial(p + G * D + G + h), load_partial2(p + 4 * c),
            load_partial2(p + 4 * c + 2));
     }
-    const float inv = MOD && l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t off = (static_cast<int64_t>(g.q_row) * hq + static_cast<int64_t>(g.kvh) * G) * D + 4 * c;
     store_out<OT>(out, off + 0, o0 * inv);
     store_out<OT>(out, off + 1, o1 * inv);
@@ -443,7 +445,7 @@ __device__ __forceinline__ void merge_group_direct(const MergeGroup& g, const fl
 // (merge groups `group` .. `group + n_rows - 1`, which share their spans) and
 // returns the counter to zero, so the plan image can be launched again.
 // `lds` needs one int and must be free when this is called.
-template <int D, int G, int OT, int NT, bool MOD>
+template <int D, int G, int OT, int NT>
 __device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n_rows, float* lds, uint32_t tid) {
   __builtin_amdgcn_s_waitcnt(0);   // this thread's partial stores have completed
   __syncthreads();
@@ -457,7 +459,7 @@ __device__ __forceinline__ void finish_split(const AttnArgs& a, int group, int n
   __syncthreads();
   if (!*flag) return;
   for (int r = 0; r < n_rows; ++r)
-    merge_group_direct<D, G, OT, NT, MOD>(a.groups[group + r], a.partials, a.out, a.hq, tid);
+    merge_group_direct<D, G, OT, NT>(a.groups[group + r], a.partials, a.out, a.hq, tid);
 }
 
 // A value at a wave-uniform address that no kernel of the launch writes: a
@@ -481,7 +483,7 @@ constexpr int row_lds_stride(int d) { return d + 4; }
 // split-K partial. A thread takes up to four neighbouring dims of one head,
 // so that a group of eight heads is one pass over the workgroup with the
 // statistics read once, and partials leave in 8-byte stores.
-template <int D, int G, int OT, int NW, bool MOD>
+template <int D, int G, int OT, int NW>
 __device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnArgs& a, float* lds, uint32_t tid) {
   constexpr int ROW = row_lds_stride(D);
   constexpr int W = G * D >= 4 * 64 * NW ? 4 : 2;   // dims per thread
@@ -511,7 +513,7 @@ __device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnAr
     if (it.part < 0) {
       const int64_t off = (static_cast<int64_t>(it.q_row0) * a.hq + static_cast<int64_t>(kvh) * G + h) * D + d;
 #pragma unroll
-      for (int k = 0; k < W; ++k) store_out<OT>(a.out, off + k, over_sum(os[k], ls, MOD));
+      for (int k = 0; k < W; ++k) store_out<OT>(a.out, off + k, over_sum(os[k], ls));
     } else {
       float* pp = a.partials + static_cast<int64_t>(it.part) * aug::partial_floats(G, D);
 #pragma unroll
@@ -522,7 +524,7 @@ __device__ __forceinline__ void row_merge_waves(const WorkItem& it, const AttnAr
       }
     }
   }
-  if (it.part >= 0) finish_split<D, G, OT, 64 * NW, MOD>(a, it.group, 1, lds, tid);
+  if (it.part >= 0) finish_split<D, G, OT, 64 * NW>(a, it.group, 1, lds, tid);
 }
 
 // Reduction of a row item's lane groups (lanes with equal `dl`; they differ
@@ -881,7 +883,7 @@ __device__ void row_item(const WorkItem& it, const Args<MOD>& a, float* lds) {
 #pragma unroll
     for (int h = 0; h < G; ++h) lds[(wave * G + h) * ROW + D] = mg[h];
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, threadIdx.x);
+  row_merge_waves<D, G, OT, NW>(it, a, lds, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -1210,7 +1212,7 @@ __device__ void row_item_mfma(const WorkItem& it, const Args<MOD>& a, float* lds
       dst[D + 1] = l_tot;
     }
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, threadIdx.x);
+  row_merge_waves<D, G, OT, NW>(it, a, lds, threadIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -1468,7 +1470,7 @@ __device__ void row_item_mx(const WorkItem& it, const Args<MOD>& a, float* lds) 
       dst[D + 1] = l_tot;
     }
   }
-  row_merge_waves<D, G, OT, NW, MOD>(it, a, lds, 64 * wave + lane_end);
+  row_merge_waves<D, G, OT, NW>(it, a, lds, 64 * wave + lane_end);
 }
 
 // ---------------------------------------------------------------------------
@@ -1774,7 +1776,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       key_first = it.reserved[2];
     }
   }
-  const int t_full = bad && !DMA ? t0 : max(t0, min(t1, min(until, key_end) / 64));
+  const int t_full = bad ? t0 : max(t0, min(t1, min(until, key_end) / 64));
   const int t_load = !MOD ? t_full : bad ? t0 : key_end / 64;   // tiles loaded without conditions
 
   // fp8 through registers (bf16 takes none of this): a thread stages KPT
@@ -2177,7 +2179,24 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
         for (int e = 0; e < 16; ++e)
           if (!live(mb, e)) sacc[mb][e] = -INFINITY;
     };
-    if constexpr (MASK && !MOD) mask();
+    // Keys of a block outside the pool; items that have such take masked steps only. The
+    // branch costs up to 2 % (64 chunks of 32 rows 13.7 -> 14.0 us, 8 of 1000 278 ->
+    // 279); a loop of its own for these items cost 5 % in spilled registers.
+    const auto mask_bad = [&] {
+      if (!bad) return;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int tok0 = k0 + 16 * b;
+        const int bid = __builtin_amdgcn_readfirstlane(tok0 < key_end ? ids[(tok0 >> 4) - blk_first] : 0);
+        if (static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks)) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sacc[b >> 1][8 * (b & 1) + e] = -INFINITY;
+      }
+    };
+    if constexpr (MASK && !MOD) {
+      mask();
+      mask_bad();
+    }
     // log2-domain coefficient of the raw score, per block (fp8: K scale folded in)
     float coef[4], vlog[4], vinv[4];
 #pragma unroll
@@ -2217,7 +2236,10 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
           coef[b] = 1.f;
         }
       }
-      if constexpr (MASK) mask();
+      if constexpr (MASK) {
+        mask();
+        mask_bad();
+      }
     }
     // row maximum of the scaled scores: block maxima of the raw scores times
     // the (non-negative) block coefficients. The raw scores are finite or
@@ -2357,7 +2379,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   const float l_tot = sum_across_halves(l_run);
   if (it.part < 0) {
     if (!row_ok) return;
-    const float inv = MOD && l_tot == 0.f ? 0.f : 1.f / l_tot;
+    const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
     const int64_t ooff = (static_cast<int64_t>(it.q_row0 + p) * a.hq + static_cast<int64_t>(kvh) * G + gh) * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -2478,7 +2500,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
 // Merge launch for split prefill tiles: one workgroup per (row, KV head)
 // group; the attention launch before it wrote the partials.
-template <int D, int G, int OT, bool MOD>
+template <int D, int G, int OT>
 __global__ __launch_bounds__(kThreads) void tile_merge_kernel(AttnArgs a) {
   // Every thread merges four consecutive output dims of one head on its own:
   // it reads each span's (m, l) of that head and its four partial values,
@@ -2528,7 +2550,7 @@ __global__ __launch_bounds__(kThreads) void tile_merge_kernel(AttnArgs a) {
       o.w = o.w * a0 + os.w * a1;
       mx = mn;
     }
-    const float inv = MOD && l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t off = (static_cast<int64_t>(g.q_row) * a.hq + static_cast<int64_t>(g.kvh) * G) * D + 4 * c;
     store_out<OT>(a.out, off + 0, o.x * inv);
     store_out<OT>(a.out, off + 1, o.y * inv);
@@ -2596,7 +2618,7 @@ aug_status launch(const Args<MOD>& a, const aug_attn_plan_info& info, hipStream_
       return aug::fail(AUG_ERR_HIP, "aug_attn_mixed: launch failed: %s", hipGetErrorString(e));
   }
   if (info.num_tile_merge_groups > 0) {
-    hipLaunchKernelGGL((tile_merge_kernel<D, G, OT, MOD>), dim3(info.num_tile_merge_groups), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((tile_merge_kernel<D, G, OT>), dim3(info.num_tile_merge_groups), dim3(kThreads), 0, st, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess)
       return aug::fail(AUG_ERR_HIP, "aug_attn_mixed: merge launch failed: %s", hipGetErrorString(e));
   }
