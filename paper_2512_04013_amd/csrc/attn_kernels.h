@@ -2206,9 +2206,10 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
       vinv[b] = FP8 ? stage_scales[stage * L::NSC + 8 + b] : 1.f;
     }
     if constexpr (MOD) {
-      // a zero key scale is taken as 2^-100, or it would make NaN of masked scores
+      // a zero key scale is taken as the smallest normal number, or it would make NaN of
+      // masked scores
 #pragma unroll
-      for (int b = 0; b < 4; ++b) coef[b] = FP8 ? fmaxf(coef[b], 0x1p-100f) : coef[b];
+      for (int b = 0; b < 4; ++b) coef[b] = FP8 ? fmaxf(coef[b], 0x1p-126f) : coef[b];
       // the cap leaves -1 / (1 + 2^(..)) in the place of the raw score, with one
       // positive coefficient; the bias leaves the score itself
       if (a.cap_in != 0.f) {
