@@ -57,7 +57,7 @@ typedef enum {
   AUG_OK = 0,
   AUG_ERR_INVALID = -1,      /* an argument is out of its documented range */
   AUG_ERR_UNSUPPORTED = -2,  /* a valid combination the library does not run */
-  AUG_ERR_NO_SPACE = -3,     /* a caller buffer is too small */
+  AUG_ERR_NO_SPACE = -3,     /* a caller buffer is too small, or host memory ran out */
   AUG_ERR_HIP = -4           /* the HIP runtime reported an error */
 } aug_status;
 
@@ -217,7 +217,8 @@ typedef struct {
  * blocks, block id outside the pool, kv_split_tokens above 2^24; with the
  * host block table, a block that would receive new tokens of two requests or
  * twice from one), AUG_ERR_UNSUPPORTED (dtype set, head_dim, block_size, a
- * context above 2^24 tokens), AUG_ERR_NO_SPACE (plan_cap < plan_bytes). */
+ * context above 2^24 tokens), AUG_ERR_NO_SPACE (plan_cap < plan_bytes, or no
+ * host memory for the planner's lists). */
 aug_status aug_attn_plan(const aug_attn_shape* shape, const aug_batch_desc* batch,
                          int32_t kv_split_tokens, void* plan_host, size_t plan_cap,
                          aug_attn_plan_info* info);
@@ -538,7 +539,8 @@ typedef struct {
  * IEEE double precision with a fixed operation order.
  * Errors: AUG_ERR_INVALID (NULL pointers, pred_out < 1 for a candidate,
  * negative sizes, t_iter <= 0, chunk_cap < 1, block_size < 1, unknown state),
- * AUG_ERR_NO_SPACE (more than `cap` entries in any output list). */
+ * AUG_ERR_NO_SPACE (more than `cap` entries in any output list, or no host
+ * memory). */
 aug_status aug_form_batch(const aug_request* reqs, int32_t n, int64_t free_blocks, double now,
                           const aug_former_params* params, aug_batch_plan* out);
 

@@ -113,11 +113,9 @@ int64_t token_budget(const aug_former_params& p, int64_t free_blocks, int64_t pr
 
 bool is_candidate(int32_t s) { return s == AUG_WAITING || s == AUG_RUNNING || s == AUG_SWAPPED; }
 
-}  // namespace
-
-extern "C" aug_status aug_form_batch(const aug_request* reqs, int32_t n, int64_t free_blocks,
-                                     double now, const aug_former_params* params,
-                                     aug_batch_plan* out) {
+// aug_form_batch; may throw where memory runs out.
+aug_status form_batch(const aug_request* reqs, int32_t n, int64_t free_blocks, double now,
+                      const aug_former_params* params, aug_batch_plan* out) {
   if (!params || !out || n < 0 || (n > 0 && !reqs))
     return aug::fail(AUG_ERR_INVALID, "aug_form_batch: NULL argument or negative count");
   const aug_former_params& p = *params;
@@ -233,6 +231,14 @@ extern "C" aug_status aug_form_batch(const aug_request* reqs, int32_t n, int64_t
   out->n_park = n_park;
   out->n_free = n_free;
   return AUG_OK;
+}
+
+}  // namespace
+
+extern "C" aug_status aug_form_batch(const aug_request* reqs, int32_t n, int64_t free_blocks,
+                                     double now, const aug_former_params* params,
+                                     aug_batch_plan* out) {
+  return aug::without_exceptions("aug_form_batch", [&] { return form_batch(reqs, n, free_blocks, now, params, out); });
 }
 
 namespace {

@@ -451,28 +451,9 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
   return best;
 }
 
-}  // namespace
-}  // namespace aug
-
-using namespace aug;
-
-extern "C" aug_status aug_attn_plan(const aug_attn_shape* s, const aug_batch_desc* b,
-                                    int32_t kv_split_tokens, void* plan_host, size_t plan_cap,
-                                    aug_attn_plan_info* info) {
-  const aug_plan_options opts{kv_split_tokens, AUG_ROWS_AUTO, AUG_TILES_AUTO, 0};
-  return aug_attn_plan_opts(s, b, &opts, plan_host, plan_cap, info);
-}
-
-extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batch_desc* b,
-                                         const aug_plan_options* opts, void* plan_host, size_t plan_cap,
-                                         aug_attn_plan_info* info) {
-  return aug_attn_plan_masked(s, b, opts, nullptr, plan_host, plan_cap, info);
-}
-
-extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_batch_desc* b,
-                                           const aug_plan_options* opts, const aug_row_mask* mask, void* plan_host,
-                                           size_t plan_cap, aug_attn_plan_info* info) {
-  const char* who = "aug_attn_plan";
+// aug_attn_plan_masked; may throw where memory runs out.
+aug_status plan_masked(const char* who, const aug_attn_shape* s, const aug_batch_desc* b, const aug_plan_options* opts,
+                       const aug_row_mask* mask, void* plan_host, size_t plan_cap, aug_attn_plan_info* info) {
   if (aug_status st = check_shape(s, who); st != AUG_OK) return st;
   if (!opts) return fail(AUG_ERR_INVALID, "%s: options are NULL", who);
   if (opts->reserved != 0) return fail(AUG_ERR_INVALID, "%s: the reserved option field must be zero", who);
@@ -904,6 +885,31 @@ extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_ba
       }
   }
   return AUG_OK;
+}
+
+}  // namespace
+}  // namespace aug
+
+using namespace aug;
+
+extern "C" aug_status aug_attn_plan(const aug_attn_shape* s, const aug_batch_desc* b,
+                                    int32_t kv_split_tokens, void* plan_host, size_t plan_cap,
+                                    aug_attn_plan_info* info) {
+  const aug_plan_options opts{kv_split_tokens, AUG_ROWS_AUTO, AUG_TILES_AUTO, 0};
+  return aug_attn_plan_opts(s, b, &opts, plan_host, plan_cap, info);
+}
+
+extern "C" aug_status aug_attn_plan_opts(const aug_attn_shape* s, const aug_batch_desc* b,
+                                         const aug_plan_options* opts, void* plan_host, size_t plan_cap,
+                                         aug_attn_plan_info* info) {
+  return aug_attn_plan_masked(s, b, opts, nullptr, plan_host, plan_cap, info);
+}
+
+extern "C" aug_status aug_attn_plan_masked(const aug_attn_shape* s, const aug_batch_desc* b,
+                                           const aug_plan_options* opts, const aug_row_mask* mask, void* plan_host,
+                                           size_t plan_cap, aug_attn_plan_info* info) {
+  const char* who = "aug_attn_plan";
+  return without_exceptions(who, [&] { return plan_masked(who, s, b, opts, mask, plan_host, plan_cap, info); });
 }
 
 extern "C" aug_status aug_attn_workspace_size(const aug_attn_shape* s, const aug_batch_desc* b,
