@@ -174,8 +174,15 @@ def row_spans(q_start, ctx_len, window: int = 0, prefix_len=None, doc_start=None
     * ``window`` > 0: the row's own key and the window - 1 before it;
     * ``prefix_len`` (per request): keys before it are seen by every row of the
       request, later ones causally;
-    * ``doc_start`` (per row): no key before it, the first of the row's document.
+    * ``doc_start`` (per row): no key before it, the first of the row's document,
+      nor of a prefix.
+
+    A window and a prefix do not go together: a row behind both sees two spans.
     """
+    if window > 0 and prefix_len is not None:
+        raise ValueError("a window and a prefix: a row's keys are not one span")
+    if window < 0:
+        raise ValueError(f"a window of {window} keys (0: none)")
     q_start, ctx_len = np.asarray(q_start, np.int64), np.asarray(ctx_len, np.int64)
     q_len = np.diff(q_start)
     pos = np.arange(int(q_start[-1])) - np.repeat(q_start[:-1] - (ctx_len - q_len), q_len)
