@@ -93,9 +93,13 @@ typedef enum { AUG_ORDER_THETA = 0, AUG_ORDER_FCFS = 1, AUG_ORDER_SSJF = 2 } aug
  * MXFP4 caches hold 4.25 bits per element: E2M1 codes (sign, then the index
  * into 0, 0.5, 1, 1.5, 2, 3, 4, 6) in groups of 32 dims of one token, each with
  * a power-of-two scale X as one byte X + 127 (the OCP microscaling format);
- * value = code * 2^X. A pool is [num_pool_blocks][num_kv_heads * 1088] bytes,
- * 16-byte aligned (queries over them are finite): of every block, first the codes of all heads, 1024 bytes
- * each, then their scales, 64 bytes each. No k_scale and v_scale arrays.
+ * value = code * 2^X, with X from -125 to 125 (bytes 2 to 252, all that the append
+ * writes), so that every value is zero or a normal bf16 number. A pool is [num_pool_blocks][num_kv_heads * 1088] bytes,
+ * 16-byte aligned: of every block, first the codes of all heads, 1024 bytes
+ * each, then their scales, 64 bytes each. No k_scale and v_scale arrays. Queries
+ * over them are finite and multiplied as the sum of two E4M3 codes per element,
+ * exact down to 2^-14 of the largest magnitude of their vector and off by 2^-21
+ * of that below.
  *   K: codes [16 tokens][128 dims], scales [16 tokens][4 groups]
  *   V: codes [4 token quads][16 octets of dims][4 tokens][8 dims],
  *      scales [4 groups][16 tokens]
@@ -285,11 +289,15 @@ aug_status aug_plan_upload(const void* host_src, void* dev_dst, size_t bytes, vo
 /* Mixed-batch paged attention: for every row of every request of the planned
  * batch, O = softmax(softmax_scale * q K^T, causal) V over the request's
  * paged keys (see aug_batch_desc). Device memory:
- *   plan_dev   the plan image of aug_attn_plan (info->plan_bytes bytes). Its
- *              last 4 * info->num_merge_groups bytes are completion counters
- *              of the split decode rows, which the launch increments and
+ *   plan_dev   the plan image of aug_attn_plan (info->plan_bytes bytes): a header of
+ *              64 bytes, 48 bytes for each of info->num_items, 16 for each of
+ *              info->num_merge_groups, then 4 for each merge group, and behind
+ *              these what aug_kv_append reads and, in a plan with a mask, the
+ *              rows' spans. The 4 bytes of a group are the completion counter of
+ *              its split decode rows, which the launch increments and
  *              returns to zero, so the same device copy can be launched
- *              again; calls that overlap on one copy race
+ *              again; calls that overlap on one copy race. (After a launch that
+ *              did not end, upload the image again.)
  *   q          [total_rows][num_q_heads][head_dim], q_dtype
  *   k_cache,   [num_pool_blocks][num_kv_heads][block_size][head_dim], kv_dtype
  *   v_cache    (MXFP4: see aug_attn_shape)
@@ -302,10 +310,13 @@ aug_status aug_plan_upload(const void* host_src, void* dev_dst, size_t bytes, vo
  * Slots past a request's context and blocks it does not list never influence
  * its output, whatever they hold. Keys of a block id outside the pool (in a table
  * that the planner has not checked) count for nothing, and a row that has no other
- * gives zeros. Enqueued on `stream` as one kernel launch:
- * split decode rows are merged in it by the workgroup that finishes each
- * row's last span; split prefill tiles are merged by a second small launch
- * when info->num_tile_merge_groups > 0.
+ * gives zeros. Sums and softmax statistics are fp32. Over every cache but F32, prefill
+ * tiles and decode rows take each probability as bf16 (off by at most 2^-8 of it, in
+ * the row's sum as in its products); decode rows over MXFP4, and in groups of four
+ * heads on the MFMA path over fp8, multiply what that rounds off as well.
+ * Enqueued on `stream` as one kernel launch: split decode rows are merged in it
+ * by the workgroup that finishes each row's last span; split prefill tiles are
+ * merged by a second small launch when info->num_tile_merge_groups > 0.
  * Errors: AUG_ERR_INVALID (NULL pointers, info inconsistent, or a shape
  * other than the one the plan was built for: heads, head_dim or dtypes),
  * AUG_ERR_NO_SPACE (workspace_bytes too small), AUG_ERR_HIP (launch). */
@@ -354,7 +365,8 @@ aug_status aug_attn_mixed_scored(const aug_attn_shape* shape, const aug_attn_pla
  * held until the process ends) instead of a caller workspace. The caller
  * still passes the plan image, inputs and output. The array's device address
  * is looked up once per device, on the first call made with that device
- * current; `stream` must belong to the current device. Nothing in the array
+ * current; `stream` must belong to the current device. Plans with a mask are
+ * taken; a softcap and slopes need aug_attn_mixed_scored and a workspace. Nothing in the array
  * needs to start at zero (every partial is written before it is read), and
  * it keeps the last call's contents. All calls on one GPU share the array:
  * calls that overlap in time on that GPU (other streams, other threads)
@@ -415,7 +427,7 @@ aug_status aug_kv_append(const aug_attn_shape* shape, const aug_attn_plan_info* 
  * rounded to bf16 (nearest even). These are the rows that aug_kv_append takes,
  * so a request moves from one cache format to another through them. Rows of
  * slots outside the pool (negative ones too) become zero; k_out and v_out must
- * not overlap the cache. Device memory:
+ * not overlap the cache or each other. Device memory:
  *   slots      int64 [n]
  * and the caches as for aug_attn_mixed; outputs 16-byte aligned. Enqueued on
  * `stream` as one kernel launch (none for n = 0); no allocation.

@@ -2124,8 +2124,8 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
     // lanes i/4, 4 + i/4, 8 + i/4 and 12 + i/4 of its group, so addressing
     // row (lane % 16) / 4 at column 4 (lane % 4) hands each lane four
     // consecutive keys of one dimension: the operand layout of V^T.
-    // With modified scores a step of them is read when it is multiplied: the scores
-    // take the registers.
+    // With modified scores they are left to the product's place: the scores take the
+    // registers, and the compiler reads a step of them shortly before its MFMAs.
     const auto v_operand = [&](int s, int db) {
       const uint16_t* v0 = vs + (16 * s) * L::VS + 32 * db + v_lane_off;
       const uint16_t* v1 = v0 + 8 * L::VS;
@@ -2280,7 +2280,10 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
 
     // p = 2^(s * coef - m) (fp8: times the block's V scale, through its log2),
     // packed to bf16 pairs for the PV MFMAs; the row sum adds exactly the
-    // packed values (fp8: weighted back by 1/vs)
+    // packed values (fp8: weighted back by 1/vs). That rounding, 2^-8 of a
+    // probability at most, adds to a tile's error (1.7e-3 of the outputs' norm from
+    // their own rounding to bf16, 1.9e-3 to 2.3e-3 with it, over every cache);
+    // multiplying the rest as well would double the PV MFMAs.
     // O^T += V^T P^T, 16 keys (one block) per step; k-slots of lane half hh
     // are keys {16s+4hh+j, 16s+8+4hh+j}, exactly the S^T entries this lane holds
     if constexpr (PV8) {
