@@ -1581,7 +1581,7 @@ __device__ void tile_item(const WorkItem& it, const Args<MOD>& a, unsigned char*
   // of 4 bits (its value rounded, and 32 times the rest), which is exact down to
   // 2^-14 of its vector's largest magnitude, and 2^-21 of that off below. 16 chunks of
   // 512 rows, 64/8 heads: 402 us with the keys converted to bf16 on their way into
-  // LDS, 383 so (971 TFLOP/s; a large bf16 matrix product reaches 1227 on the card).
+  // LDS, 386 so (962 TFLOP/s; a large bf16 matrix product reaches 1227 on the card).
   constexpr bool QK4 = L::K4;
   constexpr bool KDMA = DMA || QK8 || QK4;   // the keys, at least, come by direct loads
   constexpr bool PV8 = F8 >= 2;
