@@ -140,7 +140,9 @@ class MixedAttention:
         default to the planned ones; another layer of the same batch passes its
         own pool, block ids (same table shape) and output, and reuses the plan.
         ``softcap``: scores become softcap * tanh(score / softcap); ``slopes``
-        (float32 [num_q_heads]): less slope * |position - key|."""
+        (float32 [num_q_heads]): less slope * |position - key|. ``stream`` has to
+        wait for the stream that was torch's current one when the batch was
+        planned: its plan is uploaded and its memory allocated there."""
         kv = self.kv if kv is None else kv
         out = self.out if out is None else out
         if slopes is not None and (slopes.shape != (self.shape.num_q_heads,) or slopes.dtype != torch.float32 or
