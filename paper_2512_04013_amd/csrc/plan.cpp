@@ -378,9 +378,9 @@ int32_t balance_split(const aug_attn_shape& s, const std::vector<RowLoad>& rows,
   // together are many, the rows go in the longest spans that it knows beside tiles: 64
   // decodes beside 2048 tiles (fp8, 64/8 heads) 173 -> 161 us, beside 880 (bf16, 32/8)
   // 237 -> 229, 250 beside 128 (head_dim 64, 16/8) 119 -> 115; with masks and caps alike.
-  // Of 12 such batches, plain, capped and masked, the worst lost 3 % (48 decodes beside
-  // 1152 tiles of prefixes, head_dim 64: 144 -> 148), most gained 2-8. Below the limit
-  // every split is priced.
+  // Of 14 such batches, each plain, capped and masked, most gained 1-9 %, the others
+  // stayed within 2 but for one (48 decodes beside 1152 tiles of prefixes, head_dim 64:
+  // 144 -> 148). Below the limit every split is priced.
   if (!rows_only && n_before >= kManyItems) {
     before = std::max(before, kBesideTilesMax);
     n_before = count(before);
