@@ -1,0 +1,787 @@
+"""A step of drafted tokens whose lengths are known on the GPU only: block tables
+and slot maps, rotary positions with the append, attention of a tree of drafts,
+and sampling. The passes whose speed is followed, their plain forms and exact
+results.
+
+Kinds of pass:
+
+* ``tables``: the step's tables from lengths on the GPU, twice: lengths after an
+  accepted step (blocks come back), then the next step's drafts (blocks are taken);
+* ``append``: new K/V rows, rotated by their positions, into the slots of a paged
+  cache, and the rotated queries;
+* ``rotate``: queries and keys rotated where no cache is written; with
+  ``inverse`` by negated positions, which is how a gradient goes back;
+* ``tree``: attention of drafted tokens over a paged cache: a row sees the
+  request's committed keys, and of its drafts itself and its ancestors;
+* ``sample``: tokens from logits and given uniform numbers.
+
+Lengths and trees come from a case alone; data, block placement and random
+numbers come from the seed.
+"""
+
+from __future__ import annotations
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+BLOCK = 16
+DEVICE = "cuda"
+CELL = 1088            # bytes of one (block, KV head) of a 4-bit pool: 1024 of codes, 64 of scales
+F8 = torch.float8_e4m3fn
+
+# (query heads, KV heads, head_dim, KV format)
+LAYERS = {
+    "f32-4x4-d64": (4, 4, 64, "f32"),
+    "f32-8x2-d128": (8, 2, 128, "f32"),
+    "bf16-16x8-d64": (16, 8, 64, "bf16"),
+    "bf16-16x4-d64": (16, 4, 64, "bf16"),
+    "bf16-32x8-d128": (32, 8, 128, "bf16"),
+    "bf16-64x8-d128": (64, 8, 128, "bf16"),
+    "fp8-32x8-d128": (32, 8, 128, "fp8"),
+    "fp8-64x8-d128": (64, 8, 128, "fp8"),
+    "fp4-8x8-d128": (8, 8, 128, "fp4"),
+    "fp4-32x8-d128": (32, 8, 128, "fp4"),
+    "fp4-64x8-d128": (64, 8, 128, "fp4"),
+}
+
+# Angles of a rotation: share of the head's dims, pairs, base, and how they are stretched for long contexts.
+ROPES = {
+    "half": dict(part=1.0, interleaved=False, base=10000.0, scaling="none"),
+    "interleaved-part": dict(part=0.5, interleaved=True, base=10000.0, scaling="linear", factor=4.0),
+    "half-bands": dict(part=1.0, interleaved=False, base=500000.0, scaling="bands", factor=8.0, low=1.0, high=4.0, original_len=8192),
+    "half-ramp": dict(part=1.0, interleaved=False, base=1000000.0, scaling="ramp", factor=4.0, low=1.0, high=32.0, original_len=32768,
+                      magnitude=0.1 * math.log(4.0) + 1.0),
+}
+
+# "reqs" requests with contexts lognormal around "ctx" (sigma 0.8, capped) or uniform from "ctx" to "cap"; each has "drafts" rows
+# ("fewer": a share of them, at least one) in a tree of up to "branch" children, or "drafts" rows in a chain where branch is 1.
+# sampling: "rows" x "vocab" logits, rows "pad" elements further apart.
+_BASE = {"kind": "", "layer": "", "reqs": 0, "ctx": 1, "cap": 1, "dist": "lognormal", "drafts": 1, "fewer": False, "branch": 1, "lengths": 0,
+         "rope": "half", "far": 0, "inverse": False, "rows": 0, "vocab": 0, "pad": 0, "dtype": "f32", "mix": "", "share": 0.0}
+
+
+def _case(**kw):
+    return {**_BASE, **kw}
+
+
+def listed():
+    return [
+        # the tables of a lightly loaded server: latency
+        _case(name="tables-64", kind="tables", reqs=64, ctx=1200, cap=8192, drafts=8, branch=3, share=0.1),
+        # the tables of many requests with large trees
+        _case(name="tables-2000", kind="tables", reqs=2000, ctx=700, cap=8192, drafts=32, branch=4, fewer=True, share=0.1),
+        # a decode step's queries and rows out of one fused projection
+        _case(name="append-decode-8b", kind="append", layer="bf16-32x8-d128", reqs=64, ctx=1200, cap=8192),
+        # the rows of an 8192-token budget into an fp8 cache, far positions, ragged ends of blocks
+        _case(name="append-prefill-fp8-64x8", kind="append", layer="fp8-64x8-d128", reqs=15, ctx=2048, cap=8192, drafts=541, rope="half-bands", far=100_000),
+        # the gradient of interleaved pairs in half of the head, in fp32
+        _case(name="rotate-back-f32", kind="rotate", layer="f32-8x2-d128", reqs=4, ctx=1, cap=1, drafts=1001, rope="interleaved-part", inverse=True),
+        # one request with a handful of drafts: latency
+        _case(name="tree-tiny", kind="tree", layer="bf16-16x8-d64", reqs=1, ctx=40, cap=40, dist="uniform", drafts=5, branch=2),
+        # drafted decoding at moderate concurrency, four query heads per KV head
+        _case(name="tree-8b", kind="tree", layer="bf16-32x8-d128", reqs=64, ctx=2500, cap=16384, drafts=8, branch=3),
+        # larger trees over the fp8 cache, eight query heads per KV head, trees of different sizes
+        _case(name="tree-fp8-64x8", kind="tree", layer="fp8-64x8-d128", reqs=128, ctx=2500, cap=8192, drafts=16, branch=3, fewer=True),
+        # few long requests with the largest trees, over the 4-bit cache
+        _case(name="tree-long-fp4", kind="tree", layer="fp4-32x8-d128", reqs=8, ctx=16384, cap=32768, dist="uniform", drafts=64, branch=4),
+        # one request's next token: latency
+        _case(name="sample-1", kind="sample", rows=1, vocab=32000, dtype="bf16", mix="k"),
+        # the drafts of a few requests, odd vocabulary, padded rows, nucleus alone
+        _case(name="sample-64", kind="sample", rows=64, vocab=50257, pad=47, mix="p"),
+        # a full batch, every request with settings of its own
+        _case(name="sample-512", kind="sample", rows=512, vocab=128000, dtype="bf16", mix="all"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    """One more case: the listed kinds over their ranges, odd sizes included."""
+    kind = rng.choice(["tables", "append", "append", "rotate", "tree", "tree", "tree", "sample", "sample", "sample"])
+    seed = rng.randrange(1, 1 << 20)
+    if kind == "tables":
+        return _case(kind=kind, reqs=_log_int(rng, 1, 1900), ctx=_log_int(rng, 16, 700), cap=8192, drafts=_log_int(rng, 1, 32), branch=rng.randint(1, 4),
+                     fewer=True, share=rng.choice([0.0, 0.1, 0.5]), lengths=seed)
+    if kind in ("append", "rotate"):
+        n = _log_int(rng, 1, 400)
+        return _case(kind=kind, layer=rng.choice(sorted(LAYERS)), reqs=n, ctx=_log_int(rng, 1, 2000), cap=8192,
+                     drafts=_log_int(rng, 1, max(1, 4000 // n)), fewer=True, rope=rng.choice(sorted(ROPES)),
+                     far=rng.choice([0, 0, 100_000, 1_000_000]), inverse=kind == "rotate" and rng.random() < 0.5, lengths=seed)
+    if kind == "tree":
+        layer = rng.choice(sorted(LAYERS))
+        small = layer.startswith("f32")          # fp32 is the small, exact configuration
+        n = _log_int(rng, 1, 32 if small else 128)
+        ctx = _log_int(rng, 1, min(512 if small else 16384, (4000 if small else 160_000) // n))
+        return _case(kind=kind, layer=layer, reqs=n, ctx=ctx, cap=3 * ctx, dist=rng.choice(["uniform", "lognormal"]),
+                     drafts=_log_int(rng, 1, 64 if n <= 16 else 16), branch=rng.randint(1, 5), fewer=rng.random() < 0.5, lengths=seed)
+    return _case(kind=kind, rows=_log_int(rng, 1, 400), vocab=_log_int(rng, 1000, 128000), pad=rng.choice([0, 0, 1, 64]),
+                 dtype=rng.choice(["f32", "bf16"]), mix=rng.choice(["", "k", "p", "m", "all", "all"]))
+
+
+# ---- lengths and trees ------------------------------------------------------------------------
+
+def _lengths(case):
+    """(committed context, rows) of each request."""
+    rng = random.Random(case["lengths"])
+    ctx, rows = [], []
+    for _ in range(case["reqs"]):
+        if case["dist"] == "uniform":
+            c = rng.randint(case["ctx"], case["cap"])
+        else:
+            c = min(case["cap"], max(1, round(rng.lognormvariate(math.log(case["ctx"]), 0.8))))
+        ctx.append(c)
+        rows.append(rng.randint(1, case["drafts"]) if case["fewer"] else case["drafts"])
+    return np.array(ctx, np.int64), np.array(rows, np.int64)
+
+
+def _parents(case, rows):
+    """The parent of every row within its request, -1 for the first: as a drafting model makes them, level by level."""
+    rng = random.Random(case["lengths"] + 1)
+    out = []
+    for n in rows.tolist():
+        children = [0] * n
+        open_ = [0]
+        out.append(-1)
+        for i in range(1, n):
+            while children[open_[0]] >= case["branch"]:
+                open_.pop(0)
+            p = open_[0] if case["branch"] == 1 or rng.random() < 0.6 else rng.choice(open_)
+            if children[p] >= case["branch"]:
+                p = open_[0]
+            children[p] += 1
+            open_.append(i)
+            out.append(p)
+    return np.array(out, np.int32)
+
+
+# ---- the cache formats, in 32-bit torch ----------------------------------------------------------
+
+_LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+_BOUNDS = (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)    # midpoints: a tie goes to the even index
+
+
+def _quantise4(x):
+    """x [..., 128] float32 -> codes [..., 128] and scale bytes [..., 4], uint8."""
+    g = x.unflatten(-1, (4, 32))
+    a = g.abs().amax(-1)
+    bits = (a.view(torch.int32) + (1 << 21)) >> 23       # exponent field, one more from 1.75 * 2^k on
+    byte = (bits - 2).clamp(2, 252)
+    y = torch.ldexp(g, (127 - byte)[..., None])
+    m = y.abs()
+    b = torch.tensor(_BOUNDS, device=x.device)
+    code = torch.where(torch.arange(7, device=x.device) % 2 == 0, m[..., None] > b, m[..., None] >= b).sum(-1).to(torch.uint8)
+    return (code + 8 * torch.signbit(y).to(torch.uint8)).flatten(-2), byte.to(torch.uint8)
+
+
+def _values4(codes, scales):
+    level = torch.tensor(_LEVELS + tuple(-v for v in _LEVELS), dtype=torch.float32, device=codes.device)
+    return torch.ldexp(level[codes.int()].unflatten(-1, (4, 32)), (scales.int() - 127)[..., None]).flatten(-2)
+
+
+def _pack4(code):
+    return code[..., 0::2] | (code[..., 1::2] << 4)
+
+
+def _unpack4(byte):
+    return torch.stack((byte & 15, byte >> 4), -1).flatten(-2)
+
+
+def _views4(pool, hkv, is_v):
+    """Views of a 4-bit pool's codes and scales, by (block, head, token ...)."""
+    codes, scales = pool[:, :hkv * 1024], pool[:, hkv * 1024:]
+    if is_v:
+        return codes.view(-1, hkv, 4, 16, 4, 4), scales.view(-1, hkv, 4, 16)
+    return codes.view(-1, hkv, 16, 64), scales.view(-1, hkv, 16, 4)
+
+
+def _load4(pool, hkv, is_v, blk, slot):
+    codes, scales = _views4(pool, hkv, is_v)
+    if is_v:
+        c = codes[blk, :, slot // 4, :, slot % 4]
+        return _values4(_unpack4(c.flatten(-2)), scales[blk, :, :, slot])
+    return _values4(_unpack4(codes[blk, :, slot]), scales[blk, :, slot])
+
+
+def _store4(pool, hkv, is_v, blk, slot, x):
+    codes, scales = _views4(pool, hkv, is_v)
+    c, s = _quantise4(x)
+    c = _pack4(c)
+    if is_v:
+        codes[blk, :, slot // 4, :, slot % 4] = c.unflatten(-1, (16, 4))
+        scales[blk, :, :, slot] = s
+    else:
+        codes[blk, :, slot] = c
+        scales[blk, :, slot] = s
+
+
+def _store8(pool, scale, blk, slot, x):
+    """Rows x [n, hkv, d] into an fp8 pool: rows that follow each other in one block share its scale, which grows with them."""
+    lead = torch.ones(len(blk), dtype=torch.bool, device=x.device)
+    lead[1:] = (blk[1:] != blk[:-1]) | (slot[1:] != slot[:-1] + 1)
+    run = lead.cumsum(0) - 1
+    runs = len(blk)                                          # at most
+    need = torch.zeros(runs, x.shape[1], device=x.device).index_reduce_(0, run, x.abs().amax(-1), "amax") / 448.0
+    first = torch.zeros(runs, dtype=torch.int64, device=x.device).index_put_((run,), torch.where(lead, slot, 0), accumulate=True)
+    block = torch.zeros(runs, dtype=torch.int64, device=x.device).index_put_((run,), torch.where(lead, blk, 0), accumulate=True)
+    live = torch.arange(runs, device=x.device) <= run[-1]
+    old = scale[block]
+    new = torch.where((first == 0)[:, None], need, torch.maximum(old, need))
+    grown = ((first > 0) & live)[:, None] & (need > old)
+    codes = pool.view(F8)
+    earlier = codes[block].float() * (old[..., None, None]) / torch.where(new > 0, new, 1.0)[..., None, None]
+    move = grown[..., None] & (torch.arange(BLOCK, device=x.device) < first[:, None, None])       # [runs, hkv, 16]
+    at = move.nonzero(as_tuple=True)
+    pool[block[at[0]], at[1], at[2]] = earlier[at].clamp(-448.0, 448.0).to(F8).view(torch.uint8)
+    s = new[run]
+    y = torch.where(s[..., None] > 0, x / torch.where(s > 0, s, 1.0)[..., None], 0.0)
+    pool[blk, :, slot] = y.clamp(-448.0, 448.0).to(F8).view(torch.uint8)
+    scale[block[live]] = new[live]
+
+
+# ---- inputs ---------------------------------------------------------------------------------
+
+class _Pages:
+    """Lengths, placement and data of a case over a paged cache."""
+
+    def __init__(self, case, seed):
+        self.hq, self.hkv, self.d, self.kv = LAYERS[case["layer"]]
+        self.ctx, self.n = _lengths(case)
+        self.q_start = np.concatenate([[0], np.cumsum(self.n)])
+        self.rows = int(self.q_start[-1])
+        nblk = -(-(self.ctx + self.n) // BLOCK)
+        used = int(nblk.sum())
+        self.pool = used + used // 4 + 64
+        self.width = int(nblk.max())
+        self.gen = torch.Generator(device=DEVICE)
+        self.gen.manual_seed(seed)
+        perm = torch.randperm(self.pool, generator=self.gen, device=DEVICE).to(torch.int32)
+        self.nblk = torch.from_numpy(nblk).to(DEVICE)
+        first = self.nblk.cumsum(0) - self.nblk
+        col = torch.arange(self.width, device=DEVICE)
+        self.listed = col < self.nblk[:, None]
+        self.table = torch.where(self.listed, perm[(first[:, None] + col).clamp(max=used - 1)], 0).to(torch.int32)
+        self.free = perm[used:].contiguous()
+        self.dtype = torch.float32 if self.kv == "f32" else torch.bfloat16
+        req = np.repeat(np.arange(len(self.n)), self.n)
+        token = np.arange(self.rows) - self.q_start[req] + self.ctx[req]
+        self.req, self.token = torch.from_numpy(req).to(DEVICE), torch.from_numpy(token).to(DEVICE)
+        self.blk = self.table[self.req, self.token // BLOCK].long()
+        self.slot = self.token % BLOCK
+
+    def normal(self, *shape):
+        return torch.randn(shape, generator=self.gen, device=DEVICE, dtype=self.dtype)
+
+    def cache(self):
+        """A pool of K or V, every slot filled, and its scales (fp8)."""
+        shape = (self.pool, self.hkv, BLOCK, self.d)
+        if self.kv in ("f32", "bf16"):
+            return self.normal(*shape), None
+        step = 1 << 11
+        if self.kv == "fp4":
+            # codes and scales in the places of K: V's places permute equal distributions
+            pool = torch.empty(self.pool, CELL * self.hkv, dtype=torch.uint8, device=DEVICE)
+            codes, scales = _views4(pool, self.hkv, False)
+            for b0 in range(0, self.pool, step):
+                c, s = _quantise4(self.normal(min(step, self.pool - b0), *shape[1:]).float())
+                codes[b0:b0 + step] = _pack4(c)
+                scales[b0:b0 + step] = s
+            return pool, None
+        codes = torch.empty(shape, dtype=torch.uint8, device=DEVICE)
+        scale = torch.empty(shape[:2], dtype=torch.float32, device=DEVICE)
+        for b0 in range(0, self.pool, step):
+            x = self.normal(min(step, self.pool - b0), *shape[1:]).float()
+            s = (x.abs().amax(dim=(2, 3)) / 448.0).clamp_min(1e-12)
+            codes[b0:b0 + step] = (x / s[:, :, None, None]).clamp(-448.0, 448.0).to(F8).view(torch.uint8)
+            scale[b0:b0 + step] = s
+        return codes, scale
+
+
+def _inputs(case, seed):
+    """Everything a pass reads, as plain tensors."""
+    s = {"case": case}
+    gen = torch.Generator(device=DEVICE)
+    gen.manual_seed(seed + 1)
+    dev = lambda a, t=torch.int32: torch.from_numpy(np.ascontiguousarray(a)).to(DEVICE).to(t)  # noqa: E731
+    if case["kind"] == "sample":
+        rows, vocab = case["rows"], case["vocab"]
+        # a broad bulk and a few dozen candidates above it
+        x = torch.randn(rows, vocab + case["pad"], generator=gen, device=DEVICE) * 2.0
+        top = torch.randint(0, vocab, (rows, 48), generator=gen, device=DEVICE)
+        x.scatter_add_(1, top, torch.rand(rows, 48, generator=gen, device=DEVICE) * 12.0)
+        s["logits"] = (x if case["dtype"] == "f32" else x.to(torch.bfloat16))[:, :vocab]
+        s["uniform"] = torch.rand(rows, generator=gen, device=DEVICE)
+        pick = lambda *v: torch.tensor(v, device=DEVICE)[torch.randint(0, len(v), (rows,), generator=gen, device=DEVICE)]  # noqa: E731
+        mix = case["mix"]
+        s["temperature"] = pick(0.0, 0.6, 0.8, 1.0, 1.3) if mix == "all" else pick(0.8)
+        s["top_k"] = (pick(0, 0, 1, 20, 50, 1000) if mix == "all" else pick(50)).to(torch.int32) if mix in ("all", "k") else None
+        s["top_p"] = (pick(1.0, 0.5, 0.9, 0.95) if mix == "all" else pick(0.95)) if mix in ("all", "p", "k") else None
+        s["min_p"] = (pick(0.0, 0.0, 0.05) if mix == "all" else pick(0.05)) if mix in ("all", "m") else None
+        return s
+    if case["kind"] == "tables":
+        ctx, n = _lengths(case)
+        rng = random.Random(case["lengths"] + 2)
+        before = np.array([0 if rng.random() < case["share"] else max(1, c - rng.randint(0, 20)) for c in ctx.tolist()])
+        s["width"] = -(-(case["cap"] + case["drafts"]) // BLOCK)
+        s["max_rows"] = int(n.sum()) + 5
+        s["pool"] = int((-(-(ctx + n) // BLOCK)).sum()) * 5 // 4 + 16
+        s["ctx0"], s["ctx"], s["n"], s["parents"] = dev(before), dev(ctx), dev(n), dev(_parents(case, n))
+        s["parents"] = torch.cat([s["parents"], torch.full((5,), -1, dtype=torch.int32, device=DEVICE)])
+        s["none"] = torch.zeros_like(s["n"])
+        s["free"] = torch.randperm(s["pool"], generator=gen, device=DEVICE).to(torch.int32)
+        return s
+    b = s["b"] = _Pages(case, seed)
+    if case["kind"] == "tree":
+        s["parents"] = dev(_parents(case, b.n))
+        s["ctx"], s["n"] = dev(b.ctx), dev(b.n)
+        s["q"] = b.normal(b.rows, b.hq, b.d)
+        s["k"], s["k_scale"] = b.cache()
+        s["v"], s["v_scale"] = b.cache()
+        return s
+    # queries, keys and values as one projection gives them
+    qkv = b.normal(b.rows, (b.hq + 2 * b.hkv) * b.d)
+    cut = [b.hq * b.d, (b.hq + b.hkv) * b.d]
+    s["q"] = qkv[:, :cut[0]].view(b.rows, b.hq, b.d)
+    s["k_new"] = qkv[:, cut[0]:cut[1]].view(b.rows, b.hkv, b.d)
+    s["v_new"] = qkv[:, cut[1]:].view(b.rows, b.hkv, b.d)
+    s["positions"] = ((b.token + case["far"]) * (-1 if case["inverse"] else 1)).to(torch.int32)
+    if case["kind"] == "append":
+        s["slots"] = (b.blk * BLOCK + b.slot).contiguous()
+        s["k"], s["k_scale"] = b.cache()
+        s["v"], s["v_scale"] = b.cache()
+    return s
+
+
+def _frequencies(name, d):
+    """Radians per position of every pair, in 64 bits."""
+    r = ROPES[name]
+    dim = int(d * r["part"])
+    i = torch.arange(dim // 2, dtype=torch.float64)
+    w = r["base"] ** (-2.0 * i / dim)
+    if r["scaling"] == "linear":
+        w = w / r["factor"]
+    elif r["scaling"] == "bands":
+        turns = r["original_len"] * w / (2 * math.pi)
+        mix = ((turns - r["low"]) / (r["high"] - r["low"])).clamp(0.0, 1.0)
+        w = w * mix + w / r["factor"] * (1.0 - mix)
+    elif r["scaling"] == "ramp":
+        at = lambda turns: dim * math.log(r["original_len"] / (2 * math.pi * turns)) / (2 * math.log(r["base"]))  # noqa: E731
+        lo, hi = max(math.floor(at(r["high"])), 0), min(math.ceil(at(r["low"])), dim - 1)
+        mix = ((i - lo) / max(hi - lo, 0.001)).clamp(0.0, 1.0)
+        w = w / r["factor"] * mix + w * (1.0 - mix)
+    return w.to(DEVICE), r.get("magnitude", 1.0)
+
+
+def _shape(b):
+    import paper_2512_04013_amd as aug
+    io = "f32" if b.kv == "f32" else "bf16"
+    return aug.make_shape(b.hq, b.hkv, b.d, io, b.kv, io, 1.0 / math.sqrt(b.d))
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    kind = case["kind"]
+    if kind == "sample":
+        s["tokens"] = torch.empty(case["rows"], dtype=torch.int32, device=DEVICE)
+        s["probs"] = torch.empty(case["rows"], dtype=torch.float32, device=DEVICE)
+        return s
+    if kind == "tables":
+        reqs, rows = case["reqs"], s["max_rows"]
+        zeros = lambda *shape, t=torch.int32: torch.zeros(shape, dtype=t, device=DEVICE)  # noqa: E731
+        if own:
+            from paper_2512_04013_amd import runtime as rt
+            s["tables"] = rt.StepTables(reqs, rows, s["width"], s["pool"], max_draft=64, device=DEVICE, free_ids=s["free"].clone())
+        else:
+            s["t"] = {"block_table": zeros(reqs, s["width"]), "held": zeros(reqs), "free_ids": s["free"].clone(), "free_count": zeros(1) + s["pool"],
+                      "q_start": zeros(reqs + 1), "kv_len": zeros(reqs), "state": zeros(reqs), "positions": zeros(rows),
+                      "slots": zeros(rows, t=torch.int64), "seen": zeros(rows, t=torch.int64)}
+        return s
+    b = s["b"]
+    if own:
+        from paper_2512_04013_amd import runtime as rt
+        r = ROPES[case["rope"]]
+        s["shape"] = _shape(b)
+        s["rope"] = rt.Rope(int(b.d * r["part"]), **{k: v for k, v in r.items() if k != "part"})
+        if kind != "rotate":
+            s["kv"] = rt.PagedKV(s["shape"], s["k"], s["v"], s["k_scale"], s["v_scale"], staging_bytes=1)
+        if kind == "tree":
+            t = rt.StepTables(len(b.n), b.rows, b.width, b.pool, max_draft=64, device=DEVICE, block_table=b.table, held=b.nblk.to(torch.int32),
+                              free_ids=torch.cat([b.free, b.free.new_zeros(b.pool - len(b.free))]), free_count=len(b.free))
+            t.update(s["ctx"], s["n"], s["parents"])
+            s["att"] = rt.TreeAttention(s["shape"], s["kv"], t)
+            s["att"].plan()
+    else:
+        s["freq"], s["magnitude"] = _frequencies(case["rope"], b.d)
+        if kind == "tree":
+            n = int(b.n.max())
+            s["closure"] = _closure(s["parents"], torch.from_numpy(b.q_start).to(DEVICE), n)
+    if kind == "append":
+        s["rows"] = [torch.empty(b.rows, b.hkv, b.d, dtype=b.dtype, device=DEVICE) for _ in range(2)]
+        s["q_out"] = torch.empty(b.rows, b.hq, b.d, dtype=b.dtype, device=DEVICE)
+    return s
+
+
+# ---- one pass ---------------------------------------------------------------------------------
+
+def run(state):
+    case = state["case"]
+    kind = case["kind"]
+    if kind == "tables":
+        if own:
+            t = state["tables"]
+            t.update(state["ctx0"], state["none"])
+            t.update(state["ctx"], state["n"], state["parents"])
+            return {"block_table": t.block_table, "held": t.held, "free_ids": t.free_ids, "free_count": t.free_count, "q_start": t.q_start,
+                    "kv_len": t.kv_len, "state": t.state, "positions": t.positions, "slots": t.slots, "seen": t.seen}
+        _plain_tables(state["t"], state["ctx0"], state["none"], None)
+        _plain_tables(state["t"], state["ctx"], state["n"], state["parents"])
+        return state["t"]
+    if kind == "append":
+        if own:
+            kv = state["kv"]
+            kv.append_rows(state["slots"], state["k_new"], state["v_new"], q=state["q"], rope=state["rope"], positions=state["positions"],
+                           q_out=state["q_out"])
+            return (state["q_out"], *kv.read(state["slots"], *state["rows"]))
+        return _plain_append(state)
+    if kind == "rotate":
+        if own:
+            from paper_2512_04013_amd import runtime as rt
+            return rt.rope_rows(state["shape"], state["rope"], state["positions"], state["q"], state["k_new"])
+        dtype = state["b"].dtype
+        return tuple(_plain_rotate(state, state[name].float()).to(dtype) for name in ("q", "k_new"))
+    if kind == "tree":
+        return state["att"].run(state["q"]) if own else _plain_tree(state)
+    if own:
+        from paper_2512_04013_amd import runtime as rt
+        return rt.sample(state["logits"], state["uniform"], temperature=state["temperature"], top_k=state["top_k"], top_p=state["top_p"],
+                         min_p=state["min_p"], tokens=state["tokens"], probs=state["probs"])
+    return _plain_sample(state)
+
+
+def _closure(parents, q_start, n):
+    """Which rows of its request every row descends from, itself among them: bool [requests, n, n] (row, ancestor)."""
+    i = torch.arange(n, device=DEVICE)
+    at = q_start[:-1, None] + i
+    live = at < q_start[1:, None]
+    p = torch.where(live, parents[at.clamp(max=len(parents) - 1)].long(), -1)
+    reach = (i[:, None] == i).float() + (p[..., None] == i).float()
+    for _ in range(6):                                   # up to 64 rows: paths of up to 63 steps
+        reach = (torch.bmm(reach, reach) > 0).float()
+    return (reach > 0) & live[..., None]
+
+
+def _plain_tables(t, ctx, n, parents):
+    """The tables of requests with ctx tokens in the cache and n more of this step: blocks beyond what a request needs go
+    back to the list of free ones, blocks that it lacks are taken from its end, requests in order."""
+    ctx, n, held = ctx.long(), n.long(), t["held"].long()
+    width, max_rows, pool = t["block_table"].shape[1], len(t["positions"]), len(t["free_ids"])
+    rows = n.clamp(min=0)
+    end = rows.cumsum(0)
+    start = (end - rows).clamp(max=max_rows)
+    need = (ctx + n + BLOCK - 1) // BLOCK
+    valid = (ctx >= 0) & (n >= 0) & (n <= 64) & (need <= width) & (held >= 0) & (held <= width) & (end <= max_rows)
+    give = torch.where(valid, (held - need).clamp(min=0), 0)
+    take = torch.where(valid, (need - held).clamp(min=0), 0)
+    count = t["free_count"].long()
+    before = give.cumsum(0) - give
+    total = give.sum()
+    col = torch.arange(width, device=DEVICE)
+    k = before[:, None] + col - need[:, None]                            # order among the blocks that come back
+    back = valid[:, None] & (col >= need[:, None]) & (col < held[:, None])
+    list_ = torch.cat([t["free_ids"], t["free_ids"].new_zeros(1)])       # the last place takes what goes nowhere
+    list_[torch.where(back, (count + total - 1 - k).clamp(0, pool), pool)] = t["block_table"]
+    t["free_ids"].copy_(list_[:pool])
+    asked = take.cumsum(0)
+    ok = valid & ((take == 0) | (asked <= count + total))
+    k = (asked - take)[:, None] + col - held[:, None]                    # order among the blocks that are taken
+    new = ok[:, None] & (col >= held[:, None]) & (col < need[:, None])
+    t["block_table"].copy_(torch.where(new, list_[(count + total - 1 - k).clamp(0, pool)], t["block_table"]))
+    t["held"].copy_(torch.where(ok, need, held))
+    t["free_count"].copy_(count + total - torch.where(ok, take, 0).sum())
+    t["state"].copy_(torch.where(ok, 0, torch.where(valid, 1, 2)))
+    t["kv_len"].copy_(torch.where(ok, ctx + n, 0))
+    t["q_start"].copy_(torch.cat([start, end[-1:].clamp(max=max_rows)]))
+    row = torch.arange(max_rows, device=DEVICE)
+    r = torch.searchsorted(t["q_start"][1:].long(), row, right=True).clamp(max=len(ctx) - 1)
+    i = row - start[r]
+    live, good = row < end[-1], ok[r]
+    token = ctx[r] + i
+    place = t["block_table"][r, (token // BLOCK).clamp(0, width - 1)].long() * BLOCK + token % BLOCK
+    t["slots"].copy_(torch.where(live, torch.where(good, place, -1), t["slots"]))
+    if parents is None:
+        parents = i - 1
+    tree = _closure(parents, t["q_start"].long(), 64)[r, i.clamp(0, 63)]
+    bits = (tree.long() << torch.arange(64, device=DEVICE)).sum(-1)
+    depth = tree.sum(-1) - 1
+    t["seen"].copy_(torch.where(live, torch.where(good, bits, 0), t["seen"]))
+    t["positions"].copy_(torch.where(live, torch.where(good, ctx[r] + depth, 0), t["positions"]))
+
+
+def _plain_rotate(state, x):
+    """x [rows, heads, d] in 32 bits, rotated; angles in 64."""
+    r = ROPES[state["case"]["rope"]]
+    a = state["positions"].double()[:, None] * state["freq"]
+    c, s = ((f(a) * state["magnitude"]).float()[:, None, :] for f in (torch.cos, torch.sin))
+    dim = 2 * a.shape[1]
+    rot, rest = x[..., :dim], x[..., dim:]
+    if r["interleaved"]:
+        u, v = rot[..., 0::2], rot[..., 1::2]
+        y = torch.stack((u * c - v * s, v * c + u * s), -1).flatten(-2)
+    else:
+        u, v = rot[..., :dim // 2], rot[..., dim // 2:]
+        y = torch.cat((u * c - v * s, v * c + u * s), -1)
+    return torch.cat((y, rest), -1)
+
+
+def _plain_rows(state, name, blk, slot):
+    """Rows of the K or V cache at (blk, slot): float32 [n, hkv, d]."""
+    b, pool = state["b"], state[name]
+    if b.kv == "fp4":
+        return _load4(pool, b.hkv, name == "v", blk, slot)
+    x = pool[blk, :, slot]
+    if b.kv == "fp8":
+        return x.view(F8).float() * state[name + "_scale"][blk][:, :, None]
+    return x.float()
+
+
+def _plain_append(state):
+    b = state["b"]
+    q = _plain_rotate(state, state["q"].float()).to(b.dtype)
+    new = {"k": _plain_rotate(state, state["k_new"].float()), "v": state["v_new"].float()}
+    for name, x in new.items():
+        if b.kv == "fp4":
+            _store4(state[name], b.hkv, name == "v", b.blk, b.slot, x)
+        elif b.kv == "fp8":
+            _store8(state[name], state[name + "_scale"], b.blk, b.slot, x)
+        else:
+            state[name][b.blk, :, b.slot] = x.to(b.dtype)
+    return (q, *(_plain_rows(state, name, b.blk, b.slot).to(b.dtype) for name in ("k", "v")))
+
+
+def _plain_tree(state):
+    """softmax(scaled scores) V in 32 bits, all requests at once, each padded to the longest."""
+    b = state["b"]
+    g, reqs, n = b.hq // b.hkv, len(b.n), state["closure"].shape[1]
+    ids = b.table.reshape(-1).long()
+    keys = b.width * BLOCK
+    blk, slot = ids.repeat_interleave(BLOCK), torch.arange(BLOCK, device=DEVICE).repeat(len(ids))
+    k = _plain_rows(state, "k", blk, slot).view(reqs, keys, b.hkv, b.d).permute(0, 2, 3, 1).reshape(reqs * b.hkv, b.d, keys)
+    i = torch.arange(n, device=DEVICE)
+    start, count, ctx = torch.from_numpy(b.q_start[:-1]).to(DEVICE), state["n"].long(), state["ctx"].long()
+    live = i < count[:, None]
+    x = state["q"].float()[torch.where(live, start[:, None] + i, 0)]                       # [reqs, n, hq, d]
+    x = x.view(reqs, n, b.hkv, g, b.d).transpose(1, 2).reshape(reqs * b.hkv, n * g, b.d)
+    s = torch.bmm(x, k).mul_(1.0 / math.sqrt(b.d)).view(reqs, b.hkv, n, g, keys)
+    del k
+    j = torch.arange(keys, device=DEVICE) - ctx[:, None]                                   # of drafts
+    draft = torch.gather(state["closure"], 2, j.clamp(0, n - 1)[:, None, :].expand(reqs, n, keys))
+    sees = (j < 0)[:, None, :] | (draft & (j < count[:, None])[:, None, :])
+    s.masked_fill_(~sees[:, None, :, None, :], -math.inf)
+    s.sub_(s.amax(-1, keepdim=True).clamp_min(-3e38)).exp_()
+    total = s.sum(-1, keepdim=True)
+    s /= torch.where(total == 0, 1.0, total)
+    v = _plain_rows(state, "v", blk, slot).view(reqs, keys, b.hkv, b.d).transpose(1, 2).reshape(reqs * b.hkv, keys, b.d)
+    o = torch.bmm(s.view(reqs * b.hkv, n * g, keys), v).view(reqs, b.hkv, n, g, b.d).transpose(1, 2).reshape(reqs, n, b.hq, b.d)
+    return o[b.req, torch.arange(b.rows, device=DEVICE) - start[b.req]].to(b.dtype)
+
+
+def _plain_sample(state):
+    """Tokens in 64 bits: which side of a border a number falls on decides a token."""
+    x = state["logits"]
+    rows, vocab = x.shape
+    x, order = torch.sort(x.double(), dim=-1, descending=True, stable=True)      # equal logits: the lower index first
+    temp = state["temperature"].double()[:, None]
+    greedy = temp == 0
+    w = torch.exp((x - x[:, :1]) / torch.where(greedy, 1.0, temp))
+    rank = torch.arange(vocab, device=DEVICE)
+    keep = rank < torch.where(greedy, 1, vocab)
+    if state["top_k"] is not None:
+        k = state["top_k"].long()[:, None]
+        keep &= rank < torch.where((k <= 0) | (k > vocab), vocab, k)
+    if state["top_p"] is not None:
+        p = state["top_p"].double()[:, None]
+        mass = torch.where(keep, w, 0.0)
+        before = mass.cumsum(-1) - mass
+        keep &= (p >= 1) | (rank == 0) | (before < p * mass.sum(-1, keepdim=True))
+    if state["min_p"] is not None:
+        keep &= (rank == 0) | (w >= state["min_p"].double()[:, None])
+    w = torch.where(keep, w, 0.0)
+    mass = torch.zeros_like(w).scatter_(1, order, w)                             # by index again
+    total = mass.sum(-1, keepdim=True)
+    token = (mass.cumsum(-1) <= state["uniform"].double()[:, None] * total).sum(-1).clamp(max=vocab - 1)
+    return token.to(torch.int32), (mass.gather(1, token[:, None]) / total)[:, 0].float()
+
+
+# ---- what a pass cannot do without --------------------------------------------------------------
+
+def work(case):
+    kind = case["kind"]
+    if kind == "sample":
+        return {"bytes": case["rows"] * (case["vocab"] * (4 if case["dtype"] == "f32" else 2) + 28), "flops": 0}
+    ctx, n = _lengths(case)
+    rows = int(n.sum())
+    if kind == "tables":
+        # lengths in, tables out, twice; parents in; position, slot and mask out; a block's id out of the list or back
+        return {"bytes": 2 * len(ctx) * (12 + 16) + rows * (4 + 20) + 2 * 8 * len(ctx), "flops": 0}
+    hq, hkv, d, kv = LAYERS[case["layer"]]
+    io = 4 if kv == "f32" else 2
+    row = {"f32": 4 * d, "bf16": 2 * d, "fp8": d, "fp4": 68}[kv]        # bytes of one cached row of K or V
+    if kind == "rotate":
+        return {"bytes": rows * (2 * (hq + hkv) * d * io + 4), "flops": 0}
+    if kind == "append":                                                 # and the rows read back
+        return {"bytes": rows * (2 * hq * d * io + 2 * hkv * d * io + 2 * hkv * row + 12 + hkv * 2 * (row + io * d) + 8), "flops": 0}
+    keys = int((ctx + n).sum())
+    b = keys * hkv * 2 * row + (keys // BLOCK) * (4 + (8 * hkv if kv == "fp8" else 0)) + rows * (2 * hq * d * io + 8)
+    seen = int((n * ctx).sum())                                          # drafts among themselves: a few
+    return {"bytes": b, "flops": 4 * d * hq * seen}
+
+
+# ---- exact results ----------------------------------------------------------------------------------
+
+def _turn64(case, positions, x):
+    """x rotated by its angles, pair by pair, as a product of complex numbers in 64 bits."""
+    r = ROPES[case["rope"]]
+    w, magnitude = _frequencies(case["rope"], x.shape[-1])
+    z = torch.polar(torch.full((len(positions), len(w)), magnitude, dtype=torch.float64, device=DEVICE), positions.double()[:, None] * w)
+    half = len(w)
+    y = x.double().clone()
+    lo, hi = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if r["interleaved"] else (slice(0, half), slice(half, 2 * half))
+    turned = torch.complex(y[..., lo], y[..., hi]) * z[:, None, :]
+    y[..., lo], y[..., hi] = turned.real, turned.imag
+    return y
+
+
+def _cell64(pool, hkv, ids, is_v):
+    """Blocks ids of a 4-bit pool, decoded field by field: float64 [n blocks, hkv, 16, 128]."""
+    raw = pool[ids]
+    codes = raw[:, :1024 * hkv].reshape(len(ids), hkv, 1024).long()
+    power = raw[:, 1024 * hkv:].reshape(len(ids), hkv, 64).double() - 127.0
+    nib = torch.empty(len(ids), hkv, 2048, dtype=torch.int64, device=raw.device)
+    nib[..., 0::2], nib[..., 1::2] = codes % 16, codes // 16
+    field, mant = (nib % 8) // 2, nib % 2
+    mag = torch.where(field == 0, 0.5 * mant.double(), (1.0 + 0.5 * mant.double()) * 2.0 ** (field.double() - 1.0))
+    val = torch.where(nib >= 8, -mag, mag)
+    if is_v:
+        val = val.reshape(-1, hkv, 4, 16, 4, 8).permute(0, 1, 2, 4, 3, 5).reshape(-1, hkv, 16, 128)
+        power = power.reshape(-1, hkv, 4, 16).transpose(2, 3)
+    else:
+        val, power = val.reshape(-1, hkv, 16, 128), power.reshape(-1, hkv, 16, 4)
+    return val * torch.repeat_interleave(2.0 ** power, 32, dim=-1)
+
+
+def _blocks64(s, ids, name):
+    b, pool = s["b"], s[name]
+    if b.kv == "fp4":
+        return _cell64(pool, b.hkv, ids, name == "v")
+    x = pool[ids]
+    return x.view(F8).double() * s[name + "_scale"][ids].double()[:, :, None, None] if b.kv == "fp8" else x.double()
+
+
+def _nearest4(x):
+    """The 4-bit cache's value of every element of x [n, hkv, 128]: each group's power of two from the logarithm of its
+    largest magnitude, each element the nearest multiple (the even code between two)."""
+    out = torch.empty_like(x)
+    level = torch.tensor(_LEVELS, dtype=torch.float64, device=x.device)
+    for g in range(4):
+        y = x[..., 32 * g:32 * g + 32]
+        a = y.abs().max(-1, keepdim=True).values
+        frac, e = torch.frexp(a)                              # a = frac * 2^e, frac in [0.5, 1)
+        e = torch.where(frac >= 0.875, e, e - 1)
+        scale = 2.0 ** (torch.where(a > 0, e.double(), torch.full_like(a, -200.0)) - 2.0).clamp(-125.0, 125.0)
+        gap = (y.abs() / scale).unsqueeze(-1) - level
+        gap = gap.abs() + torch.tensor([0.0, 1e-12] * 4, dtype=torch.float64, device=x.device)     # even codes win ties
+        out[..., 32 * g:32 * g + 32] = torch.copysign(level[gap.argmin(-1)] * scale, y)
+    return out
+
+
+def _nearest8(s, x, scales):
+    """The fp8 cache's value of every element of x [n, hkv, 128], block by block of every request."""
+    b = s["b"]
+    out = torch.empty_like(x)
+    for r in range(len(b.n)):
+        row, token = int(b.q_start[r]), int(b.ctx[r])
+        last = int(b.q_start[r + 1])
+        while row < last:
+            count = min(last - row, BLOCK - token % BLOCK)
+            y = x[row:row + count]
+            scale = y.abs().amax(dim=(0, 2)) / 448.0
+            if token % BLOCK:
+                scale = torch.maximum(scale, scales[int(b.table[r, token // BLOCK])].double())
+            y = y / scale[:, None]
+            step = 2.0 ** (torch.floor(torch.log2(y.abs().clamp_min(2.0 ** -6))) - 3.0)
+            out[row:row + count] = torch.round(y / step) * step * scale[:, None]
+            row, token = row + count, token + count
+    return out
+
+
+def _exact_tree(s):
+    b = s["b"]
+    g = b.hq // b.hkv
+    parents = s["parents"].tolist()
+    out = torch.zeros(b.rows, b.hq, b.d, dtype=torch.float64, device=DEVICE)
+    for r in range(len(b.n)):
+        q0, n, ctx = int(b.q_start[r]), int(b.n[r]), int(b.ctx[r])
+        sees = np.zeros((n, ctx + n), bool)
+        sees[:, :ctx] = True
+        for i in range(n):
+            j = i
+            while j >= 0:
+                sees[i, ctx + j] = True
+                j = parents[q0 + j]
+        sees = torch.from_numpy(sees).to(DEVICE)
+        ids = b.table[r, :-(-(ctx + n) // BLOCK)].long()
+        kk, vv = _blocks64(s, ids, "k"), _blocks64(s, ids, "v")
+        for h in range(b.hkv):
+            k, v = kk[:, h].reshape(-1, b.d)[:ctx + n], vv[:, h].reshape(-1, b.d)[:ctx + n]
+            for e in range(h * g, (h + 1) * g):
+                z = torch.matmul(s["q"][q0:q0 + n, e].double(), k.t().contiguous()) * b.d ** -0.5
+                out[q0:q0 + n, e] = torch.matmul(torch.softmax(torch.where(sees, z, -math.inf), -1), v)
+    return out
+
+
+def _exact_sample(s):
+    """Row by row: the chosen token, and its share of what is kept."""
+    x = s["logits"].double().cpu().numpy()
+    at = lambda name, r, off: off if s[name] is None else float(s[name][r])  # noqa: E731
+    tokens, probs = [], []
+    for r in range(len(x)):
+        order = np.argsort(-x[r], kind="stable")
+        temp = float(s["temperature"][r])
+        n = len(order) if temp > 0 else 1
+        k = int(at("top_k", r, 0))
+        if 0 < k < n:
+            n = k
+        e = np.exp((x[r][order[:n]] - x[r][order[0]]) / (temp if temp > 0 else 1.0))
+        p = at("top_p", r, 1.0)
+        if p < 1:
+            n = min(n, int(np.searchsorted(np.cumsum(e), p * e.sum(), side="left")) + 1)
+        n = min(n, max(1, int(np.count_nonzero(e >= at("min_p", r, 0.0)))))
+        kept = np.sort(order[:n])
+        e = np.exp((x[r][kept] - x[r][order[0]]) / (temp if temp > 0 else 1.0))
+        i = min(n - 1, int(np.searchsorted(np.cumsum(e), float(s["uniform"][r]) * e.sum(), side="right")))
+        tokens.append(int(kept[i]))
+        probs.append(e[i] / e.sum())
+    return torch.tensor(tokens, dtype=torch.int32), torch.tensor(probs, dtype=torch.float64)
+
+
+def exact(case, seed):
+    if case["kind"] == "tables":
+        return None                # whole numbers: nothing is rounded
+    s = _inputs(case, seed)
+    if case["kind"] == "sample":
+        return _exact_sample(s)
+    if case["kind"] == "tree":
+        return _exact_tree(s)
+    q, k = _turn64(case, s["positions"], s["q"]), _turn64(case, s["positions"], s["k_new"])
+    if case["kind"] == "rotate":
+        return q, k
+    v, kv = s["v_new"].double(), s["b"].kv
+    if kv == "fp4":
+        return q, _nearest4(k), _nearest4(v)
+    return (q, _nearest8(s, k, s["k_scale"]), _nearest8(s, v, s["v_scale"])) if kv == "fp8" else (q, k, v)
