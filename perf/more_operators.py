@@ -485,7 +485,7 @@ def _plain_tables(t, ctx, n, parents):
     end = rows.cumsum(0)
     start = (end - rows).clamp(max=max_rows)
     need = (ctx + n + BLOCK - 1) // BLOCK
-    valid = (ctx >= 0) & (n >= 0) & (n <= 64) & (need <= width) & (held >= 0) & (held <= width) & (end <= max_rows)
+    valid = (ctx >= 0) & (n >= 0) & (n <= 64) & (need <= width) & (held >= 0) & (held <= width) & (start + rows <= max_rows)
     give = torch.where(valid, (held - need).clamp(min=0), 0)
     take = torch.where(valid, (need - held).clamp(min=0), 0)
     count = t["free_count"].long()
