@@ -27,6 +27,13 @@
  *   aug_attn_plan_masked, aug_attn_mixed_scored
  *                     the same with a span of keys for every row, and with
  *                     capped or distance-biased scores
+ *   aug_step_tables   device: block tables, slot map, positions and draft masks of a
+ *                     step whose lengths are on the GPU
+ *   aug_rope_init, aug_rope_rows, aug_rope_append
+ *                     rotary positions: angles (host), rows, and rows into cache slots
+ *   aug_tree_plan, aug_attn_tree
+ *                     device: attention of drafted tokens, trees of them, over the cache
+ *   aug_sample        device: next tokens from logits
  *   aug_kv_park       device -> pinned host: swap-out of KV blocks
  *   aug_kv_resume     pinned host -> device: swap-in into (new) KV blocks
  *
@@ -437,6 +444,164 @@ aug_status aug_kv_append(const aug_attn_shape* shape, const aug_attn_plan_info* 
 aug_status aug_kv_read(const aug_attn_shape* shape, const void* k_cache, const void* v_cache,
                        const float* k_scale, const float* v_scale, const int64_t* slots, int64_t n,
                        int32_t num_pool_blocks, void* k_out, void* v_out, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Steps whose lengths are on the GPU                                         */
+/* ------------------------------------------------------------------------ */
+/* Where a step's lengths come out of the step before (how many drafted tokens were
+ * accepted), a plan made on the host would have to wait for them. The calls below
+ * take lengths, tables and trees from device memory: aug_step_tables, then for
+ * every layer aug_rope_append and aug_attn_tree, then aug_sample. None of them
+ * allocates, copies or waits, and all can be captured in a HIP graph. */
+
+#define AUG_MAX_DRAFT 64            /* most rows of one request where masks are kept */
+#define AUG_STEP_MAX_REQS 4096
+
+/* What became of a request in aug_step_tables. */
+typedef enum { AUG_STEP_OK = 0, AUG_STEP_NO_BLOCKS = 1, AUG_STEP_INVALID = 2 } aug_step_state;
+
+/* Tables of one step; device pointers.
+ *   num_reqs        0 to AUG_STEP_MAX_REQS
+ *   max_rows        rows that positions, slots, seen and parents have
+ *   max_blocks      columns of block_table, 1 to 2^20
+ *   num_pool_blocks places in free_ids
+ *   max_draft       1 to AUG_MAX_DRAFT: most rows of a request, and seen is written;
+ *                   0: any number of rows, seen and parents are NULL
+ *  read:
+ *   ctx_len[r]      tokens of request r in the cache before this step
+ *   q_len[r]        its rows in this step (0: none)
+ *   parents[row]    row of the same request, counted from its first, that the draft
+ *                   of this row follows; whatever is not an earlier row makes it a
+ *                   root. NULL: every row follows the one before
+ *  read and written:
+ *   block_table     [num_reqs][max_blocks] block ids of each request, held[r] of them
+ *   held[r]         0 before a request's first step
+ *   free_ids, free_count[1]  the free blocks, a stack of free_count ids
+ *  written:
+ *   q_start[r]      first row of request r; q_start[num_reqs] is the number of rows
+ *   kv_len[r]       ctx_len + q_len, or 0 for a request that is refused
+ *   state[r]        aug_step_state
+ *   positions[row]  ctx_len + number of the row's ancestors (a child's position is one
+ *                   more than its parent's)
+ *   slots[row]      block * 16 + slot of the row's token, which is token ctx_len + j of
+ *                   the request for its row j
+ *   seen[row]       bit j: row j of the request is the row itself or an ancestor
+ *   scratch         AUG_STEP_SCRATCH_BYTES, zero before the first call; a call leaves it
+ *                   zero. Calls that overlap need one each */
+#define AUG_STEP_SCRATCH_BYTES 16
+typedef struct {
+  int32_t num_reqs;
+  int32_t max_rows;
+  int32_t max_blocks;
+  int32_t num_pool_blocks;
+  int32_t max_draft;
+  int32_t reserved;            /* zero */
+  const int32_t* ctx_len;
+  const int32_t* q_len;
+  const int32_t* parents;
+  int32_t* block_table;
+  int32_t* held;
+  int32_t* free_ids;
+  int32_t* free_count;
+  int32_t* q_start;
+  int32_t* kv_len;
+  int32_t* state;
+  int32_t* positions;
+  int64_t* slots;
+  uint64_t* seen;
+  void* scratch;
+} aug_step_tables_args;
+
+/* The step's tables, from lengths on the GPU. A request needs ceil((ctx_len + q_len)
+ * / 16) blocks. Blocks that it holds beyond that (drafts that were not accepted, a
+ * request that has ended: ctx_len = q_len = 0) go back to the free ones, in the order
+ * of requests and columns, so that the first comes to lie on top of the stack; then
+ * requests that lack blocks take them from the top, in the order of requests. A
+ * request is refused, its blocks left as they were, its rows there with slot -1, mask
+ * 0 and position 0:
+ *   AUG_STEP_NO_BLOCKS  it takes blocks, and together with what earlier requests asked
+ *                       for there are too few
+ *   AUG_STEP_INVALID    a negative length, more than max_blocks blocks, held outside
+ *                       0 .. max_blocks, more than max_draft rows, or rows beyond max_rows
+ *                       (a row beyond is not written, and q_start goes no further)
+ * Entries of block_table beyond a request's blocks, places of free_ids above its top
+ * and rows behind the last are left as they were, except that blocks which came back
+ * stand above the top where they were taken again at once. One launch (none for no requests).
+ * Errors: AUG_ERR_INVALID (NULL pointers, sizes), AUG_ERR_UNSUPPORTED (more requests or
+ * blocks), AUG_ERR_HIP (launch). */
+aug_status aug_step_tables(const aug_step_tables_args* args, void* stream);
+
+/* Rotary positions. Pair i of the first rotary_dim dims of a head, (x, y), becomes
+ * magnitude * (x cos a - y sin a, y cos a + x sin a) with a = position * w_i; the other dims stay.
+ * Pairs: dims i and i + rotary_dim / 2, or interleaved: dims 2i and 2i + 1.
+ *   w_i = base^(-2i / rotary_dim), and then by `scaling`:
+ *   NONE    as it is
+ *   LINEAR  w_i / factor
+ *   BANDS   with t = original_len w_i / 2 pi, the turns within the original length:
+ *           w_i / factor for t <= low, w_i for t >= high, between them
+ *           w_i (m + (1 - m) / factor) with m = (t - low) / (high - low)
+ *   RAMP    with the pair number at which t falls to a given value, d(t) = rotary_dim
+ *           ln(original_len / (2 pi t)) / (2 ln base), from = max(floor(d(high)), 0) and
+ *           to = min(ceil(d(low)), rotary_dim - 1): w_i (1 - m + m / factor) with
+ *           m = (i - from) / max(to - from, 0.001), between 0 and 1 */
+typedef enum { AUG_ROPE_NONE = 0, AUG_ROPE_LINEAR = 1, AUG_ROPE_BANDS = 2, AUG_ROPE_RAMP = 3 } aug_rope_scaling;
+typedef struct {
+  int32_t rotary_dim;      /* a multiple of 16, up to 128 and the head_dim it is used with */
+  int32_t interleaved;     /* 0 or 1 */
+  int32_t scaling;         /* aug_rope_scaling */
+  int32_t original_len;    /* BANDS, RAMP: > 0 */
+  double base;             /* > 1 */
+  double factor;           /* every scaling but NONE: > 0 */
+  double low, high;        /* BANDS, RAMP: 0 < low < high, in turns */
+  double magnitude;        /* finite; 1 leaves lengths as they are */
+} aug_rope_params;
+
+/* Angles per position of every pair, in turns (w_i / 2 pi). Made once by aug_rope_init
+ * and passed by value from then on: plain host data, no ownership. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float magnitude;
+  int32_t reserved;
+  double turns[64];
+} aug_rope;
+
+/* Pure host code. Errors: AUG_ERR_INVALID (NULL, values out of the ranges above),
+ * AUG_ERR_UNSUPPORTED (rotary_dim). */
+aug_status aug_rope_init(const aug_rope_params* params, aug_rope* rope);
+
+/* Rotate the rows of q ([rows][num_q_heads][head_dim]) and k ([rows][num_kv_heads]
+ * [head_dim]) by their positions (device int32 [rows], any values: negated ones undo a
+ * rotation, and with them this is the gradient of the rotation). q or k may be NULL,
+ * with its output. float32 for f32 caches' shapes, else bf16; angles are reduced in
+ * float64, products and sums are float32 and rounded once. Consecutive rows lie
+ * *_stride elements apart (heads of a row are contiguous), a multiple of 16 bytes, at
+ * least the row's length; pointers 16-byte aligned. An output may be its input (with the same stride);
+ * no other overlap. One launch (none for no rows).
+ * Errors: AUG_ERR_INVALID (shape, NULL or misaligned pointers, strides, rows < 0, a rope
+ * that aug_rope_init has not made), AUG_ERR_UNSUPPORTED (rotary_dim above head_dim),
+ * AUG_ERR_HIP (launch). */
+aug_status aug_rope_rows(const aug_attn_shape* shape, const aug_rope* rope, const int32_t* positions, int32_t rows,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                         int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/* New K/V rows into slots of the cache (device int64 [rows], block * 16 + slot, as
+ * aug_step_tables writes them; rows of slots outside the pool are skipped), k rotated
+ * by its position on the way; and q rotated, if it is given, for the attention that
+ * follows. rope NULL: nothing is rotated (positions and q are NULL): an append by slots,
+ * which with aug_kv_read also moves rows within a cache, as after drafts that were not accepted.
+ * Caches, scales, rounding and encodings as for aug_kv_append, from the rotated float32
+ * values (rounded once). The slots of one call are distinct. fp8 caches: rows that
+ * follow one another in the call and in a block (each slot one more than the one before)
+ * share the growth of its scale, from the scale's old value unless the first of them is slot 0;
+ * the rows of one block must follow one another. Strides and alignment as for aug_rope_rows;
+ * q_out may be q, and nothing else overlaps. One launch (none for no rows).
+ * Errors: those of aug_rope_rows and aug_kv_append. */
+aug_status aug_rope_append(const aug_attn_shape* shape, const aug_rope* rope, const int32_t* positions,
+                           const int64_t* slots, int32_t rows, const void* q, int64_t q_stride, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                           void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t num_pool_blocks,
+                           void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Park / resume (Swap policy: swap-out during an external call, swap-in     */

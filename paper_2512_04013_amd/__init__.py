@@ -35,12 +35,18 @@ AUG_ROWS_AUTO, AUG_ROWS_VALU, AUG_ROWS_MFMA = 0, 1, 2
 AUG_TILES_AUTO, AUG_TILES_BF16, AUG_TILES_FP8_QK, AUG_TILES_FP8 = 0, 1, 2, 3
 
 DTYPE_CODES = {"f32": AUG_F32, "bf16": AUG_BF16, "fp8": AUG_FP8_E4M3FN, "fp4": AUG_MXFP4}
+AUG_STEP_OK, AUG_STEP_NO_BLOCKS, AUG_STEP_INVALID = 0, 1, 2
+AUG_ROPE_NONE, AUG_ROPE_LINEAR, AUG_ROPE_BANDS, AUG_ROPE_RAMP = 0, 1, 2, 3
+MAX_DRAFT, STEP_MAX_REQS, STEP_SCRATCH_BYTES = 64, 4096, 16
+
+ROPE_SCALINGS = {"none": AUG_ROPE_NONE, "linear": AUG_ROPE_LINEAR, "bands": AUG_ROPE_BANDS, "ramp": AUG_ROPE_RAMP}
 MXFP4_CELL_BYTES = 1088    # of one (block, KV head) of a 4-bit pool: uint8 [blocks][kv heads * 1088]
 
 EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked",
             "aug_attn_workspace_size",
             "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_scored", "aug_attn_mixed_noalloc",
-            "aug_kv_append", "aug_kv_read", "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
+            "aug_kv_append", "aug_kv_read", "aug_step_tables", "aug_rope_init", "aug_rope_rows", "aug_rope_append",
+            "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
             "aug_status_string", "aug_last_error", "aug_abi_version"]
 
 
@@ -86,6 +92,25 @@ class aug_row_mask(C.Structure):
 
 class aug_score_options(C.Structure):
     _fields_ = [("softcap", C.c_float), ("reserved", C.c_int32), ("slopes", C.c_void_p)]
+
+
+class aug_step_tables_args(C.Structure):
+    _fields_ = [("num_reqs", C.c_int32), ("max_rows", C.c_int32), ("max_blocks", C.c_int32), ("num_pool_blocks", C.c_int32),
+                ("max_draft", C.c_int32), ("reserved", C.c_int32), ("ctx_len", C.c_void_p), ("q_len", C.c_void_p),
+                ("parents", C.c_void_p), ("block_table", C.c_void_p), ("held", C.c_void_p), ("free_ids", C.c_void_p),
+                ("free_count", C.c_void_p), ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("state", C.c_void_p),
+                ("positions", C.c_void_p), ("slots", C.c_void_p), ("seen", C.c_void_p), ("scratch", C.c_void_p)]
+
+
+class aug_rope_params(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("original_len", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("magnitude", C.c_double)]
+
+
+class aug_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_double * 64)]
 
 
 class aug_request(C.Structure):
@@ -159,6 +184,11 @@ def lib():
     L.aug_kv_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_attn_plan_info), P, P, P, P, P,
                                 P, P, P, C.c_int32, P]
     L.aug_kv_read.argtypes = [C.POINTER(aug_attn_shape), P, P, P, P, P, C.c_int64, C.c_int32, P, P, P]
+    L.aug_step_tables.argtypes = [C.POINTER(aug_step_tables_args), P]
+    L.aug_rope_init.argtypes = [C.POINTER(aug_rope_params), C.POINTER(aug_rope)]
+    L.aug_rope_rows.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, C.c_int32] + [P, C.c_int64] * 4 + [P]
+    L.aug_rope_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, P, C.c_int32] + [P, C.c_int64] * 4 + \
+        [P, P, P, P, C.c_int32, P]
     L.aug_plan_upload.argtypes = [P, P, C.c_size_t, P]
     L.aug_kv_record_bytes.argtypes = [C.POINTER(aug_attn_shape)]
     L.aug_kv_record_bytes.restype = C.c_size_t
@@ -172,7 +202,8 @@ def lib():
     L.aug_request_return.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_double, C.c_int32]
     for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
               "aug_attn_mixed_scored", "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
-              "aug_form_batch", "aug_request_arrive", "aug_request_return"):
+              "aug_form_batch", "aug_request_arrive", "aug_request_return", "aug_step_tables", "aug_rope_init", "aug_rope_rows",
+              "aug_rope_append"):
         getattr(L, f).restype = C.c_int
     L.aug_status_string.argtypes = [C.c_int]
     L.aug_status_string.restype = C.c_char_p
@@ -407,6 +438,49 @@ def aug_kv_read(shape: aug_attn_shape, k_cache, v_cache, k_scale, v_scale, slots
     st = _stream(stream, k_out, k_cache)
     _check(lib().aug_kv_read(C.byref(shape), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
                              _ptr(slots), int(n), int(num_pool_blocks), _ptr(k_out), _ptr(v_out), st), "aug_kv_read")
+
+
+# ---- steps whose lengths are on the GPU ------------------------------------------------
+
+def aug_step_tables(args: aug_step_tables_args, stream=None):
+    """Enqueue a step's block tables, slots, positions and draft masks (``args``
+    holds device addresses: the caller keeps the tensors alive)."""
+    _check(lib().aug_step_tables(C.byref(args), _stream(stream)), "aug_step_tables")
+
+
+def aug_rope_init(rotary_dim: int, interleaved: bool = False, base: float = 10000.0, scaling="none", factor: float = 1.0,
+                  low: float = 1.0, high: float = 32.0, original_len: int = 0, magnitude: float = 1.0) -> aug_rope:
+    """The angles per position of every pair of a rotated head (see aug.h)."""
+    code = scaling if isinstance(scaling, int) else ROPE_SCALINGS[scaling]
+    p = aug_rope_params(int(rotary_dim), int(interleaved), code, int(original_len), float(base), float(factor), float(low),
+                        float(high), float(magnitude))
+    rope = aug_rope()
+    _check(lib().aug_rope_init(C.byref(p), C.byref(rope)), "aug_rope_init")
+    return rope
+
+
+def _rows_arg(t):
+    """Address and row stride (elements) of rows [rows][heads][dim] whose heads lie together."""
+    return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+
+
+def aug_rope_rows(shape: aug_attn_shape, rope: aug_rope, positions, q, k, q_out, k_out, stream=None):
+    """Enqueue the rotation of the rows of ``q`` and ``k`` (either may be None,
+    with its output) by ``positions`` (int32, one per row)."""
+    st = _stream(stream, positions)
+    _check(lib().aug_rope_rows(C.byref(shape), C.byref(rope), _ptr(positions), len(positions), *_rows_arg(q), *_rows_arg(k),
+                               *_rows_arg(q_out), *_rows_arg(k_out), st), "aug_rope_rows")
+
+
+def aug_rope_append(shape: aug_attn_shape, rope: Optional[aug_rope], positions, slots, q, k, v, q_out, k_cache, v_cache, k_scale,
+                    v_scale, num_pool_blocks: int, stream=None):
+    """Enqueue the write of rows ``k`` (rotated by ``positions``) and ``v`` into
+    ``slots`` (int64: block * 16 + slot) of the pool, and the rotation of ``q``
+    if it is given; without a rope nothing is rotated."""
+    st = _stream(stream, slots)
+    _check(lib().aug_rope_append(C.byref(shape), None if rope is None else C.byref(rope), _ptr(positions), _ptr(slots), len(slots),
+                                 *_rows_arg(q), *_rows_arg(k), *_rows_arg(v), *_rows_arg(q_out), _ptr(k_cache), _ptr(v_cache),
+                                 _ptr(k_scale), _ptr(v_scale), int(num_pool_blocks), st), "aug_rope_append")
 
 
 # ---- park / resume -------------------------------------------------------------------

@@ -24,8 +24,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libaug.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-HIP_SOURCES = ["attn.hip", "attn_scored.hip", "kvappend.hip", "kvread.hip", "kvpark.hip", "upload.hip"]
-CPP_SOURCES = ["plan.cpp", "former.cpp", "status.cpp"]
+HIP_SOURCES = ["attn.hip", "attn_scored.hip", "kvappend.hip", "kvread.hip", "kvpark.hip", "upload.hip", "tables.hip", "rope.hip"]
+CPP_SOURCES = ["plan.cpp", "former.cpp", "rope.cpp", "status.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}", "-Wall", "-Wno-unused-function"]
 HIP_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -21,6 +21,7 @@
 #include <cstdint>
 
 #include "aug.h"
+#include "cache_codes.h"
 #include "checks.h"
 #include "plan_format.h"
 #include "status.h"
@@ -29,6 +30,8 @@
 namespace {
 
 using aug::AppendItem;
+using aug::bf16_hi;
+using aug::bf16_lo;
 using aug::kBlock;
 
 constexpr int kThreads = 256;
@@ -48,62 +51,6 @@ struct AppendArgs {
   int32_t num_pool_blocks;
 };
 
-// E4M3FN code -> float, exact: exponent field 0 holds multiples of 2^-9,
-// otherwise (1 + m/8) * 2^(e - 7).
-__device__ __forceinline__ float fp8_value(uint32_t c) {
-  const uint32_t e = (c >> 3) & 15u, m = c & 7u;
-  const float mag = e == 0 ? static_cast<float>(m) * 0x1p-9f
-                           : __uint_as_float(((e + 120u) << 23) | (m << 20));
-  return (c & 0x80u) ? -mag : mag;
-}
-
-// Four floats -> four E4M3FN codes: round to nearest, ties to an even mantissa
-// (the conversion instruction's own rounding, subnormals included); every
-// magnitude from 448 up, and NaN, saturates to +-448; the sign of zero is kept.
-__device__ __forceinline__ uint32_t fp8_codes(const float* y) {
-  float v[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = fabsf(y[e]) < 448.f ? y[e] : copysignf(448.f, y[e]);
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true));
-}
-
-// x / s for many x by one s > 0. `fast` (s within 2^+-60): the correctly rounded
-// reciprocal and two exact remainders give the correctly rounded quotient; a
-// remainder that underflows belongs to a quotient below 2^-40, whose code is 0
-// either way. Otherwise the plain division. Bounded by instructions on large
-// appends: 8192 rows on the 64/8-head layer, 8 KV heads of 128 (33.6 MB of new
-// rows and 16.8 of codes), took 19.6 us with a division and a code in plain
-// operations per element and the maximum by shuffles, and take 11.75 (4.3 TB/s);
-// 256 decode rows 5.27 / 4.04.
-struct Divide {
-  float s, inv;
-  bool fast;
-  __device__ explicit Divide(float d) : s(d), inv(1.f / d), fast(d >= 0x1p-60f && d <= 0x1p60f) {}
-  __device__ __forceinline__ float operator()(float x) const {
-    if (!fast) return x / s;
-    float q = x * inv;
-    q = fmaf(fmaf(-q, s, x), inv, q);
-    q = fmaf(fmaf(-q, s, x), inv, q);
-    return copysignf(q, x);      // a NaN keeps its sign too
-  }
-};
-
-// Largest value over the wave, uniform: rotations within rows of 16 lanes, then
-// one lane of each row.
-template <int CTRL>
-__device__ __forceinline__ float max_with(float v) {
-  const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true);
-  return fmaxf(v, __int_as_float(o));
-}
-__device__ __forceinline__ float wave_max(float v) {
-  v = max_with<0x121>(max_with<0x122>(max_with<0x124>(max_with<0x128>(v))));   // row_ror
-  float m[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * i));
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-}
-
 // An append item read with one 16-byte load (the index is the same for the
 // whole wave, so it goes through the scalar cache).
 __device__ __forceinline__ AppendItem load_item(const AppendItem* items, int64_t idx) {
@@ -113,9 +60,6 @@ __device__ __forceinline__ AppendItem load_item(const AppendItem* items, int64_t
   __builtin_memcpy(&it, &raw, sizeof(it));
   return it;
 }
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // f32 and bf16 caches: the rows are stored as they come.
 template <int EB, int D>
@@ -158,72 +102,30 @@ __global__ __launch_bounds__(kThreads) void append_fp8_kernel(AppendArgs a) {
   const int32_t bid = a.block_ids[it.bt_index];
   const bool bid_ok = static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks);
   const uint16_t* src = reinterpret_cast<const uint16_t*>(is_v ? a.v_new : a.k_new);
-  uint8_t* blk = reinterpret_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) +
-                 (static_cast<int64_t>(bid) * a.hkv + kvh) * kBlock * D;
-  float* scale = (is_v ? a.v_scale : a.k_scale) + static_cast<int64_t>(bid) * a.hkv + kvh;
   const int col = (lane % LPR) * 8;
   const int r0 = lane / LPR;
 
   float x[PASSES][8];
-  float amax = 0.f;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    const int r = r0 + p * RPP;
+    const int r = r0 + p * RPP - it.slot0;
     uint4 w{0u, 0u, 0u, 0u};
-    if (r < it.n_rows)
+    if (r >= 0 && r < it.n_rows)
       w = *reinterpret_cast<const uint4*>(src + ((static_cast<int64_t>(it.q_row0) + r) * a.hkv + kvh) * D + col);
     x[p][0] = bf16_lo(w.x); x[p][1] = bf16_hi(w.x);
     x[p][2] = bf16_lo(w.y); x[p][3] = bf16_hi(w.y);
     x[p][4] = bf16_lo(w.z); x[p][5] = bf16_hi(w.z);
     x[p][6] = bf16_lo(w.w); x[p][7] = bf16_hi(w.w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[p][e]));
   }
-  const float s_old = bid_ok && it.slot0 > 0 ? *scale : 0.f;
-  amax = wave_max(amax);
   if (!bid_ok) return;
-
-  const float need = amax / 448.f;
-  float s = need;
-  if (it.slot0 > 0) {
-    if (need > s_old) {
-      // the scale grows: re-encode the block's earlier tokens
-      const Divide by(need);
-      for (int r = r0; r < it.slot0; r += RPP) {
-        uint2* q = reinterpret_cast<uint2*>(blk + r * D + col);
-        const uint2 c = *q;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = by(fp8_value(((e < 4 ? c.x : c.y) >> (8 * (e & 3))) & 0xFFu) * s_old);
-        *q = uint2{fp8_codes(v), fp8_codes(v + 4)};
-      }
-    } else {
-      s = s_old;
-    }
-  }
-  const Divide by(s);
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int r = r0 + p * RPP;
-    if (r >= it.n_rows) break;
-    uint2 c{0u, 0u};
-    if (s != 0.f) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[p][e] = by(x[p][e]);
-      c = uint2{fp8_codes(x[p]), fp8_codes(x[p] + 4)};
-    }
-    *reinterpret_cast<uint2*>(blk + (it.slot0 + r) * D + col) = c;
-  }
-  if (lane == 0) *scale = s;
+  const int64_t cell = static_cast<int64_t>(bid) * a.hkv + kvh;
+  aug::store_fp8_tokens(reinterpret_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) + cell * kBlock * D,
+                        (is_v ? a.v_scale : a.k_scale) + cell, ((1u << it.n_rows) - 1u) << it.slot0, lane,
+                        [&](int p, int e) { return x[p][e]; });
 }
 
 // MXFP4 caches (head_dim 128): bf16 rows in, codes and a scale byte for every 32
-// dims out. A lane takes eight dims of a row, so a group of 32 is a quad of lanes:
-// its maximum is two quad permutations away. The scale is a power of two (from
-// the maximum's exponent field, one higher from 1.75 * 2^k on, where the largest
-// element would otherwise lose more than an eighth to saturation), so dividing
-// by it is exact and the only rounding is the conversion's, to nearest even.
-// Rows are independent: a block's earlier tokens are left alone. 8.1k rows of 8 KV
+// dims out. A lane takes eight dims of a row. Rows are independent: a block's earlier tokens are left alone. 8.1k rows of 8 KV
 // heads (33 MB in, 9 out) take 9.5 us of GPU time, a few decodes 2.4.
 __global__ __launch_bounds__(kThreads) void append_fp4_kernel(AppendArgs a) {
   constexpr int D = 128;
@@ -249,29 +151,13 @@ __global__ __launch_bounds__(kThreads) void append_fp4_kernel(AppendArgs a) {
   }
   if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) return;
   char* block = (is_v ? a.v_cache : a.k_cache) + static_cast<int64_t>(bid) * a.hkv * aug::kMxCell;
-  char* codes = block + kvh * aug::kMxCodes;
-  char* scales = block + a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
 #pragma unroll
   for (int p = 0; p < kBlock / RPP; ++p) {
     const int r = r0 + p * RPP;
     if (r >= it.n_rows) break;
     const float x[8] = {bf16_lo(w[p].x), bf16_hi(w[p].x), bf16_lo(w[p].y), bf16_hi(w[p].y),
                         bf16_lo(w[p].z), bf16_hi(w[p].z), bf16_lo(w[p].w), bf16_hi(w[p].w)};
-    float amax = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-    amax = max_with<0x4E>(max_with<0xB1>(amax));       // over the quad: lanes ^ 1, ^ 2
-    const int field = static_cast<int>((__float_as_uint(amax) + (1u << 21)) >> 23);
-    const int byte = min(max(field - 2, 2), 252);
-    const float s = __uint_as_float(static_cast<uint32_t>(byte) << 23);
-    uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], s, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
-    const int slot = it.slot0 + r, group = oct >> 2;
-    const int at = is_v ? 256 * (slot >> 2) + 16 * oct + 4 * (slot & 3) : 64 * slot + 4 * oct;
-    *reinterpret_cast<uint32_t*>(codes + at) = c;
-    if ((oct & 3) == 0) scales[is_v ? 16 * group + slot : 4 * slot + group] = static_cast<char>(byte);
+    aug::store_fp4_octet(block, a.hkv, kvh, is_v, it.slot0 + r, oct, x);
   }
 }
 

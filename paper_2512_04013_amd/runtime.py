@@ -13,8 +13,9 @@ import time
 import numpy as np
 import torch
 
-from . import (AUG_F32, AUG_MXFP4, MXFP4_CELL_BYTES, aug_attn_mixed, aug_attn_plan, aug_kv_append, aug_kv_park, aug_kv_read,
-               aug_kv_record_bytes, aug_kv_resume, aug_plan_upload, make_shape)
+from . import (AUG_F32, AUG_MXFP4, MAX_DRAFT, MXFP4_CELL_BYTES, STEP_SCRATCH_BYTES, _current_stream, aug_attn_mixed, aug_attn_plan,
+               aug_kv_append, aug_kv_park, aug_kv_read, aug_kv_record_bytes, aug_kv_resume, aug_plan_upload, aug_rope_append,
+               aug_rope_init, aug_rope_rows, aug_step_tables, aug_step_tables_args, make_shape)
 
 _TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8, "fp4": torch.uint8}
 
@@ -40,6 +41,25 @@ def _allocating_on(stream, device):
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
     return torch.cuda.stream(stream)
+
+
+def _on(index: int):
+    """Context in which ``index`` is torch's current device: the library's calls
+    are made for the current one."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+
+def _check_rows(t, name, rows, heads, dim, dtype, index):
+    """Rows [rows][heads][dim] on a device whose heads lie together (rows may lie further apart)."""
+    if t.shape != (rows, heads, dim) or t.dtype != dtype or t.get_device() != index or t.stride(2) != 1 or \
+            (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{name}: rows of shape ({rows}, {heads}, {dim}) and {dtype} on device {index}, heads of a row together, "
+                         f"got {t.dtype} {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+
+
+def _check_vector(t, name, n, dtype, index):
+    if t.shape != (n,) or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} vector of {n} on device {index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class PagedKV:
@@ -101,6 +121,141 @@ class PagedKV:
         aug_kv_read(self.shape, self.k_cache, self.v_cache, self.k_scale, self.v_scale, slots, n,
                     self.num_pool_blocks, k_out, v_out, stream=stream)
         return k_out, v_out
+
+
+    def append_rows(self, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor = None, rope: "Rope" = None,
+                    positions: torch.Tensor = None, q_out: torch.Tensor = None, stream=None):
+        """Write K/V rows ([n][H_kv][D], rows may be strided) into ``slots`` (int64,
+        block * 16 + slot; rows of slots outside the pool are skipped), K rotated by
+        ``positions`` (int32) where a ``rope`` is given. With ``q`` its rows are
+        rotated too, into ``q_out`` (may be ``q``; allocated on ``stream`` if None),
+        which is returned. Without a rope and with what ``read`` returns, rows move
+        to other slots."""
+        n, (hkv, dim), index = len(slots), self._row, self._device
+        _check_vector(slots, "slots", n, torch.int64, index)
+        _check_rows(k, "k", n, hkv, dim, self._row_dtype, index)
+        _check_rows(v, "v", n, hkv, dim, self._row_dtype, index)
+        if rope is None and (q is not None or positions is not None):
+            raise ValueError("queries and positions need a rope")
+        if rope is not None:
+            if positions is None:
+                raise ValueError("a rope needs positions")
+            _check_vector(positions, "positions", n, torch.int32, index)
+        if q is None:
+            if q_out is not None:
+                raise ValueError("q_out without q")
+        else:
+            hq = self.shape.num_q_heads
+            _check_rows(q, "q", n, hq, dim, self._row_dtype, index)
+            if q_out is None:
+                with _allocating_on(stream, q.device):
+                    q_out = torch.empty((n, hq, dim), dtype=q.dtype, device=q.device)
+            _check_rows(q_out, "q_out", n, hq, dim, self._row_dtype, index)
+        with _on(index):
+            aug_rope_append(self.shape, None if rope is None else rope.angles, positions, slots, q, k, v, q_out, self.k_cache,
+                            self.v_cache, self.k_scale, self.v_scale, self.num_pool_blocks, stream=stream)
+        return q_out
+
+
+class Rope:
+    """Rotary positions: the angles of the first ``rotary_dim`` dims of a head, in
+    halves (dims i and i + rotary_dim / 2) or ``interleaved`` (2i and 2i + 1), with
+    ``scaling`` "none", "linear", "bands" or "ramp" for long contexts (the formulas
+    are in aug.h)."""
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling="none", factor: float = 1.0,
+                 low: float = 1.0, high: float = 32.0, original_len: int = 0, magnitude: float = 1.0):
+        self.angles = aug_rope_init(rotary_dim, interleaved, base, scaling, factor, low, high, original_len, magnitude)
+
+
+def rope_rows(shape, rope: Rope, positions: torch.Tensor, q: torch.Tensor = None, k: torch.Tensor = None, q_out: torch.Tensor = None,
+              k_out: torch.Tensor = None, stream=None):
+    """Rotate rows of q ([rows][H_q][D]) and k ([rows][H_kv][D]; either may be
+    None, rows may be strided) by ``positions`` (int32). Outputs may be the inputs;
+    those that are None are allocated on ``stream``. Returns (q_out, k_out).
+    Gradients go back through the same call with negated positions."""
+    n, index = len(positions), positions.get_device()
+    _check_vector(positions, "positions", n, torch.int32, index)
+    dtype = torch.float32 if shape.q_dtype == AUG_F32 else torch.bfloat16
+    outs = []
+    for name, x, out, heads in (("q", q, q_out, shape.num_q_heads), ("k", k, k_out, shape.num_kv_heads)):
+        if x is not None:
+            _check_rows(x, name, n, heads, shape.head_dim, dtype, index)
+            if out is None:
+                with _allocating_on(stream, x.device):
+                    out = torch.empty((n, heads, shape.head_dim), dtype=dtype, device=x.device)
+            _check_rows(out, name + "_out", n, heads, shape.head_dim, dtype, index)
+        elif out is not None:
+            raise ValueError(f"{name}_out without {name}")
+        outs.append(out)
+    with _on(index):
+        aug_rope_rows(shape, rope.angles, positions, q, k, *outs, stream=stream)
+    return tuple(outs)
+
+
+class StepTables:
+    """Tables of steps whose lengths are on the GPU: which blocks every request
+    holds, and for the step's rows where they start, their positions, slots and (with
+    ``max_draft``) the drafts of their request that each sees. All of them are device
+    tensors that ``update`` writes in place, so that it can be captured in a graph
+    together with what reads them.
+
+    ``max_reqs`` requests (unused ones have lengths 0), ``max_rows`` rows of one step,
+    ``max_blocks`` columns of the table, a pool of ``num_pool_blocks``. Without
+    ``block_table`` and ``held`` no request holds blocks; ``free_ids`` (int32
+    [num_pool_blocks], the first ``free_count`` of which are free, all by default) stands
+    for all blocks of the pool by default. Tensors given here are used, not copied."""
+
+    def __init__(self, max_reqs: int, max_rows: int, max_blocks: int, num_pool_blocks: int, max_draft: int = MAX_DRAFT, device="cuda",
+                 block_table: torch.Tensor = None, held: torch.Tensor = None, free_ids: torch.Tensor = None, free_count: int = None):
+        device = torch.device(device)
+        if (block_table is None) != (held is None) or (block_table is not None and free_ids is None):
+            raise ValueError("a block table comes with what is held and which blocks are free")
+        self.max_reqs, self.max_rows, self.max_blocks = int(max_reqs), int(max_rows), int(max_blocks)
+        self.num_pool_blocks, self.max_draft = int(num_pool_blocks), int(max_draft)
+        if free_count is None:
+            free_count = self.num_pool_blocks
+        if not 0 <= free_count <= self.num_pool_blocks:
+            raise ValueError(f"{free_count} free blocks of {self.num_pool_blocks}")
+        zeros = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+        self.block_table = zeros(self.max_reqs, self.max_blocks) if block_table is None else block_table
+        self.held = zeros(self.max_reqs) if held is None else held
+        self.free_ids = torch.arange(self.num_pool_blocks, dtype=torch.int32, device=device) if free_ids is None else free_ids
+        self.free_count = torch.full((1,), int(free_count), dtype=torch.int32, device=device)
+        self.q_start, self.kv_len, self.state = zeros(self.max_reqs + 1), zeros(self.max_reqs), zeros(self.max_reqs)
+        self.positions, self.slots = zeros(self.max_rows), zeros(self.max_rows, dtype=torch.int64)
+        self.seen = zeros(self.max_rows, dtype=torch.int64) if self.max_draft else None
+        self._scratch = zeros(STEP_SCRATCH_BYTES, dtype=torch.uint8)
+        self.device = self.q_start.device
+        self._index = index = self.q_start.get_device()
+        _check_vector(self.held, "held", self.max_reqs, torch.int32, index)
+        _check_vector(self.free_ids, "free_ids", self.num_pool_blocks, torch.int32, index)
+        t = self.block_table
+        if t.shape != (self.max_reqs, self.max_blocks) or t.dtype != torch.int32 or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"block_table: contiguous int32 of shape ({self.max_reqs}, {self.max_blocks}) on {self.device}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
+        at = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        self._args = aug_step_tables_args(
+            self.max_reqs, self.max_rows, self.max_blocks, self.num_pool_blocks, self.max_draft, 0, None, None, None, at(t), at(self.held),
+            at(self.free_ids), at(self.free_count), at(self.q_start), at(self.kv_len), at(self.state), at(self.positions),
+            at(self.slots), at(self.seen), at(self._scratch))
+
+    def update(self, ctx_len: torch.Tensor, q_len: torch.Tensor, parents: torch.Tensor = None, stream=None):
+        """Enqueue the tables of a step of ``q_len`` rows a request after ``ctx_len``
+        tokens in the cache (int32 [max_reqs]); ``parents`` (int32 [max_rows]): the row of
+        the same request that each draft follows, -1 for a root; None: every row follows
+        the one before. Blocks that requests no longer need are free again, new ones are
+        taken. ``state`` says which requests were refused."""
+        index = self._index
+        _check_vector(ctx_len, "ctx_len", self.max_reqs, torch.int32, index)
+        _check_vector(q_len, "q_len", self.max_reqs, torch.int32, index)
+        if parents is not None:
+            _check_vector(parents, "parents", self.max_rows, torch.int32, index)
+        a = self._args
+        a.ctx_len, a.q_len = ctx_len.data_ptr(), q_len.data_ptr()
+        a.parents = None if parents is None else parents.data_ptr()
+        with _on(index):
+            aug_step_tables(a, stream=_current_stream(index) if stream is None else stream)
 
 
 class MixedAttention:

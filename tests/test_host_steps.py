@@ -1,0 +1,174 @@
+"""Steps whose lengths are on the GPU, as far as the CPU goes: angles of rotary
+positions, and every call that is refused before anything is launched."""
+
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import paper_2512_04013_amd as aug
+from oracle import rope as orope
+
+ROPES = [dict(), dict(base=500000.0), dict(scaling="linear", factor=4.0),
+         dict(base=500000.0, scaling="bands", factor=8.0, low=1.0, high=4.0, original_len=8192),
+         dict(base=1e6, scaling="ramp", factor=4.0, low=1.0, high=32.0, original_len=32768),
+         dict(scaling="ramp", factor=40.0, low=1.0, high=32.0, original_len=64)]
+
+
+@pytest.mark.parametrize("dim", [16, 48, 64, 128])
+@pytest.mark.parametrize("kw", ROPES)
+def test_angles(dim, kw):
+    rope = aug.aug_rope_init(dim, **kw)
+    want = orope.frequencies(dim, **kw) / (2 * math.pi)
+    got = np.array(list(rope.turns))
+    # a power, two products and two quotients, each correct to a unit or two in the last place
+    np.testing.assert_allclose(got[:dim // 2], want, rtol=16 * 2.0 ** -53)
+    assert (got[dim // 2:] == 0).all() and rope.rotary_dim == dim
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rotary_dim=0), aug.AUG_ERR_UNSUPPORTED), (dict(rotary_dim=24), aug.AUG_ERR_UNSUPPORTED),
+    (dict(rotary_dim=144), aug.AUG_ERR_UNSUPPORTED), (dict(rotary_dim=-16), aug.AUG_ERR_UNSUPPORTED),
+    (dict(base=1.0), aug.AUG_ERR_INVALID), (dict(base=float("nan")), aug.AUG_ERR_INVALID), (dict(base=float("inf")), aug.AUG_ERR_INVALID),
+    (dict(scaling=4), aug.AUG_ERR_INVALID), (dict(scaling=-1), aug.AUG_ERR_INVALID),
+    (dict(scaling="linear", factor=0.0), aug.AUG_ERR_INVALID), (dict(scaling="linear", factor=float("nan")), aug.AUG_ERR_INVALID),
+    (dict(scaling="linear", factor=1e-5), aug.AUG_ERR_INVALID),
+    (dict(scaling="bands", factor=2.0), aug.AUG_ERR_INVALID),
+    (dict(scaling="bands", factor=2.0, original_len=10, low=4.0, high=4.0), aug.AUG_ERR_INVALID),
+    (dict(scaling="ramp", factor=2.0, original_len=10, low=0.0, high=4.0), aug.AUG_ERR_INVALID),
+    (dict(scaling="ramp", factor=2.0, original_len=10, low=1.0, high=float("inf")), aug.AUG_ERR_INVALID),
+    (dict(magnitude=float("nan")), aug.AUG_ERR_INVALID), (dict(magnitude=float("inf")), aug.AUG_ERR_INVALID)])
+def test_angles_refused(kw, status):
+    with pytest.raises(aug.AugError) as e:
+        aug.aug_rope_init(**{"rotary_dim": 64, **kw})
+    assert e.value.status == status
+
+
+def test_angles_refuse_null_and_flags():
+    p, r = aug.aug_rope_params(64, 2, 0, 0, 10000.0, 1.0, 1.0, 2.0, 1.0), aug.aug_rope()
+    assert aug.lib().aug_rope_init(C.byref(p), C.byref(r)) == aug.AUG_ERR_INVALID
+    p.interleaved = 1
+    assert aug.lib().aug_rope_init(None, C.byref(r)) == aug.AUG_ERR_INVALID
+    assert aug.lib().aug_rope_init(C.byref(p), None) == aug.AUG_ERR_INVALID
+    assert aug.lib().aug_rope_init(C.byref(p), C.byref(r)) == aug.AUG_OK
+
+
+# ---- device calls: addresses that are never used, since every call is refused -------------
+
+P = 1 << 20          # an aligned address
+
+
+def _tables(**kw):
+    f = dict(num_reqs=4, max_rows=8, max_blocks=4, num_pool_blocks=16, max_draft=4, reserved=0)
+    f.update({n: P for n, _ in aug.aug_step_tables_args._fields_[6:]})
+    f.update(kw)
+    return aug.aug_step_tables_args(**f)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_reqs=-1), aug.AUG_ERR_INVALID), (dict(max_rows=-1), aug.AUG_ERR_INVALID), (dict(max_rows=2 ** 31 - 1), aug.AUG_ERR_INVALID),
+    (dict(max_blocks=0), aug.AUG_ERR_INVALID), (dict(num_pool_blocks=0), aug.AUG_ERR_INVALID), (dict(max_draft=-1), aug.AUG_ERR_INVALID),
+    (dict(max_draft=65), aug.AUG_ERR_INVALID), (dict(reserved=1), aug.AUG_ERR_INVALID), (dict(num_reqs=4097), aug.AUG_ERR_UNSUPPORTED),
+    (dict(max_blocks=(1 << 20) + 1), aug.AUG_ERR_UNSUPPORTED), (dict(max_draft=0), aug.AUG_ERR_INVALID),
+    (dict(max_draft=0, parents=None), aug.AUG_ERR_INVALID), (dict(max_draft=0, seen=None), aug.AUG_ERR_INVALID)]
+    + [({n: None}, aug.AUG_ERR_INVALID) for n, _ in aug.aug_step_tables_args._fields_[6:] if n != "parents"])
+def test_tables_refused(kw, status):
+    a = _tables(**kw)
+    assert aug.lib().aug_step_tables(C.byref(a), None) == status, aug.aug_last_error()
+    assert aug.aug_last_error()
+
+
+def test_tables_of_nothing():
+    assert aug.lib().aug_step_tables(None, None) == aug.AUG_ERR_INVALID
+    a = aug.aug_step_tables_args(0, 0, 1, 1, 4, 0)
+    assert aug.lib().aug_step_tables(C.byref(a), None) == aug.AUG_OK
+
+
+def _shape(kv="bf16", hq=8, hkv=2, d=128):
+    io = "f32" if kv == "f32" else "bf16"
+    return aug.make_shape(hq, hkv, d, io, kv, io, 0.1)
+
+
+def _rows(shape=None, rope=None, **kw):
+    a = dict(positions=P, rows=3, q=P, q_stride=1024, k=P, k_stride=256, q_out=P, q_out_stride=1024, k_out=P, k_out_stride=256)
+    a.update(kw)
+    rope = aug.aug_rope_init(64) if rope is None else rope
+    return aug.lib().aug_rope_rows(C.byref(shape or _shape()), C.byref(rope), *a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(positions=None), dict(rows=-1), dict(q_out=None), dict(q=None), dict(k_out=None), dict(k=None),
+    dict(q=None, q_out=None, k=None, k_out=None), dict(q=P + 8), dict(k=P + 2), dict(q_out=P + 4, q=P + 4), dict(q_stride=1016, q_out_stride=1016),
+    dict(q_stride=1028), dict(k_stride=-256), dict(k_out_stride=0), dict(q_out_stride=2048), dict(k_stride=1 << 50)])
+def test_rows_refused(kw):
+    assert _rows(**kw) == aug.AUG_ERR_INVALID and aug.aug_last_error()
+
+
+def test_rows_shapes_refused():
+    assert _rows(rows=0) == aug.AUG_OK
+    assert aug.lib().aug_rope_rows(C.byref(_shape()), None, P, 1, P, 1024, None, 0, P, 1024, None, 0, None) == aug.AUG_ERR_INVALID
+    assert _rows(shape=_shape(hq=7)) == aug.AUG_ERR_INVALID
+    assert _rows(shape=_shape(d=64), rope=aug.aug_rope_init(128)) == aug.AUG_ERR_UNSUPPORTED
+    for name, value in (("rotary_dim", 24), ("rotary_dim", 0), ("interleaved", 2), ("reserved", 1)):
+        rope = aug.aug_rope_init(64)
+        setattr(rope, name, value)
+        assert _rows(rope=rope) == aug.AUG_ERR_INVALID
+
+
+def _append(shape=None, rope=True, **kw):
+    a = dict(positions=P, slots=P, rows=3, q=P, q_stride=1024, k=P, k_stride=256, v=P, v_stride=256, q_out=P, q_out_stride=1024,
+             k_cache=P, v_cache=P, k_scale=P, v_scale=P, num_pool_blocks=4)
+    a.update(kw)
+    r = C.byref(aug.aug_rope_init(64)) if rope else None
+    return aug.lib().aug_rope_append(C.byref(shape or _shape()), r, *a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(positions=None), dict(slots=None), dict(slots=P + 4), dict(rows=-1), dict(q=None), dict(q_out=None), dict(k=None), dict(v=None),
+    dict(k_cache=None), dict(v_cache=None), dict(k_cache=P + 8), dict(num_pool_blocks=0), dict(k=P + 8), dict(v_stride=128),
+    dict(v_stride=260), dict(q_out_stride=2048), dict(rope=False), dict(rope=False, positions=None),
+    dict(rope=False, q=None, q_out=None)])
+def test_append_refused(kw):
+    assert _append(**kw) == aug.AUG_ERR_INVALID and aug.aug_last_error()
+
+
+def test_append_shapes_refused():
+    assert _append(rows=0) == aug.AUG_OK
+    assert _append(shape=_shape("fp8"), k_scale=None) == aug.AUG_ERR_INVALID
+    assert _append(shape=_shape("fp8"), v_scale=None) == aug.AUG_ERR_INVALID
+    assert _append(shape=_shape("fp4", d=64)) == aug.AUG_ERR_UNSUPPORTED
+    assert _append(shape=_shape(hq=6)) == aug.AUG_ERR_UNSUPPORTED
+
+
+def test_python_refuses():
+    torch = pytest.importorskip("torch")
+    from paper_2512_04013_amd import runtime as rt
+    pool = torch.zeros(4, 2, 16, 128, dtype=torch.bfloat16)
+    kv = rt.PagedKV(_shape(), pool, pool.clone(), staging_bytes=1)
+    slots, rows = torch.zeros(3, dtype=torch.int64), torch.zeros(3, 2, 128, dtype=torch.bfloat16)
+    q, pos = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    rope = rt.Rope(64)
+    bad = [dict(slots=slots.int()), dict(slots=slots[:2]), dict(k=rows.float()), dict(v=rows[:, :1]), dict(k=rows.transpose(0, 1)),
+           dict(k=torch.zeros(3, 128, 2, dtype=torch.bfloat16).transpose(1, 2)), dict(q=q), dict(positions=pos), dict(rope=rope),
+           dict(q=q, rope=rope, positions=pos.long()), dict(q=q[:, :4], rope=rope, positions=pos),
+           dict(q_out=q, rope=rope, positions=pos), dict(q=q, q_out=q.float(), rope=rope, positions=pos)]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            kv.append_rows(**{"slots": slots, "k": rows, "v": rows, **kw})
+    for kw in (dict(q=q.float()), dict(k=rows[:2]), dict(q=q, k_out=rows), dict(q=q, q_out=q[:2])):
+        with pytest.raises(ValueError):
+            rt.rope_rows(_shape(), rope, pos, **kw)
+    with pytest.raises(ValueError):
+        rt.rope_rows(_shape(), rope, pos.long(), q)
+    table, held = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    free = torch.arange(8, dtype=torch.int32)
+    for kw in (dict(block_table=table), dict(block_table=table, held=held), dict(block_table=table[:1], held=held, free_ids=free),
+               dict(block_table=table, held=held.long(), free_ids=free), dict(free_ids=free[:4]), dict(free_count=9)):
+        with pytest.raises(ValueError):
+            rt.StepTables(2, 8, 4, 8, device="cpu", **kw)
+    t = rt.StepTables(2, 8, 4, 8, device="cpu", block_table=table, held=held, free_ids=free)
+    two = torch.zeros(2, dtype=torch.int32)
+    for args in ((two[:1], two), (two, two.long()), (two, two, two), (two.repeat(2)[::2], two)):
+        with pytest.raises(ValueError):
+            t.update(*args)
