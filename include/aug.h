@@ -603,6 +603,57 @@ aug_status aug_rope_append(const aug_attn_shape* shape, const aug_rope* rope, co
                            void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t num_pool_blocks,
                            void* stream);
 
+/* Attention of drafted tokens over the paged cache, trees of them: the rows of request r,
+ * q_start[r] .. q_start[r + 1] - 1 of q, are its last tokens, already in the cache; each
+ * sees all kv_len - n tokens before them and, of these n, row j if bit j of its mask is
+ * set (itself is no exception): O = softmax(softmax_scale q K^T) V over those keys. A row
+ * that sees nothing gives zeros, as do rows of a request with kv_len 0. A request has up
+ * to max_draft rows; one row is a plain decode.
+ *
+ * The arrays are those of aug_step_tables: device q_start [num_reqs + 1], kv_len
+ * [num_reqs], seen [max_rows], block_table [num_reqs][max_blocks]. */
+typedef struct {
+  int32_t num_reqs;            /* 0 to AUG_STEP_MAX_REQS */
+  int32_t max_rows;            /* rows of q, out and seen */
+  int32_t max_blocks;          /* columns of block_table, 1 to 2^20 */
+  int32_t max_draft;           /* 1 to AUG_MAX_DRAFT */
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  const int32_t* block_table;
+  const uint64_t* seen;
+} aug_tree_batch;
+
+/* Device bytes of the work list of aug_tree_plan and of the workspace of aug_attn_tree,
+ * for any lengths of a batch with these num_reqs and max_draft. Pure host code.
+ * Errors: AUG_ERR_INVALID (shape, NULL, sizes), AUG_ERR_UNSUPPORTED (more requests, or
+ * more work items than 2^24). */
+aug_status aug_tree_plan_size(const aug_attn_shape* shape, const aug_tree_batch* batch, size_t* plan_bytes,
+                              size_t* workspace_bytes);
+
+/* The work list of a step, made on the GPU from q_start and kv_len: once a step, for
+ * all layers of this shape. plan_dev: plan_bytes of device memory, 16-byte aligned, written.
+ * Lengths out of range (rows beyond max_rows or max_draft, keys beyond max_blocks) are
+ * cut. One launch (none for no requests or rows).
+ * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers),
+ * AUG_ERR_NO_SPACE (plan_bytes), AUG_ERR_HIP (launch). */
+aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batch, void* plan_dev, size_t plan_bytes,
+                         void* stream);
+
+/* The attention of a planned step. Device memory: q and out [max_rows][num_q_heads]
+ * [head_dim], of which rows from q_start[num_reqs] on, and those of a request beyond
+ * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out too);
+ * workspace 16-byte aligned, its contents do not matter. The caches' tokens 0 .. kv_len - 1
+ * of a request are finite where some row of it sees them; anything may stand elsewhere. Keys of
+ * block ids outside the pool count for nothing. Sums and softmax statistics are fp32;
+ * over every cache but F32 each probability is taken as bf16 (off by at most 2^-8 of it, in the row's sum as
+ * in its products). Calls that overlap need a workspace each; equal inputs give equal bits.
+ * Two launches (none for no requests or rows).
+ * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers,
+ * missing scales), AUG_ERR_NO_SPACE (workspace_bytes), AUG_ERR_HIP (launch). */
+aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batch, const void* plan_dev, const void* q,
+                         const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                         int32_t num_pool_blocks, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Park / resume (Swap policy: swap-out during an external call, swap-in     */
 /* when it returns; Appendix B, Algorithm 1 step (2))                         */

@@ -46,6 +46,7 @@ EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_at
             "aug_attn_workspace_size",
             "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_scored", "aug_attn_mixed_noalloc",
             "aug_kv_append", "aug_kv_read", "aug_step_tables", "aug_rope_init", "aug_rope_rows", "aug_rope_append",
+            "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree",
             "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
             "aug_status_string", "aug_last_error", "aug_abi_version"]
 
@@ -100,6 +101,11 @@ class aug_step_tables_args(C.Structure):
                 ("parents", C.c_void_p), ("block_table", C.c_void_p), ("held", C.c_void_p), ("free_ids", C.c_void_p),
                 ("free_count", C.c_void_p), ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("state", C.c_void_p),
                 ("positions", C.c_void_p), ("slots", C.c_void_p), ("seen", C.c_void_p), ("scratch", C.c_void_p)]
+
+
+class aug_tree_batch(C.Structure):
+    _fields_ = [("num_reqs", C.c_int32), ("max_rows", C.c_int32), ("max_blocks", C.c_int32), ("max_draft", C.c_int32),
+                ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p), ("seen", C.c_void_p)]
 
 
 class aug_rope_params(C.Structure):
@@ -189,6 +195,10 @@ def lib():
     L.aug_rope_rows.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, C.c_int32] + [P, C.c_int64] * 4 + [P]
     L.aug_rope_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, P, C.c_int32] + [P, C.c_int64] * 4 + \
         [P, P, P, P, C.c_int32, P]
+    batch = [C.POINTER(aug_attn_shape), C.POINTER(aug_tree_batch)]
+    L.aug_tree_plan_size.argtypes = batch + [C.POINTER(C.c_size_t)] * 2
+    L.aug_tree_plan.argtypes = batch + [P, C.c_size_t, P]
+    L.aug_attn_tree.argtypes = batch + [P] * 6 + [C.c_int32, P, P, C.c_size_t, P]
     L.aug_plan_upload.argtypes = [P, P, C.c_size_t, P]
     L.aug_kv_record_bytes.argtypes = [C.POINTER(aug_attn_shape)]
     L.aug_kv_record_bytes.restype = C.c_size_t
@@ -203,7 +213,7 @@ def lib():
     for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
               "aug_attn_mixed_scored", "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
               "aug_form_batch", "aug_request_arrive", "aug_request_return", "aug_step_tables", "aug_rope_init", "aug_rope_rows",
-              "aug_rope_append"):
+              "aug_rope_append", "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree"):
         getattr(L, f).restype = C.c_int
     L.aug_status_string.argtypes = [C.c_int]
     L.aug_status_string.restype = C.c_char_p
@@ -481,6 +491,27 @@ def aug_rope_append(shape: aug_attn_shape, rope: Optional[aug_rope], positions, 
     _check(lib().aug_rope_append(C.byref(shape), None if rope is None else C.byref(rope), _ptr(positions), _ptr(slots), len(slots),
                                  *_rows_arg(q), *_rows_arg(k), *_rows_arg(v), *_rows_arg(q_out), _ptr(k_cache), _ptr(v_cache),
                                  _ptr(k_scale), _ptr(v_scale), int(num_pool_blocks), st), "aug_rope_append")
+
+
+def aug_tree_plan_size(shape: aug_attn_shape, batch: aug_tree_batch):
+    """(bytes of the work list, bytes of the workspace) for any lengths of a batch."""
+    plan, workspace = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().aug_tree_plan_size(C.byref(shape), C.byref(batch), C.byref(plan), C.byref(workspace)), "aug_tree_plan_size")
+    return int(plan.value), int(workspace.value)
+
+
+def aug_tree_plan(shape: aug_attn_shape, batch: aug_tree_batch, plan_dev, stream=None):
+    """Enqueue the work list of a step's tree attention (uint8 tensor)."""
+    _check(lib().aug_tree_plan(C.byref(shape), C.byref(batch), _ptr(plan_dev), plan_dev.numel(), _stream(stream, plan_dev)),
+           "aug_tree_plan")
+
+
+def aug_attn_tree(shape: aug_attn_shape, batch: aug_tree_batch, plan_dev, q, k_cache, v_cache, k_scale, v_scale,
+                  num_pool_blocks: int, out, workspace, stream=None):
+    """Enqueue the attention of a planned step's drafts (workspace: uint8 tensor)."""
+    _check(lib().aug_attn_tree(C.byref(shape), C.byref(batch), _ptr(plan_dev), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                               _ptr(v_scale), int(num_pool_blocks), _ptr(out), _ptr(workspace), workspace.numel(),
+                               _stream(stream, q)), "aug_attn_tree")
 
 
 # ---- park / resume -------------------------------------------------------------------

@@ -1,0 +1,878 @@
+// Attention of drafted tokens (trees of them) over the paged cache, with the lengths on
+// the GPU.
+//
+// The n rows of a request and the G query heads of a KV head make n G query vectors
+// that share one K/V stream: they are the columns of the products, 16 T of them in a
+// work item, and the stream is cut into spans of keys. Per wave and step of two
+// 16-token blocks (32 keys), with lane l = 16 g + j:
+//   S^T[16 keys][16 columns] = K Q^T, D / 32 MFMAs 16x16x32 for each block and
+//     16 columns. Lane l brings token j of the block and eight dims a step, the same
+//     eight of K and Q.
+//   The result gives lane l column j and keys 4g .. 4g + 3 of each block, which is the
+//   B operand of a 16x16x32 MFMA over the 32 keys (slots 0 .. 3 of lane group g the
+//   first block's, 4 .. 7 the second's): probabilities go on without any exchange.
+//   O^T[D dims][16 columns] += V^T P^T, D / 16 MFMAs for 16 columns: row m of MFMA b is dim
+//     (D / 16) m + b, so that a lane loads neighbouring dims of its tokens and regroups them.
+// K and V operands are made once a step and used for all T column tiles. A workgroup's
+// four waves take steps in turn and are merged through LDS; spans are merged by a second launch.
+//
+// fp32 caches: the same with 16x16x4 fp32 MFMAs, one block a step.
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "attn_kernels.h"
+
+namespace {
+
+constexpr int kTreeUnit = 128;         // keys: one step of four waves
+constexpr int kTreeTarget = 1024;      // work items that a plan aims at
+constexpr int kTreeMinSpan = 2;        // units
+constexpr int kPlanThreads = 1024;
+
+struct TreeHeader {                    // 64 bytes
+  int32_t num_items;
+  int32_t num_groups;
+  int32_t reserved[14];
+};
+struct TreeItem {                      // 32 bytes
+  int32_t req;
+  int16_t kvh;
+  int16_t tile;                        // of 16 T columns
+  int32_t key_begin, key_end;
+  int32_t q_row0, n_rows;              // of the request
+  int32_t kv_len;
+  int32_t part;                        // partial result, -1: the only span
+};
+struct TreeGroup {                     // 32 bytes: one item's columns over all spans
+  int32_t q_row0, n_rows;
+  int16_t kvh;
+  int16_t tile;
+  int32_t part0, n_parts;
+  int32_t reserved[3];
+};
+static_assert(sizeof(TreeHeader) == 64 && sizeof(TreeItem) == 32 && sizeof(TreeGroup) == 32, "plan layout");
+
+// What follows from a shape and the limits of a batch, on the host.
+struct TreeSizes {
+  int32_t tiles_per_item;              // T
+  int32_t max_tiles;                   // items for the columns of one request and KV head
+  int64_t items, groups, parts;        // at most
+  int64_t plan_bytes, workspace_bytes;
+};
+
+struct TreePlanArgs {
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  char* plan;
+  int64_t items;                       // places for items: groups follow them
+  int32_t num_reqs, max_rows, max_blocks, max_draft, hkv, group, columns;   // columns of an item: 16 T
+};
+
+// Sum of v over the threads before this one.
+template <typename T>
+__device__ __forceinline__ T sum_before(T v, T* waves, T* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T upto = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const T o = __shfl_up(upto, d);
+    if (lane >= d) upto += o;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = upto;
+  __syncthreads();
+  T before = upto - v, sum = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) before += waves[w];
+    sum += waves[w];
+  }
+  *total = sum;
+  return before;
+}
+
+// One workgroup: spans of equal length for all requests, long enough that about
+// kTreeTarget items come out. With L units of keys, c the span and items = sum of
+// tiles x KV heads x ceil(L / c), c >= sum(tiles x KV heads x L) / kTreeTarget gives at most
+// kTreeTarget + requests x KV heads x tiles items, and at most 2 kTreeTarget of requests that
+// are split (L > c, so ceil(L / c) < 2 L / c).
+__global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a) {
+  extern __shared__ int32_t firsts[];                 // per request: first item, partial, group
+  __shared__ unsigned long long waves64[kPlanThreads / 64];
+  __shared__ int32_t waves[kPlanThreads / 64];
+  const int n = a.num_reqs, tid = threadIdx.x;
+  int32_t* first_item = firsts;                       // [n + 1]
+  int32_t* first_part = firsts + n + 1;
+  int32_t* first_group = firsts + 2 * n + 1;
+  struct Req { int32_t q0, rows, keys, units, tiles; };
+  const auto request = [&](int r) {
+    Req q;
+    q.q0 = min(max(a.q_start[r], 0), a.max_rows);
+    q.rows = min(max(a.q_start[r + 1] - q.q0, 0), min(a.max_draft, a.max_rows - q.q0));
+    q.keys = static_cast<int32_t>(min(static_cast<int64_t>(max(a.kv_len[r], 0)), static_cast<int64_t>(a.max_blocks) * kBlock));
+    q.units = (q.keys + kTreeUnit - 1) / kTreeUnit;
+    q.tiles = (q.rows * a.group + a.columns - 1) / a.columns;
+    return q;
+  };
+  const int per = (n + kPlanThreads - 1) / kPlanThreads;
+  const int r0 = min(tid * per, n), r1 = min(r0 + per, n);
+
+  unsigned long long work = 0, total;
+  for (int r = r0; r < r1; ++r) {
+    const Req q = request(r);
+    work += static_cast<unsigned long long>(q.units) * q.tiles * a.hkv;
+  }
+  sum_before(work, waves64, &total);
+  const int32_t span = max(kTreeMinSpan, static_cast<int32_t>((total + kTreeTarget - 1) / kTreeTarget));
+  // spans of a request: as few as that length allows, evenly long
+  const auto length_of = [&](const Req& q) {
+    const int s = max((q.units + span - 1) / span, 1);
+    return max((q.units + s - 1) / s, 1);
+  };
+  const auto spans_of = [&](const Req& q) { const int l = length_of(q); return max((q.units + l - 1) / l, 1); };
+  int32_t items = 0, parts = 0, groups = 0;
+  for (int r = r0; r < r1; ++r) {
+    const Req q = request(r);
+    const int s = spans_of(q), columns = q.tiles * a.hkv;
+    items += columns * s;
+    parts += s > 1 ? columns * s : 0;
+    groups += s > 1 ? columns : 0;
+  }
+  int32_t num_items, num_parts, num_groups;
+  int32_t item = sum_before(items, waves, &num_items);
+  int32_t part = sum_before(parts, waves, &num_parts);
+  int32_t group = sum_before(groups, waves, &num_groups);
+  for (int r = r0; r < r1; ++r) {
+    const Req q = request(r);
+    const int s = spans_of(q), columns = q.tiles * a.hkv;
+    first_item[r] = item;
+    first_part[r] = part;
+    first_group[r] = group;
+    item += columns * s;
+    part += s > 1 ? columns * s : 0;
+    group += s > 1 ? columns : 0;
+  }
+  if (tid == 0) {
+    first_item[n] = num_items;
+    *reinterpret_cast<TreeHeader*>(a.plan) = TreeHeader{num_items, num_groups, {}};
+  }
+  __syncthreads();
+  TreeItem* out = reinterpret_cast<TreeItem*>(a.plan + sizeof(TreeHeader));
+  TreeGroup* group_out = reinterpret_cast<TreeGroup*>(out + a.items);
+  for (int i = tid; i < num_items; i += kPlanThreads) {
+    int lo = 0, hi = n - 1;                           // the last request whose first item is not behind i
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first_item[mid] <= i) lo = mid; else hi = mid - 1;
+    }
+    const Req q = request(lo);
+    const int s = spans_of(q), length = length_of(q) * kTreeUnit;
+    const int local = i - first_item[lo];
+    const int tile = local % q.tiles, at = local / q.tiles % s, kvh = local / (q.tiles * s);
+    const int column = kvh * q.tiles + tile;
+    TreeItem it;
+    it.req = lo;
+    it.kvh = static_cast<int16_t>(kvh);
+    it.tile = static_cast<int16_t>(tile);
+    it.key_begin = at * length;
+    it.key_end = min(it.key_begin + length, q.keys);
+    it.q_row0 = q.q0;
+    it.n_rows = q.rows;
+    it.kv_len = q.keys;
+    it.part = s > 1 ? first_part[lo] + column * s + at : -1;
+    out[i] = it;
+    if (s > 1 && at == 0)
+      group_out[first_group[lo] + column] =
+          TreeGroup{q.q0, q.rows, it.kvh, it.tile, first_part[lo] + column * s, s, {}};
+  }
+}
+
+// ---------------------------------------------------------------------------
+
+struct TreeArgs {
+  const char* plan;
+  const void* q;
+  const char* k_cache;
+  const char* v_cache;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* block_table;
+  const uint64_t* seen;
+  void* out;
+  float* partials;
+  int64_t items;
+  int32_t max_blocks, num_pool_blocks, hq, hkv;
+  int32_t group_log2;
+  float scale_log2;
+};
+
+// Two blocks' K and V of a lane, and what the products take of them.
+template <int KVT, int D> struct TreeKv;
+template <int D> struct TreeKv<KV_BF16, D> {
+  using v_t = std::conditional_t<D == 128, uint4, uint2>;
+  struct Block { uint4 k[D / 32]; v_t v[4]; float ks = 1.f, vs = 1.f; };
+  static constexpr int EB = 2;
+  __device__ static constexpr int k_dim(int s, int g) { return 32 * s + 8 * g; }
+  __device__ static void load(const TreeArgs& a, int64_t cell, int j, int g, Block& b) {
+    const char* k = a.k_cache + (cell * kBlock + j) * D * EB + 16 * g;
+    const char* v = a.v_cache + ((cell * kBlock + 4 * g) * D + D / 16 * j) * EB;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) b.k[i] = *reinterpret_cast<const uint4*>(k + 64 * i);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) b.v[t] = *reinterpret_cast<const v_t*>(v + t * D * EB);
+  }
+  __device__ static uint4 k_operand(const Block& b, int s) { return b.k[s]; }
+  __device__ static void drop_v(Block& b, int t) { b.v[t] = v_t{}; }
+  // dims 2i and 2i + 1 of the lane's, over the keys of both blocks
+  __device__ static void v_operands(const Block& b0, const Block& b1, int i, uint4& even, uint4& odd) {
+    const auto word = [&](const Block& b, int t) { return reinterpret_cast<const uint32_t*>(&b.v[t])[i]; };
+    const auto pair = [&](uint32_t which) {
+      return uint4{__builtin_amdgcn_perm(word(b0, 1), word(b0, 0), which), __builtin_amdgcn_perm(word(b0, 3), word(b0, 2), which),
+                   __builtin_amdgcn_perm(word(b1, 1), word(b1, 0), which), __builtin_amdgcn_perm(word(b1, 3), word(b1, 2), which)};
+    };
+    even = pair(0x05040100u);
+    odd = pair(0x07060302u);
+  }
+};
+template <> struct TreeKv<KV_FP8, 128> {
+  struct Block { uint4 k[2]; uint2 v[4]; float ks = 1.f, vs = 1.f; };
+  static constexpr int D = 128;
+  __device__ static constexpr int k_dim(int s, int g) { return 64 * (s >> 1) + 16 * g + 8 * (s & 1); }
+  __device__ static void load(const TreeArgs& a, int64_t cell, int j, int g, Block& b) {
+    const char* k = a.k_cache + (cell * kBlock + j) * D + 16 * g;
+    const char* v = a.v_cache + (cell * kBlock + 4 * g) * D + 8 * j;
+    b.k[0] = *reinterpret_cast<const uint4*>(k);
+    b.k[1] = *reinterpret_cast<const uint4*>(k + 64);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) b.v[t] = *reinterpret_cast<const uint2*>(v + t * D);
+    b.ks = load_uniform(a.k_scale + cell);
+    b.vs = load_uniform(a.v_scale + cell);
+  }
+  __device__ static uint4 k_operand(const Block& b, int s) {
+    const uint4& w = b.k[s >> 1];
+    const uint32_t lo = (s & 1) ? w.z : w.x, hi = (s & 1) ? w.w : w.y;
+    return uint4{fp8x2_to_bf16x2<false>(lo), fp8x2_to_bf16x2<true>(lo), fp8x2_to_bf16x2<false>(hi), fp8x2_to_bf16x2<true>(hi)};
+  }
+  __device__ static void drop_v(Block& b, int t) { b.v[t] = uint2{0u, 0u}; }
+  __device__ static void v_operands(const Block& b0, const Block& b1, int i, uint4& even, uint4& odd) {
+    // bytes of dims 2i and 2i + 1 of two tokens side by side: a byte pair converts to the
+    // bf16 pair of one dim
+    const auto word = [&](const Block& b, int t) { return i & 2 ? b.v[t].y : b.v[t].x; };
+    const uint32_t which = i & 1 ? 0x07030602u : 0x05010400u;
+    const uint32_t a01 = __builtin_amdgcn_perm(word(b0, 1), word(b0, 0), which), a23 = __builtin_amdgcn_perm(word(b0, 3), word(b0, 2), which);
+    const uint32_t c01 = __builtin_amdgcn_perm(word(b1, 1), word(b1, 0), which), c23 = __builtin_amdgcn_perm(word(b1, 3), word(b1, 2), which);
+    even = uint4{fp8x2_to_bf16x2<false>(a01), fp8x2_to_bf16x2<false>(a23), fp8x2_to_bf16x2<false>(c01), fp8x2_to_bf16x2<false>(c23)};
+    odd = uint4{fp8x2_to_bf16x2<true>(a01), fp8x2_to_bf16x2<true>(a23), fp8x2_to_bf16x2<true>(c01), fp8x2_to_bf16x2<true>(c23)};
+  }
+};
+template <> struct TreeKv<KV_FP4, 128> {
+  struct Block { uint4 k; uint4 v; uint32_t kb, vb; float ks = 1.f, vs = 1.f; };
+  __device__ static constexpr int k_dim(int s, int g) { return 32 * g + 8 * s; }
+  __device__ static void load(const TreeArgs& a, int64_t cell, int j, int g, Block& b) {
+    const int64_t block = cell / a.hkv;
+    const int kvh = static_cast<int>(cell - block * a.hkv);
+    const int64_t at = block * a.hkv * aug::kMxCell;
+    const int codes = kvh * aug::kMxCodes, scales = a.hkv * aug::kMxCodes + kvh * aug::kMxScales;
+    b.k = *reinterpret_cast<const uint4*>(a.k_cache + at + codes + 64 * j + 16 * g);
+    b.v = *reinterpret_cast<const uint4*>(a.v_cache + at + codes + 256 * g + 16 * j);
+    b.kb = *reinterpret_cast<const uint8_t*>(a.k_cache + at + scales + 4 * j + g);
+    b.vb = *reinterpret_cast<const uint32_t*>(a.v_cache + at + scales + 16 * (j >> 2) + 4 * g);
+  }
+  __device__ static uint4 k_operand(const Block& b, int s) {
+    const uint32_t w = s == 0 ? b.k.x : s == 1 ? b.k.y : s == 2 ? b.k.z : b.k.w;
+    return fp4x8_to_bf16x8(w, fp4_scale(b.kb, 0));
+  }
+  // value and scale (255 stands for NaN) zero
+  __device__ static void drop_v(Block& b, int t) {
+    (t == 0 ? b.v.x : t == 1 ? b.v.y : t == 2 ? b.v.z : b.v.w) = 0u;
+    b.vb &= ~(0xFFu << (8 * t));
+  }
+  template <int E>
+  __device__ static void decode(const Block& b, uint32_t (&x)[4]) {
+    const uint32_t w[4] = {b.v.x, b.v.y, b.v.z, b.v.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      x[t] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], fp4_scale(b.vb, t), E));
+  }
+  __device__ static void v_operands(const Block& b0, const Block& b1, int i, uint4& even, uint4& odd) {
+    uint32_t x[4], y[4];
+    switch (i) {
+      case 0: decode<0>(b0, x); decode<0>(b1, y); break;
+      case 1: decode<1>(b0, x); decode<1>(b1, y); break;
+      case 2: decode<2>(b0, x); decode<2>(b1, y); break;
+      default: decode<3>(b0, x); decode<3>(b1, y); break;
+    }
+    const auto pair = [&](uint32_t which) {
+      return uint4{__builtin_amdgcn_perm(x[1], x[0], which), __builtin_amdgcn_perm(x[3], x[2], which),
+                   __builtin_amdgcn_perm(y[1], y[0], which), __builtin_amdgcn_perm(y[3], y[2], which)};
+    };
+    even = pair(0x05040100u);
+    odd = pair(0x07060302u);
+  }
+};
+
+constexpr int kTreeWaves = 4;
+constexpr int tree_row(int D) { return D + 4; }      // floats of a wave's result of one column in LDS
+constexpr int tree_merge_floats(int D) { return kTreeWaves * 16 * tree_row(D); }
+constexpr int64_t tree_partial_floats(int T, int D) { return int64_t{16} * T * (D + 2); }
+
+// A tile of 16 columns is written: out (bf16 or fp32), or its part of the item's partial.
+// Thread `tid` takes D / 16 dims of column tid / 16.
+template <int D, bool F32>
+__device__ __forceinline__ void tree_store(const TreeArgs& a, int q_row0, int n_rows, int kvh, int column, int dim, const float* o) {
+  const int row = column >> a.group_log2, head = column & ((1 << a.group_log2) - 1);
+  if (row >= n_rows) return;
+  const int64_t at = (static_cast<int64_t>(q_row0 + row) * a.hq + (kvh << a.group_log2) + head) * D + dim;
+  constexpr int N = D / 16;
+  if constexpr (F32) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at + i) = uint2{pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3])};
+  }
+}
+
+// The four waves' results of column tile t (lds: o[D], maximum and sum of each wave and
+// column) joined, and stored as the result or as the item's partial.
+template <int D, int T, bool F32>
+__device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it, int t, const float* lds, int tid) {
+  constexpr int ROW = tree_row(D), N = D / 16;
+  const int c = tid >> 4, dim = N * (tid & 15);
+  float m = kNegBig;
+#pragma unroll
+  for (int w = 0; w < kTreeWaves; ++w) m = fmaxf(m, lds[(w * 16 + c) * ROW + D]);
+  float l = 0.f, o[N] = {};
+#pragma unroll
+  for (int w = 0; w < kTreeWaves; ++w) {
+    const float* p = lds + (w * 16 + c) * ROW;
+    const float f = __builtin_amdgcn_exp2f(p[D] - m);
+    l = fmaf(f, p[D + 1], l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = fmaf(f, p[dim + i], o[i]);
+  }
+  if (it.part < 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = over_sum(o[i], l);
+    tree_store<D, F32>(a, it.q_row0, it.n_rows, it.kvh, (it.tile * T + t) * 16 + c, dim, o);
+    return;
+  }
+  float* part = a.partials + it.part * tree_partial_floats(T, D);
+  float* dst = part + (16 * t + c) * D + dim;
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(dst + i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+  if ((tid & 15) == 0) {
+    part[16 * T * D + 16 * t + c] = m;
+    part[16 * T * (D + 1) + 16 * t + c] = l;
+  }
+}
+
+__device__ __forceinline__ TreeItem load_tree_item(const TreeItem* p) {
+  typedef int32_t words_t __attribute__((ext_vector_type(8)));
+  const words_t raw = load_uniform(reinterpret_cast<const words_t*>(p));
+  TreeItem it;
+  __builtin_memcpy(&it, &raw, sizeof(it));
+  return it;
+}
+
+// The columns of a lane: query operand addresses and masks.
+struct TreeColumn {
+  bool live;
+  int64_t q;              // elements before the query vector
+  uint64_t seen;
+};
+__device__ __forceinline__ TreeColumn tree_column(const TreeArgs& a, const TreeItem& it, int column, int D) {
+  TreeColumn c;
+  const int row = column >> a.group_log2, head = column & ((1 << a.group_log2) - 1);
+  c.live = row < it.n_rows;
+  c.q = (static_cast<int64_t>(it.q_row0 + row) * a.hq + (it.kvh << a.group_log2) + head) * D;
+  c.seen = c.live ? a.seen[it.q_row0 + row] : 0;
+  return c;
+}
+// Drafts that some column of the wave sees.
+__device__ __forceinline__ uint64_t seen_by_any(uint64_t m) {
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) m |= static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(m), d));
+  return m;
+}
+
+template <int KVT, int D, int T>
+__global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
+  using KV = TreeKv<KVT, D>;
+  constexpr int KS = D / 32, NB = D / 16;
+  constexpr bool FP8 = KVT == KV_FP8;
+  constexpr int kQuery = T * KS * 64;                  // 16-byte query operands
+  constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
+  __shared__ __align__(16) char lds[kLds];
+  if (static_cast<int>(blockIdx.x) >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items)) return;
+  const TreeItem it = load_tree_item(reinterpret_cast<const TreeItem*>(a.plan + sizeof(TreeHeader)) + blockIdx.x);
+  const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int base = it.kv_len - it.n_rows;              // tokens before the drafts
+
+  uint64_t seen[T], any = 0;
+  uint4* query = reinterpret_cast<uint4*>(lds);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const TreeColumn c = tree_column(a, it, (it.tile * T + t) * 16 + j, D);
+    seen[t] = c.seen;
+    any |= c.seen;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      if ((t * KS + s) % kTreeWaves != wave) continue;
+      query[(t * KS + s) * 64 + lane] =
+          c.live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + c.q + KV::k_dim(s, g)) : uint4{0u, 0u, 0u, 0u};
+    }
+  }
+  any = seen_by_any(any);
+  __syncthreads();
+
+  const float sc = a.scale_log2;
+  float m_run[T], l_run[T];
+  f32x4_t oacc[T][NB];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    m_run[t] = kNegBig;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) oacc[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int blk0 = it.key_begin / kBlock;
+  const int nblk = (it.key_end - it.key_begin + kBlock - 1) / kBlock;
+  const int32_t* table = a.block_table + static_cast<int64_t>(it.req) * a.max_blocks + blk0;
+  struct Pair { typename KV::Block b[2]; int bid[2]; };
+  int next[2];
+  const auto ids = [&](int bi) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) next[i] = bi + i < nblk ? load_uniform(table + bi + i) : -1;
+  };
+  const auto usable = [&](int bid) { return static_cast<uint32_t>(bid) < static_cast<uint32_t>(a.num_pool_blocks); };
+  // A block that is none (past the span, or outside the pool) loads the pool's first one
+  // and counts for nothing.
+  const auto fetch = [&](int bi, Pair& p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      p.bid[i] = next[i];
+      KV::load(a, static_cast<int64_t>(usable(next[i]) ? next[i] : 0) * a.hkv + it.kvh, j, g, p.b[i]);
+    }
+    ids(bi + 2 * kTreeWaves);
+  };
+  const auto compute = [&](int bi, Pair& p) {
+    const int tok0 = (blk0 + bi) * kBlock;
+    const bool ok[2] = {usable(p.bid[0]), usable(p.bid[1])};
+    const bool full = ok[0] && ok[1] && tok0 + 2 * kBlock <= min(it.key_end, base);
+    float vlog[2] = {0.f, 0.f}, vinv[2] = {1.f, 1.f};
+    if constexpr (FP8) {
+      // a block's V scale enters each probability through its log2 and leaves the row sum
+      // through its reciprocal (a zero scale is taken as 2^-100; one that is not finite belongs
+      // to a block that nothing sees)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float vs = fminf(fmaxf(p.b[i].vs, 0x1p-100f), 0x1p100f);
+        vlog[i] = __builtin_amdgcn_logf(vs);
+        vinv[i] = __builtin_amdgcn_rcpf(vs);
+      }
+    }
+    f32x4_t sacc[T][2];
+#pragma unroll
+    for (int t = 0; t < T; ++t) sacc[t][0] = sacc[t][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bf16x8_t k0 = as_bf16x8(KV::k_operand(p.b[0], s)), k1 = as_bf16x8(KV::k_operand(p.b[1], s));
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const bf16x8_t qop = as_bf16x8(query[(t * KS + s) * 64 + lane]);
+        sacc[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qop, sacc[t][0], 0, 0, 0);
+        sacc[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qop, sacc[t][1], 0, 0, 0);
+      }
+    }
+    const auto token = [&](int r) { return tok0 + kBlock * (r >> 2) + 4 * g + (r & 3); };
+    const auto visible = [&](int r, uint64_t mask) {
+      const int tok = token(r);
+      return ok[r >> 2] && tok < it.key_end && (tok < base || ((mask >> ((tok - base) & 63)) & 1));
+    };
+    if (!full) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (!visible(r, any)) KV::drop_v(p.b[r >> 2], r & 3);      // zero, so 0 * value never meets NaN
+    }
+    bf16x8_t pop[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      float sv[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) sv[r] = sacc[t][r >> 2][r & 3] * (FP8 ? sc * p.b[r >> 2].ks : sc);
+      if (!full) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sv[r] = visible(r, seen[t]) ? sv[r] : -INFINITY;
+      }
+      float top = sv[0];
+#pragma unroll
+      for (int r = 1; r < 8; ++r) top = fmaxf(top, sv[r]);
+      const float mn = fmaxf(m_run[t], group4_max(top));
+      if (__any(mn > m_run[t] + kRescaleSlack)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) oacc[t][b] *= alpha;
+        m_run[t] = mn;
+      }
+      uint32_t pp[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float bias = vlog[r >> 1] - m_run[t];
+        pp[r] = pack_bf16(__builtin_amdgcn_exp2f(sv[2 * r] + bias), __builtin_amdgcn_exp2f(sv[2 * r + 1] + bias));
+      }
+      // exactly the packed probabilities
+      const float s0 = dot2_bf16(pp[1], kBf16PairOne, dot2_bf16(pp[0], kBf16PairOne, 0.f));
+      const float s1 = dot2_bf16(pp[3], kBf16PairOne, dot2_bf16(pp[2], kBf16PairOne, 0.f));
+      l_run[t] = FP8 ? fmaf(s0, vinv[0], fmaf(s1, vinv[1], l_run[t])) : l_run[t] + (s0 + s1);
+      pop[t] = as_bf16x8(uint4{pp[0], pp[1], pp[2], pp[3]});
+    }
+#pragma unroll
+    for (int i = 0; i < NB / 2; ++i) {
+      uint4 even, odd;
+      KV::v_operands(p.b[0], p.b[1], i, even, odd);
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        oacc[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pop[t], oacc[t][2 * i], 0, 0, 0);
+        oacc[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), pop[t], oacc[t][2 * i + 1], 0, 0, 0);
+      }
+    }
+  };
+  // two pairs of blocks in turns: the loads of one are on their way while the other is computed
+  Pair p0, p1;
+  int bi = 2 * wave;
+  ids(bi);
+  fetch(bi, p0);
+  for (; bi < nblk; bi += 4 * kTreeWaves) {
+    fetch(bi + 2 * kTreeWaves, p1);
+    compute(bi, p0);
+    if (bi + 2 * kTreeWaves >= nblk) break;
+    fetch(bi + 4 * kTreeWaves, p0);
+    compute(bi + 2 * kTreeWaves, p1);
+  }
+
+  float* merge = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    __syncthreads();                                   // the queries, or the tile before, have been read
+    const float l = group4_sum(l_run[t]);
+    float* dst = merge + (wave * 16 + j) * tree_row(D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int b = 0; b < NB; b += 4)
+        *reinterpret_cast<float4*>(dst + NB * (4 * g + r) + b) =
+            float4{oacc[t][b][r], oacc[t][b + 1][r], oacc[t][b + 2][r], oacc[t][b + 3][r]};
+    if (g == 0) {
+      dst[D] = m_run[t];
+      dst[D + 1] = l;
+    }
+    __syncthreads();
+    tree_join<D, T, false>(a, it, t, merge, threadIdx.x);
+  }
+}
+
+// fp32: one block a step, 16x16x4 MFMAs. Lane l brings four dims 16i + 4g .. of K and Q
+// a load, one of which a step takes; and of V tokens 4g .. 4g + 3, one a step.
+template <int D, int T>
+__global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
+  constexpr int KS = D / 16, NB = D / 16;
+  constexpr int kQuery = T * KS * 64;
+  constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
+  __shared__ __align__(16) char lds[kLds];
+  if (static_cast<int>(blockIdx.x) >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items)) return;
+  const TreeItem it = load_tree_item(reinterpret_cast<const TreeItem*>(a.plan + sizeof(TreeHeader)) + blockIdx.x);
+  const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int base = it.kv_len - it.n_rows;
+
+  uint64_t seen[T], any = 0;
+  float4* query = reinterpret_cast<float4*>(lds);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const TreeColumn c = tree_column(a, it, (it.tile * T + t) * 16 + j, D);
+    seen[t] = c.seen;
+    any |= c.seen;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      if ((t * KS + s) % kTreeWaves != wave) continue;
+      query[(t * KS + s) * 64 + lane] =
+          c.live ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + c.q + 16 * s + 4 * g) : float4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  any = seen_by_any(any);
+  __syncthreads();
+
+  float m_run[T], l_run[T];
+  f32x4_t oacc[T][NB];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    m_run[t] = kNegBig;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) oacc[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int blk0 = it.key_begin / kBlock;
+  const int nblk = (it.key_end - it.key_begin + kBlock - 1) / kBlock;
+  const int32_t* table = a.block_table + static_cast<int64_t>(it.req) * a.max_blocks + blk0;
+  for (int bi = wave; bi < nblk; bi += kTreeWaves) {
+    const int bid = load_uniform(table + bi);
+    if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) continue;
+    const int64_t cell = static_cast<int64_t>(bid) * a.hkv + it.kvh;
+    const int tok0 = (blk0 + bi) * kBlock;
+    const float* kp = reinterpret_cast<const float*>(a.k_cache) + (cell * kBlock + j) * D + 4 * g;
+    const float* vp = reinterpret_cast<const float*>(a.v_cache) + (cell * kBlock + 4 * g) * D + NB * j;
+    float k[KS][4], v[4][NB];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) __builtin_memcpy(k[s], reinterpret_cast<const float4*>(kp + 16 * s), 16);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int b = 0; b < NB; b += 4) __builtin_memcpy(&v[r][b], reinterpret_cast<const float4*>(vp + r * D + b), 16);
+    const bool full = tok0 + kBlock <= min(it.key_end, base);
+    const auto visible = [&](int r, uint64_t mask) {
+      const int tok = tok0 + 4 * g + r;
+      return tok < it.key_end && (tok < base || ((mask >> ((tok - base) & 63)) & 1));
+    };
+    if (!full) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!visible(r, any)) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) v[r][b] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const float4 q4 = query[(t * KS + s) * 64 + lane];
+        const float q[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sacc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[s][c], q[c], sacc, 0, 0, 0);
+      }
+      float sv[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sv[r] = full || visible(r, seen[t]) ? sacc[r] * a.scale_log2 : -INFINITY;
+      const float mn = fmaxf(m_run[t], group4_max(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]))));
+      if (__any(mn > m_run[t] + kRescaleSlack)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) oacc[t][b] *= alpha;
+        m_run[t] = mn;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(sv[r] - m_run[t]);
+        l_run[t] += p;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) oacc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][b], p, oacc[t][b], 0, 0, 0);
+      }
+    }
+  }
+
+  float* merge = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    __syncthreads();
+    const float l = group4_sum(l_run[t]);
+    float* dst = merge + (wave * 16 + j) * tree_row(D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int b = 0; b < NB; b += 4)
+        *reinterpret_cast<float4*>(dst + NB * (4 * g + r) + b) =
+            float4{oacc[t][b][r], oacc[t][b + 1][r], oacc[t][b + 2][r], oacc[t][b + 3][r]};
+    if (g == 0) {
+      dst[D] = m_run[t];
+      dst[D + 1] = l;
+    }
+    __syncthreads();
+    tree_join<D, T, true>(a, it, t, merge, threadIdx.x);
+  }
+}
+
+// The spans of 16 columns joined by log-sum-exp, in their order.
+template <int D, int T, bool F32>
+__global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeArgs a) {
+  constexpr int N = D / 16;
+  const int group = blockIdx.x / T, t = blockIdx.x % T;
+  if (group >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_groups)) return;
+  const TreeGroup gr = reinterpret_cast<const TreeGroup*>(a.plan + sizeof(TreeHeader) + a.items * sizeof(TreeItem))[group];
+  const int c = 16 * t + (threadIdx.x >> 4), dim = N * (threadIdx.x & 15);
+  const int column = gr.tile * 16 * T + c;
+  if ((column >> a.group_log2) >= gr.n_rows) return;
+  const float* part = a.partials + gr.part0 * tree_partial_floats(T, D);
+  float m = kNegBig, l = 0.f, o[N] = {};
+  constexpr int U = 4;
+  for (int s = 0; s < gr.n_parts; s += U) {
+    float ms[U], ls[U];
+    float4 x[U][N / 4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* p = part + min(s + u, gr.n_parts - 1) * tree_partial_floats(T, D);
+      ms[u] = s + u < gr.n_parts ? p[16 * T * D + c] : kNegBig;
+      ls[u] = s + u < gr.n_parts ? p[16 * T * (D + 1) + c] : 0.f;
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) x[u][i] = *reinterpret_cast<const float4*>(p + c * D + dim + 4 * i);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= gr.n_parts) break;
+      const float mn = fmaxf(m, ms[u]);
+      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(ms[u] - mn);
+      l = l * f0 + ls[u] * f1;
+      m = mn;
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        o[4 * i] = o[4 * i] * f0 + x[u][i].x * f1;
+        o[4 * i + 1] = o[4 * i + 1] * f0 + x[u][i].y * f1;
+        o[4 * i + 2] = o[4 * i + 2] * f0 + x[u][i].z * f1;
+        o[4 * i + 3] = o[4 * i + 3] * f0 + x[u][i].w * f1;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = over_sum(o[i], l);
+  tree_store<D, F32>(a, gr.q_row0, gr.n_rows, gr.kvh, column, dim, o);
+}
+
+// ---------------------------------------------------------------------------
+
+aug_status tree_sizes(const char* who, const aug_attn_shape* s, const aug_tree_batch* b, TreeSizes* z) {
+  if (aug_status st = aug::check_shape(s, who); st != AUG_OK) return st;
+  if (!b) return aug::fail(AUG_ERR_INVALID, "%s: batch is NULL", who);
+  if (b->num_reqs < 0 || b->max_rows < 0 || b->max_blocks < 1)
+    return aug::fail(AUG_ERR_INVALID, "%s: %d requests, %d rows, %d columns", who, b->num_reqs, b->max_rows, b->max_blocks);
+  if (b->max_draft < 1 || b->max_draft > AUG_MAX_DRAFT)
+    return aug::fail(AUG_ERR_INVALID, "%s: max_draft %d (1 to %d)", who, b->max_draft, AUG_MAX_DRAFT);
+  if (b->num_reqs > AUG_STEP_MAX_REQS || b->max_blocks > (1 << 20))
+    return aug::fail(AUG_ERR_UNSUPPORTED, "%s: %d requests of up to %d blocks (supported: %d, %d)", who, b->num_reqs,
+                     b->max_blocks, AUG_STEP_MAX_REQS, 1 << 20);
+  const int columns = b->max_draft * (s->num_q_heads / s->num_kv_heads);
+  // columns of one item: all of them up to 64 (32 in fp32, whose K and V take twice the registers)
+  z->tiles_per_item = columns <= 16 ? 1 : columns <= 32 || s->kv_dtype == AUG_F32 ? 2 : 4;
+  z->max_tiles = (columns + 16 * z->tiles_per_item - 1) / (16 * z->tiles_per_item);
+  const int64_t whole = static_cast<int64_t>(b->num_reqs) * s->num_kv_heads * z->max_tiles;
+  z->items = kTreeTarget + whole;
+  z->groups = whole < kTreeTarget ? whole : kTreeTarget;
+  z->parts = z->items < 2 * kTreeTarget ? z->items : 2 * kTreeTarget;
+  if (z->items > (1 << 24))
+    return aug::fail(AUG_ERR_UNSUPPORTED, "%s: up to %lld work items", who, (long long)z->items);
+  z->plan_bytes = sizeof(TreeHeader) + z->items * sizeof(TreeItem) + z->groups * sizeof(TreeGroup);
+  z->workspace_bytes = z->parts * tree_partial_floats(z->tiles_per_item, s->head_dim) * 4;
+  return AUG_OK;
+}
+
+template <int D, int T>
+void launch_f32(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
+  hipLaunchKernelGGL((tree_kernel_f32<D, T>), dim3(z.items), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((tree_merge_kernel<D, T, true>), dim3(z.groups * T), dim3(kThreads), 0, st, a);
+}
+template <int KVT, int D, int T>
+void launch_tree(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
+  hipLaunchKernelGGL((tree_kernel<KVT, D, T>), dim3(z.items), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((tree_merge_kernel<D, T, false>), dim3(z.groups * T), dim3(kThreads), 0, st, a);
+}
+template <int KVT, int D>
+void launch_tiles(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
+  if (z.tiles_per_item == 1) launch_tree<KVT, D, 1>(a, z, st);
+  else if (z.tiles_per_item == 2) launch_tree<KVT, D, 2>(a, z, st);
+  else launch_tree<KVT, D, 4>(a, z, st);
+}
+
+bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
+
+}  // namespace
+
+extern "C" aug_status aug_tree_plan_size(const aug_attn_shape* s, const aug_tree_batch* b, size_t* plan_bytes,
+                                         size_t* workspace_bytes) {
+  const char* who = "aug_tree_plan_size";
+  TreeSizes z;
+  if (aug_status st = tree_sizes(who, s, b, &z); st != AUG_OK) return st;
+  if (!plan_bytes || !workspace_bytes) return aug::fail(AUG_ERR_INVALID, "%s: NULL pointer", who);
+  *plan_bytes = static_cast<size_t>(z.plan_bytes);
+  *workspace_bytes = static_cast<size_t>(z.workspace_bytes);
+  return AUG_OK;
+}
+
+extern "C" aug_status aug_tree_plan(const aug_attn_shape* s, const aug_tree_batch* b, void* plan_dev, size_t plan_bytes,
+                                    void* stream) {
+  const char* who = "aug_tree_plan";
+  TreeSizes z;
+  if (aug_status st = tree_sizes(who, s, b, &z); st != AUG_OK) return st;
+  if (b->num_reqs == 0 || b->max_rows == 0) return AUG_OK;
+  if (!b->q_start || !b->kv_len || !plan_dev) return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
+  if (misaligned(plan_dev)) return aug::fail(AUG_ERR_INVALID, "%s: the plan must be 16-byte aligned", who);
+  if (plan_bytes < static_cast<size_t>(z.plan_bytes))
+    return aug::fail(AUG_ERR_NO_SPACE, "%s: plan %zu < %lld bytes", who, plan_bytes, (long long)z.plan_bytes);
+  const TreePlanArgs a{b->q_start, b->kv_len, static_cast<char*>(plan_dev), z.items, b->num_reqs, b->max_rows, b->max_blocks,
+                       b->max_draft, s->num_kv_heads, s->num_q_heads / s->num_kv_heads, 16 * z.tiles_per_item};
+  const uint32_t lds = (3u * b->num_reqs + 1) * sizeof(int32_t);
+  hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(kPlanThreads), lds, static_cast<hipStream_t>(stream), a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess)
+    return aug::fail(AUG_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return AUG_OK;
+}
+
+extern "C" aug_status aug_attn_tree(const aug_attn_shape* s, const aug_tree_batch* b, const void* plan_dev, const void* q,
+                                    const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                    int32_t num_pool_blocks, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "aug_attn_tree";
+  TreeSizes z;
+  if (aug_status st = tree_sizes(who, s, b, &z); st != AUG_OK) return st;
+  if (num_pool_blocks < 1) return aug::fail(AUG_ERR_INVALID, "%s: empty pool", who);
+  if (b->num_reqs == 0 || b->max_rows == 0) return AUG_OK;
+  if (!plan_dev || !q || !k_cache || !v_cache || !b->block_table || !b->seen || !out)
+    return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
+  if (s->kv_dtype == AUG_FP8_E4M3FN && (!k_scale || !v_scale))
+    return aug::fail(AUG_ERR_INVALID, "%s: fp8 KV needs k_scale and v_scale", who);
+  if (misaligned(plan_dev) || misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(out) || misaligned(workspace))
+    return aug::fail(AUG_ERR_INVALID, "%s: plan, rows, caches and workspace must be 16-byte aligned", who);
+  if (!workspace || workspace_bytes < static_cast<size_t>(z.workspace_bytes))
+    return aug::fail(AUG_ERR_NO_SPACE, "%s: workspace %zu < %lld bytes", who, workspace_bytes, (long long)z.workspace_bytes);
+  TreeArgs a{};
+  a.plan = static_cast<const char*>(plan_dev);
+  a.q = q;
+  a.k_cache = static_cast<const char*>(k_cache);
+  a.v_cache = static_cast<const char*>(v_cache);
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.block_table = b->block_table;
+  a.seen = b->seen;
+  a.out = out;
+  a.partials = static_cast<float*>(workspace);
+  a.items = z.items;
+  a.max_blocks = b->max_blocks;
+  a.num_pool_blocks = num_pool_blocks;
+  a.hq = s->num_q_heads;
+  a.hkv = s->num_kv_heads;
+  a.group_log2 = __builtin_ctz(static_cast<unsigned>(s->num_q_heads / s->num_kv_heads));
+  a.scale_log2 = s->softmax_scale * kLog2e;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (s->kv_dtype == AUG_F32) {
+    if (s->head_dim == 64 && z.tiles_per_item == 1) launch_f32<64, 1>(a, z, st);
+    else if (s->head_dim == 64) launch_f32<64, 2>(a, z, st);
+    else if (z.tiles_per_item == 1) launch_f32<128, 1>(a, z, st);
+    else launch_f32<128, 2>(a, z, st);
+  } else if (s->kv_dtype == AUG_BF16 && s->head_dim == 64) {
+    launch_tiles<KV_BF16, 64>(a, z, st);
+  } else if (s->kv_dtype == AUG_BF16) {
+    launch_tiles<KV_BF16, 128>(a, z, st);
+  } else if (s->kv_dtype == AUG_FP8_E4M3FN) {
+    launch_tiles<KV_FP8, 128>(a, z, st);
+  } else {
+    launch_tiles<KV_FP4, 128>(a, z, st);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess)
+    return aug::fail(AUG_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return AUG_OK;
+}

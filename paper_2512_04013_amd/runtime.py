@@ -14,8 +14,9 @@ import numpy as np
 import torch
 
 from . import (AUG_F32, AUG_MXFP4, MAX_DRAFT, MXFP4_CELL_BYTES, STEP_SCRATCH_BYTES, _current_stream, aug_attn_mixed, aug_attn_plan,
-               aug_kv_append, aug_kv_park, aug_kv_read, aug_kv_record_bytes, aug_kv_resume, aug_plan_upload, aug_rope_append,
-               aug_rope_init, aug_rope_rows, aug_step_tables, aug_step_tables_args, make_shape)
+               aug_attn_tree, aug_kv_append, aug_kv_park, aug_kv_read, aug_kv_record_bytes, aug_kv_resume, aug_plan_upload,
+               aug_rope_append, aug_rope_init, aug_rope_rows, aug_step_tables, aug_step_tables_args, aug_tree_batch, aug_tree_plan,
+               aug_tree_plan_size, make_shape)
 
 _TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8, "fp4": torch.uint8}
 
@@ -256,6 +257,54 @@ class StepTables:
         a.parents = None if parents is None else parents.data_ptr()
         with _on(index):
             aug_step_tables(a, stream=_current_stream(index) if stream is None else stream)
+
+
+class TreeAttention:
+    """Attention of a step's drafts over a paged cache, from ``StepTables``: ``plan``
+    once a step, ``run`` once a layer. Its work list, workspace and output belong to it:
+    layers that run at the same time need one each."""
+
+    def __init__(self, shape, kv: PagedKV, tables: StepTables):
+        if not tables.max_draft:
+            raise ValueError("the tables keep no masks (max_draft 0)")
+        if tables._index != kv._device or tables.num_pool_blocks != kv.num_pool_blocks:
+            raise ValueError(f"tables of {tables.num_pool_blocks} blocks on {tables.device}, a pool of {kv.num_pool_blocks} on "
+                             f"{kv.k_cache.device}")
+        self.shape, self.kv, self.tables = shape, kv, tables
+        self._index = kv._device
+        t = tables
+        self._batch = aug_tree_batch(t.max_reqs, t.max_rows, t.max_blocks, t.max_draft, t.q_start.data_ptr(), t.kv_len.data_ptr(),
+                                     t.block_table.data_ptr(), t.seen.data_ptr())
+        plan_bytes, workspace_bytes = aug_tree_plan_size(shape, self._batch)
+        self.plan_dev = torch.empty(plan_bytes, dtype=torch.uint8, device=t.device)
+        self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=t.device)
+        self._rows = (t.max_rows, shape.num_q_heads, shape.head_dim)
+        self._dtype = torch.float32 if shape.q_dtype == AUG_F32 else torch.bfloat16
+        # zeros: rows behind the step's last are never written
+        self.out = torch.zeros(self._rows, dtype=self._dtype, device=t.device)
+
+    def plan(self, stream=None):
+        """Enqueue the work list of the tables as they are then."""
+        with _on(self._index):
+            aug_tree_plan(self.shape, self._batch, self.plan_dev, stream=stream)
+
+    def run(self, q: torch.Tensor, out: torch.Tensor = None, stream=None, kv: PagedKV = None):
+        """Enqueue the attention of ``q`` ([max_rows][H_q][D], contiguous) into ``out``
+        (the object's own by default), over ``kv`` (another layer's pool of the same
+        size, or the planned one). Rows that see no key become zeros; rows behind the
+        step's last are left as they were."""
+        kv = self.kv if kv is None else kv
+        out = self.out if out is None else out
+        if kv.num_pool_blocks != self.kv.num_pool_blocks or kv._device != self._index:
+            raise ValueError(f"a pool of {kv.num_pool_blocks} blocks, planned for {self.kv.num_pool_blocks}")
+        for name, t in (("q", q), ("out", out)):
+            if t.shape != self._rows or t.dtype != self._dtype or not t.is_contiguous() or t.get_device() != self._index:
+                raise ValueError(f"{name}: contiguous {self._dtype} of shape {self._rows} on {self.tables.device}, got {t.dtype} "
+                                 f"{tuple(t.shape)} on {t.device}")
+        with _on(self._index):
+            aug_attn_tree(self.shape, self._batch, self.plan_dev, q, kv.k_cache, kv.v_cache, kv.k_scale, kv.v_scale,
+                          kv.num_pool_blocks, out, self.workspace, stream=stream)
+        return out
 
 
 class MixedAttention:

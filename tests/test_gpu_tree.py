@@ -1,0 +1,314 @@
+"""Attention of drafted tokens over every cache format against float64: trees and
+chains, group sizes, lengths from one key on, split spans, blocks outside the pool, rows that see nothing,
+what stands in unused slots, graphs and streams.
+
+The bound of an element is that of attn_bound.py, over the keys that the row sees."""
+
+import random
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import attention as oa  # noqa: E402
+from oracle import steps  # noqa: E402
+from oracle import tree as otree  # noqa: E402
+from oracle.codecs import storage_to_f64  # noqa: E402
+from synth.attn_inputs import make_batch_from_lengths  # noqa: E402
+from tests.attn_bound import within  # noqa: E402
+from tests.gpu_util import say  # noqa: E402
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+i32 = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+
+
+def parents_of(rows, seed, chain=False):
+    rng = random.Random(seed)
+    out = []
+    for n in rows:
+        out += [i - 1 if chain or i == 0 else rng.randint(max(-1, i - 6), i - 1) for i in range(n)]
+    return out
+
+
+class Case:
+    """A batch whose last rows are drafts, its tables on the device, and its result in float64."""
+
+    def __init__(self, layer, rows, ctx, seed=0, q_std=1.0, kv_std=1.0, chain=False, masks=None, holes=(), max_draft=None, spare=3):
+        from paper_2512_04013_amd import runtime as rt
+        hq, hkv, d, kv = layer
+        io = "f32" if kv == "f32" else "bf16"
+        nblk = [-(-c // 16) for c in ctx]
+        b = self.b = make_batch_from_lengths("tree", rows, ctx, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, q_dtype=io, kv_dtype=kv,
+                                             out_dtype=io, n_pool_blocks=sum(nblk) + spare, seed=seed, q_std=q_std, kv_std=kv_std)
+        self.rows, self.ctx = rows, ctx
+        self.shape, self.kv, q, _ = rt.upload_batch(b, staging_bytes=1)
+        width = max(nblk) + 1
+        table = np.full((len(rows), width), -1, np.int32)
+        for r in range(len(rows)):
+            table[r, :nblk[r]] = b.blocks_of(r)
+        self.holes = {}
+        for r, k, bad in holes:
+            table[r, k] = bad
+            self.holes.setdefault(r, []).append(k)
+        used = set(b.block_ids.tolist())
+        free = [x for x in range(b.num_pool_blocks) if x not in used]
+        self.parents = parents_of(rows, seed, chain)
+        total = sum(rows)
+        self.t = rt.StepTables(len(rows), total + 2, width, b.num_pool_blocks, max_draft=max_draft or max(rows), block_table=i32(table),
+                               held=i32(nblk), free_ids=i32(free + [0] * (b.num_pool_blocks - len(free))), free_count=len(free))
+        self.q = torch.cat([q, torch.full_like(q[:1], float("nan")).repeat(2, 1, 1)])
+        self.base = [c - n for c, n in zip(ctx, rows)]
+        self.t.update(i32(self.base), i32(rows), i32(self.parents + [-1, -1]))
+        assert self.t.state.tolist() == [steps.OK] * len(rows)
+        if masks is not None:
+            self.t.seen[:total] = torch.tensor([m - (1 << 64) if m >> 63 else m for m in masks], device="cuda")
+        self.att = rt.TreeAttention(self.shape, self.kv, self.t)
+
+    def run(self, **kw):
+        self.att.out.fill_(7.0)
+        self.att.plan()
+        out = self.att.run(self.q, **kw)
+        torch.cuda.synchronize()
+        n = sum(self.rows)
+        assert (out[n:] == 7.0).all(), "rows behind the last are left alone"
+        return out[:n].double().cpu().numpy()
+
+    def reference(self):
+        b = self.b
+        masks = [m % (1 << 64) for m in self.t.seen.tolist()]
+        out = np.zeros((sum(self.rows), b.num_q_heads, b.head_dim))
+        bound = np.full_like(out, 1e-30)
+        fine = b.kv_dtype == "f32"
+        g = b.num_q_heads // b.num_kv_heads
+        for r, (n, ctx) in enumerate(zip(self.rows, self.ctx)):
+            q0 = int(b.q_start[r])
+            seen = otree.sees(masks[q0:q0 + n], ctx - n, n)
+            for k in self.holes.get(r, ()):
+                seen[:, 16 * k:16 * k + 16] = False
+            k, v = (oa.materialise_kv(c, s, b.kv_dtype, b.blocks_of(r), ctx, is_v=is_v)
+                    for c, s, is_v in ((b.k_cache, b.k_scale, False), (b.v_cache, b.v_scale, True)))
+            q = storage_to_f64(b.q[q0:q0 + n], b.q_dtype)
+            for h in range(b.num_q_heads):
+                p = otree.weights(q[:, h], k[:, h // g], seen, b.softmax_scale)
+                vh = np.where(seen.any(0)[:, None], v[:, h // g], 0.0)
+                kh = np.where(seen.any(0)[:, None], k[:, h // g], 0.0)
+                o = p @ vh
+                size = (np.abs(q[:, h]) @ np.abs(kh).T).max(1, initial=0.0) * b.softmax_scale
+                d = 2.0 ** -24 * (b.head_dim * size + 32 * (1 + size) + ctx)
+                rel = d + (0.0 if fine else 2.0 ** -8)
+                out[q0:q0 + n, h] = o
+                bound[q0:q0 + n, h] += (1.01 * rel)[:, None] * (p @ np.abs(vh) + np.abs(o)) + (2.0 ** -24 if fine else 2.0 ** -8) * np.abs(o)
+        return out, bound
+
+    def check(self, what, **kw):
+        got = self.run(**kw)
+        within(got, *self.reference(), what)
+        return got
+
+
+LAYERS = [(4, 4, 64, "f32"), (8, 2, 128, "f32"), (8, 1, 64, "f32"), (16, 8, 64, "bf16"), (8, 1, 64, "bf16"), (8, 2, 128, "bf16"),
+          (8, 1, 128, "bf16"), (3, 3, 128, "bf16"), (8, 2, 128, "fp8"), (16, 2, 128, "fp8"), (2, 2, 128, "fp8"), (8, 2, 128, "fp4"),
+          (8, 1, 128, "fp4"), (4, 2, 128, "fp4"), (3, 3, 128, "fp4")]
+IDS = ["-".join(map(str, x)) for x in LAYERS]
+
+
+@pytest.mark.parametrize("layer", LAYERS, ids=IDS)
+@pytest.mark.parametrize("most", [1, 3, 8, 16, 33, 64])
+def test_trees(layer, most):
+    """Drafts alone, short and long contexts, ends inside and at the end of blocks and steps."""
+    rng = random.Random(most)
+    rows, ctx = [], []
+    for base in (0, 1, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129, 300, 700):
+        n = rng.randint(1, most)
+        rows.append(n)
+        ctx.append(base + n)
+    rows[3], ctx[3] = most, 16 + most
+    say(f"[tree] {layer} up to {most}")
+    Case(layer, rows, ctx, seed=most, max_draft=most).check(f"{layer} {most}")
+
+
+@pytest.mark.parametrize("layer", [LAYERS[i] for i in (1, 3, 5, 8, 11)], ids=[IDS[i] for i in (1, 3, 5, 8, 11)])
+def test_split_spans(layer):
+    """Long contexts of few requests: spans over many workgroups, merged."""
+    for rows, ctx in (([5], [9001]), ([1, 64], [20000, 70]), ([17, 2, 33], [4097, 16, 6000])):
+        c = Case(layer, rows, ctx, seed=1)
+        a = c.check(f"{layer} split {ctx}")
+        assert np.array_equal(a, c.run()), "equal inputs give equal bits"
+
+
+def test_chains_are_causal_attention():
+    """A chain of drafts, and a single token, against the planned mixed attention of the same rows."""
+    from paper_2512_04013_amd import runtime as rt
+    for layer in (LAYERS[0], LAYERS[5], LAYERS[8], LAYERS[11]):
+        rows, ctx = [1, 7, 64, 1], [500, 90, 130, 1]
+        c = Case(layer, rows, ctx, seed=2, chain=True)
+        got = c.check(f"chain {layer}")
+        b = c.b
+        att = rt.MixedAttention(c.shape, c.kv, b.q_start, b.ctx_len, b.bt_start, b.block_ids, i32(b.block_ids))
+        want = att.run(c.q[:sum(rows)].contiguous()).double().cpu().numpy()
+        _, bound = c.reference()
+        within(got, want, 2 * bound, "beside mixed attention")
+
+
+@pytest.mark.parametrize("layer", [LAYERS[i] for i in (0, 1, 3, 5, 9, 12)], ids=[IDS[i] for i in (0, 1, 3, 5, 9, 12)])
+def test_masks(layer):
+    """Masks that no tree makes: rows that see nothing, not themselves, or later rows; slots that no row sees hold NaN."""
+    rows, ctx = [6, 64, 9, 4], [6, 64, 200, 4]
+    rng = random.Random(5)
+    masks = [0, 0b110000, 0, 1, 0, 0b100001]
+    masks += [rng.getrandbits(64) & ~(0b1011 << 20) for _ in range(64)]
+    masks += [0, 1 << 8, 0b11, 0, 0, 0, 0b1000, 0, 0]
+    masks += [0, 0, 0, 0]
+    c = Case(layer, rows, ctx, seed=3, masks=masks)
+    # nothing is seen of row 1 and 3 of the first request, of rows 20, 21, 23 of the second and of the whole last one
+    kv, b = c.kv, c.b
+    dead = [(0, 1), (0, 2), (0, 3), (1, 20), (1, 21), (1, 23), (3, 0), (3, 1), (3, 2), (3, 3)]
+    hkv = b.num_kv_heads
+    for r, i in dead:
+        token = ctx[r] - rows[r] + i
+        if r == 1:
+            masks_seen = 0
+            for m in masks[6:70]:
+                masks_seen |= m
+            if (masks_seen >> i) & 1:
+                continue
+        block, slot = int(b.blocks_of(r)[token // 16]), token % 16
+        for pool, is_v in ((kv.k_cache, False), (kv.v_cache, True)):
+            if b.kv_dtype == "fp4":
+                at = [4 * slot + k for k in range(4)] if not is_v else [16 * k + slot for k in range(4)]
+                for h in range(hkv):
+                    for x in at:
+                        pool[block, hkv * 1024 + 64 * h + x] = 255
+            elif b.kv_dtype == "fp8":
+                pool[block, :, slot] = 0x7F
+            else:
+                pool[block, :, slot] = float("nan")
+    got = c.check(f"masks {layer}")
+    q0 = c.b.q_start
+    assert (got[q0[3]:] == 0).all() and (got[[0, 2, 4]] == 0).all()
+    if b.kv_dtype == "fp8":
+        # a block that nothing sees may have any scale
+        for scale in (float("inf"), float("nan"), 0.0, -1.0):
+            c.kv.k_scale[int(b.blocks_of(3)[0])] = scale
+            c.kv.v_scale[int(b.blocks_of(3)[0])] = scale
+            assert np.array_equal(got, c.run())
+
+
+@pytest.mark.parametrize("layer", [LAYERS[i] for i in (1, 5, 8, 11)], ids=[IDS[i] for i in (1, 5, 8, 11)])
+def test_blocks_outside_the_pool(layer):
+    rows, ctx = [5, 1, 12, 3], [100, 40, 5000, 16]
+    holes = [(0, 2, -1), (0, 6, 1 << 30), (1, 0, -2 ** 31), (2, 100, 10 ** 6), (2, 312, -7), (3, 0, 2 ** 31 - 1)]
+    got = Case(layer, rows, ctx, seed=4, holes=holes).check(f"holes {layer}")
+    assert (got[18:] == 0).all()
+
+
+@pytest.mark.parametrize("layer", [LAYERS[i] for i in (1, 5, 8, 11)], ids=[IDS[i] for i in (1, 5, 8, 11)])
+def test_sharp_scores(layer):
+    """Scores of a few hundred: one key takes all the weight, the running maximum moves often."""
+    Case(layer, [9, 30], [800, 77], seed=5, q_std=12.0, kv_std=2.0).check(f"sharp {layer}")
+
+
+def test_fp8_scales():
+    """Scales of zero, far from 1 and different from block to block."""
+    c = Case((16, 2, 128, "fp8"), [7, 20], [300, 64], seed=6)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for s, host in ((c.kv.k_scale, c.b.k_scale), (c.kv.v_scale, c.b.v_scale)):
+        f = 2.0 ** torch.randint(-12, 3, s.shape, generator=gen, device="cuda").float()
+        s.mul_(f)
+        host *= f.cpu().numpy()
+    for r, k in ((0, 3), (1, 0)):
+        block = int(c.b.blocks_of(r)[k])
+        c.kv.v_scale[block] = 0.0
+        c.b.v_scale[block] = 0.0
+    c.check("fp8 scales")
+
+
+def test_refused_requests_and_empty_ones():
+    """Requests without rows, refused ones (their rows become zeros), and lengths that the plan cuts."""
+    from paper_2512_04013_amd import runtime as rt
+    c = Case((8, 2, 128, "bf16"), [4, 2, 3], [50, 20, 35], seed=7)
+    t = c.t
+    n = sum(c.rows)
+    # the second request is refused (too many rows for the mask), the first is without rows
+    t.update(i32([46, 18, 32]), i32([0, 5, 3]), i32([-1] * (n + 2)))
+    assert t.state.tolist() == [0, steps.INVALID, 0] and t.q_start.tolist() == [0, 0, 5, 8]
+    c.att.out.fill_(7.0)
+    c.att.plan()
+    q = torch.cat([torch.zeros_like(c.q[:5]), c.q[6:9], c.q[:3]])
+    out = c.att.run(q)
+    assert (out[:4] == 0).all() and (out[4] == 7.0).all() and (out[8:] == 7.0).all()   # row 4 lies beyond max_draft
+    assert out[5:8].isfinite().all() and (out[5:8] != 7.0).any()
+    # lengths and offsets that no table makes
+    for name, value in (("kv_len", [2 ** 31 - 1, -5, 10 ** 6]), ("q_start", [-3, 2 ** 31 - 1, 5, -1]), ("q_start", [9, 8, 7, 6])):
+        t.update(i32(c.base), i32(c.rows), i32([-1] * (n + 2)))
+        getattr(t, name).copy_(i32(value))
+        c.att.plan()
+        c.att.run(c.q.nan_to_num())
+    torch.cuda.synchronize()
+    with pytest.raises(ValueError):
+        rt.TreeAttention(c.shape, c.kv, rt.StepTables(3, 8, 4, c.b.num_pool_blocks, max_draft=0))
+    with pytest.raises(ValueError):
+        rt.TreeAttention(c.shape, c.kv, rt.StepTables(3, 8, 4, c.b.num_pool_blocks + 1))
+    for bad in (dict(q=c.q[:-1]), dict(q=c.q.float()), dict(q=c.q, out=c.q[:2]), dict(q=c.q.transpose(0, 1))):
+        with pytest.raises(ValueError):
+            c.att.run(**bad)
+
+
+def test_many_requests():
+    """More requests than the plan has threads, of every length."""
+    rng = random.Random(8)
+    rows = [rng.randint(1, 3) for _ in range(1500)]
+    ctx = [n + rng.choice([0, 3, 40, 150]) for n in rows]
+    Case((2, 1, 64, "bf16"), rows, ctx, seed=8).check("1500 requests")
+
+
+@pytest.mark.parametrize("layer", [LAYERS[1], LAYERS[9]], ids=[IDS[1], IDS[9]])
+def test_replays(layer):
+    """Tables, plan and two layers in one graph, replayed with other lengths, eager work in between."""
+    from paper_2512_04013_amd import runtime as rt
+    c = Case(layer, [9] * 6, [700, 20, 9, 333, 128, 64], seed=9)
+    t, kv = c.t, c.kv
+    other = rt.PagedKV(c.shape, kv.k_cache.clone(), kv.v_cache.flip(0).contiguous(), kv.k_scale,
+                       None if kv.v_scale is None else kv.v_scale.flip(0).contiguous(), staging_bytes=1)
+    for pool in (kv, other):            # whatever a shorter request's blocks hold is finite
+        for x in (pool.k_cache, pool.v_cache, pool.k_scale, pool.v_scale):
+            if x is not None and x.dtype != torch.uint8:
+                x.nan_to_num_(0.5)
+            elif x is not None:
+                x[(x & 0x7F) == 0x7F] = 0x11
+    ctx, rows, par = i32(c.base), i32(c.rows), i32(c.parents + [-1, -1])
+    q = c.q.nan_to_num()
+    outs = [torch.zeros_like(c.att.out) for _ in range(2)]
+
+    def step(att, into):
+        t.update(ctx, rows, par)
+        att.plan()
+        att.run(q, out=into[0])
+        att.run(q, out=into[1], kv=other)
+
+    step(c.att, outs)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(c.att, outs)
+    eager = rt.TreeAttention(c.shape, kv, t)
+    rng = random.Random(1)
+    for k in range(4):
+        n = [rng.randint(0, 9) for _ in range(6)]
+        ctx.copy_(i32([rng.randint(0, b) for b in c.base]))
+        rows.copy_(i32(n))
+        tree = parents_of(n, k)
+        par.copy_(i32(tree + [-1] * (56 - len(tree))))
+        for o in outs:
+            o.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        want = [torch.full_like(o, 3.0) for o in outs]
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            step(eager, want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
+        assert not outs[0][:sum(n)].isnan().any()

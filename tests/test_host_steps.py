@@ -172,3 +172,65 @@ def test_python_refuses():
     for args in ((two[:1], two), (two, two.long()), (two, two, two), (two.repeat(2)[::2], two)):
         with pytest.raises(ValueError):
             t.update(*args)
+
+
+# ---- attention of drafts ---------------------------------------------------------------------
+
+def _batch(**kw):
+    f = dict(num_reqs=4, max_rows=32, max_blocks=8, max_draft=8, q_start=P, kv_len=P, block_table=P, seen=P)
+    f.update(kw)
+    return aug.aug_tree_batch(**f)
+
+
+def test_tree_sizes():
+    """Room for any lengths: the items of every request in one span and those of the splits; partials of 2048 split
+    items of 16, 32 or 64 columns."""
+    for draft, hq, kv, tiles, items in ((1, 8, "bf16", 1, 1024 + 8), (8, 8, "bf16", 2, 1024 + 8), (9, 8, "bf16", 4, 1024 + 8),
+                                        (64, 8, "bf16", 4, 1024 + 8 * 4), (64, 8, "f32", 2, 1024 + 8 * 8), (4, 8, "f32", 1, 1024 + 8)):
+        shape = _shape(kv, hq=hq)
+        plan, workspace = aug.aug_tree_plan_size(shape, _batch(max_draft=draft))
+        groups = min(1024, items - 1024)
+        assert plan == 64 + 32 * items + 32 * groups
+        assert workspace == min(items, 2048) * 16 * tiles * 130 * 4
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_reqs=-1), aug.AUG_ERR_INVALID), (dict(max_rows=-1), aug.AUG_ERR_INVALID), (dict(max_blocks=0), aug.AUG_ERR_INVALID),
+    (dict(max_draft=0), aug.AUG_ERR_INVALID), (dict(max_draft=65), aug.AUG_ERR_INVALID), (dict(num_reqs=4097), aug.AUG_ERR_UNSUPPORTED),
+    (dict(max_blocks=(1 << 20) + 1), aug.AUG_ERR_UNSUPPORTED)])
+def test_tree_batches_refused(kw, status):
+    s, b, n = _shape(), _batch(**kw), C.c_size_t()
+    L = aug.lib()
+    assert L.aug_tree_plan_size(C.byref(s), C.byref(b), C.byref(n), C.byref(n)) == status
+    assert L.aug_tree_plan(C.byref(s), C.byref(b), P, 1 << 40, None) == status
+    assert L.aug_attn_tree(C.byref(s), C.byref(b), P, P, P, P, P, P, 4, P, P, 1 << 40, None) == status
+
+
+def test_tree_calls_refused():
+    L, s, n = aug.lib(), _shape(), C.c_size_t()
+    b = _batch()
+    assert L.aug_tree_plan_size(C.byref(s), None, C.byref(n), C.byref(n)) == aug.AUG_ERR_INVALID
+    assert L.aug_tree_plan_size(C.byref(s), C.byref(b), None, C.byref(n)) == aug.AUG_ERR_INVALID
+    assert L.aug_tree_plan_size(None, C.byref(b), C.byref(n), C.byref(n)) == aug.AUG_ERR_INVALID
+    many = _batch(num_reqs=4096, max_draft=64)
+    assert L.aug_tree_plan_size(C.byref(_shape(hq=8192, hkv=1024)), C.byref(many), C.byref(n), C.byref(n)) == aug.AUG_ERR_UNSUPPORTED
+    plan = lambda **kw: L.aug_tree_plan(C.byref(s), C.byref(_batch(**{k: v for k, v in kw.items() if k in ("q_start", "kv_len")})),  # noqa: E731
+                                        kw.get("plan", P), kw.get("size", 1 << 40), None)
+    for kw in (dict(q_start=None), dict(kv_len=None), dict(plan=None), dict(plan=P + 8)):
+        assert plan(**kw) == aug.AUG_ERR_INVALID
+    assert plan(size=100) == aug.AUG_ERR_NO_SPACE
+
+    def attend(shape=s, **kw):
+        batch = _batch(**{k: kw.pop(k) for k in ("block_table", "seen", "num_reqs", "max_rows") if k in kw})
+        a = dict(plan=P, q=P, k=P, v=P, ks=P, vs=P, pool=4, out=P, workspace=P, size=1 << 40)
+        a.update(kw)
+        return L.aug_attn_tree(C.byref(shape), C.byref(batch), *a.values(), None)
+
+    for kw in (dict(plan=None), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(block_table=None), dict(seen=None),
+               dict(pool=0), dict(plan=P + 4), dict(q=P + 8), dict(k=P + 8), dict(v=P + 2), dict(out=P + 8), dict(workspace=P + 8)):
+        assert attend(**kw) == aug.AUG_ERR_INVALID, kw
+    for kw in (dict(workspace=None), dict(size=1000)):
+        assert attend(**kw) == aug.AUG_ERR_NO_SPACE, kw
+    assert attend(_shape("fp8"), ks=None) == aug.AUG_ERR_INVALID
+    assert attend(_shape("fp8"), vs=None) == aug.AUG_ERR_INVALID
+    assert attend(num_reqs=0, plan=None) == aug.AUG_OK and attend(max_rows=0, q=None) == aug.AUG_OK
