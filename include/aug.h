@@ -654,6 +654,46 @@ aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batc
                          const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                          int32_t num_pool_blocks, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Next tokens. Row r of logits ([rows][vocab], rows `stride` elements apart, float32 or
+ * bf16) gives one token:
+ *   x_i      the logits; NaN counts as -infinity
+ *   w_i      exp((x_i - max x) / temperature[r]); infinite logits share the weight 1
+ *   order    falling x, equal ones by rising index
+ *   top_k    of the order, the first top_k[r] (0 and below, or vocab and above: all)
+ *   top_p    of these, the shortest beginning that holds at least top_p[r] of their weight
+ *            (at least one token; 1 and above: all)
+ *   min_p    of these, tokens with w_i >= min(min_p[r], 1) (0 and below: all)
+ * and of what is kept the first token in rising index at which the sum of weights up to
+ * and with it exceeds uniform[r] (in [0, 1)) times their whole sum. temperature 0 (below, or NaN): the
+ * first token of the order. A row without a logit above -infinity gives -1.
+ * Arrays are device memory, one entry a row; temperature, top_k, top_p and min_p may be
+ * NULL: 1 and all. probs (may be NULL) receives the token's share of what is kept.
+ *
+ * Which side of a border a number falls on decides tokens, so weights are computed in
+ * float64 and summed exactly as integers, multiples of 2^-s with s = min(51, 62 -
+ * ceil(log2 vocab)) (a weight below 2^-(s+1) is none): equal inputs give equal tokens, and sums
+ * that differ by more than some 2^-s are told apart. */
+typedef struct {
+  int32_t rows;
+  int32_t vocab;               /* 1 to 2^20 */
+  int32_t dtype;               /* AUG_F32 or AUG_BF16 */
+  int32_t reserved;            /* zero */
+  int64_t stride;              /* at least vocab */
+  const void* logits;          /* aligned to its elements */
+  const float* uniform;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* tokens;
+  float* probs;
+} aug_sample_args;
+
+/* One launch (none for no rows); no workspace.
+ * Errors: AUG_ERR_INVALID (NULL or misaligned pointers, sizes, dtype, reserved),
+ * AUG_ERR_UNSUPPORTED (vocab above 2^20), AUG_ERR_HIP (launch). */
+aug_status aug_sample(const aug_sample_args* args, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Park / resume (Swap policy: swap-out during an external call, swap-in     */
 /* when it returns; Appendix B, Algorithm 1 step (2))                         */

@@ -46,7 +46,7 @@ EXPORTED = ["aug_request_arrive", "aug_request_return", "aug_attn_plan", "aug_at
             "aug_attn_workspace_size",
             "aug_plan_upload", "aug_attn_mixed", "aug_attn_mixed_scored", "aug_attn_mixed_noalloc",
             "aug_kv_append", "aug_kv_read", "aug_step_tables", "aug_rope_init", "aug_rope_rows", "aug_rope_append",
-            "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree",
+            "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree", "aug_sample",
             "aug_kv_record_bytes", "aug_kv_park", "aug_kv_resume", "aug_form_batch",
             "aug_status_string", "aug_last_error", "aug_abi_version"]
 
@@ -106,6 +106,12 @@ class aug_step_tables_args(C.Structure):
 class aug_tree_batch(C.Structure):
     _fields_ = [("num_reqs", C.c_int32), ("max_rows", C.c_int32), ("max_blocks", C.c_int32), ("max_draft", C.c_int32),
                 ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p), ("seen", C.c_void_p)]
+
+
+class aug_sample_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32), ("stride", C.c_int64),
+                ("logits", C.c_void_p), ("uniform", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("tokens", C.c_void_p), ("probs", C.c_void_p)]
 
 
 class aug_rope_params(C.Structure):
@@ -199,6 +205,7 @@ def lib():
     L.aug_tree_plan_size.argtypes = batch + [C.POINTER(C.c_size_t)] * 2
     L.aug_tree_plan.argtypes = batch + [P, C.c_size_t, P]
     L.aug_attn_tree.argtypes = batch + [P] * 6 + [C.c_int32, P, P, C.c_size_t, P]
+    L.aug_sample.argtypes = [C.POINTER(aug_sample_args), P]
     L.aug_plan_upload.argtypes = [P, P, C.c_size_t, P]
     L.aug_kv_record_bytes.argtypes = [C.POINTER(aug_attn_shape)]
     L.aug_kv_record_bytes.restype = C.c_size_t
@@ -213,7 +220,7 @@ def lib():
     for f in ("aug_attn_plan", "aug_attn_plan_opts", "aug_attn_plan_masked", "aug_attn_workspace_size", "aug_plan_upload", "aug_attn_mixed",
               "aug_attn_mixed_scored", "aug_attn_mixed_noalloc", "aug_kv_append", "aug_kv_read", "aug_kv_park", "aug_kv_resume",
               "aug_form_batch", "aug_request_arrive", "aug_request_return", "aug_step_tables", "aug_rope_init", "aug_rope_rows",
-              "aug_rope_append", "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree"):
+              "aug_rope_append", "aug_tree_plan_size", "aug_tree_plan", "aug_attn_tree", "aug_sample"):
         getattr(L, f).restype = C.c_int
     L.aug_status_string.argtypes = [C.c_int]
     L.aug_status_string.restype = C.c_char_p
@@ -512,6 +519,12 @@ def aug_attn_tree(shape: aug_attn_shape, batch: aug_tree_batch, plan_dev, q, k_c
     _check(lib().aug_attn_tree(C.byref(shape), C.byref(batch), _ptr(plan_dev), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
                                _ptr(v_scale), int(num_pool_blocks), _ptr(out), _ptr(workspace), workspace.numel(),
                                _stream(stream, q)), "aug_attn_tree")
+
+
+def aug_sample(args: aug_sample_args, stream=None):
+    """Enqueue the sampling of one token a row (``args`` holds device addresses:
+    the caller keeps the tensors alive)."""
+    _check(lib().aug_sample(C.byref(args), _stream(stream)), "aug_sample")
 
 
 # ---- park / resume -------------------------------------------------------------------

@@ -24,7 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libaug.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-HIP_SOURCES = ["attn.hip", "attn_scored.hip", "kvappend.hip", "kvread.hip", "kvpark.hip", "upload.hip", "tables.hip", "rope.hip", "tree.hip"]
+HIP_SOURCES = ["attn.hip", "attn_scored.hip", "kvappend.hip", "kvread.hip", "kvpark.hip", "upload.hip", "tables.hip", "rope.hip", "tree.hip", "sample.hip"]
 CPP_SOURCES = ["plan.cpp", "former.cpp", "rope.cpp", "status.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}", "-Wall", "-Wno-unused-function"]

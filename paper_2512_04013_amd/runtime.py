@@ -13,9 +13,9 @@ import time
 import numpy as np
 import torch
 
-from . import (AUG_F32, AUG_MXFP4, MAX_DRAFT, MXFP4_CELL_BYTES, STEP_SCRATCH_BYTES, _current_stream, aug_attn_mixed, aug_attn_plan,
+from . import (AUG_BF16, AUG_F32, AUG_MXFP4, MAX_DRAFT, MXFP4_CELL_BYTES, STEP_SCRATCH_BYTES, _current_stream, aug_attn_mixed, aug_attn_plan,
                aug_attn_tree, aug_kv_append, aug_kv_park, aug_kv_read, aug_kv_record_bytes, aug_kv_resume, aug_plan_upload,
-               aug_rope_append, aug_rope_init, aug_rope_rows, aug_step_tables, aug_step_tables_args, aug_tree_batch, aug_tree_plan,
+               aug_rope_append, aug_rope_init, aug_rope_rows, aug_sample, aug_sample_args, aug_step_tables, aug_step_tables_args, aug_tree_batch, aug_tree_plan,
                aug_tree_plan_size, make_shape)
 
 _TORCH_STORAGE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.uint8, "fp4": torch.uint8}
@@ -305,6 +305,37 @@ class TreeAttention:
             aug_attn_tree(self.shape, self._batch, self.plan_dev, q, kv.k_cache, kv.v_cache, kv.k_scale, kv.v_scale,
                           kv.num_pool_blocks, out, self.workspace, stream=stream)
         return out
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tensor = None, top_k: torch.Tensor = None,
+           top_p: torch.Tensor = None, min_p: torch.Tensor = None, tokens: torch.Tensor = None, probs: torch.Tensor = None, stream=None):
+    """One token for each row of ``logits`` ([rows][vocab], float32 or bf16; rows may be
+    strided) from ``uniform`` (float32 [rows] in [0, 1)), with a ``temperature`` (float32,
+    0: greedy), ``top_k`` (int32, 0: all), ``top_p`` and ``min_p`` (float32) of each row, or None.
+    Returns (tokens int32, probs float32: each token's share of what was kept), allocated
+    on ``stream`` where they are not given. What exactly is drawn stands in aug.h."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.get_device() < 0 or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: float32 or bf16 rows of contiguous logits on a GPU, got {logits.dtype} {tuple(logits.shape)}, strides "
+                         f"{logits.stride()} on {logits.device}")
+    rows, vocab = logits.shape
+    index = logits.get_device()
+    _check_vector(uniform, "uniform", rows, torch.float32, index)
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32), ("tokens", tokens, torch.int32), ("probs", probs, torch.float32)):
+        if t is not None:
+            _check_vector(t, name, rows, dtype, index)
+    if tokens is None or probs is None:
+        with _allocating_on(stream, logits.device):
+            tokens = torch.empty(rows, dtype=torch.int32, device=logits.device) if tokens is None else tokens
+            probs = torch.empty(rows, dtype=torch.float32, device=logits.device) if probs is None else probs
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    args = aug_sample_args(rows, vocab, AUG_F32 if logits.dtype == torch.float32 else AUG_BF16, 0, max(logits.stride(0), vocab) if rows < 2 else
+                           logits.stride(0), logits.data_ptr(), uniform.data_ptr(), at(temperature), at(top_k), at(top_p), at(min_p),
+                           tokens.data_ptr(), probs.data_ptr())
+    with _on(index):
+        aug_sample(args, stream=_current_stream(index) if stream is None else stream)
+    return tokens, probs
 
 
 class MixedAttention:

@@ -234,3 +234,34 @@ def test_tree_calls_refused():
     assert attend(_shape("fp8"), ks=None) == aug.AUG_ERR_INVALID
     assert attend(_shape("fp8"), vs=None) == aug.AUG_ERR_INVALID
     assert attend(num_reqs=0, plan=None) == aug.AUG_OK and attend(max_rows=0, q=None) == aug.AUG_OK
+
+
+# ---- sampling ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=-1), aug.AUG_ERR_INVALID), (dict(vocab=0), aug.AUG_ERR_INVALID), (dict(vocab=-5), aug.AUG_ERR_INVALID),
+    (dict(vocab=(1 << 20) + 1, stride=1 << 21), aug.AUG_ERR_UNSUPPORTED), (dict(dtype=aug.AUG_FP8_E4M3FN), aug.AUG_ERR_INVALID),
+    (dict(dtype=-1), aug.AUG_ERR_INVALID), (dict(reserved=1), aug.AUG_ERR_INVALID), (dict(stride=99), aug.AUG_ERR_INVALID),
+    (dict(stride=-100), aug.AUG_ERR_INVALID), (dict(stride=1 << 41), aug.AUG_ERR_INVALID), (dict(logits=None), aug.AUG_ERR_INVALID),
+    (dict(logits=P + 2), aug.AUG_ERR_INVALID), (dict(logits=P + 1, dtype=aug.AUG_BF16), aug.AUG_ERR_INVALID),
+    (dict(uniform=None), aug.AUG_ERR_INVALID), (dict(tokens=None), aug.AUG_ERR_INVALID)])
+def test_sample_refused(kw, status):
+    f = dict(rows=2, vocab=100, dtype=aug.AUG_F32, reserved=0, stride=100, logits=P, uniform=P, temperature=P, top_k=P, top_p=P, min_p=P,
+             tokens=P, probs=P)
+    f.update(kw)
+    assert aug.lib().aug_sample(C.byref(aug.aug_sample_args(**f)), None) == status and aug.aug_last_error()
+
+
+def test_sample_of_nothing():
+    assert aug.lib().aug_sample(None, None) == aug.AUG_ERR_INVALID
+    assert aug.lib().aug_sample(C.byref(aug.aug_sample_args(0, 5, aug.AUG_F32, 0, 5)), None) == aug.AUG_OK
+
+
+def test_oracle_draws():
+    """The oracle itself, where the answer is plain."""
+    from oracle import sampling
+    x = [0.0, 3.0, 1.0, 3.0]
+    assert sampling.draw(x, 0.9, temperature=0.0)[0] == 1 and sampling.draw(x, 0.99, top_k=1)[0] == 1
+    assert sampling.draw(x, 0.6, top_k=2)[:2] == (3, 0.5) and sampling.draw(x, 0.4, top_p=0.5)[0] in (1, 3)
+    assert sampling.draw(x, 0.99, min_p=0.5)[0] == 3 and sampling.draw([float("nan"), -np.inf], 0.5)[0] == -1
+    assert sampling.draw([np.inf, 0.0, np.inf], 0.5)[:2] == (2, 0.5)
