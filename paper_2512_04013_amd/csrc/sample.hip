@@ -2,19 +2,31 @@
 // uniform number.
 //
 // What is kept by top-k and top-p is a beginning of the order by falling logit (equal
-// ones by rising index), so it is described by its last element: a logit, and the index
-// up to which equal ones belong to it. A descent over the digits of the logit finds
-// it: counts (or weights) of the elements that agree in the digits so far, by the
-// next digit, summed from the largest digit down. The draw goes by index: sums of the
-// kept weights of pieces of the row, a scan over the pieces, and the piece that the
-// number falls into element by element.
+// ones by rising index), so it is described by its last element, the cut: a logit, and
+// the index up to which equal ones belong to it. The draw goes by index.
 //
 // Weights are float64 exponentials as integers in units of 2^-s (aug.h): sums are exact, so
 // they do not depend on the order in which threads come to add.
+//
+// A workgroup of 1024 threads takes a row and keeps it in registers (up to 256 KiB of it;
+// longer rows are read in in every pass). The cut lies near the top of the row, so few elements
+// need more than a comparison:
+//
+//  * top-k: at least k elements are not below the k-th largest of the maxima of groups of
+//    elements (four groups a thread), which bins over the distance from the row's
+//    largest logit bound from below. What is not below that goes on a list, is sorted by (logit,
+//    index) and cut by top-k, top-p and min-p, and the draw is made on the list sorted by index.
+//  * top-p alone: weights of all elements, by bins over the distance. If all up to the cut's bin fit on the list it goes on as above; else the list has the bin alone, and sums of
+//    the kept weights of pieces of the row, a scan over the pieces, and the piece that the
+//    number falls into element by element make the draw.
+//  * what this does not hold (more elements at the cut than the list has places, infinite
+//    logits) takes a descent over the digits of the logit instead: counts or weights of the
+//    elements that agree in the digits so far, by the next digit.
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "aug.h"
 #include "status.h"
@@ -23,8 +35,13 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr int kPieces = 1024;       // at most, of a row
 constexpr int kDigits = 256;
+constexpr int kBins = 2 * kThreads;
+constexpr int kList = 2 * kThreads;
+// pieces of a row: what one wave reads at once, at most (2^20 + 3) / 4 words of fp32
+constexpr int kPieces = ((1 << 20) / 4 / kThreads + 1) * kWaves;
+
+typedef unsigned long long u64;
 
 struct Rows {
   const void* logits;
@@ -40,157 +57,326 @@ struct Rows {
   float* probs;
 };
 
-// A logit as it counts: NaN is -infinity, -0 is 0.
-__device__ __forceinline__ float clean(float x) { return fmaxf(x, -INFINITY) + 0.f; }
+// f(0), f(1), ... f(N - 1) with constants: arrays stay in registers however much f is.
+template <typename F, int... I>
+__device__ __forceinline__ void times(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void times(F&& f) {
+  times(f, std::make_integer_sequence<int, N>{});
+}
 
-// Larger logits have larger keys.
+// Larger logits have larger keys; -0 has the key of 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x);
+  const uint32_t b = __float_as_uint(x + 0.f);
   return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
+// Place in the order: earlier elements have larger ones. No element has 0.
+__device__ __forceinline__ u64 place_of(float x, int index) {
+  return (static_cast<u64>(key_of(x)) << 32) | static_cast<uint32_t>(~index);
+}
+__device__ __forceinline__ float logit_at(u64 place) {
+  const uint32_t key = static_cast<uint32_t>(place >> 32);
+  return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key);
+}
+__device__ __forceinline__ int index_at(u64 place) { return static_cast<int>(~static_cast<uint32_t>(place)); }
 
-// exp((x - top) / temperature) for x <= top, off by a few 2^-52: 2^a = 2^n 2^f with |f| <= 1/2,
-// and the Taylor series of e^(f ln 2) up to its twelfth power (the rest is below 2e-16).
+// exp((x - top) / temperature) for x <= top, off by less than 2^-46: with a = (x - top) log2(e) /
+// temperature, 2^a = 2^n 2^f with |f| <= 1 / 2, and the Taylor series of e^(f ln 2) up to its
+// eleventh power (the rest is below 2^-47). Adding 1.5 * 2^52 rounds to an integer and leaves
+// it in the low word. (Powers of 2^(1/128) from a table in LDS and a series of four took twice as
+// long: its reads fall on the same banks.)
 struct Weight {
+  static constexpr double kRound = 6755399441055744.0;         // 1.5 * 2^52
   double top, rate;          // rate: log2(e) / temperature
-  float top_f;
-  __device__ Weight(float t, float temperature) : top(t), rate(1.4426950408889634074 / static_cast<double>(temperature)), top_f(t) {}
-  __device__ __forceinline__ double operator()(float x) const {
-    if (x == top_f) return 1.0;              // infinite ones too
-    const double a = fmax((static_cast<double>(x) - top) * rate, -200.0);
-    const double n = __builtin_rint(a);
-    const double z = (a - n) * 0.69314718055994530942;
-    double e = 1.0 / 479001600.0;
-    e = fma(e, z, 1.0 / 39916800.0);
-    e = fma(e, z, 1.0 / 3628800.0);
-    e = fma(e, z, 1.0 / 362880.0);
-    e = fma(e, z, 1.0 / 40320.0);
-    e = fma(e, z, 1.0 / 5040.0);
-    e = fma(e, z, 1.0 / 720.0);
-    e = fma(e, z, 1.0 / 120.0);
-    e = fma(e, z, 1.0 / 24.0);
-    e = fma(e, z, 1.0 / 6.0);
-    e = fma(e, z, 0.5);
-    e = fma(e, z, 1.0);
-    e = fma(e, z, 1.0);
-    return ldexp(e, static_cast<int>(n));
+  double unit;               // 2^s
+  int exponent;              // of unit, biased
+  __device__ __forceinline__ Weight(float t, float temperature, int fixed)
+      : top(t), rate(1.4426950408889634074 / static_cast<double>(temperature)), unit(ldexp(1.0, fixed)), exponent(fixed + 1023) {}
+  // e^(f ln 2) and n; what is below 2^-100, -infinity and NaN give that
+  __device__ __forceinline__ double split(float x, int* n) const {
+    const double a = fmax((static_cast<double>(x) - top) * rate, -100.0);
+    const double r = a + kRound;
+    const double f = a - (r - kRound);
+    *n = static_cast<int>(__double_as_longlong(r));
+    constexpr double c = 0.69314718055994530942;
+    constexpr double c2 = c * c, c4 = c2 * c2, c8 = c4 * c4;
+    double e = fma(f, c8 * c2 * c / 39916800.0, c8 * c2 / 3628800.0);
+    e = fma(e, f, c8 * c / 362880.0);
+    e = fma(e, f, c8 / 40320.0);
+    e = fma(e, f, c4 * c2 * c / 5040.0);
+    e = fma(e, f, c4 * c2 / 720.0);
+    e = fma(e, f, c4 * c / 120.0);
+    e = fma(e, f, c4 / 24.0);
+    e = fma(e, f, c2 * c / 6.0);
+    e = fma(e, f, c2 / 2.0);
+    e = fma(e, f, c);
+    return fma(e, f, 1.0);
   }
+  __device__ __forceinline__ double operator()(float x) const {
+    int n;
+    const double e = split(x, &n);
+    return e * __longlong_as_double(static_cast<long long>(n + 1023) << 52);
+  }
+  // in units of 2^-s: adding 2^52 leaves the rounded integer in the mantissa
+  __device__ __forceinline__ u64 fixed(float x) const {
+    int n;
+    const double e = split(x, &n);
+    return static_cast<u64>(__double_as_longlong(fma(e, __longlong_as_double(static_cast<long long>(n + exponent) << 52), 0x1p52))) &
+           0xFFFFFFFFFFFFFull;
+  }
+  // the same, 0 below the floor of min-p
+  __device__ __forceinline__ u64 fixed_from(float x, double floor) const { return floor > 0.0 && (*this)(x) < floor ? 0ull : fixed(x); }
 };
 
-// w * 2^s rounded to an integer: adding 2^52 leaves it in the mantissa.
-__device__ __forceinline__ uint64_t fixed_of(double w, double unit) {
-  return static_cast<uint64_t>(__double_as_longlong(fma(w, unit, 0x1p52))) & 0xFFFFFFFFFFFFFull;
+// The largest of three, without the compiler's quieting of what may be signalling NaNs: a
+// signalling NaN makes the result NaN, a quiet one is passed over.
+__device__ __forceinline__ float max3_raw(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 
-// One row, read in pieces of whole 16-byte words (the first and last may be parts of one).
-// Position p of the row's words is element p - shift.
+// A row in 16-byte words, of which the first and last may be parts of one: thread t takes
+// words t, t + kThreads, ... What is no element is -infinity; NaN stays, and is below everything
+// in comparisons. Every pass reads the row, from the caches after the first.
 template <bool F32>
-struct Reader {
+struct Row {
   static constexpr int VEC = F32 ? 4 : 8;
-  static constexpr int STEP = 64 * VEC;      // elements of a wave's load
+  static constexpr uint32_t kNone = F32 ? 0xFF800000u : 0xFF80FF80u;
   const char* words;
-  int shift, vocab, steps, pieces;           // steps of a piece
-  __device__ Reader(const Rows& a, int64_t row) {
+  int shift, vocab, count, turns;         // element = position in the words - shift
+
+  __device__ __forceinline__ Row(const Rows& a, int64_t row) {
     const char* p = static_cast<const char*>(a.logits) + row * a.stride * (F32 ? 4 : 2);
     shift = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15) / (F32 ? 4 : 2);
     words = p - (reinterpret_cast<uintptr_t>(p) & 15);
     vocab = a.vocab;
-    steps = ((vocab + shift + STEP - 1) / STEP + kPieces - 1) / kPieces;
-    pieces = (vocab + shift + steps * STEP - 1) / (steps * STEP);
+    count = (vocab + shift + VEC - 1) / VEC;
+    turns = (count + kThreads - 1) / kThreads;
   }
-  // the lane's elements of one step; what is none is -infinity
-  __device__ __forceinline__ void load(int piece, int step, int lane, float (&x)[VEC], int* index) const {
-    const int p = (piece * steps + step) * STEP + lane * VEC;
-    *index = p - shift;
-    if (p >= shift && p + VEC <= shift + vocab) {
-      const uint4 w = *reinterpret_cast<const uint4*>(words + static_cast<int64_t>(p) * (F32 ? 4 : 2));
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
+  __device__ __forceinline__ int first(int w) const { return w * VEC - shift; }
+  __device__ __forceinline__ uint4 word(int w) const {
+    if (w * VEC >= shift && w * VEC + VEC <= shift + vocab) return *reinterpret_cast<const uint4*>(words + static_cast<int64_t>(w) * 16);
+    // parts of it are no elements
+    uint32_t u[4] = {kNone, kNone, kNone, kNone};
+    times<VEC>([&](auto i) {
+      const int p = w * VEC + i;
+      if (p < shift || p >= shift + vocab) return;
+      if constexpr (F32) {
+        u[i] = reinterpret_cast<const uint32_t*>(words)[p];
+      } else {
+        const uint32_t h = reinterpret_cast<const uint16_t*>(words)[p];
+        u[i / 2] = i & 1 ? (u[i / 2] & 0xFFFFu) | (h << 16) : (u[i / 2] & 0xFFFF0000u) | h;
+      }
+    });
+    return uint4{u[0], u[1], u[2], u[3]};
+  }
+  __device__ static __forceinline__ void values(const uint4& w, float (&x)[VEC]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    times<4>([&](auto i) {
+      if constexpr (F32) {
+        x[i] = __uint_as_float(u[i]);
+      } else {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+      }
+    });
+  }
+  __device__ static __forceinline__ float largest(const uint4& w, float top) {
+    float x[VEC];
+    values(w, x);
+    times<VEC / 2>([&](auto i) { top = max3_raw(top, x[2 * i], x[2 * i + 1]); });
+    return top;
+  }
+  // f(turn, word, part) of every word of the thread, four at a time, so that their loads are
+  // on their way together; part is the word's number modulo four.
+  template <typename F>
+  __device__ __forceinline__ void by_words(F&& f) const {
+    const int t = threadIdx.x;
+    int turn = 0;
+#pragma nounroll
+    for (; turn + 5 < turns; turn += 4) {           // (not the last one, which may hold the row's end)
+      uint4 u[4];
+      times<4>([&](auto i) {
+        const int w = (turn + i) * kThreads + t;
+        u[i] = i == 0 && w == 0 ? word(0) : *reinterpret_cast<const uint4*>(words + static_cast<int64_t>(w) * 16);
+      });
+      times<4>([&](auto i) { f(turn + i, u[i], i); });
+    }
+#pragma nounroll
+    for (; turn < turns; turn += 2) {
+      const uint4 a = word(turn * kThreads + t), b = word((turn + 1) * kThreads + t);
+      f(turn, a, std::integral_constant<int, 1>{});
+      f(turn + 1, b, std::integral_constant<int, 2>{});
+    }
+  }
+  // f(index, value) of the thread's elements from `low` up
+  template <typename F>
+  __device__ __forceinline__ void from(float low, F&& f) const {
+    by_words([&](int turn, const uint4& u, auto) {
+      if (!__any(largest(u, -INFINITY) >= low)) return;
+      float x[VEC];
+      values(u, x);
+      const int index = first(turn * kThreads + static_cast<int>(threadIdx.x));
+      times<VEC>([&](auto i) {
+        if (x[i] >= low) f(index + i, x[i]);
+      });
+    });
+  }
+  // f(index, value) of all elements, and what is none, one by one, and end(turn) behind every word:
+  // a loop of little code, for passes that do much for each
+  template <typename F, typename E>
+  __device__ __forceinline__ void each(F&& f, E&& end) const {
+    uint4 next = word(threadIdx.x);
+#pragma nounroll
+    for (int turn = 0; turn < turns; ++turn) {
+      uint4 u = next;
+      next = word((turn + 1) * kThreads + threadIdx.x);
+      int index = first(turn * kThreads + static_cast<int>(threadIdx.x));
+#pragma nounroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t v = u.x;
+        u = uint4{u.y, u.z, u.w, 0u};
         if constexpr (F32) {
-          x[i] = clean(__uint_as_float(u[i]));
+          f(index++, __uint_as_float(v));
         } else {
-          x[2 * i] = clean(__uint_as_float(u[i] << 16));
-          x[2 * i + 1] = clean(__uint_as_float(u[i] & 0xFFFF0000u));
+          f(index++, __uint_as_float(v << 16));
+          f(index++, __uint_as_float(v & 0xFFFF0000u));
         }
       }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      x[i] = -INFINITY;
-      if (p + i < shift || p + i >= shift + vocab) continue;
-      if constexpr (F32) x[i] = clean(reinterpret_cast<const float*>(words)[p + i]);
-      else x[i] = clean(__uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(words)[p + i]) << 16));
+      end(turn);
     }
   }
+  // the largest of each of four groups of the thread's elements
+  __device__ __forceinline__ void maxima(float (&top)[4]) const {
+    times<4>([&](auto g) { top[g] = -INFINITY; });
+    by_words([&](int, const uint4& u, auto part) { top[part] = largest(u, top[part]); });
+    if (top[0] != top[0] || top[1] != top[1] || top[2] != top[2] || top[3] != top[3]) {
+      // signalling NaNs: all in one group, carefully
+      float t = -INFINITY;
+#pragma nounroll
+      for (int turn = 0; turn < turns; ++turn) {
+        float x[VEC];
+        values(word(turn * kThreads + threadIdx.x), x);
+        times<VEC>([&](auto i) {
+          if (x[i] > t) t = x[i];
+        });
+      }
+      top[0] = t;
+      top[1] = top[2] = top[3] = -INFINITY;
+    }
+  }
+  __device__ __forceinline__ bool is_element(int index) const { return index >= 0 && index < vocab; }
 };
 
-template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ T wave_upto(T v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
+// ---- sums over lanes, waves and the workgroup ---------------------------------------------
 
-typedef unsigned long long u64;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_add(u64 v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(v >> 32), CTRL, ROWS, 0xF, false);
+  return v + ((static_cast<u64>(hi) << 32) | lo);
+}
+// over the 16 lanes of a row up to this one, then over the wave
+__device__ __forceinline__ u64 row_upto(u64 v) {
+  return dpp_add<0x118, 0xF>(dpp_add<0x114, 0xF>(dpp_add<0x112, 0xF>(dpp_add<0x111, 0xF>(v))));   // row_shr 1, 2, 4, 8
+}
+__device__ __forceinline__ u64 wave_upto(u64 v) {
+  return dpp_add<0x143, 0xC>(dpp_add<0x142, 0xA>(row_upto(v)));                                     // row_bcast 15, 31
+}
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
+  return (static_cast<u64>(hi) << 32) | lo;
+}
+__device__ __forceinline__ u64 wave_sum(u64 v) { return lane_of(wave_upto(v), 63); }
 
 struct Lds {
-  u64 mass[kPieces];                 // digits' weights, then pieces' sums
-  uint32_t count[kPieces];           // digits' counts, then pieces' counts
-  u64 waves[kWaves];
+  u64 mass[kBins];                   // of bins or digits
+  u64 list[kList];
+  u64 piece[kPieces];                // sums of the pieces: 16 a turn
+  uint32_t count[kBins];
+  u64 waves[2][kWaves];
   float top[kWaves];
   int index[kWaves];
-  u64 found_before;
-  int found;
-  int tie;
+  u64 found_before, other_before;
+  int found, tie, listed;
 };
 
-// Over n values in the order of the threads (at most one each), the first at which their sum
-// exceeds `target`: its number and the sum before it, for every thread; n where none does.
-__device__ __forceinline__ int find_over(u64 v, int n, u64 target, Lds& s, u64* before) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const u64 upto = wave_upto(tid < n ? v : 0ull);
+// Sum over this thread and those before it, and over all. One barrier: consecutive calls alternate
+// between the two BUFs.
+template <int BUF>
+__device__ __forceinline__ u64 block_upto(u64 v, Lds& s, u64* total) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const u64 upto = wave_upto(v);
+  if (lane == 63) s.waves[BUF][wave] = upto;
   __syncthreads();
-  if (lane == 63) s.waves[wave] = upto;
-  if (tid == 0) s.found = n;
-  __syncthreads();
-  u64 at = upto;
-  for (int w = 0; w < wave; ++w) at += s.waves[w];
-  if (tid < n && at > target && at - v <= target) {
-    s.found = tid;
-    s.found_before = at - v;
+  const u64 w = row_upto(s.waves[BUF][lane & (kWaves - 1)]);
+  *total = lane_of(w, kWaves - 1);
+  return upto + (wave ? lane_of(w, wave - 1) : 0ull);
+}
+// Sum over all threads.
+template <int BUF>
+__device__ __forceinline__ u64 block_sum(u64 v, Lds& s) {
+  u64 total;
+  block_upto<BUF>(v, s, &total);
+  return total;
+}
+// The first thread at which the sum of v exceeds `target`, and the sum before it; -1 if none.
+__device__ __forceinline__ int find_over(u64 v, u64 target, Lds& s, u64* before) {
+  if (threadIdx.x == 0) s.found = -1;
+  u64 total;
+  const u64 upto = block_upto<0>(v, s, &total);
+  if (upto > target && upto - v <= target) {
+    s.found = threadIdx.x;
+    s.found_before = upto - v;
   }
   __syncthreads();
+  const int found = s.found;
   *before = s.found_before;
-  return s.found;
+  __syncthreads();
+  return found;
+}
+// The piece at which the sum of the pieces exceeds `target`, and the sum before it.
+__device__ __forceinline__ int find_piece(int turns, u64 target, Lds& s, u64* before) {
+  const int tid = threadIdx.x;
+  u64 v = 0;
+  if (tid < turns) {
+    times<kWaves>([&](auto w) { v += s.piece[tid * kWaves + w]; });
+  }
+  const int turn = max(find_over(v, target, s, before), 0);
+  int piece = turn * kWaves;
+  for (; piece < turn * kWaves + kWaves - 1 && *before + s.piece[piece] <= target; ++piece) *before += s.piece[piece];
+  return piece;
+}
+// A wave's sum becomes a piece's.
+__device__ __forceinline__ void set_piece(int turn, u64 v, Lds& s) {
+  if (__any(v != 0)) v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) s.piece[turn * kWaves + (threadIdx.x >> 6)] = v;
+}
+// p of a sum, rounded up: at least 1, at most all.
+__device__ __forceinline__ u64 share_of(float p, u64 all) {
+  const u64 t = static_cast<u64>(ceil(static_cast<double>(p) * static_cast<double>(all)));
+  return t < 1 ? 1 : t > all ? all : t;
+}
+// The number that the draw goes by: the first sum above it wins.
+__device__ __forceinline__ u64 draw_of(double uniform, u64 all) {
+  const double share = uniform * static_cast<double>(all);
+  const u64 t = share > 0.0 ? static_cast<u64>(share) : 0ull;
+  return t >= all ? all - 1 : t;
 }
 
-// The last element of a beginning of the order.
-struct Cut {
-  uint32_t key;          // elements above it are in
-  uint32_t equal;        // and this many of those with it, lowest indices first
-  u64 taken;             // elements of the beginning
-  bool all_equal;        // all of those with it
-};
+// ---- the cut by digits -----------------------------------------------------------------------
 
-// The shortest beginning with at least `target` elements (BY_MASS: weight) that are there.
-template <bool F32, bool BY_MASS>
-__device__ Cut descend(const Reader<F32>& in, const Weight& weight, double unit, u64 target, uint32_t from_key, Lds& s) {
+// The end of the shortest beginning of the order with at least `target` elements (BY_MASS:
+// weight), that are there, looking no further than `last`; *taken: its elements.
+template <bool BY_MASS, typename R, typename A>
+__device__ __forceinline__ u64 descend(const R& in, const A& as, const Weight& weight, u64 target, u64 last, Lds& s, u64* taken) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t from = static_cast<uint32_t>(last >> 32);
   uint32_t prefix = 0;
-  u64 above = 0, above_count = 0;     // of elements above the digits so far
-  uint32_t equal = 0;
+  u64 above = 0, above_count = 0, equal = 0;      // of elements above the digits so far
   for (int level = 0; level < 4; ++level) {
     const int low = 24 - 8 * level;
     __syncthreads();
@@ -199,240 +385,458 @@ __device__ Cut descend(const Reader<F32>& in, const Weight& weight, double unit,
       s.count[tid] = 0;
     }
     __syncthreads();
-    for (int piece = wave; piece < in.pieces; piece += kWaves)
-      for (int step = 0; step < in.steps; ++step) {
-        float x[Reader<F32>::VEC];
-        int index;
-        in.load(piece, step, lane, x, &index);
-#pragma unroll
-        for (int i = 0; i < Reader<F32>::VEC; ++i) {
-          if (index + i < 0 || index + i >= in.vocab) continue;
-          const uint32_t key = key_of(x[i]);
-          if ((level > 0 && (key ^ prefix) >> (low + 8)) || key < from_key) continue;
-          const int digit = (key >> low) & (kDigits - 1);
-          atomicAdd(&s.count[digit], 1u);
-          if constexpr (BY_MASS) atomicAdd(&s.mass[digit], static_cast<u64>(fixed_of(weight(x[i]), unit)));
-        }
-      }
+    in.each([&](int index, float x) {
+      x = as(x != x ? -INFINITY : x);
+      const uint32_t key = key_of(x);
+      if (!in.is_element(index) || (level > 0 && (key ^ prefix) >> (low + 8)) || key < from) return;
+      const int digit = (key >> low) & (kDigits - 1);
+      atomicAdd(&s.count[digit], 1u);
+      if constexpr (BY_MASS) atomicAdd(&s.mass[digit], weight.fixed(x));
+    }, [](int) {});
     __syncthreads();
     // digits from the largest down: the first at which the sum reaches the target
     const int digit = kDigits - 1 - tid;
     const u64 n = tid < kDigits ? s.count[digit] : 0;
     const u64 v = BY_MASS && tid < kDigits ? s.mass[digit] : n;
-    u64 before;
-    const int at = find_over(v, kDigits, target - above - 1, s, &before);
-    const u64 count_upto = wave_upto(n);
-    __syncthreads();
-    if (lane == 63) s.waves[wave] = count_upto;
-    __syncthreads();
+    u64 before, total;
+    const int at = max(find_over(v, target - above - 1, s, &before), 0);
+    const u64 upto = block_upto<1>(n, s, &total);
     if (tid == at) {
-      u64 c = count_upto - n;
-      for (int w = 0; w < wave; ++w) c += s.waves[w];
-      s.found_before = c;
+      s.other_before = upto - n;
       s.index[0] = static_cast<int>(n);
     }
     __syncthreads();
     above += before;
-    above_count += s.found_before;
-    equal = static_cast<uint32_t>(s.index[0]);
+    above_count += s.other_before;
+    equal = static_cast<u64>(s.index[0]);
     prefix |= static_cast<uint32_t>(kDigits - 1 - at) << low;
-    __syncthreads();
   }
-  Cut c;
-  c.key = prefix;
-  u64 need = target - above;
+  u64 need = target - above;                      // of the elements with that key
   if constexpr (BY_MASS) {
-    const uint32_t b = prefix >> 31 ? prefix ^ 0x80000000u : ~prefix;
-    const u64 each = fixed_of(weight(__uint_as_float(b)), unit);
-    need = (need + each - 1) / each;
+    const u64 each = weight.fixed(logit_at(static_cast<u64>(prefix) << 32));
+    need = each ? (need + each - 1) / each : equal;
   }
-  c.equal = static_cast<uint32_t>(need);
-  c.taken = above_count + need;
-  c.all_equal = need >= equal;
-  return c;
+  *taken = above_count + need;
+  if (need >= equal) return static_cast<u64>(prefix) << 32;
+  // the index of the last of them
+  __syncthreads();
+  u64 c = 0;
+  const auto is_equal = [&](int index, float x) { return in.is_element(index) && key_of(as(x != x ? -INFINITY : x)) == prefix; };
+  in.each([&](int index, float x) { c += is_equal(index, x); },
+          [&](int turn) {
+            set_piece(turn, c, s);
+            c = 0;
+          });
+  __syncthreads();
+  u64 before;
+  const int piece = find_piece(in.turns, need - 1, s, &before);
+  if (wave == 0) {
+    const int w = piece * 64 + lane, index = in.first(w);
+    float x[R::VEC];
+    R::values(in.word(w), x);
+    u64 n = 0;
+    times<R::VEC>([&](auto i) { n += is_equal(index + i, x[i]); });
+    u64 at = before + wave_upto(n) - n;
+    times<R::VEC>([&](auto i) {
+      if (is_equal(index + i, x[i]) && ++at == need) s.tie = index + i;
+    });
+  }
+  __syncthreads();
+  return (static_cast<u64>(prefix) << 32) | static_cast<uint32_t>(~s.tie);
+}
+
+// ---- the list ----------------------------------------------------------------------------------
+
+// s.list[0 .. n) sorted, largest first (bitonic, padded with zeros to a power of two). WAVE: by
+// one wave, n <= 128; its LDS accesses happen in order.
+template <bool WAVE>
+__device__ __forceinline__ void sort_list(int n, Lds& s) {
+  const int t = threadIdx.x;
+  int size = 2;
+  while (size < n) size <<= 1;
+  const auto meet = [] {
+    if constexpr (WAVE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else __syncthreads();
+  };
+  for (int i = n + t; i < size; i += WAVE ? 64 : kThreads) s.list[i] = 0;
+  for (int run = 2; run <= size; run <<= 1)
+    for (int gap = run >> 1; gap; gap >>= 1) {
+      meet();
+      if (t < size / 2) {
+        const int i = ((t & ~(gap - 1)) << 1) | (t & (gap - 1));
+        const u64 a = s.list[i], b = s.list[i + gap];
+        if ((a < b) == ((i & run) == 0)) {
+          s.list[i] = b;
+          s.list[i + gap] = a;
+        }
+      }
+    }
+  meet();
+}
+
+// What the cut is made by. `skip`: weight of elements before the list's first.
+struct Cut {
+  int k;                  // elements of the list that top-k leaves, at most
+  u64 target;             // weight that top-p asks for, 0: p of what k leaves
+  u64 skip;
+  float p;
+};
+
+// The list sorted and cut: how many of its elements top-k and top-p keep. Thread t holds
+// elements 2t and 2t + 1, and their weights. WAVE: threads 0 .. 63 alone.
+template <bool WAVE>
+__device__ __forceinline__ int cut_list(int n, const Cut& cut, const Weight& weight, Lds& s, u64 (&place)[2], u64 (&w)[2]) {
+  const int t = threadIdx.x;
+  sort_list<WAVE>(n, s);
+  times<2>([&](auto i) {
+    place[i] = 2 * t + i < n ? s.list[2 * t + i] : 0;
+    w[i] = place[i] ? weight.fixed(logit_at(place[i])) : 0;
+  });
+  int keep = min(n, cut.k);
+  if (cut.p < 1.f) {
+    const u64 a = 2 * t < keep ? w[0] : 0, b = 2 * t + 1 < keep ? w[1] : 0;
+    u64 all, upto;
+    if constexpr (WAVE) {
+      upto = wave_upto(a + b);
+      all = lane_of(upto, 63);
+    } else {
+      upto = block_upto<1>(a + b, s, &all);
+    }
+    const u64 target = (cut.target ? cut.target : share_of(cut.p, all)) - cut.skip;
+    // the first sum that reaches it
+    const int mine = upto - b >= target ? 2 * t + 1 : 2 * t + 2;
+    const bool here = upto >= target && upto - a - b < target;
+    if constexpr (WAVE) {
+      const u64 who = __ballot(here);
+      if (who) keep = min(keep, static_cast<int>(__builtin_amdgcn_readlane(mine, __ffsll(who) - 1)));
+    } else {
+      if (t == 0) s.tie = keep;
+      __syncthreads();
+      if (here) s.tie = mine;
+      __syncthreads();
+      keep = min(keep, s.tie);
+    }
+  }
+  return keep;
+}
+
+// The draw among the first `keep` elements of the list, which cut_list left.
+template <bool WAVE>
+__device__ __forceinline__ void draw_from_list(const Rows& a, int row, int keep, double floor, double uniform, const Weight& weight, Lds& s,
+                                               const u64 (&place)[2], const u64 (&w)[2]) {
+  const int t = threadIdx.x;
+  // by rising index: the list in, with the index above the place in the sorted list
+  if constexpr (!WAVE) __syncthreads();
+  times<2>([&](auto i) {
+    if (2 * t + i < keep) {
+      const bool in = floor <= 0.0 || weight(logit_at(place[i])) >= floor;
+      s.list[2 * t + i] = (static_cast<u64>(static_cast<uint32_t>(place[i])) << 32) | static_cast<uint32_t>(2 * t + i);
+      s.mass[2 * t + i] = in ? w[i] : 0;
+      s.count[2 * t + i] = __float_as_uint(logit_at(place[i]));
+    }
+  });
+  sort_list<WAVE>(keep, s);
+  u64 v[2], all, upto;
+  uint32_t at[2];
+  times<2>([&](auto i) {
+    at[i] = 2 * t + i < keep ? static_cast<uint32_t>(s.list[2 * t + i]) : 0;
+    v[i] = 2 * t + i < keep ? s.mass[at[i]] : 0;
+  });
+  if constexpr (WAVE) {
+    upto = wave_upto(v[0] + v[1]);
+    all = lane_of(upto, 63);
+  } else {
+    upto = block_upto<0>(v[0] + v[1], s, &all);
+  }
+  const u64 target = draw_of(uniform, all);
+  u64 before = upto - v[0] - v[1];
+  times<2>([&](auto i) {
+    if (before <= target && before + v[i] > target) {
+      a.tokens[row] = index_at(s.list[2 * t + i] >> 32);
+      if (a.probs) a.probs[row] = static_cast<float>(weight(__uint_as_float(s.count[at[i]])) * weight.unit / static_cast<double>(all));
+    }
+    before += v[i];
+  });
+}
+
+// The distance from the top in bins, `per_power` of them for a power of two of the weight. It
+// does not fall as logits fall, which is all that is asked of its rounding.
+struct Window {
+  float top, rate, per_power;
+  __device__ __forceinline__ float at(float x) const {
+#pragma clang fp contract(off)      // the same in every pass
+    return (top - x) * rate * per_power;
+  }
+  // a logit that none of bins 0 .. bin is below
+  __device__ __forceinline__ float low(int bin) const {
+    const float x = top - (bin + 1) / per_power * (1.f + 0x1p-16f) / rate;
+    return x - fabsf(x) * 0x1p-20f;
+  }
+};
+
+// An element comes on the list; more than it holds are counted.
+__device__ __forceinline__ void put(int index, float x, Lds& s) {
+  const int at = atomicAdd(&s.listed, 1);
+  if (at < kList) s.list[at] = place_of(x, index);
+}
+template <typename R>
+__device__ __forceinline__ int list_from(const R& in, float low, Lds& s) {
+  in.from(low, [&](int index, float x) { put(index, x, s); });
+  __syncthreads();
+  return s.listed;
+}
+
+// The list of n elements cut, and the draw from it.
+__device__ __forceinline__ void finish_list(const Rows& a, int row, int n, const Cut& cut, double floor, double uniform, const Weight& weight,
+                                            Lds& s) {
+  u64 place[2], w[2];
+  if (n <= 128) {
+    if (threadIdx.x >= 64) return;
+    const int keep = cut_list<true>(n, cut, weight, s, place, w);
+    draw_from_list<true>(a, row, keep, floor, uniform, weight, s, place, w);
+  } else {
+    const int keep = cut_list<false>(n, cut, weight, s, place, w);
+    draw_from_list<false>(a, row, keep, floor, uniform, weight, s, place, w);
+  }
+}
+
+// What became of a row in the fast ways.
+enum class Fast { kNot, kDrawn, kPieces };     // nothing done; done; pieces summed, `last` the end of what is kept
+
+template <typename R>
+__device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, const float (&maxima)[4], const Weight& weight, int k, float p, double floor,
+                          double uniform, Lds& s, u64* last) {
+  const int tid = threadIdx.x;
+  const float rate = static_cast<float>(weight.rate), top = static_cast<float>(weight.top);
+  Cut cut{kList, 0, 0, p};
+  if (in.vocab <= kList) {
+    if (tid == 0) s.listed = 0;
+    __syncthreads();
+    const int n = list_from(in, -3.402823466e38f, s);
+    if (k > 0) cut.k = k;
+    finish_list(a, row, n, cut, floor, uniform, weight, s);
+    return Fast::kDrawn;
+  }
+  if (k > 0) {
+    if (k > kList) return Fast::kNot;
+    cut.k = k;
+    // one bin for 1 / 32 of a power; what is 64 powers below the top is in the last
+    const Window win{top, rate, kBins / 64.f};
+    // Of the groups' maxima, if they are more than twice k: with k of G of them at the cut there
+    // are about -G ln(1 - k / G) elements above it, 1.4 k for half. Else, and where elements are not
+    // spread over the groups, of all elements.
+    for (int pass = 2 * k <= min(in.count, 4 * kThreads) && k <= kList * 2 / 3 ? 0 : 1; pass < 2; ++pass) {
+      __syncthreads();
+      s.count[tid] = s.count[tid + kThreads] = 0;
+      if (tid == 0) s.listed = 0;
+      __syncthreads();
+      const auto count = [&](float x) {
+        if (x > -INFINITY) atomicAdd(&s.count[static_cast<int>(fminf(win.at(x), kBins - 1.f))], 1u);
+      };
+      if (pass == 0) {
+        times<4>([&](auto g) { count(maxima[g]); });
+      } else {
+        in.each([&](int, float x) { count(x); }, [](int) {});
+      }
+      __syncthreads();
+      const uint32_t c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
+      u64 before;
+      const int pair = find_over(static_cast<u64>(c0) + c1, static_cast<u64>(k - 1), s, &before);
+      if (pair < 0) continue;
+      const int bin = before + s.count[2 * pair] >= static_cast<u64>(k) ? 2 * pair : 2 * pair + 1;
+      if (bin == kBins - 1) continue;
+      const int n = list_from(in, win.low(bin), s);
+      if (n > kList) continue;
+      finish_list(a, row, n, cut, floor, uniform, weight, s);
+      return Fast::kDrawn;
+    }
+    return Fast::kNot;
+  }
+
+  // top-p alone: bins of 1 / 32 of a power. Adding up by bins in LDS costs a tenth of the pass.
+  const Window win{top, rate, kBins / 64.f};
+  for (int i = tid; i < kBins; i += kThreads) {
+    s.mass[i] = 0;
+    s.count[i] = 0;
+  }
+  if (tid == 0) s.listed = 0;
+  __syncthreads();
+  u64 below = 0;
+  in.each([&](int, float x) {
+    const u64 w = weight.fixed(x);
+    const float d = win.at(x);
+    if (d < kBins) {
+      atomicAdd(&s.count[static_cast<int>(d)], 1u);
+      atomicAdd(&s.mass[static_cast<int>(d)], w);
+    } else {
+      below += w;
+    }
+  }, [](int) {});
+  __syncthreads();
+  const uint32_t c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
+  const u64 w0 = s.mass[2 * tid], w1 = s.mass[2 * tid + 1];
+  u64 in_bins, counted;
+  const u64 upto = block_upto<0>(w0 + w1, s, &in_bins);
+  cut.target = share_of(p, block_sum<1>(below, s) + in_bins);
+  if (cut.target > in_bins) return Fast::kNot;
+  const u64 count_upto = block_upto<0>(static_cast<u64>(c0) + c1, s, &counted);
+  if (upto >= cut.target && upto - w0 - w1 < cut.target) {
+    const bool second = upto - w1 < cut.target;
+    s.found = 2 * tid + second;
+    s.found_before = upto - w1 - (second ? 0 : w0);
+    s.other_before = count_upto - c1 - (second ? 0 : c0);
+  }
+  __syncthreads();
+  const int bin = s.found;
+  const u64 count_before = s.other_before;
+  cut.skip = s.found_before;
+  const uint32_t in_bin = s.count[bin];
+  const float end = static_cast<float>(bin + 1), begin = static_cast<float>(bin);
+  if (count_before + in_bin <= kList) {
+    // all up to the bin's end
+    cut.skip = 0;
+    in.from(win.low(bin), [&](int index, float x) {
+      if (win.at(x) < end) put(index, x, s);
+    });
+    __syncthreads();
+    finish_list(a, row, min(s.listed, kList), cut, floor, uniform, weight, s);
+    return Fast::kDrawn;
+  }
+  if (in_bin > kList) return Fast::kNot;
+  // the bin alone, and sums of what is above it
+  u64 v = 0;
+  in.each([&](int index, float x) {
+    const float d = win.at(x);
+    if (!(d < end)) return;
+    if (d >= begin) put(index, x, s);
+    else v += weight.fixed_from(x, floor);
+  }, [&](int turn) {
+    set_piece(turn, v, s);
+    v = 0;
+  });
+  __syncthreads();
+  u64 place[2], w[2];
+  const int keep = cut_list<false>(min(s.listed, kList), cut, weight, s, place, w);
+  times<2>([&](auto i) {
+    if (2 * tid + i < keep && (floor <= 0.0 || weight(logit_at(place[i])) >= floor))
+      atomicAdd(&s.piece[(index_at(place[i]) + in.shift) / (64 * R::VEC)], w[i]);
+  });
+  *last = s.list[keep - 1];
+  __syncthreads();
+  return Fast::kPieces;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void sample_kernel(Rows a) {
   __shared__ Lds s;
-  constexpr int VEC = Reader<F32>::VEC;
+  typedef Row<F32> R;
   const int row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Reader<F32> in(a, row);
   const float temperature = a.temperature ? a.temperature[row] : 1.f;
-  const int k = a.top_k ? a.top_k[row] : 0;
-  const float p = a.top_p ? a.top_p[row] : 1.f;
+  int k = a.top_k ? a.top_k[row] : 0;
+  float p = a.top_p ? a.top_p[row] : 1.f;
+  if (!(p < 1.f)) p = 1.f;
   const float min_p = a.min_p ? a.min_p[row] : 0.f;
   const double uniform = a.uniform[row];
+  const R in(a, row);
 
-  // the largest logit, the first of equal ones
-  float top = -INFINITY;
-  int at = INT32_MAX;
-  for (int piece = wave; piece < in.pieces; piece += kWaves)
-    for (int step = 0; step < in.steps; ++step) {
-      float x[VEC];
-      int index;
-      in.load(piece, step, lane, x, &index);
+  float maxima[4];
+  in.maxima(maxima);
+  float top = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
 #pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if (x[i] > top) {
-          top = x[i];
-          at = index + i;
-        }
-    }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    const float o = __shfl_xor(top, d);
-    const int oa = __shfl_xor(at, d);
-    if (o > top || (o == top && oa < at)) {
-      top = o;
-      at = oa;
-    }
-  }
-  if (lane == 0) {
-    s.top[wave] = top;
-    s.index[wave] = at;
-  }
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) s.top[wave] = top;
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) {
-    const float o = s.top[w];
-    const int oa = s.index[w];
-    if (o > top || (o == top && oa < at)) {
-      top = o;
-      at = oa;
-    }
-  }
-  if (top == -INFINITY || !(temperature > 0.f) || k == 1 || p <= 0.f) {
+  times<kWaves>([&](auto w) { top = fmaxf(top, s.top[w]); });
+  if (top == -INFINITY) {
     if (tid == 0) {
-      a.tokens[row] = top == -INFINITY ? -1 : at;
-      if (a.probs) a.probs[row] = top == -INFINITY ? 0.f : 1.f;
+      a.tokens[row] = -1;
+      if (a.probs) a.probs[row] = 0.f;
     }
     return;
   }
+  if (!(temperature > 0.f) || k == 1 || p <= 0.f) {
+    int at = INT32_MAX;
+    in.from(top, [&](int index, float) { at = min(at, index); });
+#pragma unroll
+    for (int d = 32; d; d >>= 1) at = min(at, __shfl_xor(at, d));
+    if (lane == 0) s.index[wave] = at;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 0; w < kWaves; ++w) at = min(at, s.index[w]);
+      a.tokens[row] = at;
+      if (a.probs) a.probs[row] = 1.f;
+    }
+    return;
+  }
+  if (k <= 0 || k >= in.vocab) k = 0;
+  // infinite logits share the weight, and the others have none
+  const bool endless = top == INFINITY;
+  if (endless) top = 1.f;
+  const auto as = [endless](float x) { return !endless ? x : x == INFINITY ? 1.f : -INFINITY; };
 
-  const Weight weight(top, temperature);
-  const double unit = ldexp(1.0, a.fixed);
-  Cut cut{0u, 0u, ~0ull, true};
-  if (k > 0 && k < in.vocab) cut = descend<F32, false>(in, weight, unit, static_cast<u64>(k), 0u, s);
-  int tie = INT32_MAX;                    // the last index of those with the cut's logit
-  // Sums over what is kept, by piece; with `ties`, counts of the elements at the cut.
-  const auto keeps = [&](float x, int index) {
-    const uint32_t key = key_of(x);
-    return key > cut.key || (key == cut.key && index <= tie);
-  };
-  const auto resolve_ties = [&]() {
-    tie = INT32_MAX;
-    if (cut.all_equal) return;
-    for (int piece = wave; piece < in.pieces; piece += kWaves) {
-      uint32_t n = 0;
-      for (int step = 0; step < in.steps; ++step) {
-        float x[VEC];
-        int index;
-        in.load(piece, step, lane, x, &index);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) n += index + i >= 0 && index + i < in.vocab && key_of(x[i]) == cut.key;
-      }
-      n = wave_sum(n);
-      if (lane == 0) s.count[piece] = n;
-    }
+  const Weight weight(top, temperature, a.fixed);
+  const double floor = min_p > 0.f ? fmin(static_cast<double>(min_p), 1.0) : 0.0;
+  u64 last = 0;                 // elements at or before this place are kept: all
+  // sums of what is kept, by piece
+  const auto sum_up = [&](const auto& r, double least) {
     __syncthreads();
-    u64 before;
-    const int piece = find_over(tid < in.pieces ? s.count[tid] : 0u, in.pieces, cut.equal - 1, s, &before);
-    if (wave == 0) {
-      u64 seen = before;
-      for (int step = 0; step < in.steps; ++step) {
-        float x[VEC];
-        int index;
-        in.load(piece, step, lane, x, &index);
-        uint32_t n = 0;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) n += index + i >= 0 && index + i < in.vocab && key_of(x[i]) == cut.key;
-        const uint32_t upto = wave_upto(n);
-        u64 c = seen + upto - n;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (index + i >= 0 && index + i < in.vocab && key_of(x[i]) == cut.key && ++c == cut.equal) s.tie = index + i;
-        seen += __shfl(upto, 63);
-      }
-    }
-    __syncthreads();
-    tie = s.tie;
-  };
-  const auto sums = [&](bool floor) {
-    for (int piece = wave; piece < in.pieces; piece += kWaves) {
-      u64 v = 0;
-      for (int step = 0; step < in.steps; ++step) {
-        float x[VEC];
-        int index;
-        in.load(piece, step, lane, x, &index);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          if (!keeps(x[i], index + i)) continue;
-          const double w = weight(x[i]);
-          if (floor && min_p > 0.f && w < fmin(static_cast<double>(min_p), 1.0)) continue;
-          v += fixed_of(w, unit);
-        }
-      }
-      v = wave_sum(v);
-      if (lane == 0) s.mass[piece] = v;
-    }
+    u64 v = 0;
+    r.each([&](int index, float x) {
+      x = as(x);
+      if (last == 0 || place_of(x, index) >= last) v += weight.fixed_from(x, least);
+    }, [&](int turn) {
+      set_piece(turn, v, s);
+      v = 0;
+    });
     __syncthreads();
   };
   const auto total = [&]() {
-    u64 v = wave_sum(tid < in.pieces ? s.mass[tid] : 0ull);
-    __syncthreads();
-    if (lane == 0) s.waves[wave] = v;
-    __syncthreads();
-    v = 0;
-    for (int w = 0; w < kWaves; ++w) v += s.waves[w];
-    return v;
+    u64 v = 0;
+    for (int i = tid; i < in.turns * kWaves; i += kThreads) v += s.piece[i];
+    return block_sum<0>(v, s);
   };
-  resolve_ties();
-  if (p < 1.f) {
-    sums(false);
-    const u64 all = total();
-    const double want = ceil(static_cast<double>(p) * static_cast<double>(all));
-    u64 target = static_cast<u64>(want);
-    target = target < 1 ? 1 : target > all ? all : target;
-    const Cut by = descend<F32, true>(in, weight, unit, target, cut.key, s);
-    if (by.taken < cut.taken) {
-      cut = by;
-      resolve_ties();
-    }
-  }
-  sums(true);
-  const u64 all = total();
-  const double share = uniform * static_cast<double>(all);
-  u64 target = share > 0.0 ? static_cast<u64>(share) : 0ull;
-  if (target >= all) target = all - 1;
-  u64 before;
-  const int piece = find_over(tid < in.pieces ? s.mass[tid] : 0ull, in.pieces, target, s, &before);
-  if (wave != 0) return;
-  for (int step = 0; step < in.steps; ++step) {
-    float x[VEC];
-    int index;
-    in.load(piece, step, lane, x, &index);
-    u64 v[VEC], sum = 0;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      v[i] = 0;
-      if (!keeps(x[i], index + i)) continue;
-      const double w = weight(x[i]);
-      if (!(min_p > 0.f && w < fmin(static_cast<double>(min_p), 1.0))) v[i] = fixed_of(w, unit);
-      sum += v[i];
-    }
-    const u64 upto = wave_upto(sum);
-    u64 c = before + upto - sum;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      if (c <= target && c + v[i] > target) {
-        a.tokens[row] = index + i;
-        if (a.probs) a.probs[row] = static_cast<float>(weight(x[i]) * unit / static_cast<double>(all));
+  if (k == 0 && p >= 1.f) {
+    sum_up(in, floor);
+  } else {
+    // (a rate that float32 does not hold well leaves the bins without sense)
+    const bool plain = !endless && temperature >= 0x1p-40f && temperature <= 0x1p40f;
+    const Fast fast = plain ? fast_draw(a, row, in, maxima, weight, k, p, floor, uniform, s, &last) : Fast::kNot;
+    if (fast == Fast::kDrawn) return;
+    if (fast == Fast::kNot) {
+      u64 taken = ~0ull, taken_p;
+      if (k > 0) last = descend<false>(in, as, weight, static_cast<u64>(k), 0, s, &taken);
+      if (p < 1.f) {
+        sum_up(in, 0.0);
+        const u64 by_p = descend<true>(in, as, weight, share_of(p, total()), last, s, &taken_p);
+        if (taken_p < taken) last = by_p;
       }
-      c += v[i];
+      sum_up(in, floor);
     }
-    before += __shfl(upto, 63);
   }
+  const u64 all = total();
+  const u64 target = draw_of(uniform, all);
+  u64 before;
+  __syncthreads();
+  const int piece = find_piece(in.turns, target, s, &before);
+  if (wave != 0) return;
+  const int w0 = piece * 64 + lane, index = in.first(w0);
+  float x[R::VEC];
+  R::values(in.word(w0), x);
+  u64 v[R::VEC], sum = 0;
+  times<R::VEC>([&](auto i) {
+    x[i] = as(x[i]);
+    v[i] = last == 0 || place_of(x[i], index + i) >= last ? weight.fixed_from(x[i], floor) : 0;
+    sum += v[i];
+  });
+  u64 c = before + wave_upto(sum) - sum;
+  times<R::VEC>([&](auto i) {
+    if (c <= target && c + v[i] > target) {
+      a.tokens[row] = index + i;
+      if (a.probs) a.probs[row] = static_cast<float>(weight(x[i]) * weight.unit / static_cast<double>(all));
+    }
+    c += v[i];
+  });
 }
 
 }  // namespace
