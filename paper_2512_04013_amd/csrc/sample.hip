@@ -83,51 +83,68 @@ __device__ __forceinline__ float logit_at(u64 place) {
 __device__ __forceinline__ int index_at(u64 place) { return static_cast<int>(~static_cast<uint32_t>(place)); }
 
 // exp((x - top) / temperature) for x <= top, off by less than 2^-46: with a = (x - top) log2(e) /
-// temperature, 2^a = 2^n 2^f with |f| <= 1 / 2, and the Taylor series of e^(f ln 2) up to its
-// eleventh power (the rest is below 2^-47). Adding 1.5 * 2^52 rounds to an integer and leaves
-// it in the low word. (Powers of 2^(1/128) from a table in LDS and a series of four took twice as
-// long: its reads fall on the same banks.)
+// temperature and m = 32 a rounded, 2^a = 2^(m >> 5) 2^((m & 31) / 32) 2^f with |f| <= 1 / 64, from a
+// table of 2^(j / 32) and the Taylor series of e^(f ln 2) up to its fifth power (the rest is below
+// 2^-48). Adding 1.5 * 2^52 rounds to an integer and leaves it in the low word. The table is
+// 256 bytes of LDS, every bank once, so that its reads never wait for one another (128
+// entries, with a shorter series, took twice as long), and -m is the element's bin below.
+constexpr int kPowers = 32;
 struct Weight {
   static constexpr double kRound = 6755399441055744.0;         // 1.5 * 2^52
   double top, rate;          // rate: log2(e) / temperature
   double unit;               // 2^s
-  int exponent;              // of unit, biased
-  __device__ __forceinline__ Weight(float t, float temperature, int fixed)
-      : top(t), rate(1.4426950408889634074 / static_cast<double>(temperature)), unit(ldexp(1.0, fixed)), exponent(fixed + 1023) {}
-  // e^(f ln 2) and n; what is below 2^-100, -infinity and NaN give that
-  __device__ __forceinline__ double split(float x, int* n) const {
-    const double a = fmax((static_cast<double>(x) - top) * rate, -100.0);
-    const double r = a + kRound;
-    const double f = a - (r - kRound);
-    *n = static_cast<int>(__double_as_longlong(r));
+  const u64* powers;         // LDS: 2^(j / 32), as bits
+  int fixed_bits;            // s
+  __device__ __forceinline__ Weight(float t, float temperature, int s, const u64* table)
+      : top(t), rate(1.4426950408889634074 / static_cast<double>(temperature)), unit(ldexp(1.0, s)), powers(table), fixed_bits(s) {}
+  // what is below 2^-100, -infinity and NaN count as that
+  __device__ __forceinline__ double power_of(float x) const { return fmax((static_cast<double>(x) - top) * rate, -100.0); }
+  // e^(f ln 2) and the bits of 2^(m / 32) times 2^up
+  __device__ __forceinline__ double split(double a, int up, double* power, int* m) const {
+    const double r = fma(a, 32.0, kRound);
+    const double f = fma(r - kRound, -1.0 / 32.0, a);
+    *m = static_cast<int>(__double_as_longlong(r));
+    const u64 p = powers[*m & (kPowers - 1)];
+    const int hi = static_cast<int>(p >> 32) + (((*m >> 5) + up) << 20);
+    *power = __longlong_as_double(static_cast<long long>((static_cast<u64>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(p)));
     constexpr double c = 0.69314718055994530942;
-    constexpr double c2 = c * c, c4 = c2 * c2, c8 = c4 * c4;
-    double e = fma(f, c8 * c2 * c / 39916800.0, c8 * c2 / 3628800.0);
-    e = fma(e, f, c8 * c / 362880.0);
-    e = fma(e, f, c8 / 40320.0);
-    e = fma(e, f, c4 * c2 * c / 5040.0);
-    e = fma(e, f, c4 * c2 / 720.0);
-    e = fma(e, f, c4 * c / 120.0);
-    e = fma(e, f, c4 / 24.0);
-    e = fma(e, f, c2 * c / 6.0);
-    e = fma(e, f, c2 / 2.0);
+    double e = fma(f, c * c * c * c * c / 120.0, c * c * c * c / 24.0);
+    e = fma(e, f, c * c * c / 6.0);
+    e = fma(e, f, c * c / 2.0);
     e = fma(e, f, c);
     return fma(e, f, 1.0);
   }
   __device__ __forceinline__ double operator()(float x) const {
-    int n;
-    const double e = split(x, &n);
-    return e * __longlong_as_double(static_cast<long long>(n + 1023) << 52);
+    double p;
+    int m;
+    const double e = split(power_of(x), 0, &p, &m);
+    return e * p;
   }
-  // in units of 2^-s: adding 2^52 leaves the rounded integer in the mantissa
+  // In units of 2^-s: adding 2^52 leaves the rounded integer in the mantissa. *m: 32 times the
+  // logarithm, rounded.
+  __device__ __forceinline__ u64 fixed(float x, int* m) const {
+    double p;
+    const double e = split(power_of(x), fixed_bits, &p, m);
+    return static_cast<u64>(__double_as_longlong(fma(e, p, 0x1p52))) & 0xFFFFFFFFFFFFFull;
+  }
   __device__ __forceinline__ u64 fixed(float x) const {
-    int n;
-    const double e = split(x, &n);
-    return static_cast<u64>(__double_as_longlong(fma(e, __longlong_as_double(static_cast<long long>(n + exponent) << 52), 0x1p52))) &
-           0xFFFFFFFFFFFFFull;
+    int m;
+    return fixed(x, &m);
   }
-  // the same, 0 below the floor of min-p
-  __device__ __forceinline__ u64 fixed_from(float x, double floor) const { return floor > 0.0 && (*this)(x) < floor ? 0ull : fixed(x); }
+  // the same, 0 below `floor`
+  __device__ __forceinline__ u64 fixed_from(float x, u64 floor) const {
+    const u64 v = fixed(x);
+    return v < floor ? 0ull : v;
+  }
+  // the distance from the top in bins of 1 / 32 of a power
+  __device__ __forceinline__ int bin(float x) const {
+    return -static_cast<int>(__double_as_longlong(fma(power_of(x), 32.0, kRound)));
+  }
+  // a logit that none of bins 0 .. bin is below
+  __device__ __forceinline__ float low(int bin) const {
+    const double x = top - (bin + 0.51) / 32.0 / rate;
+    return static_cast<float>(x - fabs(x) * 0x1p-22);
+  }
 };
 
 // The largest of three, without the compiler's quieting of what may be signalling NaNs: a
@@ -297,6 +314,7 @@ struct Lds {
   u64 list[kList];
   u64 piece[kPieces];                // sums of the pieces: 16 a turn
   uint32_t count[kBins];
+  u64 powers[kPowers];
   u64 waves[2][kWaves];
   float top[kWaves];
   int index[kWaves];
@@ -447,31 +465,83 @@ __device__ __forceinline__ u64 descend(const R& in, const A& as, const Weight& w
 
 // ---- the list ----------------------------------------------------------------------------------
 
-// s.list[0 .. n) sorted, largest first (bitonic, padded with zeros to a power of two). WAVE: by
-// one wave, n <= 128; its LDS accesses happen in order.
-template <bool WAVE>
-__device__ __forceinline__ void sort_list(int n, Lds& s) {
-  const int t = threadIdx.x;
-  int size = 2;
+// Of the list, thread t holds elements list_pos(0) and list_pos(1): a wave has 128 in a row, its
+// lanes the first 64 and the second.
+__device__ __forceinline__ int list_pos(int i) { return 128 * (threadIdx.x >> 6) + 64 * i + (threadIdx.x & 63); }
+
+// The value of lane ^ MASK.
+template <int MASK>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  const int x = static_cast<int>(v);
+  if constexpr (MASK == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true);         // quad_perm
+  if constexpr (MASK == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true);
+  if constexpr (MASK == 4)                                                     // lane ^ 7, then ^ 3
+    return __builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+  if constexpr (MASK == 8) return __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, true);        // row_ror:8
+  if constexpr (MASK == 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? a[0] : a[1];
+  }
+  if constexpr (MASK == 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? a[0] : a[1];
+  }
+}
+// the larger of two, or the smaller
+__device__ __forceinline__ u64 pick(u64 a, u64 b, bool larger) { return (a < b) == larger ? b : a; }
+
+// The list of n elements (in registers: v, 0 behind the last) sorted, largest first: bitonic. Pairs
+// up to 32 apart are lanes of a wave, 64 apart a lane's own two, and wider ones meet in s.list.
+__device__ __forceinline__ void sort_list(int n, u64 (&v)[2], Lds& s) {
+  const int pos[2] = {list_pos(0), list_pos(1)};
+  int size = 256;
   while (size < n) size <<= 1;
-  const auto meet = [] {
-    if constexpr (WAVE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    else __syncthreads();
+  const bool mine = __builtin_amdgcn_readfirstlane(pos[0]) < size;     // other waves have nothing
+  const auto lanes = [&](auto gap, int run) {
+    if (gap * 2 > run) return;
+    times<2>([&](auto e) {
+      const u64 other = (static_cast<u64>(lane_xor<gap>(static_cast<uint32_t>(v[e] >> 32))) << 32) | lane_xor<gap>(static_cast<uint32_t>(v[e]));
+      v[e] = pick(v[e], other, ((pos[e] & gap) == 0) == ((pos[e] & run) == 0));
+    });
   };
-  for (int i = n + t; i < size; i += WAVE ? 64 : kThreads) s.list[i] = 0;
-  for (int run = 2; run <= size; run <<= 1)
-    for (int gap = run >> 1; gap; gap >>= 1) {
-      meet();
-      if (t < size / 2) {
-        const int i = ((t & ~(gap - 1)) << 1) | (t & (gap - 1));
-        const u64 a = s.list[i], b = s.list[i + gap];
-        if ((a < b) == ((i & run) == 0)) {
-          s.list[i] = b;
-          s.list[i + gap] = a;
-        }
-      }
+#pragma nounroll
+  for (int run = 2; run <= size; run <<= 1) {
+#pragma nounroll
+    for (int gap = run >> 1; gap >= 128; gap >>= 1) {
+      __syncthreads();
+      if (mine) times<2>([&](auto e) { s.list[pos[e]] = v[e]; });
+      __syncthreads();
+      if (mine) times<2>([&](auto e) { v[e] = pick(v[e], s.list[pos[e] ^ gap], ((pos[e] & gap) == 0) == ((pos[e] & run) == 0)); });
     }
-  meet();
+    if (!mine) continue;
+    if (run >= 128) {
+      const bool down = (pos[0] & run) == 0;
+      const u64 a = pick(v[0], v[1], down), b = pick(v[0], v[1], !down);
+      v[0] = a;
+      v[1] = b;
+    }
+    lanes(std::integral_constant<int, 32>{}, run);
+    lanes(std::integral_constant<int, 16>{}, run);
+    lanes(std::integral_constant<int, 8>{}, run);
+    lanes(std::integral_constant<int, 4>{}, run);
+    lanes(std::integral_constant<int, 2>{}, run);
+    lanes(std::integral_constant<int, 1>{}, run);
+  }
+}
+
+// Sums of a thread's two over the list up to each.
+template <int BUF>
+__device__ __forceinline__ void list_upto(u64 a, u64 b, Lds& s, u64 (&upto)[2], u64* all) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  upto[0] = wave_upto(a);
+  upto[1] = wave_upto(b) + lane_of(upto[0], 63);
+  if (lane == 63) s.waves[BUF][wave] = upto[1];
+  __syncthreads();
+  const u64 w = row_upto(s.waves[BUF][lane & (kWaves - 1)]);
+  *all = lane_of(w, kWaves - 1);
+  const u64 before = wave ? lane_of(w, wave - 1) : 0ull;
+  upto[0] += before;
+  upto[1] += before;
 }
 
 // What the cut is made by. `skip`: weight of elements before the list's first.
@@ -482,97 +552,125 @@ struct Cut {
   float p;
 };
 
-// The list sorted and cut: how many of its elements top-k and top-p keep. Thread t holds
-// elements 2t and 2t + 1, and their weights. WAVE: threads 0 .. 63 alone.
-template <bool WAVE>
+// The list sorted and cut: how many of its elements top-k and top-p keep. The thread's places and
+// their weights come back.
 __device__ __forceinline__ int cut_list(int n, const Cut& cut, const Weight& weight, Lds& s, u64 (&place)[2], u64 (&w)[2]) {
-  const int t = threadIdx.x;
-  sort_list<WAVE>(n, s);
-  times<2>([&](auto i) {
-    place[i] = 2 * t + i < n ? s.list[2 * t + i] : 0;
-    w[i] = place[i] ? weight.fixed(logit_at(place[i])) : 0;
-  });
+  times<2>([&](auto i) { place[i] = list_pos(i) < n ? s.list[list_pos(i)] : 0; });
+  sort_list(n, place, s);
+  times<2>([&](auto i) { w[i] = place[i] ? weight.fixed(logit_at(place[i])) : 0; });
   int keep = min(n, cut.k);
   if (cut.p < 1.f) {
-    const u64 a = 2 * t < keep ? w[0] : 0, b = 2 * t + 1 < keep ? w[1] : 0;
-    u64 all, upto;
-    if constexpr (WAVE) {
-      upto = wave_upto(a + b);
-      all = lane_of(upto, 63);
-    } else {
-      upto = block_upto<1>(a + b, s, &all);
-    }
+    u64 v[2], upto[2], all;
+    times<2>([&](auto i) { v[i] = list_pos(i) < keep ? w[i] : 0; });
+    list_upto<1>(v[0], v[1], s, upto, &all);
     const u64 target = (cut.target ? cut.target : share_of(cut.p, all)) - cut.skip;
     // the first sum that reaches it
-    const int mine = upto - b >= target ? 2 * t + 1 : 2 * t + 2;
-    const bool here = upto >= target && upto - a - b < target;
-    if constexpr (WAVE) {
-      const u64 who = __ballot(here);
-      if (who) keep = min(keep, static_cast<int>(__builtin_amdgcn_readlane(mine, __ffsll(who) - 1)));
-    } else {
-      if (t == 0) s.tie = keep;
-      __syncthreads();
-      if (here) s.tie = mine;
-      __syncthreads();
-      keep = min(keep, s.tie);
-    }
+    if (threadIdx.x == 0) s.tie = keep;
+    __syncthreads();
+    times<2>([&](auto i) {
+      if (upto[i] >= target && upto[i] - v[i] < target) s.tie = list_pos(i) + 1;
+    });
+    __syncthreads();
+    keep = min(keep, s.tie);
   }
   return keep;
 }
 
+__device__ __forceinline__ void write_token(const Rows& a, int row, int index, float x, u64 all, const Weight& weight) {
+  a.tokens[row] = index;
+  if (a.probs) a.probs[row] = static_cast<float>(weight(x) * weight.unit / static_cast<double>(all));
+}
+
 // The draw among the first `keep` elements of the list, which cut_list left.
-template <bool WAVE>
-__device__ __forceinline__ void draw_from_list(const Rows& a, int row, int keep, double floor, double uniform, const Weight& weight, Lds& s,
+__device__ __forceinline__ void draw_from_list(const Rows& a, int row, int keep, u64 floor, double uniform, const Weight& weight, Lds& s,
                                                const u64 (&place)[2], const u64 (&w)[2]) {
-  const int t = threadIdx.x;
-  // by rising index: the list in, with the index above the place in the sorted list
-  if constexpr (!WAVE) __syncthreads();
+  // by rising index: ~index above the position, which finds the weight again
+  u64 v[2];
   times<2>([&](auto i) {
-    if (2 * t + i < keep) {
-      const bool in = floor <= 0.0 || weight(logit_at(place[i])) >= floor;
-      s.list[2 * t + i] = (static_cast<u64>(static_cast<uint32_t>(place[i])) << 32) | static_cast<uint32_t>(2 * t + i);
-      s.mass[2 * t + i] = in ? w[i] : 0;
-      s.count[2 * t + i] = __float_as_uint(logit_at(place[i]));
-    }
+    const int pos = list_pos(i);
+    v[i] = 0;
+    if (pos >= keep) return;
+    v[i] = (place[i] << 32) | static_cast<uint32_t>(pos);
+    s.mass[pos] = w[i] >= floor ? w[i] : 0;
+    s.count[pos] = __float_as_uint(logit_at(place[i]));
   });
-  sort_list<WAVE>(keep, s);
-  u64 v[2], all, upto;
-  uint32_t at[2];
-  times<2>([&](auto i) {
-    at[i] = 2 * t + i < keep ? static_cast<uint32_t>(s.list[2 * t + i]) : 0;
-    v[i] = 2 * t + i < keep ? s.mass[at[i]] : 0;
-  });
-  if constexpr (WAVE) {
-    upto = wave_upto(v[0] + v[1]);
-    all = lane_of(upto, 63);
-  } else {
-    upto = block_upto<0>(v[0] + v[1], s, &all);
-  }
+  sort_list(keep, v, s);
+  __syncthreads();
+  u64 x[2], upto[2], all;
+  times<2>([&](auto i) { x[i] = list_pos(i) < keep ? s.mass[static_cast<uint32_t>(v[i])] : 0; });
+  list_upto<0>(x[0], x[1], s, upto, &all);
   const u64 target = draw_of(uniform, all);
-  u64 before = upto - v[0] - v[1];
   times<2>([&](auto i) {
-    if (before <= target && before + v[i] > target) {
-      a.tokens[row] = index_at(s.list[2 * t + i] >> 32);
-      if (a.probs) a.probs[row] = static_cast<float>(weight(__uint_as_float(s.count[at[i]])) * weight.unit / static_cast<double>(all));
-    }
-    before += v[i];
+    if (upto[i] > target && upto[i] - x[i] <= target)
+      write_token(a, row, index_at(v[i] >> 32), __uint_as_float(s.count[static_cast<uint32_t>(v[i])]), all, weight);
   });
 }
 
-// The distance from the top in bins, `per_power` of them for a power of two of the weight. It
-// does not fall as logits fall, which is all that is asked of its rounding.
-struct Window {
-  float top, rate, per_power;
-  __device__ __forceinline__ float at(float x) const {
-#pragma clang fp contract(off)      // the same in every pass
-    return (top - x) * rate * per_power;
+// Cut and draw of a list of up to 128 elements without sorting it: eight threads an element
+// count the elements before it in the order and add their weights, sixteen others each; then the
+// same over those before it by index that are kept. Half the time of two sorts.
+__device__ __forceinline__ void finish_short(const Rows& a, int row, int n, const Cut& cut, u64 floor, double uniform, const Weight& weight, Lds& s) {
+  constexpr int kShort = 128, kParts = kThreads / kShort, kEach = kShort / kParts;
+  const int t = threadIdx.x, e = t & (kShort - 1), part = t / kShort;
+  u64* before = s.mass + kShort;          // weights before each, in the order, then by index
+  const u64 mine = e < n ? s.list[e] : 0;
+  const float x = logit_at(mine);
+  const u64 w = mine ? weight.fixed(x) : 0;
+  if (part == 0) {
+    s.list[e] = mine;
+    s.mass[e] = w;
+    before[e] = before[kShort + e] = 0;
+    s.count[e] = 0;
   }
-  // a logit that none of bins 0 .. bin is below
-  __device__ __forceinline__ float low(int bin) const {
-    const float x = top - (bin + 1) / per_power * (1.f + 0x1p-16f) / rate;
-    return x - fabsf(x) * 0x1p-20f;
+  __syncthreads();
+  uint32_t rank = 0;
+  u64 sum = 0;
+#pragma unroll 4
+  for (int j = part * kEach; j < part * kEach + kEach; ++j) {
+    const bool first = s.list[j] > mine;
+    rank += first;
+    sum += first ? s.mass[j] : 0;
   }
-};
+  if (mine) {
+    atomicAdd(&s.count[e], rank);
+    atomicAdd(&before[e], sum);
+  }
+  __syncthreads();
+  rank = s.count[e];
+  sum = before[e];
+  int keep = min(n, cut.k);
+  if (cut.p < 1.f) {
+    u64 target = cut.target;
+    if (!target) {
+      if (part == 0 && mine && static_cast<int>(rank) == keep - 1) s.found_before = sum + w;
+      __syncthreads();
+      target = share_of(cut.p, s.found_before);
+    }
+    if (part == 0 && mine && sum < target && sum + w >= target) s.tie = static_cast<int>(rank) + 1;
+    __syncthreads();
+    keep = min(keep, s.tie);
+  }
+  const u64 v = static_cast<int>(rank) < keep && w >= floor ? w : 0;
+  if (part == 0) s.mass[e] = v;
+  __syncthreads();
+  sum = 0;
+  u64 all = 0;
+  const uint32_t index = ~static_cast<uint32_t>(mine);
+#pragma unroll 4
+  for (int j = part * kEach; j < part * kEach + kEach; ++j) {
+    const u64 o = s.mass[j];
+    sum += ~static_cast<uint32_t>(s.list[j]) < index ? o : 0;
+    all += o;
+  }
+  if (mine) atomicAdd(&before[kShort + e], sum);
+  if (e == 0) s.waves[0][part] = all;
+  __syncthreads();
+  all = 0;
+  times<kParts>([&](auto i) { all += s.waves[0][i]; });
+  const u64 target = draw_of(uniform, all);
+  sum = before[kShort + e];
+  if (part == 0 && v && sum <= target && sum + v > target) write_token(a, row, static_cast<int>(index), x, all, weight);
+}
 
 // An element comes on the list; more than it holds are counted.
 __device__ __forceinline__ void put(int index, float x, Lds& s) {
@@ -587,16 +685,14 @@ __device__ __forceinline__ int list_from(const R& in, float low, Lds& s) {
 }
 
 // The list of n elements cut, and the draw from it.
-__device__ __forceinline__ void finish_list(const Rows& a, int row, int n, const Cut& cut, double floor, double uniform, const Weight& weight,
+__device__ __forceinline__ void finish_list(const Rows& a, int row, int n, const Cut& cut, u64 floor, double uniform, const Weight& weight,
                                             Lds& s) {
-  u64 place[2], w[2];
   if (n <= 128) {
-    if (threadIdx.x >= 64) return;
-    const int keep = cut_list<true>(n, cut, weight, s, place, w);
-    draw_from_list<true>(a, row, keep, floor, uniform, weight, s, place, w);
+    finish_short(a, row, n, cut, floor, uniform, weight, s);
   } else {
-    const int keep = cut_list<false>(n, cut, weight, s, place, w);
-    draw_from_list<false>(a, row, keep, floor, uniform, weight, s, place, w);
+    u64 place[2], w[2];
+    const int keep = cut_list(n, cut, weight, s, place, w);
+    draw_from_list(a, row, keep, floor, uniform, weight, s, place, w);
   }
 }
 
@@ -607,7 +703,6 @@ template <typename R>
 __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, const float (&maxima)[4], const Weight& weight, int k, float p, double floor,
                           double uniform, Lds& s, u64* last) {
   const int tid = threadIdx.x;
-  const float rate = static_cast<float>(weight.rate), top = static_cast<float>(weight.top);
   Cut cut{kList, 0, 0, p};
   if (in.vocab <= kList) {
     if (tid == 0) s.listed = 0;
@@ -620,9 +715,7 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
   if (k > 0) {
     if (k > kList) return Fast::kNot;
     cut.k = k;
-    // one bin for 1 / 32 of a power; what is 64 powers below the top is in the last
-    const Window win{top, rate, kBins / 64.f};
-    // Of the groups' maxima, if they are more than twice k: with k of G of them at the cut there
+    // What is 64 powers below the top is in the last bin. Of the groups' maxima, if they are more than twice k: with k of G of them at the cut there
     // are about -G ln(1 - k / G) elements above it, 1.4 k for half. Else, and where elements are not
     // spread over the groups, of all elements.
     for (int pass = 2 * k <= min(in.count, 4 * kThreads) && k <= kList * 2 / 3 ? 0 : 1; pass < 2; ++pass) {
@@ -631,7 +724,7 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
       if (tid == 0) s.listed = 0;
       __syncthreads();
       const auto count = [&](float x) {
-        if (x > -INFINITY) atomicAdd(&s.count[static_cast<int>(fminf(win.at(x), kBins - 1.f))], 1u);
+        if (x > -INFINITY) atomicAdd(&s.count[min(weight.bin(x), kBins - 1)], 1u);
       };
       if (pass == 0) {
         times<4>([&](auto g) { count(maxima[g]); });
@@ -645,7 +738,7 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
       if (pair < 0) continue;
       const int bin = before + s.count[2 * pair] >= static_cast<u64>(k) ? 2 * pair : 2 * pair + 1;
       if (bin == kBins - 1) continue;
-      const int n = list_from(in, win.low(bin), s);
+      const int n = list_from(in, weight.low(bin), s);
       if (n > kList) continue;
       finish_list(a, row, n, cut, floor, uniform, weight, s);
       return Fast::kDrawn;
@@ -653,8 +746,7 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
     return Fast::kNot;
   }
 
-  // top-p alone: bins of 1 / 32 of a power. Adding up by bins in LDS costs a tenth of the pass.
-  const Window win{top, rate, kBins / 64.f};
+  // top-p alone. Adding up by bins in LDS costs a tenth of the pass.
   for (int i = tid; i < kBins; i += kThreads) {
     s.mass[i] = 0;
     s.count[i] = 0;
@@ -663,11 +755,11 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
   __syncthreads();
   u64 below = 0;
   in.each([&](int, float x) {
-    const u64 w = weight.fixed(x);
-    const float d = win.at(x);
-    if (d < kBins) {
-      atomicAdd(&s.count[static_cast<int>(d)], 1u);
-      atomicAdd(&s.mass[static_cast<int>(d)], w);
+    int m;
+    const u64 w = weight.fixed(x, &m);
+    if (-m < kBins) {
+      atomicAdd(&s.count[-m], 1u);
+      atomicAdd(&s.mass[-m], w);
     } else {
       below += w;
     }
@@ -691,12 +783,11 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
   const u64 count_before = s.other_before;
   cut.skip = s.found_before;
   const uint32_t in_bin = s.count[bin];
-  const float end = static_cast<float>(bin + 1), begin = static_cast<float>(bin);
   if (count_before + in_bin <= kList) {
     // all up to the bin's end
     cut.skip = 0;
-    in.from(win.low(bin), [&](int index, float x) {
-      if (win.at(x) < end) put(index, x, s);
+    in.from(weight.low(bin), [&](int index, float x) {
+      if (weight.bin(x) <= bin) put(index, x, s);
     });
     __syncthreads();
     finish_list(a, row, min(s.listed, kList), cut, floor, uniform, weight, s);
@@ -706,32 +797,56 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
   // the bin alone, and sums of what is above it
   u64 v = 0;
   in.each([&](int index, float x) {
-    const float d = win.at(x);
-    if (!(d < end)) return;
-    if (d >= begin) put(index, x, s);
-    else v += weight.fixed_from(x, floor);
+    int m;
+    const u64 w = weight.fixed(x, &m);
+    v += -m < bin && w >= floor ? w : 0;
+    if (-m == bin) put(index, x, s);
   }, [&](int turn) {
     set_piece(turn, v, s);
     v = 0;
   });
   __syncthreads();
   u64 place[2], w[2];
-  const int keep = cut_list<false>(min(s.listed, kList), cut, weight, s, place, w);
+  const int keep = cut_list(min(s.listed, kList), cut, weight, s, place, w);
   times<2>([&](auto i) {
-    if (2 * tid + i < keep && (floor <= 0.0 || weight(logit_at(place[i])) >= floor))
+    if (list_pos(i) < keep && w[i] >= floor)
       atomicAdd(&s.piece[(index_at(place[i]) + in.shift) / (64 * R::VEC)], w[i]);
   });
-  *last = s.list[keep - 1];
+  times<2>([&](auto i) {
+    if (list_pos(i) == keep - 1) s.found_before = place[i];
+  });
+  __syncthreads();
+  *last = s.found_before;
   __syncthreads();
   return Fast::kPieces;
+}
+
+// The row of a workgroup. More rows than there are compute units start one after another, and those
+// that compute something for every element (no top-k) take up to five times as long as the others: they
+// go first (512 rows of 128000, a third of them such: 140 us in the order they come).
+__device__ __forceinline__ int row_of_block(const Rows& a, Lds& s) {
+  const int b = blockIdx.x, rows = gridDim.x;
+  if (rows <= 256 || rows > kThreads || !a.top_k) return b;
+  const int t = threadIdx.x;
+  bool slow = false;
+  if (t < rows) {
+    const int k = a.top_k[t];
+    slow = (k <= 0 || k >= a.vocab) && (!a.temperature || a.temperature[t] > 0.f);
+  }
+  u64 count;
+  const u64 upto = block_upto<1>(slow, s, &count);
+  const int place = static_cast<int>(slow ? upto - 1 : count + t - upto);
+  if (t < rows && place == b) s.found = t;
+  __syncthreads();
+  return s.found;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void sample_kernel(Rows a) {
   __shared__ Lds s;
   typedef Row<F32> R;
-  const int row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row = row_of_block(a, s);
   const float temperature = a.temperature ? a.temperature[row] : 1.f;
   int k = a.top_k ? a.top_k[row] : 0;
   float p = a.top_p ? a.top_p[row] : 1.f;
@@ -740,6 +855,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows a) {
   const double uniform = a.uniform[row];
   const R in(a, row);
 
+  if (tid < kPowers) s.powers[tid] = static_cast<u64>(__double_as_longlong(exp2(static_cast<double>(tid) / kPowers)));
   float maxima[4];
   in.maxima(maxima);
   float top = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
@@ -775,11 +891,12 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows a) {
   if (endless) top = 1.f;
   const auto as = [endless](float x) { return !endless ? x : x == INFINITY ? 1.f : -INFINITY; };
 
-  const Weight weight(top, temperature, a.fixed);
-  const double floor = min_p > 0.f ? fmin(static_cast<double>(min_p), 1.0) : 0.0;
+  const Weight weight(top, temperature, a.fixed, s.powers);
+  // min-p as the least weight (what rounds to it is kept)
+  const u64 floor = min_p > 0.f ? static_cast<u64>(__builtin_rint(fmin(static_cast<double>(min_p), 1.0) * weight.unit)) : 0;
   u64 last = 0;                 // elements at or before this place are kept: all
   // sums of what is kept, by piece
-  const auto sum_up = [&](const auto& r, double least) {
+  const auto sum_up = [&](const auto& r, u64 least) {
     __syncthreads();
     u64 v = 0;
     r.each([&](int index, float x) {
@@ -807,7 +924,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows a) {
       u64 taken = ~0ull, taken_p;
       if (k > 0) last = descend<false>(in, as, weight, static_cast<u64>(k), 0, s, &taken);
       if (p < 1.f) {
-        sum_up(in, 0.0);
+        sum_up(in, 0);
         const u64 by_p = descend<true>(in, as, weight, share_of(p, total()), last, s, &taken_p);
         if (taken_p < taken) last = by_p;
       }
