@@ -2,19 +2,22 @@
 // the GPU.
 //
 // The n rows of a request and the G query heads of a KV head make n G query vectors
-// that share one K/V stream: they are the columns of the products, 16 T of them in a
-// work item, and the stream is cut into spans of keys. Per wave and step of two
-// 16-token blocks (32 keys), with lane l = 16 g + j:
+// that share one K/V stream: they are the columns of the products, and the stream is cut
+// into spans of keys. A wave takes 32 columns (kTiles tiles of 16). The four waves of a workgroup
+// share out 32, 64 or 128 columns (`wide` = 1, 2 or 4 groups of them) and the span's steps: with
+// more columns fewer waves share the steps, and those with other columns find K and V in
+// the caches. Per wave and step of two 16-token blocks (32 keys), with lane l = 16 g + j:
 //   S^T[16 keys][16 columns] = K Q^T, D / 32 MFMAs 16x16x32 for each block and
-//     16 columns. Lane l brings token j of the block and eight dims a step, the same
+//     tile. Lane l brings token j of the block and eight dims a step, the same
 //     eight of K and Q.
 //   The result gives lane l column j and keys 4g .. 4g + 3 of each block, which is the
 //   B operand of a 16x16x32 MFMA over the 32 keys (slots 0 .. 3 of lane group g the
 //   first block's, 4 .. 7 the second's): probabilities go on without any exchange.
 //   O^T[D dims][16 columns] += V^T P^T, D / 16 MFMAs for 16 columns: row m of MFMA b is dim
 //     (D / 16) m + b, so that a lane loads neighbouring dims of its tokens and regroups them.
-// K and V operands are made once a step and used for all T column tiles. A workgroup's
-// four waves take steps in turn and are merged through LDS; spans are merged by a second launch.
+// K and V operands are made once a step and used for both tiles (for four, which a wave has
+// registers for only alone on its SIMD, half the rate). Waves with the same columns are
+// merged through LDS, spans by a second launch.
 //
 // fp32 caches: the same with 16x16x4 fp32 MFMAs, one block a step.
 
@@ -26,6 +29,8 @@
 
 namespace {
 
+constexpr int kTiles = 2;              // of 16 columns, of a wave
+constexpr int kTreeWaves = 4;
 constexpr int kTreeUnit = 128;         // keys: one step of four waves
 constexpr int kTreeTarget = 1024;      // work items that a plan aims at
 constexpr int kTreeMinSpan = 2;        // units
@@ -39,25 +44,25 @@ struct TreeHeader {                    // 64 bytes
 struct TreeItem {                      // 32 bytes
   int32_t req;
   int16_t kvh;
-  int16_t tile;                        // of 16 T columns
+  int8_t tile;                         // of 32 * wide columns
+  int8_t wide;
   int32_t key_begin, key_end;
   int32_t q_row0, n_rows;              // of the request
   int32_t kv_len;
-  int32_t part;                        // partial result, -1: the only span
+  int32_t part;                        // first of `wide` partial results, -1: the only span
 };
 struct TreeGroup {                     // 32 bytes: one item's columns over all spans
   int32_t q_row0, n_rows;
   int16_t kvh;
-  int16_t tile;
-  int32_t part0, n_parts;
+  int8_t tile;
+  int8_t wide;
+  int32_t part0, n_parts;              // those of a span follow those of the one before
   int32_t reserved[3];
 };
 static_assert(sizeof(TreeHeader) == 64 && sizeof(TreeItem) == 32 && sizeof(TreeGroup) == 32, "plan layout");
 
 // What follows from a shape and the limits of a batch, on the host.
 struct TreeSizes {
-  int32_t tiles_per_item;              // T
-  int32_t max_tiles;                   // items for the columns of one request and KV head
   int64_t items, groups, parts;        // at most
   int64_t plan_bytes, workspace_bytes;
 };
@@ -67,7 +72,7 @@ struct TreePlanArgs {
   const int32_t* kv_len;
   char* plan;
   int64_t items;                       // places for items: groups follow them
-  int32_t num_reqs, max_rows, max_blocks, max_draft, hkv, group, columns;   // columns of an item: 16 T
+  int32_t num_reqs, max_rows, max_blocks, max_draft, hkv, group;
 };
 
 // Sum of v over the threads before this one.
@@ -92,11 +97,14 @@ __device__ __forceinline__ T sum_before(T v, T* waves, T* total) {
   return before;
 }
 
-// One workgroup: spans of equal length for all requests, long enough that about
-// kTreeTarget items come out. With L units of keys, c the span and items = sum of
-// tiles x KV heads x ceil(L / c), c >= sum(tiles x KV heads x L) / kTreeTarget gives at most
+// Groups of 32 columns that a workgroup takes, for a request's columns.
+__host__ __device__ __forceinline__ int wide_for(int columns) { return columns <= 32 ? 1 : columns <= 64 ? 2 : 4; }
+
+// One workgroup: spans that take equally long (keys x wide), long enough that about
+// kTreeTarget items come out. With L units of keys, c / wide the span and items = sum of
+// tiles x KV heads x ceil(L wide / c), c >= sum(tiles x KV heads x L x wide) / kTreeTarget gives at most
 // kTreeTarget + requests x KV heads x tiles items, and at most 2 kTreeTarget of requests that
-// are split (L > c, so ceil(L / c) < 2 L / c).
+// are split (L wide > c, so ceil(L wide / c) < 2 L wide / c).
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a) {
   extern __shared__ int32_t firsts[];                 // per request: first item, partial, group
   __shared__ unsigned long long waves64[kPlanThreads / 64];
@@ -105,14 +113,15 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
   int32_t* first_item = firsts;                       // [n + 1]
   int32_t* first_part = firsts + n + 1;
   int32_t* first_group = firsts + 2 * n + 1;
-  struct Req { int32_t q0, rows, keys, units, tiles; };
+  struct Req { int32_t q0, rows, keys, units, tiles, wide; };
   const auto request = [&](int r) {
     Req q;
     q.q0 = min(max(a.q_start[r], 0), a.max_rows);
     q.rows = min(max(a.q_start[r + 1] - q.q0, 0), min(a.max_draft, a.max_rows - q.q0));
     q.keys = static_cast<int32_t>(min(static_cast<int64_t>(max(a.kv_len[r], 0)), static_cast<int64_t>(a.max_blocks) * kBlock));
     q.units = (q.keys + kTreeUnit - 1) / kTreeUnit;
-    q.tiles = (q.rows * a.group + a.columns - 1) / a.columns;
+    q.wide = wide_for(q.rows * a.group);
+    q.tiles = (q.rows * a.group + 32 * q.wide - 1) / (32 * q.wide);
     return q;
   };
   const int per = (n + kPlanThreads - 1) / kPlanThreads;
@@ -121,13 +130,13 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
   unsigned long long work = 0, total;
   for (int r = r0; r < r1; ++r) {
     const Req q = request(r);
-    work += static_cast<unsigned long long>(q.units) * q.tiles * a.hkv;
+    work += static_cast<unsigned long long>(q.units) * q.tiles * q.wide * a.hkv;
   }
   sum_before(work, waves64, &total);
-  const int32_t span = max(kTreeMinSpan, static_cast<int32_t>((total + kTreeTarget - 1) / kTreeTarget));
+  const int32_t span = max(kTreeMinSpan, static_cast<int32_t>((total + kTreeTarget - 1) / kTreeTarget));   // x wide
   // spans of a request: as few as that length allows, evenly long
   const auto length_of = [&](const Req& q) {
-    const int s = max((q.units + span - 1) / span, 1);
+    const int s = max(static_cast<int>((static_cast<int64_t>(q.units) * q.wide + span - 1) / span), 1);
     return max((q.units + s - 1) / s, 1);
   };
   const auto spans_of = [&](const Req& q) { const int l = length_of(q); return max((q.units + l - 1) / l, 1); };
@@ -136,7 +145,7 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
     const Req q = request(r);
     const int s = spans_of(q), columns = q.tiles * a.hkv;
     items += columns * s;
-    parts += s > 1 ? columns * s : 0;
+    parts += s > 1 ? columns * q.wide * s : 0;
     groups += s > 1 ? columns : 0;
   }
   int32_t num_items, num_parts, num_groups;
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
     first_part[r] = part;
     first_group[r] = group;
     item += columns * s;
-    part += s > 1 ? columns * s : 0;
+    part += s > 1 ? columns * q.wide * s : 0;
     group += s > 1 ? columns : 0;
   }
   if (tid == 0) {
@@ -174,17 +183,18 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
     TreeItem it;
     it.req = lo;
     it.kvh = static_cast<int16_t>(kvh);
-    it.tile = static_cast<int16_t>(tile);
+    it.tile = static_cast<int8_t>(tile);
+    it.wide = static_cast<int8_t>(q.wide);
     it.key_begin = at * length;
     it.key_end = min(it.key_begin + length, q.keys);
     it.q_row0 = q.q0;
     it.n_rows = q.rows;
     it.kv_len = q.keys;
-    it.part = s > 1 ? first_part[lo] + column * s + at : -1;
+    it.part = s > 1 ? first_part[lo] + (column * s + at) * q.wide : -1;
     out[i] = it;
     if (s > 1 && at == 0)
       group_out[first_group[lo] + column] =
-          TreeGroup{q.q0, q.rows, it.kvh, it.tile, first_part[lo] + column * s, s, {}};
+          TreeGroup{q.q0, q.rows, it.kvh, it.tile, it.wide, it.part, s, {}};
   }
 }
 
@@ -312,10 +322,9 @@ template <> struct TreeKv<KV_FP4, 128> {
   }
 };
 
-constexpr int kTreeWaves = 4;
 constexpr int tree_row(int D) { return D + 4; }      // floats of a wave's result of one column in LDS
 constexpr int tree_merge_floats(int D) { return kTreeWaves * 16 * tree_row(D); }
-constexpr int64_t tree_partial_floats(int T, int D) { return int64_t{16} * T * (D + 2); }
+constexpr int64_t tree_partial_floats(int D) { return int64_t{16} * kTiles * (D + 2); }
 
 // A tile of 16 columns is written: out (bf16 or fp32), or its part of the item's partial.
 // Thread `tid` takes D / 16 dims of column tid / 16.
@@ -336,18 +345,17 @@ __device__ __forceinline__ void tree_store(const TreeArgs& a, int q_row0, int n_
   }
 }
 
-// The four waves' results of column tile t (lds: o[D], maximum and sum of each wave and
-// column) joined, and stored as the result or as the item's partial.
-template <int D, int T, bool F32>
-__device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it, int t, const float* lds, int tid) {
+// The results of tile t of a group's columns (lds: o[D], maximum and sum of each wave and
+// column) of the waves that have them, group, group + wide, ..., joined, and stored as the result or as
+// the item's partial.
+template <int D, bool F32>
+__device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it, int group, int t, const float* lds, int tid) {
   constexpr int ROW = tree_row(D), N = D / 16;
   const int c = tid >> 4, dim = N * (tid & 15);
   float m = kNegBig;
-#pragma unroll
-  for (int w = 0; w < kTreeWaves; ++w) m = fmaxf(m, lds[(w * 16 + c) * ROW + D]);
+  for (int w = group; w < kTreeWaves; w += it.wide) m = fmaxf(m, lds[(w * 16 + c) * ROW + D]);
   float l = 0.f, o[N] = {};
-#pragma unroll
-  for (int w = 0; w < kTreeWaves; ++w) {
+  for (int w = group; w < kTreeWaves; w += it.wide) {
     const float* p = lds + (w * 16 + c) * ROW;
     const float f = __builtin_amdgcn_exp2f(p[D] - m);
     l = fmaf(f, p[D + 1], l);
@@ -357,16 +365,16 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it,
   if (it.part < 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = over_sum(o[i], l);
-    tree_store<D, F32>(a, it.q_row0, it.n_rows, it.kvh, (it.tile * T + t) * 16 + c, dim, o);
+    tree_store<D, F32>(a, it.q_row0, it.n_rows, it.kvh, ((it.tile * it.wide + group) * kTiles + t) * 16 + c, dim, o);
     return;
   }
-  float* part = a.partials + it.part * tree_partial_floats(T, D);
+  float* part = a.partials + (it.part + group) * tree_partial_floats(D);
   float* dst = part + (16 * t + c) * D + dim;
 #pragma unroll
   for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(dst + i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
   if ((tid & 15) == 0) {
-    part[16 * T * D + 16 * t + c] = m;
-    part[16 * T * (D + 1) + 16 * t + c] = l;
+    part[16 * kTiles * D + 16 * t + c] = m;
+    part[16 * kTiles * (D + 1) + 16 * t + c] = l;
   }
 }
 
@@ -399,12 +407,12 @@ __device__ __forceinline__ uint64_t seen_by_any(uint64_t m) {
   return m;
 }
 
-template <int KVT, int D, int T>
-__global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
+template <int KVT, int D>
+__global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeArgs a) {
   using KV = TreeKv<KVT, D>;
-  constexpr int KS = D / 32, NB = D / 16;
+  constexpr int KS = D / 32, NB = D / 16, T = kTiles;
   constexpr bool FP8 = KVT == KV_FP8;
-  constexpr int kQuery = T * KS * 64;                  // 16-byte query operands
+  constexpr int kQuery = kTreeWaves * T * KS * 64;     // 16-byte query operands
   constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
   __shared__ __align__(16) char lds[kLds];
   if (static_cast<int>(blockIdx.x) >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items)) return;
@@ -413,22 +421,22 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int base = it.kv_len - it.n_rows;              // tokens before the drafts
 
+  // the wave's columns, and its share of the steps
+  const int group = wave & (it.wide - 1), turn = wave / it.wide, turns = kTreeWaves / it.wide;
+  const int columns = (it.n_rows << a.group_log2) - (it.tile * it.wide + group) * 16 * T;    // from the wave's first on
   uint64_t seen[T], any = 0;
-  uint4* query = reinterpret_cast<uint4*>(lds);
+  uint4* query = reinterpret_cast<uint4*>(lds) + wave * T * KS * 64;
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const TreeColumn c = tree_column(a, it, (it.tile * T + t) * 16 + j, D);
+    const TreeColumn c = tree_column(a, it, ((it.tile * it.wide + group) * T + t) * 16 + j, D);
     seen[t] = c.seen;
     any |= c.seen;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      if ((t * KS + s) % kTreeWaves != wave) continue;
+    for (int s = 0; s < KS; ++s)
       query[(t * KS + s) * 64 + lane] =
           c.live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + c.q + KV::k_dim(s, g)) : uint4{0u, 0u, 0u, 0u};
-    }
   }
   any = seen_by_any(any);
-  __syncthreads();
 
   const float sc = a.scale_log2;
   float m_run[T], l_run[T];
@@ -459,8 +467,9 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
       p.bid[i] = next[i];
       KV::load(a, static_cast<int64_t>(usable(next[i]) ? next[i] : 0) * a.hkv + it.kvh, j, g, p.b[i]);
     }
-    ids(bi + 2 * kTreeWaves);
+    ids(bi + 2 * turns);
   };
+  const bool both = columns > 16;                      // the second tile has columns
   const auto compute = [&](int bi, Pair& p) {
     const int tok0 = (blk0 + bi) * kBlock;
     const bool ok[2] = {usable(p.bid[0]), usable(p.bid[1])};
@@ -485,6 +494,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
       const bf16x8_t k0 = as_bf16x8(KV::k_operand(p.b[0], s)), k1 = as_bf16x8(KV::k_operand(p.b[1], s));
 #pragma unroll
       for (int t = 0; t < T; ++t) {
+        if (t > 0 && !both) continue;
         const bf16x8_t qop = as_bf16x8(query[(t * KS + s) * 64 + lane]);
         sacc[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qop, sacc[t][0], 0, 0, 0);
         sacc[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qop, sacc[t][1], 0, 0, 0);
@@ -503,6 +513,8 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
     bf16x8_t pop[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
+      pop[t] = bf16x8_t{};
+      if (t > 0 && !both) continue;
       float sv[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) sv[r] = sacc[t][r >> 2][r & 3] * (FP8 ? sc * p.b[r >> 2].ks : sc);
@@ -539,6 +551,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
       KV::v_operands(p.b[0], p.b[1], i, even, odd);
 #pragma unroll
       for (int t = 0; t < T; ++t) {
+        if (t > 0 && !both) continue;
         oacc[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pop[t], oacc[t][2 * i], 0, 0, 0);
         oacc[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), pop[t], oacc[t][2 * i + 1], 0, 0, 0);
       }
@@ -546,15 +559,16 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
   };
   // two pairs of blocks in turns: the loads of one are on their way while the other is computed
   Pair p0, p1;
-  int bi = 2 * wave;
+  const int step = 2 * turns;
+  int bi = columns > 0 ? 2 * turn : nblk;
   ids(bi);
   fetch(bi, p0);
-  for (; bi < nblk; bi += 4 * kTreeWaves) {
-    fetch(bi + 2 * kTreeWaves, p1);
+  for (; bi < nblk; bi += 2 * step) {
+    fetch(bi + step, p1);
     compute(bi, p0);
-    if (bi + 2 * kTreeWaves >= nblk) break;
-    fetch(bi + 4 * kTreeWaves, p0);
-    compute(bi + 2 * kTreeWaves, p1);
+    if (bi + step >= nblk) break;
+    fetch(bi + 2 * step, p0);
+    compute(bi + step, p1);
   }
 
   float* merge = reinterpret_cast<float*>(lds);
@@ -574,16 +588,16 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(TreeArgs a) {
       dst[D + 1] = l;
     }
     __syncthreads();
-    tree_join<D, T, false>(a, it, t, merge, threadIdx.x);
+    for (int g2 = 0; g2 < it.wide; ++g2) tree_join<D, false>(a, it, g2, t, merge, threadIdx.x);
   }
 }
 
 // fp32: one block a step, 16x16x4 MFMAs. Lane l brings four dims 16i + 4g .. of K and Q
 // a load, one of which a step takes; and of V tokens 4g .. 4g + 3, one a step.
-template <int D, int T>
-__global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
-  constexpr int KS = D / 16, NB = D / 16;
-  constexpr int kQuery = T * KS * 64;
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void tree_kernel_f32(TreeArgs a) {
+  constexpr int KS = D / 16, NB = D / 16, T = kTiles;
+  constexpr int kQuery = kTreeWaves * T * KS * 64;
   constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
   __shared__ __align__(16) char lds[kLds];
   if (static_cast<int>(blockIdx.x) >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items)) return;
@@ -592,22 +606,22 @@ __global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int base = it.kv_len - it.n_rows;
 
+  // the wave's columns, and its share of the steps
+  const int group = wave & (it.wide - 1), turn = wave / it.wide, turns = kTreeWaves / it.wide;
+  const int columns = (it.n_rows << a.group_log2) - (it.tile * it.wide + group) * 16 * T;    // from the wave's first on
   uint64_t seen[T], any = 0;
-  float4* query = reinterpret_cast<float4*>(lds);
+  float4* query = reinterpret_cast<float4*>(lds) + wave * T * KS * 64;
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const TreeColumn c = tree_column(a, it, (it.tile * T + t) * 16 + j, D);
+    const TreeColumn c = tree_column(a, it, ((it.tile * it.wide + group) * T + t) * 16 + j, D);
     seen[t] = c.seen;
     any |= c.seen;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      if ((t * KS + s) % kTreeWaves != wave) continue;
+    for (int s = 0; s < KS; ++s)
       query[(t * KS + s) * 64 + lane] =
           c.live ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + c.q + 16 * s + 4 * g) : float4{0.f, 0.f, 0.f, 0.f};
-    }
   }
   any = seen_by_any(any);
-  __syncthreads();
 
   float m_run[T], l_run[T];
   f32x4_t oacc[T][NB];
@@ -621,7 +635,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
   const int blk0 = it.key_begin / kBlock;
   const int nblk = (it.key_end - it.key_begin + kBlock - 1) / kBlock;
   const int32_t* table = a.block_table + static_cast<int64_t>(it.req) * a.max_blocks + blk0;
-  for (int bi = wave; bi < nblk; bi += kTreeWaves) {
+  for (int bi = columns > 0 ? turn : nblk; bi < nblk; bi += turns) {
     const int bid = load_uniform(table + bi);
     if (static_cast<uint32_t>(bid) >= static_cast<uint32_t>(a.num_pool_blocks)) continue;
     const int64_t cell = static_cast<int64_t>(bid) * a.hkv + it.kvh;
@@ -650,6 +664,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
     }
 #pragma unroll
     for (int t = 0; t < T; ++t) {
+      if (16 * t >= columns) break;
       f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -696,53 +711,56 @@ __global__ __launch_bounds__(kThreads) void tree_kernel_f32(TreeArgs a) {
       dst[D + 1] = l;
     }
     __syncthreads();
-    tree_join<D, T, true>(a, it, t, merge, threadIdx.x);
+    for (int g2 = 0; g2 < it.wide; ++g2) tree_join<D, true>(a, it, g2, t, merge, threadIdx.x);
   }
 }
 
 // The spans of 16 columns joined by log-sum-exp, in their order.
-template <int D, int T, bool F32>
+template <int D, bool F32>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeArgs a) {
-  constexpr int N = D / 16;
-  const int group = blockIdx.x / T, t = blockIdx.x % T;
-  if (group >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_groups)) return;
-  const TreeGroup gr = reinterpret_cast<const TreeGroup*>(a.plan + sizeof(TreeHeader) + a.items * sizeof(TreeItem))[group];
-  const int c = 16 * t + (threadIdx.x >> 4), dim = N * (threadIdx.x & 15);
-  const int column = gr.tile * 16 * T + c;
-  if ((column >> a.group_log2) >= gr.n_rows) return;
-  const float* part = a.partials + gr.part0 * tree_partial_floats(T, D);
-  float m = kNegBig, l = 0.f, o[N] = {};
-  constexpr int U = 4;
-  for (int s = 0; s < gr.n_parts; s += U) {
-    float ms[U], ls[U];
-    float4 x[U][N / 4];
+  constexpr int N = D / 16, kMost = 4 * kTiles;         // tiles of a group
+  const int groups = load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_groups);
+  for (int at = blockIdx.x; at < groups * kMost; at += gridDim.x) {
+    const int t = at % kMost;
+    const TreeGroup gr = reinterpret_cast<const TreeGroup*>(a.plan + sizeof(TreeHeader) + a.items * sizeof(TreeItem))[at / kMost];
+    const int c = 16 * (t % kTiles) + (threadIdx.x >> 4), dim = N * (threadIdx.x & 15);
+    const int column = (gr.tile * gr.wide * kTiles + t) * 16 + (threadIdx.x >> 4);
+    if (t >= gr.wide * kTiles || (column >> a.group_log2) >= gr.n_rows) continue;
+    const float* part = a.partials + (gr.part0 + t / kTiles) * tree_partial_floats(D);
+    const int64_t stride = gr.wide * tree_partial_floats(D);
+    float m = kNegBig, l = 0.f, o[N] = {};
+    constexpr int U = 4;
+    for (int s = 0; s < gr.n_parts; s += U) {
+      float ms[U], ls[U];
+      float4 x[U][N / 4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float* p = part + min(s + u, gr.n_parts - 1) * tree_partial_floats(T, D);
-      ms[u] = s + u < gr.n_parts ? p[16 * T * D + c] : kNegBig;
-      ls[u] = s + u < gr.n_parts ? p[16 * T * (D + 1) + c] : 0.f;
+      for (int u = 0; u < U; ++u) {
+        const float* p = part + min(s + u, gr.n_parts - 1) * stride;
+        ms[u] = s + u < gr.n_parts ? p[16 * kTiles * D + c] : kNegBig;
+        ls[u] = s + u < gr.n_parts ? p[16 * kTiles * (D + 1) + c] : 0.f;
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) x[u][i] = *reinterpret_cast<const float4*>(p + c * D + dim + 4 * i);
-    }
+        for (int i = 0; i < N / 4; ++i) x[u][i] = *reinterpret_cast<const float4*>(p + c * D + dim + 4 * i);
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u >= gr.n_parts) break;
-      const float mn = fmaxf(m, ms[u]);
-      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(ms[u] - mn);
-      l = l * f0 + ls[u] * f1;
-      m = mn;
+      for (int u = 0; u < U; ++u) {
+        if (s + u >= gr.n_parts) break;
+        const float mn = fmaxf(m, ms[u]);
+        const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(ms[u] - mn);
+        l = l * f0 + ls[u] * f1;
+        m = mn;
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        o[4 * i] = o[4 * i] * f0 + x[u][i].x * f1;
-        o[4 * i + 1] = o[4 * i + 1] * f0 + x[u][i].y * f1;
-        o[4 * i + 2] = o[4 * i + 2] * f0 + x[u][i].z * f1;
-        o[4 * i + 3] = o[4 * i + 3] * f0 + x[u][i].w * f1;
+        for (int i = 0; i < N / 4; ++i) {
+          o[4 * i] = o[4 * i] * f0 + x[u][i].x * f1;
+          o[4 * i + 1] = o[4 * i + 1] * f0 + x[u][i].y * f1;
+          o[4 * i + 2] = o[4 * i + 2] * f0 + x[u][i].z * f1;
+          o[4 * i + 3] = o[4 * i + 3] * f0 + x[u][i].w * f1;
+        }
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = over_sum(o[i], l);
-  tree_store<D, F32>(a, gr.q_row0, gr.n_rows, gr.kvh, column, dim, o);
+    for (int i = 0; i < N; ++i) o[i] = over_sum(o[i], l);
+    tree_store<D, F32>(a, gr.q_row0, gr.n_rows, gr.kvh, column, dim, o);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -758,35 +776,31 @@ aug_status tree_sizes(const char* who, const aug_attn_shape* s, const aug_tree_b
     return aug::fail(AUG_ERR_UNSUPPORTED, "%s: %d requests of up to %d blocks (supported: %d, %d)", who, b->num_reqs,
                      b->max_blocks, AUG_STEP_MAX_REQS, 1 << 20);
   const int columns = b->max_draft * (s->num_q_heads / s->num_kv_heads);
-  // columns of one item: all of them up to 64 (32 in fp32, whose K and V take twice the registers)
-  z->tiles_per_item = columns <= 16 ? 1 : columns <= 32 || s->kv_dtype == AUG_F32 ? 2 : 4;
-  z->max_tiles = (columns + 16 * z->tiles_per_item - 1) / (16 * z->tiles_per_item);
-  const int64_t whole = static_cast<int64_t>(b->num_reqs) * s->num_kv_heads * z->max_tiles;
+  // items that no split makes: a request's columns in tiles (of the widest that it can have, or of 32
+  // or 64 if they are fewer)
+  const int64_t whole = static_cast<int64_t>(b->num_reqs) * s->num_kv_heads * ((columns + 127) / 128);
   z->items = kTreeTarget + whole;
   z->groups = whole < kTreeTarget ? whole : kTreeTarget;
-  z->parts = z->items < 2 * kTreeTarget ? z->items : 2 * kTreeTarget;
+  const int64_t split = z->items < 2 * kTreeTarget ? z->items : 2 * kTreeTarget;
+  z->parts = split * wide_for(columns);
   if (z->items > (1 << 24))
     return aug::fail(AUG_ERR_UNSUPPORTED, "%s: up to %lld work items", who, (long long)z->items);
   z->plan_bytes = sizeof(TreeHeader) + z->items * sizeof(TreeItem) + z->groups * sizeof(TreeGroup);
-  z->workspace_bytes = z->parts * tree_partial_floats(z->tiles_per_item, s->head_dim) * 4;
+  z->workspace_bytes = z->parts * tree_partial_floats(s->head_dim) * 4;
   return AUG_OK;
 }
 
-template <int D, int T>
-void launch_f32(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
-  hipLaunchKernelGGL((tree_kernel_f32<D, T>), dim3(z.items), dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL((tree_merge_kernel<D, T, true>), dim3(z.groups * T), dim3(kThreads), 0, st, a);
-}
-template <int KVT, int D, int T>
-void launch_tree(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
-  hipLaunchKernelGGL((tree_kernel<KVT, D, T>), dim3(z.items), dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL((tree_merge_kernel<D, T, false>), dim3(z.groups * T), dim3(kThreads), 0, st, a);
-}
 template <int KVT, int D>
-void launch_tiles(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
-  if (z.tiles_per_item == 1) launch_tree<KVT, D, 1>(a, z, st);
-  else if (z.tiles_per_item == 2) launch_tree<KVT, D, 2>(a, z, st);
-  else launch_tree<KVT, D, 4>(a, z, st);
+void launch_tree(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
+  const int64_t tiles = z.groups * 4 * kTiles;
+  const dim3 merge(static_cast<uint32_t>(tiles < 1024 ? tiles : 1024));
+  if constexpr (KVT == KV_F32) {
+    hipLaunchKernelGGL((tree_kernel_f32<D>), dim3(z.items), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((tree_merge_kernel<D, true>), merge, dim3(kThreads), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((tree_kernel<KVT, D>), dim3(z.items), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((tree_merge_kernel<D, false>), merge, dim3(kThreads), 0, st, a);
+  }
 }
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
@@ -815,7 +829,7 @@ extern "C" aug_status aug_tree_plan(const aug_attn_shape* s, const aug_tree_batc
   if (plan_bytes < static_cast<size_t>(z.plan_bytes))
     return aug::fail(AUG_ERR_NO_SPACE, "%s: plan %zu < %lld bytes", who, plan_bytes, (long long)z.plan_bytes);
   const TreePlanArgs a{b->q_start, b->kv_len, static_cast<char*>(plan_dev), z.items, b->num_reqs, b->max_rows, b->max_blocks,
-                       b->max_draft, s->num_kv_heads, s->num_q_heads / s->num_kv_heads, 16 * z.tiles_per_item};
+                       b->max_draft, s->num_kv_heads, s->num_q_heads / s->num_kv_heads};
   const uint32_t lds = (3u * b->num_reqs + 1) * sizeof(int32_t);
   hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(kPlanThreads), lds, static_cast<hipStream_t>(stream), a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess)
@@ -858,20 +872,12 @@ extern "C" aug_status aug_attn_tree(const aug_attn_shape* s, const aug_tree_batc
   a.group_log2 = __builtin_ctz(static_cast<unsigned>(s->num_q_heads / s->num_kv_heads));
   a.scale_log2 = s->softmax_scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (s->kv_dtype == AUG_F32) {
-    if (s->head_dim == 64 && z.tiles_per_item == 1) launch_f32<64, 1>(a, z, st);
-    else if (s->head_dim == 64) launch_f32<64, 2>(a, z, st);
-    else if (z.tiles_per_item == 1) launch_f32<128, 1>(a, z, st);
-    else launch_f32<128, 2>(a, z, st);
-  } else if (s->kv_dtype == AUG_BF16 && s->head_dim == 64) {
-    launch_tiles<KV_BF16, 64>(a, z, st);
-  } else if (s->kv_dtype == AUG_BF16) {
-    launch_tiles<KV_BF16, 128>(a, z, st);
-  } else if (s->kv_dtype == AUG_FP8_E4M3FN) {
-    launch_tiles<KV_FP8, 128>(a, z, st);
-  } else {
-    launch_tiles<KV_FP4, 128>(a, z, st);
-  }
+  if (s->kv_dtype == AUG_F32 && s->head_dim == 64) launch_tree<KV_F32, 64>(a, z, st);
+  else if (s->kv_dtype == AUG_F32) launch_tree<KV_F32, 128>(a, z, st);
+  else if (s->kv_dtype == AUG_BF16 && s->head_dim == 64) launch_tree<KV_BF16, 64>(a, z, st);
+  else if (s->kv_dtype == AUG_BF16) launch_tree<KV_BF16, 128>(a, z, st);
+  else if (s->kv_dtype == AUG_FP8_E4M3FN) launch_tree<KV_FP8, 128>(a, z, st);
+  else launch_tree<KV_FP4, 128>(a, z, st);
   if (hipError_t e = hipGetLastError(); e != hipSuccess)
     return aug::fail(AUG_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
   return AUG_OK;

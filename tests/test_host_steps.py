@@ -183,15 +183,17 @@ def _batch(**kw):
 
 
 def test_tree_sizes():
-    """Room for any lengths: the items of every request in one span and those of the splits; partials of 2048 split
-    items of 16, 32 or 64 columns."""
-    for draft, hq, kv, tiles, items in ((1, 8, "bf16", 1, 1024 + 8), (8, 8, "bf16", 2, 1024 + 8), (9, 8, "bf16", 4, 1024 + 8),
-                                        (64, 8, "bf16", 4, 1024 + 8 * 4), (64, 8, "f32", 2, 1024 + 8 * 8), (4, 8, "f32", 1, 1024 + 8)):
+    """Room for any lengths: the items of every request in one span (128 columns each at most) and those of the splits;
+    partials of 2048 split items of 32, 64 or 128 columns."""
+    for draft, hq, kv, tiles, columns in ((1, 8, "bf16", 1, 32), (8, 8, "bf16", 1, 32), (9, 8, "bf16", 1, 64), (17, 8, "f32", 1, 128),
+                                          (64, 8, "bf16", 2, 128), (64, 16, "bf16", 4, 128)):
         shape = _shape(kv, hq=hq)
         plan, workspace = aug.aug_tree_plan_size(shape, _batch(max_draft=draft))
-        groups = min(1024, items - 1024)
-        assert plan == 64 + 32 * items + 32 * groups
-        assert workspace == min(items, 2048) * 16 * tiles * 130 * 4
+        whole = 4 * 2 * tiles
+        assert plan == 64 + 32 * (1024 + whole) + 32 * whole
+        assert workspace == (1024 + whole) * columns * 130 * 4
+    plan, workspace = aug.aug_tree_plan_size(_shape(), _batch(num_reqs=4096, max_draft=1))
+    assert plan == 64 + 32 * (1024 + 8192) + 32 * 1024 and workspace == 2048 * 32 * 130 * 4
 
 
 @pytest.mark.parametrize("kw,status", [
