@@ -13,9 +13,15 @@
 //
 // fp8 caches share a scale per block, so there one wave takes all rows of a block, which
 // follow one another in the call, for one KV head and K or V, as the append of a planned
-// batch does; the wave of a row that is not the first of its block ends at once.
+// batch does. A wave looks for the blocks that begin among `window` rows: one where rows are
+// few, 16 where they are many (a wave a row, of which 15 of 16 end at once: 143 us below).
 //
-// HBM-bound: rows in, rows and cache out.
+// HBM-bound: rows in, rows and cache out. Two groups of heads have their loads on their
+// way at once, which leaves four waves a SIMD beside the fp8 part (four groups: 10 us more
+// below; rows and blocks in launches of their own, as much together). 8115 rows of 64/8
+// heads of 128 into an fp8 cache: 98 us, 316 MB; the rows alone take 57 us and the blocks 33,
+// as much instructions (angles, quotients, codes) as traffic. 1001 rows of 8 + 2 fp32 heads
+// in and out: 10 us.
 
 #include <hip/hip_runtime.h>
 
@@ -51,6 +57,7 @@ struct RopeArgs {
   int64_t num_slots;       // of the pool
   int32_t rows;
   int32_t shares;          // waves that share a row's heads
+  int32_t window;          // rows whose blocks a wave writes (fp8)
   int32_t rotary_dim;      // 0: nothing is rotated
   int32_t interleaved;
   float magnitude;
@@ -59,18 +66,25 @@ struct RopeArgs {
 
 struct Octet { float x[8]; };
 
+// An octet as it is in a row.
+template <bool F32> struct Raw { uint4 w[F32 ? 2 : 1]; };
 template <bool F32>
-__device__ __forceinline__ Octet load_octet(const char* p) {
-  Octet o;
+__device__ __forceinline__ Raw<F32> load_raw(const char* p) {
+  Raw<F32> r;
+  r.w[0] = reinterpret_cast<const uint4*>(p)[0];
+  if constexpr (F32) r.w[1] = reinterpret_cast<const uint4*>(p)[1];
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ Octet octet_of(const Raw<F32>& r) {
+  const uint4 w = r.w[0];
   if constexpr (F32) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    o = Octet{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    o = Octet{{aug::bf16_lo(w.x), aug::bf16_hi(w.x), aug::bf16_lo(w.y), aug::bf16_hi(w.y), aug::bf16_lo(w.z),
-               aug::bf16_hi(w.z), aug::bf16_lo(w.w), aug::bf16_hi(w.w)}};
+    const uint4 z = r.w[1];
+    return Octet{{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w), __uint_as_float(z.x),
+                  __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)}};
   }
-  return o;
+  return Octet{{aug::bf16_lo(w.x), aug::bf16_hi(w.x), aug::bf16_lo(w.y), aug::bf16_hi(w.y), aug::bf16_lo(w.z),
+                aug::bf16_hi(w.z), aug::bf16_lo(w.w), aug::bf16_hi(w.w)}};
 }
 
 // Rows are rounded to their type here, once.
@@ -106,10 +120,15 @@ __device__ __forceinline__ void sin_cos_turns(double t, float* s, float* c) {
   *c = (k + 1) & 2 ? -w : w;
 }
 
+__device__ __forceinline__ int partner_of(const RopeArgs& a, int octet) {
+  const int half = a.rotary_dim / 16;              // octets
+  return a.interleaved || octet >= 2 * half ? 0 : octet >= half ? -half : half;
+}
+
 __device__ __forceinline__ Angles angles_of(const RopeArgs& a, int position, int octet) {
   Angles g;
   g.turn = 8 * octet < a.rotary_dim;
-  g.partner = 0;
+  g.partner = partner_of(a, octet);
   if (!g.turn) return g;
   const double pos = position;
   if (a.interleaved) {
@@ -124,7 +143,6 @@ __device__ __forceinline__ Angles angles_of(const RopeArgs& a, int position, int
   } else {
     const int half = a.rotary_dim / 16;            // octets
     const bool second = octet >= half;
-    g.partner = second ? -half : half;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float s, c;
@@ -136,15 +154,13 @@ __device__ __forceinline__ Angles angles_of(const RopeArgs& a, int position, int
   return g;
 }
 
-// An octet of a row at p, turned.
+// An octet turned; `y` is the one it is paired with, or itself.
 template <bool F32>
-__device__ __forceinline__ Octet turned(const Angles& g, const char* p) {
-  Octet o = load_octet<F32>(p);
-  if (!g.turn) return o;
-  Octet other;
-  if (g.partner != 0) {
-    other = load_octet<F32>(p + g.partner * (F32 ? 32 : 16));
-  } else {
+__device__ __forceinline__ Octet turned(const Angles& g, bool turn, const Raw<F32>& x, const Raw<F32>& y) {
+  Octet o = octet_of<F32>(x);
+  if (!g.turn || !turn) return o;
+  Octet other = octet_of<F32>(y);
+  if (g.partner == 0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) other.x[i] = o.x[i ^ 1];
   }
@@ -159,6 +175,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   constexpr int OCTETS = D / 8;              // lanes of a head
   constexpr int HEADS = 64 / OCTETS;         // of a wave at a time
   constexpr int EB = F32 ? 4 : 2;
+  constexpr int U = 2;
   const int lane = threadIdx.x & 63;
   const int octet = lane % OCTETS, sub = lane / OCTETS;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -181,20 +198,43 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
       block = slot / kBlock;
       t = static_cast<int>(slot % kBlock);
     }
-    for (int i = share; i < groups; i += a.shares) {
-      const bool is_q = i < nq, is_v = i >= nq + nk;
-      const Rows& r = is_q ? a.q : is_v ? a.v : a.k;
-      const int head = (i - (is_q ? 0 : is_v ? nq + nk : nq)) * HEADS + sub;
-      if (head >= r.heads) continue;
-      const char* p = r.in + row * r.in_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB;
-      const Octet o = turned<F32>(is_v ? still : g, p);
-      if (is_q || KV < 0) {
-        store_octet<F32>(r.out + row * r.out_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB, o);
-      } else if (ok) {
-        if constexpr (KV == AUG_MXFP4)
-          aug::store_fp4_octet(r.out + block * r.heads * aug::kMxCell, r.heads, head, is_v, t, octet, o.x);
-        else if constexpr (KV >= 0)
-          store_octet<F32>(r.out + (((block * r.heads + head) * kBlock + t) * D + 8 * octet) * EB, o);
+    // the loads of U groups, then their stores: a group's own loads are before its stores, also in place
+    for (int first = share; first < groups; first += U * a.shares) {
+      Raw<F32> x[U], y[U];
+      const auto of = [&](int u, bool& is_q, bool& is_v, int& head) -> const Rows& {
+        const int i = first + u * a.shares;
+        is_q = i < nq;
+        is_v = i >= nq + nk;
+        const Rows& r = is_q ? a.q : is_v ? a.v : a.k;
+        head = i < groups ? (i - (is_q ? 0 : is_v ? nq + nk : nq)) * HEADS + sub : r.heads;
+        return r;
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        bool is_q, is_v;
+        int head;
+        const Rows& r = of(u, is_q, is_v, head);
+        if (head >= r.heads) continue;
+        const char* p = r.in + row * r.in_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB;
+        x[u] = load_raw<F32>(p);
+        y[u] = x[u];
+        if (g.partner != 0 && !is_v) y[u] = load_raw<F32>(p + g.partner * (8 * EB));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        bool is_q, is_v;
+        int head;
+        const Rows& r = of(u, is_q, is_v, head);
+        if (head >= r.heads) continue;
+        const Octet o = turned<F32>(g, !is_v, x[u], y[u]);
+        if (is_q || KV < 0) {
+          store_octet<F32>(r.out + row * r.out_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB, o);
+        } else if (ok) {
+          if constexpr (KV == AUG_MXFP4)
+            aug::store_fp4_octet(r.out + block * r.heads * aug::kMxCell, r.heads, head, is_v, t, octet, o.x);
+          else if constexpr (KV >= 0)
+            store_octet<F32>(r.out + (((block * r.heads + head) * kBlock + t) * D + 8 * octet) * EB, o);
+        }
       }
     }
     return;
@@ -202,52 +242,69 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
 
   if constexpr (KV == AUG_FP8_E4M3FN) {
     const int64_t u = unit - row_units;
-    const int hkv = a.k.heads;
-    if (u >= static_cast<int64_t>(a.rows) * hkv * 2) return;
-    const int row = static_cast<int>(u / (2 * hkv));
+    const int hkv = a.k.heads, windows = (a.rows + a.window - 1) / a.window;
+    if (u >= static_cast<int64_t>(windows) * hkv * 2) return;
+    const int row0 = static_cast<int>(u / (2 * hkv)) * a.window;
     const int head = static_cast<int>((u >> 1) % hkv);
     const bool is_v = u & 1;
-    const int64_t slot = a.slots[row];
-    if (static_cast<uint64_t>(slot) >= static_cast<uint64_t>(a.num_slots)) return;
-    const int64_t block = slot / kBlock;
     const auto in_pool = [&](int64_t x) { return static_cast<uint64_t>(x) < static_cast<uint64_t>(a.num_slots); };
-    // the row before, of those that go anywhere: if it is of this block, its wave or an earlier one has this row too
-    for (int at = row - 1; at >= 0; at -= 64) {
+    const int64_t mine = lane < a.window && row0 + lane < a.rows ? a.slots[row0 + lane] : -1;
+    uint64_t live = __ballot(in_pool(mine));
+    if (live == 0) return;
+    // the block of the last row before these that goes anywhere: rows of it here are written with that one
+    int64_t done = -1;
+    for (int at = row0 - 1; at >= 0; at -= 64) {
       const int64_t x = at - lane >= 0 ? a.slots[at - lane] : -1;
       const uint64_t some = __ballot(in_pool(x));
       if (some == 0) continue;
-      if (__ballot(in_pool(x) && x / kBlock == block) >> (__ffsll(static_cast<unsigned long long>(some)) - 1) & 1) return;
+      done = __shfl(static_cast<long long>(x / kBlock), __ffsll(static_cast<unsigned long long>(some)) - 1);
       break;
     }
-    // the rows of the block: lane t has one more than how far behind `row` that of slot t is
-    int behind = 0;
-    for (int at = row; at < a.rows; at += 64) {
-      const int64_t x = at + lane < a.rows ? a.slots[at + lane] : -1;
-      const uint64_t here = __ballot(in_pool(x) && x / kBlock == block), others = __ballot(in_pool(x) && x / kBlock != block);
-      const uint64_t take = others ? here & ((others & -others) - 1) : here;      // up to the first of another block
-      int found = 0;
-      if ((take >> lane) & 1) found = at - row + lane + 1;
-      found = __builtin_amdgcn_ds_permute(4 * ((take >> lane) & 1 ? static_cast<int>(x % kBlock) : lane < 16 ? 63 : lane), found);
-      if (lane < kBlock && found) behind = found;
-      if (others) break;
-    }
-    const uint32_t tokens = static_cast<uint32_t>(__ballot(behind > 0));
-    const Rows& r = is_v ? a.v : a.k;
-    constexpr int PASSES = kBlock / HEADS;
-    Octet o[PASSES];
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int from = __shfl(behind, sub + p * HEADS);
-      o[p] = Octet{};
-      if (from) {
-        const int64_t i = static_cast<int64_t>(row) + from - 1;
-        const Angles g = a.rotary_dim && !is_v ? angles_of(a, a.positions[i], octet) : still;
-        o[p] = turned<F32>(g, r.in + i * r.in_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB);
+    for (; live; live &= live - 1) {
+      const int nth = __ffsll(static_cast<unsigned long long>(live)) - 1, row = row0 + nth;
+      const int64_t block = __shfl(static_cast<long long>(mine / kBlock), nth);
+      if (block == done) continue;
+      done = block;
+      // the rows of the block: lane t has one more than how far behind `row` that of slot t is
+      int behind = 0;
+      for (int at = row; at < a.rows; at += 64) {
+        const int64_t x = at + lane < a.rows ? a.slots[at + lane] : -1;
+        const uint64_t here = __ballot(in_pool(x) && x / kBlock == block), others = __ballot(in_pool(x) && x / kBlock != block);
+        const uint64_t take = others ? here & ((others & -others) - 1) : here;      // up to the first of another block
+        int found = 0;
+        if ((take >> lane) & 1) found = at - row + lane + 1;
+        found = __builtin_amdgcn_ds_permute(4 * ((take >> lane) & 1 ? static_cast<int>(x % kBlock) : lane < 16 ? 63 : lane), found);
+        if (lane < kBlock && found) behind = found;
+        if (others) break;
       }
+      const uint32_t tokens = static_cast<uint32_t>(__ballot(behind > 0));
+      const Rows& r = is_v ? a.v : a.k;
+      constexpr int PASSES = kBlock / HEADS;
+      const bool turn = a.rotary_dim && !is_v;
+      Raw<F32> x[PASSES], y[PASSES];
+      int position[PASSES];
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int from = __shfl(behind, sub + p * HEADS);
+        x[p] = y[p] = Raw<F32>{};
+        position[p] = 0;
+        if (from) {
+          const int64_t i = static_cast<int64_t>(row) + from - 1;
+          const char* src = r.in + i * r.in_stride + (static_cast<int64_t>(head) * D + 8 * octet) * EB;
+          x[p] = load_raw<F32>(src);
+          if (turn) {
+            position[p] = a.positions[i];
+            y[p] = load_raw<F32>(src + partner_of(a, octet) * (8 * EB));
+          }
+        }
+      }
+      Octet o[PASSES];
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) o[p] = turn ? turned<F32>(angles_of(a, position[p], octet), true, x[p], y[p]) : octet_of<F32>(x[p]);
+      const int64_t cell = block * hkv + head;
+      aug::store_fp8_tokens(reinterpret_cast<uint8_t*>(r.out) + cell * kBlock * D, a.scale[is_v] + cell, tokens, lane,
+                            [&](int p, int e) { return o[p].x[e]; });
     }
-    const int64_t cell = block * hkv + head;
-    aug::store_fp8_tokens(reinterpret_cast<uint8_t*>(r.out) + cell * kBlock * D, a.scale[is_v] + cell, tokens, lane,
-                          [&](int p, int e) { return o[p].x[e]; });
   }
 }
 
@@ -291,7 +348,11 @@ aug_status launch(const char* who, const aug_attn_shape* s, RopeArgs& a, void* s
   const int groups = KV == AUG_FP8_E4M3FN ? groups_of(a.q) : groups_of(a.q) + groups_of(a.k) + groups_of(a.v);
   a.shares = groups ? shares_of(a.rows, groups) : 0;
   int64_t units = static_cast<int64_t>(a.rows) * a.shares;
-  if (KV == AUG_FP8_E4M3FN) units += static_cast<int64_t>(a.rows) * a.k.heads * 2;
+  if (KV == AUG_FP8_E4M3FN) {
+    const int64_t most = static_cast<int64_t>(a.rows) * a.k.heads * 2 / 8192;
+    a.window = static_cast<int>(most < 1 ? 1 : most > kBlock ? kBlock : most);
+    units += static_cast<int64_t>((a.rows + a.window - 1) / a.window) * a.k.heads * 2;
+  }
   const int64_t grid = (units + kWaves - 1) / kWaves;
   if (grid > INT32_MAX) return aug::fail(AUG_ERR_UNSUPPORTED, "%s: %lld units", who, (long long)units);
   hipStream_t st = static_cast<hipStream_t>(stream);
