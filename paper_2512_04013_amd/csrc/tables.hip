@@ -8,10 +8,14 @@
 // for k < back it is the one that came back as k-th, read where its request held
 // it, so nothing that one workgroup writes is read by another.
 //
-// One launch: every workgroup makes all sums for itself (12 bytes a request, from L2)
-// and then writes its own requests' blocks and rows. What the sums were made from
+// One launch: every workgroup makes all sums for itself (12 bytes a request, from L2) and
+// then takes its share of the blocks that come back, of those that are taken, and of the
+// rows; whose a block or row is, is looked up in the sums. What the sums were made from
 // (held, free_count) is overwritten by the workgroup that finishes last, when all
 // others have read it.
+//
+// Bound by the chain of loads: lengths, sums, table or stack, stores. 64 requests of 8 drafts:
+// 6.1 us; 2000 of up to 32, 11.3 (with a workgroup a request, its rows behind its blocks: 42).
 
 #include <hip/hip_runtime.h>
 
@@ -25,34 +29,54 @@ namespace {
 
 using aug::kBlock;
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kEach = 4;               // requests of a thread, at most
+constexpr int kFew = 1024;             // requests up to which a workgroup has kFew / kEach threads
 
-// Sum of v over the threads before this one; *total over all of them. Two barriers.
-__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* waves, uint32_t* total) {
+// Sums of a and b over the threads before this one, in place; totals. Two barriers.
+template <int THREADS>
+__device__ __forceinline__ void sums_before(uint64_t& a, uint64_t& b, uint64_t* waves, uint64_t* a_total, uint64_t* b_total) {
+  constexpr int W = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t upto = v;
+  uint64_t x = a, y = b;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(upto, d);
-    if (lane >= d) upto += o;
+    const uint64_t ox = __shfl_up(static_cast<unsigned long long>(x), d), oy = __shfl_up(static_cast<unsigned long long>(y), d);
+    if (lane >= d) {
+      x += ox;
+      y += oy;
+    }
   }
   __syncthreads();
-  if (lane == 63) waves[wave] = upto;
+  if (lane == 63) {
+    waves[wave] = x;
+    waves[W + wave] = y;
+  }
   __syncthreads();
-  uint32_t before = upto - v, sum = 0;
+  a = x - a;
+  b = y - b;
+  *a_total = *b_total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += waves[w];
-    sum += waves[w];
+  for (int w = 0; w < W; ++w) {
+    if (w < wave) {
+      a += waves[w];
+      b += waves[W + w];
+    }
+    *a_total += waves[w];
+    *b_total += waves[W + w];
   }
-  *total = sum;
-  return before;
 }
 
-// Sums stay below 2^32: rows are cut to max_rows + 1 each and saturate, blocks are at most
-// 4096 * 2^20 - 1 (a request that asks for 2^20 of a table of 2^20 holds none).
-__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return a + b < a ? ~0u : a + b; }
+__device__ __forceinline__ uint32_t cut(uint64_t v) { return v > ~0u ? ~0u : static_cast<uint32_t>(v); }
+
+// The last of n ascending values that is not above x; values[0] is not.
+__device__ __forceinline__ int last_not_above(const uint32_t* values, int n, uint32_t x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (values[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
 
 struct Request {
   int32_t ctx, rows, held, need;
@@ -74,63 +98,56 @@ __device__ __forceinline__ Request load_request(const aug_step_tables_args& a, i
 }
 
 // LDS, per request: first row (cut to max_rows), blocks that came back before it,
-// blocks asked for up to and with it.
-__global__ __launch_bounds__(kThreads) void tables_kernel(aug_step_tables_args a) {
+// blocks asked for before it.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void tables_kernel(aug_step_tables_args a) {
   extern __shared__ uint32_t lds[];
-  __shared__ uint32_t waves[kWaves];
+  __shared__ uint64_t waves[2 * (THREADS / 64)];
   __shared__ int32_t last;
   const int n = a.num_reqs, tid = threadIdx.x;
   uint32_t* start = lds;              // [n + 1]
   uint32_t* back_before = lds + n + 1;
-  uint32_t* asked = lds + 2 * n + 1;
-  const int per = (n + kThreads - 1) / kThreads;
+  uint32_t* asked_before = lds + 2 * n + 1;
+  const int per = (n + THREADS - 1) / THREADS;
   const int r0 = min(tid * per, n), r1 = min(r0 + per, n);
   const uint32_t cap = static_cast<uint32_t>(a.max_rows);
   const int32_t count0 = min(max(*a.free_count, 0), a.num_pool_blocks);
 
-  uint32_t rows = 0;
-  for (int r = r0; r < r1; ++r) {
-    const uint32_t q = min(static_cast<uint32_t>(max(a.q_len[r], 0)), cap + 1);
-    rows = min(rows + q, cap + 1);   // at most 2^32 - 1, as cap < 2^31
+  Request mine[kEach];
+  uint64_t at = 0, unused = 0, rows_sum, unused_sum;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    mine[i] = r0 + i < r1 ? load_request(a, r0 + i) : Request{};
+    at += mine[i].rows;
   }
-  // 256 sums of up to 2^31 would not fit: they are scanned a half at a time
-  uint32_t high_total, low_total;
-  const uint32_t high = block_before(rows >> 16, waves, &high_total);
-  const uint32_t low = block_before(rows & 0xFFFFu, waves, &low_total);
-  const auto joined = [&](uint32_t h, uint32_t l) {
-    const uint64_t s = (static_cast<uint64_t>(h) << 16) + l;
-    return static_cast<uint32_t>(s > cap + 1ull ? cap + 1ull : s);
-  };
-  uint32_t at = joined(high, low);
-  const uint32_t rows_total = min(joined(high_total, low_total), cap);
-  uint32_t back = 0, ask = 0;
-  for (int r = r0; r < r1; ++r) {
-    const Request q = load_request(a, r);
-    start[r] = min(at, cap);
-    at = min(at + min(static_cast<uint32_t>(q.rows), cap + 1), cap + 1);
-    const bool valid = q.valid && start[r] + static_cast<uint32_t>(q.rows) <= cap;
-    back += valid ? max(q.held - q.need, 0) : 0;
-    ask = add_sat(ask, valid ? max(q.need - q.held, 0) : 0);
+  sums_before<THREADS>(at, unused, waves, &rows_sum, &unused_sum);
+  const int32_t rows_total = static_cast<int32_t>(rows_sum < cap ? rows_sum : cap);
+  uint64_t back = 0, ask = 0, back_sum, ask_sum;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (r0 + i >= r1) break;
+    const uint32_t first = static_cast<uint32_t>(at < cap ? at : cap);
+    start[r0 + i] = first;
+    at += mine[i].rows;
+    mine[i].valid = mine[i].valid && static_cast<uint64_t>(first) + mine[i].rows <= cap;
+    back += mine[i].valid ? max(mine[i].held - mine[i].need, 0) : 0;
+    ask += mine[i].valid ? max(mine[i].need - mine[i].held, 0) : 0;
   }
   if (tid == 0) start[n] = rows_total;
-  uint32_t back_total, ask_high, ask_low;
-  uint32_t b = block_before(back, waves, &back_total);
-  const uint32_t ah = block_before(ask >> 16, waves, &ask_high);
-  const uint32_t al = block_before(ask & 0xFFFFu, waves, &ask_low);
-  const uint64_t before = (static_cast<uint64_t>(ah) << 16) + al;
-  uint32_t k = before > ~0u ? ~0u : static_cast<uint32_t>(before);
+  sums_before<THREADS>(back, ask, waves, &back_sum, &ask_sum);
+  const uint32_t back_total = cut(back_sum);
   // blocks on the stack once all have come back
-  const uint32_t avail = min(static_cast<uint32_t>(count0) + back_total, static_cast<uint32_t>(a.num_pool_blocks));
+  const uint32_t avail = static_cast<uint32_t>(min(count0 + back_sum, static_cast<uint64_t>(a.num_pool_blocks)));
   uint32_t taken = 0;
-  for (int r = r0; r < r1; ++r) {
-    const Request q = load_request(a, r);
-    const bool valid = q.valid && start[r] + static_cast<uint32_t>(q.rows) <= cap;
-    back_before[r] = b;
-    b += valid ? max(q.held - q.need, 0) : 0;
-    const uint32_t take = valid ? max(q.need - q.held, 0) : 0;
-    k = add_sat(k, take);
-    asked[r] = k;
-    if (take > 0 && k <= avail) taken = k;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (r0 + i >= r1) break;
+    back_before[r0 + i] = cut(back);
+    asked_before[r0 + i] = cut(ask);
+    back += mine[i].valid ? max(mine[i].held - mine[i].need, 0) : 0;
+    const uint32_t take = mine[i].valid ? max(mine[i].need - mine[i].held, 0) : 0;
+    ask += take;
+    if (take > 0 && ask <= avail) taken = static_cast<uint32_t>(ask);
   }
   // the last request that got blocks got all that were asked for up to it
 #pragma unroll
@@ -139,84 +156,98 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(aug_step_tables_args a
   if ((tid & 63) == 0) waves[tid >> 6] = taken;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) taken = max(taken, waves[w]);
+  for (int w = 0; w < THREADS / 64; ++w) taken = max(taken, static_cast<uint32_t>(waves[w]));
 
   const auto outcome = [&](int r, const Request& q) {
-    if (!q.valid || start[r] + static_cast<uint32_t>(q.rows) > cap) return AUG_STEP_INVALID;
-    return q.need > q.held && asked[r] > avail ? AUG_STEP_NO_BLOCKS : AUG_STEP_OK;
+    if (!q.valid || static_cast<uint64_t>(start[r]) + q.rows > cap) return AUG_STEP_INVALID;
+    return q.need > q.held && static_cast<uint64_t>(asked_before[r]) + (q.need - q.held) > avail ? AUG_STEP_NO_BLOCKS : AUG_STEP_OK;
+  };
+  const auto table_of = [&](int r) { return a.block_table + static_cast<int64_t>(r) * a.max_blocks; };
+  const auto place_of = [&](uint32_t nth) { return static_cast<int64_t>(count0) + back_total - 1 - nth; };
+  const auto in_stack = [&](int64_t place) { return place >= 0 && place < a.num_pool_blocks; };
+  // the block that came back as nth
+  const auto given = [&](uint32_t nth) {
+    const int r = last_not_above(back_before, n, nth);
+    const int64_t col = static_cast<int64_t>(load_request(a, r).need) + (nth - back_before[r]);
+    return col < a.max_blocks ? table_of(r)[col] : -1;
+  };
+  // the block that is taken as nth
+  const auto block = [&](uint32_t nth) {
+    if (nth < back_total) return given(nth);
+    const int64_t place = place_of(nth);
+    return in_stack(place) ? a.free_ids[place] : -1;
+  };
+  // the block of a column that the request has from now on
+  const auto column = [&](int r, const Request& q, int64_t col) {
+    return col < q.held ? table_of(r)[col] : block(asked_before[r] + static_cast<uint32_t>(col - q.held));
   };
 
-  for (int r = blockIdx.x; r < n; r += gridDim.x) {
+  const uint32_t threads = gridDim.x * THREADS, thread = blockIdx.x * THREADS + tid;
+  for (uint64_t nth = thread; nth < back_total; nth += threads) {
+    const int64_t place = place_of(static_cast<uint32_t>(nth));
+    if (in_stack(place)) a.free_ids[place] = given(static_cast<uint32_t>(nth));
+  }
+  for (uint64_t nth = thread; nth < taken; nth += threads) {
+    const int r = last_not_above(asked_before, n, static_cast<uint32_t>(nth));
+    const int64_t col = static_cast<int64_t>(a.held[r]) + static_cast<uint32_t>(nth - asked_before[r]);
+    if (col < a.max_blocks) table_of(r)[col] = block(static_cast<uint32_t>(nth));
+  }
+  for (uint32_t r = thread; r < static_cast<uint32_t>(n); r += threads) {
     const Request q = load_request(a, r);
     const aug_step_state st = outcome(r, q);
-    int32_t* table = a.block_table + static_cast<int64_t>(r) * a.max_blocks;
-    if (st == AUG_STEP_OK) {
-      for (int j = q.need + tid; j < q.held; j += kThreads) {
-        const int64_t place = static_cast<int64_t>(count0) + back_total - 1 - (back_before[r] + (j - q.need));
-        if (place >= 0 && place < a.num_pool_blocks) a.free_ids[place] = table[j];
-      }
-      for (int j = q.held + tid; j < q.need; j += kThreads) {
-        const uint32_t nth = asked[r] - (q.need - q.held) + (j - q.held);
-        if (nth < back_total) {
-          // the request that gave it back: the last one with back_before <= nth that gave any
-          int lo = 0, hi = n - 1;
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (back_before[mid] <= nth) lo = mid; else hi = mid - 1;
-          }
-          const Request from = load_request(a, lo);
-          const int64_t col = static_cast<int64_t>(from.need) + (nth - back_before[lo]);
-          table[j] = col < a.max_blocks ? a.block_table[static_cast<int64_t>(lo) * a.max_blocks + col] : -1;
-        } else {
-          const int64_t place = static_cast<int64_t>(count0) + back_total - 1 - nth;
-          table[j] = place >= 0 && place < a.num_pool_blocks ? a.free_ids[place] : -1;
-        }
-      }
+    a.q_start[r] = static_cast<int32_t>(start[r]);
+    a.kv_len[r] = st == AUG_STEP_OK ? q.ctx + q.rows : 0;
+    a.state[r] = st;
+  }
+  if (thread == 0) a.q_start[n] = rows_total;
+
+  if (a.max_draft == 0) {
+    for (uint32_t i = thread; i < static_cast<uint32_t>(rows_total); i += threads) {
+      const int r = last_not_above(start, n, i);
+      const Request q = load_request(a, r);
+      const bool ok = outcome(r, q) == AUG_STEP_OK;
+      const int64_t token = static_cast<int64_t>(q.ctx) + (i - start[r]);
+      a.slots[i] = ok ? static_cast<int64_t>(column(r, q, token / kBlock)) * kBlock + token % kBlock : -1;
+      a.positions[i] = ok ? static_cast<int32_t>(token) : 0;
     }
-    const int32_t first = static_cast<int32_t>(start[r]), next = static_cast<int32_t>(start[r + 1]);
-    if (tid == 0) {
-      a.q_start[r] = first;
-      a.kv_len[r] = st == AUG_STEP_OK ? q.ctx + q.rows : 0;
-      a.state[r] = st;
-    }
-    __syncthreads();      // the table's new entries
-    const int rows_here = next - first;
-    for (int i = tid; i < rows_here; i += kThreads) {
-      const int64_t token = static_cast<int64_t>(q.ctx) + i;
-      a.slots[first + i] = st == AUG_STEP_OK ? static_cast<int64_t>(table[token / kBlock]) * kBlock + token % kBlock : -1;
-      if (a.max_draft == 0) a.positions[first + i] = st == AUG_STEP_OK ? q.ctx + i : 0;
-    }
-    if (a.max_draft > 0) {
-      if (st != AUG_STEP_OK) {
-        for (int i = tid; i < rows_here; i += kThreads) {
+  } else {
+    // a wave a request: lane i has its row i
+    const int lane = tid & 63;
+    for (int r = static_cast<int>(thread >> 6); r < n; r += static_cast<int>(threads >> 6)) {
+      const Request q = load_request(a, r);
+      const bool ok = outcome(r, q) == AUG_STEP_OK;
+      const int first = static_cast<int>(start[r]), rows = static_cast<int>(start[r + 1]) - first;
+      if (!ok) {                                       // may be more rows than a wave has lanes
+        for (int i = lane; i < rows; i += 64) {
+          a.slots[first + i] = -1;
           a.seen[first + i] = 0;
           a.positions[first + i] = 0;
         }
-      } else if (tid < 64) {
-        // Row `tid` sees itself and what its parent sees. Six rounds of looking twice as
-        // far up reach the root of any path of 64.
-        int up = tid - 1;
-        if (a.parents) up = tid < rows_here ? a.parents[first + tid] : -1;
-        if (up < 0 || up >= tid) up = -1;
-        uint64_t m = 1ull << tid;
+        continue;
+      }
+      // Row i sees itself and what its parent sees. Six rounds of looking twice as
+      // far up reach the root of any path of 64.
+      int up = lane - 1;
+      if (a.parents) up = lane < rows ? a.parents[first + lane] : -1;
+      if (up < 0 || up >= lane) up = -1;
+      uint64_t m = 1ull << lane;
 #pragma unroll
-        for (int d = 0; d < 6; ++d) {
-          const int from = max(up, 0);
-          const uint64_t om = static_cast<uint64_t>(__shfl(static_cast<unsigned long long>(m), from));
-          const int ou = __shfl(up, from);
-          if (up >= 0) {
-            m |= om;
-            up = ou;
-          }
-        }
-        if (tid < rows_here) {
-          a.seen[first + tid] = m;
-          a.positions[first + tid] = q.ctx + __popcll(m) - 1;
+      for (int d = 0; d < 6; ++d) {
+        const int from = max(up, 0);
+        const uint64_t om = static_cast<uint64_t>(__shfl(static_cast<unsigned long long>(m), from));
+        const int ou = __shfl(up, from);
+        if (up >= 0) {
+          m |= om;
+          up = ou;
         }
       }
+      if (lane >= rows) continue;
+      const int64_t token = static_cast<int64_t>(q.ctx) + lane;
+      a.slots[first + lane] = static_cast<int64_t>(column(r, q, token / kBlock)) * kBlock + token % kBlock;
+      a.seen[first + lane] = m;
+      a.positions[first + lane] = q.ctx + __popcll(m) - 1;
     }
   }
-  if (blockIdx.x == 0 && tid == 0) a.q_start[n] = static_cast<int32_t>(rows_total);
 
   __syncthreads();
   if (tid == 0) {
@@ -226,11 +257,20 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(aug_step_tables_args a
   }
   __syncthreads();
   if (!last) return;
-  for (int r = tid; r < n; r += kThreads) {
+  for (int r = tid; r < n; r += THREADS) {
     const Request q = load_request(a, r);
     if (outcome(r, q) == AUG_STEP_OK) a.held[r] = q.need;
   }
   if (tid == 0) *a.free_count = static_cast<int32_t>(avail - taken);
+}
+
+// Enough workgroups for a wave a request, or a thread a row, up to one a compute unit.
+template <int THREADS>
+void launch(const aug_step_tables_args& t, hipStream_t st) {
+  const int64_t threads = t.max_draft > 0 ? int64_t{64} * t.num_reqs : t.max_rows > t.num_reqs ? t.max_rows : t.num_reqs;
+  const int64_t groups = (threads + THREADS - 1) / THREADS;
+  const uint32_t lds = (3u * t.num_reqs + 1) * sizeof(uint32_t);
+  hipLaunchKernelGGL((tables_kernel<THREADS>), dim3(static_cast<uint32_t>(groups < 256 ? groups : 256)), dim3(THREADS), lds, st, t);
 }
 
 }  // namespace
@@ -255,9 +295,9 @@ extern "C" aug_status aug_step_tables(const aug_step_tables_args* t, void* strea
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   if (t->max_rows > 0 && (!t->positions || !t->slots || (t->max_draft > 0 && !t->seen)))
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
-  const uint32_t lds = (3u * t->num_reqs + 1) * sizeof(uint32_t);
-  const int grid = t->num_reqs < 1024 ? t->num_reqs : 1024;
-  hipLaunchKernelGGL(tables_kernel, dim3(grid), dim3(kThreads), lds, static_cast<hipStream_t>(stream), *t);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (t->num_reqs <= kFew) launch<kFew / kEach>(*t, st);
+  else launch<AUG_STEP_MAX_REQS / kEach>(*t, st);
   if (hipError_t e = hipGetLastError(); e != hipSuccess)
     return aug::fail(AUG_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
   return AUG_OK;
