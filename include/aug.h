@@ -484,7 +484,8 @@ typedef enum { AUG_STEP_OK = 0, AUG_STEP_NO_BLOCKS = 1, AUG_STEP_INVALID = 2 } a
  *   positions[row]  ctx_len + number of the row's ancestors (a child's position is one
  *                   more than its parent's)
  *   slots[row]      block * 16 + slot of the row's token, which is token ctx_len + j of
- *                   the request for its row j
+ *                   the request for its row j; -1 for the rows behind the last, so that
+ *                   an append of max_rows rows skips them
  *   seen[row]       bit j: row j of the request is the row itself or an ancestor
  *   scratch         AUG_STEP_SCRATCH_BYTES, zero before the first call; a call leaves it
  *                   zero. Calls that overlap need one each */
@@ -525,8 +526,8 @@ typedef struct {
  *                       0 .. max_blocks, more than max_draft rows, or rows beyond max_rows
  *                       (a row beyond is not written, and q_start goes no further)
  * Entries of block_table beyond a request's blocks, places of free_ids above its top
- * and rows behind the last are left as they were, except that blocks which came back
- * stand above the top where they were taken again at once. One launch (none for no requests).
+ * and positions and masks behind the last row are left as they were, except that blocks
+ * which came back stand above the top where they were taken again at once. One launch (none for no requests).
  * Errors: AUG_ERR_INVALID (NULL pointers, sizes), AUG_ERR_UNSUPPORTED (more requests or
  * blocks), AUG_ERR_HIP (launch). */
 aug_status aug_step_tables(const aug_step_tables_args* args, void* stream);

@@ -224,7 +224,7 @@ class StepTables:
         self.free_ids = torch.arange(self.num_pool_blocks, dtype=torch.int32, device=device) if free_ids is None else free_ids
         self.free_count = torch.full((1,), int(free_count), dtype=torch.int32, device=device)
         self.q_start, self.kv_len, self.state = zeros(self.max_reqs + 1), zeros(self.max_reqs), zeros(self.max_reqs)
-        self.positions, self.slots = zeros(self.max_rows), zeros(self.max_rows, dtype=torch.int64)
+        self.positions, self.slots = zeros(self.max_rows), zeros(self.max_rows, dtype=torch.int64).fill_(-1)
         self.seen = zeros(self.max_rows, dtype=torch.int64) if self.max_draft else None
         self._scratch = zeros(STEP_SCRATCH_BYTES, dtype=torch.uint8)
         self.device = self.q_start.device
