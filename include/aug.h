@@ -484,8 +484,7 @@ typedef enum { AUG_STEP_OK = 0, AUG_STEP_NO_BLOCKS = 1, AUG_STEP_INVALID = 2 } a
  *   positions[row]  ctx_len + number of the row's ancestors (a child's position is one
  *                   more than its parent's)
  *   slots[row]      block * 16 + slot of the row's token, which is token ctx_len + j of
- *                   the request for its row j; -1 for the rows behind the last, so that
- *                   an append of max_rows rows skips them
+ *                   the request for its row j
  *   seen[row]       bit j: row j of the request is the row itself or an ancestor
  *   scratch         AUG_STEP_SCRATCH_BYTES, zero before the first call; a call leaves it
  *                   zero. Calls that overlap need one each */
@@ -526,8 +525,8 @@ typedef struct {
  *                       0 .. max_blocks, more than max_draft rows, or rows beyond max_rows
  *                       (a row beyond is not written, and q_start goes no further)
  * Entries of block_table beyond a request's blocks, places of free_ids above its top
- * and positions and masks behind the last row are left as they were, except that blocks
- * which came back stand above the top where they were taken again at once. One launch (none for no requests).
+ * and rows behind the last are left as they were, except that blocks which came back
+ * stand above the top where they were taken again at once. One launch (none for no requests).
  * Errors: AUG_ERR_INVALID (NULL pointers, sizes), AUG_ERR_UNSUPPORTED (more requests or
  * blocks), AUG_ERR_HIP (launch). */
 aug_status aug_step_tables(const aug_step_tables_args* args, void* stream);
@@ -596,11 +595,14 @@ aug_status aug_rope_rows(const aug_attn_shape* shape, const aug_rope* rope, cons
  * follow one another in the call and in a block (each slot one more than the one before)
  * share the growth of its scale, from the scale's old value unless the first of them is slot 0;
  * the rows of one block must follow one another. Strides and alignment as for aug_rope_rows;
- * q_out may be q, and nothing else overlaps. One launch (none for no rows).
+ * q_out may be q, and nothing else overlaps. live_rows (device, or NULL): how many of the rows
+ * there are, the others are passed over: a captured step passes its largest number of rows and
+ * q_start + num_reqs of aug_step_tables, since the slots behind a step's last row are those of
+ * an earlier step. One launch (none for no rows).
  * Errors: those of aug_rope_rows and aug_kv_append. */
 aug_status aug_rope_append(const aug_attn_shape* shape, const aug_rope* rope, const int32_t* positions,
-                           const int64_t* slots, int32_t rows, const void* q, int64_t q_stride, const void* k,
-                           int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                           const int64_t* slots, int32_t rows, const int32_t* live_rows, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
                            void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t num_pool_blocks,
                            void* stream);
 

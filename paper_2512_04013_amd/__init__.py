@@ -199,7 +199,7 @@ def lib():
     L.aug_step_tables.argtypes = [C.POINTER(aug_step_tables_args), P]
     L.aug_rope_init.argtypes = [C.POINTER(aug_rope_params), C.POINTER(aug_rope)]
     L.aug_rope_rows.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, C.c_int32] + [P, C.c_int64] * 4 + [P]
-    L.aug_rope_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, P, C.c_int32] + [P, C.c_int64] * 4 + \
+    L.aug_rope_append.argtypes = [C.POINTER(aug_attn_shape), C.POINTER(aug_rope), P, P, C.c_int32, P] + [P, C.c_int64] * 4 + \
         [P, P, P, P, C.c_int32, P]
     batch = [C.POINTER(aug_attn_shape), C.POINTER(aug_tree_batch)]
     L.aug_tree_plan_size.argtypes = batch + [C.POINTER(C.c_size_t)] * 2
@@ -490,13 +490,14 @@ def aug_rope_rows(shape: aug_attn_shape, rope: aug_rope, positions, q, k, q_out,
 
 
 def aug_rope_append(shape: aug_attn_shape, rope: Optional[aug_rope], positions, slots, q, k, v, q_out, k_cache, v_cache, k_scale,
-                    v_scale, num_pool_blocks: int, stream=None):
+                    v_scale, num_pool_blocks: int, live_rows=None, stream=None):
     """Enqueue the write of rows ``k`` (rotated by ``positions``) and ``v`` into
     ``slots`` (int64: block * 16 + slot) of the pool, and the rotation of ``q``
-    if it is given; without a rope nothing is rotated."""
+    if it is given; without a rope nothing is rotated. ``live_rows`` (int32 on the
+    device): how many of the rows there are."""
     st = _stream(stream, slots)
     _check(lib().aug_rope_append(C.byref(shape), None if rope is None else C.byref(rope), _ptr(positions), _ptr(slots), len(slots),
-                                 *_rows_arg(q), *_rows_arg(k), *_rows_arg(v), *_rows_arg(q_out), _ptr(k_cache), _ptr(v_cache),
+                                 _ptr(live_rows), *_rows_arg(q), *_rows_arg(k), *_rows_arg(v), *_rows_arg(q_out), _ptr(k_cache), _ptr(v_cache),
                                  _ptr(k_scale), _ptr(v_scale), int(num_pool_blocks), st), "aug_rope_append")
 
 

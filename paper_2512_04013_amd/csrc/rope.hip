@@ -54,6 +54,7 @@ struct RopeArgs {
   float* scale[2];         // of K and V (fp8)
   const int32_t* positions;
   const int64_t* slots;
+  const int32_t* live_rows;   // how many of `rows` there are, NULL: all
   int64_t num_slots;       // of the pool
   int32_t rows;
   int32_t shares;          // waves that share a row's heads
@@ -180,10 +181,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   const int octet = lane % OCTETS, sub = lane / OCTETS;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row_units = static_cast<int64_t>(a.rows) * a.shares;
+  const int rows = a.live_rows ? min(max(*a.live_rows, 0), a.rows) : a.rows;
   const Angles still{{}, {}, 0, false};
 
   if (unit < row_units) {
     const int row = static_cast<int>(unit / a.shares), share = static_cast<int>(unit % a.shares);
+    if (row >= rows) return;
     const Angles g = a.rotary_dim ? angles_of(a, a.positions[row], octet) : still;
     const int nq = (a.q.heads + HEADS - 1) / HEADS, nk = (a.k.heads + HEADS - 1) / HEADS;
     const int nv = (a.v.heads + HEADS - 1) / HEADS;
@@ -242,13 +245,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
 
   if constexpr (KV == AUG_FP8_E4M3FN) {
     const int64_t u = unit - row_units;
-    const int hkv = a.k.heads, windows = (a.rows + a.window - 1) / a.window;
+    const int hkv = a.k.heads, windows = (rows + a.window - 1) / a.window;
     if (u >= static_cast<int64_t>(windows) * hkv * 2) return;
     const int row0 = static_cast<int>(u / (2 * hkv)) * a.window;
     const int head = static_cast<int>((u >> 1) % hkv);
     const bool is_v = u & 1;
     const auto in_pool = [&](int64_t x) { return static_cast<uint64_t>(x) < static_cast<uint64_t>(a.num_slots); };
-    const int64_t mine = lane < a.window && row0 + lane < a.rows ? a.slots[row0 + lane] : -1;
+    const int64_t mine = lane < a.window && row0 + lane < rows ? a.slots[row0 + lane] : -1;
     uint64_t live = __ballot(in_pool(mine));
     if (live == 0) return;
     // the block of the last row before these that goes anywhere: rows of it here are written with that one
@@ -267,8 +270,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
       done = block;
       // the rows of the block: lane t has one more than how far behind `row` that of slot t is
       int behind = 0;
-      for (int at = row; at < a.rows; at += 64) {
-        const int64_t x = at + lane < a.rows ? a.slots[at + lane] : -1;
+      for (int at = row; at < rows; at += 64) {
+        const int64_t x = at + lane < rows ? a.slots[at + lane] : -1;
         const uint64_t here = __ballot(in_pool(x) && x / kBlock == block), others = __ballot(in_pool(x) && x / kBlock != block);
         const uint64_t take = others ? here & ((others & -others) - 1) : here;      // up to the first of another block
         int found = 0;
@@ -401,8 +404,8 @@ extern "C" aug_status aug_rope_rows(const aug_attn_shape* s, const aug_rope* rop
 }
 
 extern "C" aug_status aug_rope_append(const aug_attn_shape* s, const aug_rope* rope, const int32_t* positions,
-                                      const int64_t* slots, int32_t rows, const void* q, int64_t q_stride, const void* k,
-                                      int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                                      const int64_t* slots, int32_t rows, const int32_t* live_rows, const void* q,
+                                      int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
                                       void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t num_pool_blocks,
                                       void* stream) {
   const char* who = "aug_rope_append";
@@ -421,8 +424,8 @@ extern "C" aug_status aug_rope_append(const aug_attn_shape* s, const aug_rope* r
   const bool fp8 = s->kv_dtype == AUG_FP8_E4M3FN;
   if (fp8 && (!k_scale || !v_scale)) return aug::fail(AUG_ERR_INVALID, "%s: fp8 cache without scales", who);
   const auto bits = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
-  if (((bits(k_cache) | bits(v_cache)) & 15) || (bits(slots) & 7))
-    return aug::fail(AUG_ERR_INVALID, "%s: caches must be 16-byte aligned, slots 8-byte aligned", who);
+  if (((bits(k_cache) | bits(v_cache)) & 15) || (bits(slots) & 7) || (bits(live_rows) & 3))
+    return aug::fail(AUG_ERR_INVALID, "%s: caches must be 16-byte aligned, slots 8-byte and live_rows 4-byte aligned", who);
   const int eb = s->q_dtype == AUG_F32 ? 4 : 2;
   const int64_t least = static_cast<int64_t>(s->num_kv_heads) * s->head_dim;
   if (q) {
@@ -439,6 +442,7 @@ extern "C" aug_status aug_rope_append(const aug_attn_shape* s, const aug_rope* r
   a.scale[0] = k_scale;
   a.scale[1] = v_scale;
   a.slots = slots;
+  a.live_rows = live_rows;
   a.num_slots = static_cast<int64_t>(num_pool_blocks) * kBlock;
   a.rows = rows;
   if (fp8) return launch<AUG_FP8_E4M3FN>(who, s, a, stream);

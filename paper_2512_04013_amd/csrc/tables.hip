@@ -200,8 +200,6 @@ __global__ __launch_bounds__(THREADS) void tables_kernel(aug_step_tables_args a)
     a.state[r] = st;
   }
   if (thread == 0) a.q_start[n] = rows_total;
-  // none for the rows behind the last: an append of max_rows rows skips them
-  for (uint64_t i = static_cast<uint64_t>(rows_total) + thread; i < cap; i += threads) a.slots[i] = -1;
 
   if (a.max_draft == 0) {
     for (uint32_t i = thread; i < static_cast<uint32_t>(rows_total); i += threads) {

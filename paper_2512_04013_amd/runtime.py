@@ -125,17 +125,20 @@ class PagedKV:
 
 
     def append_rows(self, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor = None, rope: "Rope" = None,
-                    positions: torch.Tensor = None, q_out: torch.Tensor = None, stream=None):
+                    positions: torch.Tensor = None, q_out: torch.Tensor = None, live_rows: torch.Tensor = None, stream=None):
         """Write K/V rows ([n][H_kv][D], rows may be strided) into ``slots`` (int64,
         block * 16 + slot; rows of slots outside the pool are skipped), K rotated by
         ``positions`` (int32) where a ``rope`` is given. With ``q`` its rows are
         rotated too, into ``q_out`` (may be ``q``; allocated on ``stream`` if None),
         which is returned. Without a rope and with what ``read`` returns, rows move
-        to other slots."""
+        to other slots. ``live_rows`` (int32 [1], such as ``StepTables.live_rows``): how
+        many of the rows there are; those behind are passed over."""
         n, (hkv, dim), index = len(slots), self._row, self._device
         _check_vector(slots, "slots", n, torch.int64, index)
         _check_rows(k, "k", n, hkv, dim, self._row_dtype, index)
         _check_rows(v, "v", n, hkv, dim, self._row_dtype, index)
+        if live_rows is not None:
+            _check_vector(live_rows, "live_rows", 1, torch.int32, index)
         if rope is None and (q is not None or positions is not None):
             raise ValueError("queries and positions need a rope")
         if rope is not None:
@@ -154,7 +157,7 @@ class PagedKV:
             _check_rows(q_out, "q_out", n, hq, dim, self._row_dtype, index)
         with _on(index):
             aug_rope_append(self.shape, None if rope is None else rope.angles, positions, slots, q, k, v, q_out, self.k_cache,
-                            self.v_cache, self.k_scale, self.v_scale, self.num_pool_blocks, stream=stream)
+                            self.v_cache, self.k_scale, self.v_scale, self.num_pool_blocks, live_rows=live_rows, stream=stream)
         return q_out
 
 
@@ -199,7 +202,8 @@ class StepTables:
     holds, and for the step's rows where they start, their positions, slots and (with
     ``max_draft``) the drafts of their request that each sees. All of them are device
     tensors that ``update`` writes in place, so that it can be captured in a graph
-    together with what reads them.
+    together with what reads them. What stands behind the step's rows is of an earlier
+    step: an append of ``max_rows`` rows takes ``live_rows`` (int32 [1]) along.
 
     ``max_reqs`` requests (unused ones have lengths 0), ``max_rows`` rows of one step,
     ``max_blocks`` columns of the table, a pool of ``num_pool_blocks``. Without
@@ -224,7 +228,8 @@ class StepTables:
         self.free_ids = torch.arange(self.num_pool_blocks, dtype=torch.int32, device=device) if free_ids is None else free_ids
         self.free_count = torch.full((1,), int(free_count), dtype=torch.int32, device=device)
         self.q_start, self.kv_len, self.state = zeros(self.max_reqs + 1), zeros(self.max_reqs), zeros(self.max_reqs)
-        self.positions, self.slots = zeros(self.max_rows), zeros(self.max_rows, dtype=torch.int64).fill_(-1)
+        self.live_rows = self.q_start[self.max_reqs:]     # the step's rows
+        self.positions, self.slots = zeros(self.max_rows), zeros(self.max_rows, dtype=torch.int64)
         self.seen = zeros(self.max_rows, dtype=torch.int64) if self.max_draft else None
         self._scratch = zeros(STEP_SCRATCH_BYTES, dtype=torch.uint8)
         self.device = self.q_start.device

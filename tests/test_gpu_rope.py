@@ -1,6 +1,8 @@
 """Rotary positions on the GPU: rows against float64, their gradient, and rows
 rotated into the slots of every cache format."""
 
+import random
+
 import numpy as np
 import pytest
 
@@ -339,3 +341,61 @@ def test_rows_of_an_fp8_block_in_any_order():
     for a, b in ((plain.k_cache, mixed.k_cache), (plain.v_cache, mixed.v_cache), (plain.k_scale, mixed.k_scale), (plain.v_scale, mixed.v_scale)):
         assert torch.equal(a, b)
     assert not torch.equal(plain.k_cache, pools[0])
+
+
+@pytest.mark.parametrize("kv,d", FORMATS)
+def test_live_rows(kv, d):
+    """Rows from live_rows on are as if they were not there, in every tensor: their slots are others' slots."""
+    from paper_2512_04013_amd import runtime as rt
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    hkv, dtype, rope = 2, torch.float32 if kv == "f32" else torch.bfloat16, rt.Rope(d)
+    shape = _shape(kv, 4, hkv, d)
+    pools, scales = _pool(kv, 40, hkv, d, gen)
+    for n in (3, 40, 600):
+        slots = torch.arange(n, device="cuda") + 5
+        pos = torch.arange(n, dtype=torch.int32, device="cuda")
+        k, v, q = (_rows(gen, n, h, d, dtype) for h in (hkv, hkv, 4))
+        for live in (-1, 0, 1, n // 2, n - 1, n, n + 1):
+            m = min(max(live, 0), n)
+            a, b = (_kv(shape, _copy(pools), _copy(scales)) for _ in range(2))
+            stale = slots.clone()
+            stale[m:] = slots[:n - m] if m else slots       # of live rows
+            out = torch.full((n, 4, d), 3.0, dtype=dtype, device="cuda")
+            a.append_rows(stale, k, v, q=q, rope=rope, positions=pos, q_out=out, live_rows=torch.tensor([live], dtype=torch.int32, device="cuda"))
+            want = torch.full_like(out, 3.0)
+            if m:
+                want[:m] = b.append_rows(slots[:m], k[:m], v[:m], q=q[:m], rope=rope, positions=pos[:m])
+            assert torch.equal(out, want), (n, live)
+            for x, y in ((a.k_cache, b.k_cache), (a.v_cache, b.v_cache), (a.k_scale, b.k_scale), (a.v_scale, b.v_scale)):
+                assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8)), (n, live)
+
+
+@pytest.mark.parametrize("rows,hkv", [(1100, 8), (2500, 8), (9000, 8), (40000, 1)])
+def test_many_rows_into_an_fp8_cache(rows, hkv):
+    """Waves that look for blocks among several rows: blocks that begin or go on in another wave's rows, rows that go
+    nowhere, rows behind the last; bit for bit what one call a request writes."""
+    rng = random.Random(rows)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    blocks = rows // 8 + 300
+    pools, scales = _pool("fp8", blocks, hkv, 128, gen)
+    shape = _shape("fp8", hkv, hkv)
+    one, each = _kv(shape, _copy(pools), _copy(scales)), _kv(shape, _copy(pools), _copy(scales))
+    free = list(range(blocks))
+    rng.shuffle(free)
+    slots, ends = [], []
+    while len(slots) < rows - 300 and len(free) > 20:
+        n, first = rng.choice([1, 1, 3, 16, 30, 100, 270]), rng.randrange(16)
+        ids = [free.pop() for _ in range(-(-(first + n) // 16))]
+        slots += [ids[(first + i) // 16] * 16 + (first + i) % 16 for i in range(n)]
+        slots += [-1] * rng.choice([0, 0, 1, 20, 130])
+        ends.append(len(slots))
+    live = len(slots)
+    slots += slots[:rows - live]
+    k, v = (_rows(gen, rows, hkv, 128, torch.bfloat16) for _ in range(2))
+    slots = torch.tensor(slots, device="cuda")
+    one.append_rows(slots, k, v, live_rows=torch.tensor([live], dtype=torch.int32, device="cuda"))
+    for a, b in zip([0] + ends, ends):
+        each.append_rows(slots[a:b].contiguous(), k[a:b], v[a:b])
+    for a, b in ((one.k_cache, each.k_cache), (one.v_cache, each.v_cache), (one.k_scale, each.k_scale), (one.v_scale, each.v_scale)):
+        assert torch.equal(a, b)
+    assert not torch.equal(one.k_cache, pools[0])

@@ -117,8 +117,8 @@ def test_rows_shapes_refused():
 
 
 def _append(shape=None, rope=True, **kw):
-    a = dict(positions=P, slots=P, rows=3, q=P, q_stride=1024, k=P, k_stride=256, v=P, v_stride=256, q_out=P, q_out_stride=1024,
-             k_cache=P, v_cache=P, k_scale=P, v_scale=P, num_pool_blocks=4)
+    a = dict(positions=P, slots=P, rows=3, live_rows=None, q=P, q_stride=1024, k=P, k_stride=256, v=P, v_stride=256, q_out=P,
+             q_out_stride=1024, k_cache=P, v_cache=P, k_scale=P, v_scale=P, num_pool_blocks=4)
     a.update(kw)
     r = C.byref(aug.aug_rope_init(64)) if rope else None
     return aug.lib().aug_rope_append(C.byref(shape or _shape()), r, *a.values(), None)
@@ -128,7 +128,7 @@ def _append(shape=None, rope=True, **kw):
     dict(positions=None), dict(slots=None), dict(slots=P + 4), dict(rows=-1), dict(q=None), dict(q_out=None), dict(k=None), dict(v=None),
     dict(k_cache=None), dict(v_cache=None), dict(k_cache=P + 8), dict(num_pool_blocks=0), dict(k=P + 8), dict(v_stride=128),
     dict(v_stride=260), dict(q_out_stride=2048), dict(rope=False), dict(rope=False, positions=None),
-    dict(rope=False, q=None, q_out=None)])
+    dict(rope=False, q=None, q_out=None), dict(live_rows=P + 2)])
 def test_append_refused(kw):
     assert _append(**kw) == aug.AUG_ERR_INVALID and aug.aug_last_error()
 
@@ -152,7 +152,8 @@ def test_python_refuses():
     bad = [dict(slots=slots.int()), dict(slots=slots[:2]), dict(k=rows.float()), dict(v=rows[:, :1]), dict(k=rows.transpose(0, 1)),
            dict(k=torch.zeros(3, 128, 2, dtype=torch.bfloat16).transpose(1, 2)), dict(q=q), dict(positions=pos), dict(rope=rope),
            dict(q=q, rope=rope, positions=pos.long()), dict(q=q[:, :4], rope=rope, positions=pos),
-           dict(q_out=q, rope=rope, positions=pos), dict(q=q, q_out=q.float(), rope=rope, positions=pos)]
+           dict(q_out=q, rope=rope, positions=pos), dict(q=q, q_out=q.float(), rope=rope, positions=pos),
+           dict(live_rows=slots[:1]), dict(live_rows=pos)]
     for kw in bad:
         with pytest.raises(ValueError):
             kv.append_rows(**{"slots": slots, "k": rows, "v": rows, **kw})
