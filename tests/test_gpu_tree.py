@@ -256,12 +256,13 @@ def test_refused_requests_and_empty_ones():
             c.att.run(**bad)
 
 
-def test_many_requests():
-    """More requests than the plan has threads, of every length."""
+@pytest.mark.parametrize("reqs", [1500, 4096])
+def test_many_requests(reqs):
+    """More requests than the plan has threads, up to the most that it takes, of every length."""
     rng = random.Random(8)
-    rows = [rng.randint(1, 3) for _ in range(1500)]
-    ctx = [n + rng.choice([0, 3, 40, 150]) for n in rows]
-    Case((2, 1, 64, "bf16"), rows, ctx, seed=8).check("1500 requests")
+    rows = [rng.randint(1, 3) for _ in range(reqs)]
+    ctx = [n + rng.choice([0, 3, 40, 150, 150, 1000 if reqs < 2000 else 0]) for n in rows]
+    Case((2, 1, 64, "bf16"), rows, ctx, seed=8).check(f"{reqs} requests")
 
 
 @pytest.mark.parametrize("layer", [LAYERS[1], LAYERS[9]], ids=[IDS[1], IDS[9]])
