@@ -650,7 +650,8 @@ aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batc
  * block ids outside the pool count for nothing. Sums and softmax statistics are fp32;
  * over every cache but F32 each probability is taken as bf16 (off by at most 2^-8 of it, in the row's sum as
  * in its products). Calls that overlap need a workspace each; equal inputs give equal bits.
- * Two launches (none for no requests or rows).
+ * Two launches, one where max_blocks are too few for any request to be split (none for no
+ * requests or rows).
  * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers,
  * missing scales), AUG_ERR_NO_SPACE (workspace_bytes), AUG_ERR_HIP (launch). */
 aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batch, const void* plan_dev, const void* q,

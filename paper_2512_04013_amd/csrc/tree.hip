@@ -930,11 +930,14 @@ aug_status tree_sizes(const char* who, const aug_attn_shape* s, const aug_tree_b
   // registers for them (260 against 268)
   z->tiles = columns > 32 && s->kv_dtype == AUG_MXFP4 ? 4 : 2;
   z->parts = split * wide_for(columns, z->tiles);
+  // tables too narrow for any request to be split: nothing to merge
+  const int64_t units = (static_cast<int64_t>(b->max_blocks) * kBlock + kTreeUnit - 1) / kTreeUnit;
+  if (units == 1 || units * wide_for(columns, z->tiles) <= kTreeMinSpan) z->groups = z->parts = 0;
   z->merge_tiles = columns < 128 ? (columns + 15) / 16 : 8;
   if (z->items > (1 << 24))
     return aug::fail(AUG_ERR_UNSUPPORTED, "%s: up to %lld work items", who, (long long)z->items);
   z->plan_bytes = sizeof(TreeHeader) + z->items * sizeof(TreeItem) + z->groups * sizeof(TreeGroup);
-  z->workspace_bytes = z->parts * tree_partial_floats(s->head_dim, z->tiles) * 4;
+  z->workspace_bytes = 16 + z->parts * tree_partial_floats(s->head_dim, z->tiles) * 4;
   return AUG_OK;
 }
 
@@ -944,13 +947,13 @@ void launch_tree(const TreeArgs& a, const TreeSizes& z, hipStream_t st) {
   const dim3 merge(static_cast<uint32_t>(tiles < 2048 ? tiles : 2048));
   if constexpr (KVT == KV_F32) {
     hipLaunchKernelGGL((tree_kernel_f32<D>), dim3(z.items), dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((tree_merge_kernel<D, 2, true>), merge, dim3(kThreads), 0, st, a);
+    if (tiles) hipLaunchKernelGGL((tree_merge_kernel<D, 2, true>), merge, dim3(kThreads), 0, st, a);
   } else if (z.tiles == 2) {
     hipLaunchKernelGGL((tree_kernel<KVT, D, 2>), dim3(z.items), dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((tree_merge_kernel<D, 2, false>), merge, dim3(kThreads), 0, st, a);
+    if (tiles) hipLaunchKernelGGL((tree_merge_kernel<D, 2, false>), merge, dim3(kThreads), 0, st, a);
   } else if constexpr (KVT == KV_FP4) {
     hipLaunchKernelGGL((tree_kernel<KVT, D, 4>), dim3(z.items), dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((tree_merge_kernel<D, 4, false>), merge, dim3(kThreads), 0, st, a);
+    if (tiles) hipLaunchKernelGGL((tree_merge_kernel<D, 4, false>), merge, dim3(kThreads), 0, st, a);
   }
 }
 

@@ -178,23 +178,27 @@ def test_python_refuses():
 # ---- attention of drafts ---------------------------------------------------------------------
 
 def _batch(**kw):
-    f = dict(num_reqs=4, max_rows=32, max_blocks=8, max_draft=8, q_start=P, kv_len=P, block_table=P, seen=P)
+    f = dict(num_reqs=4, max_rows=32, max_blocks=17, max_draft=8, q_start=P, kv_len=P, block_table=P, seen=P)
     f.update(kw)
     return aug.aug_tree_batch(**f)
 
 
 def test_tree_sizes():
     """Room for any lengths: the items of every request in one span (128 columns each at most) and those of the splits;
-    partials of 2048 split items of 32, 64 or 128 columns."""
+    partials of 2048 split items of 32, 64 or 128 columns; nothing of these for tables of 128 keys, or of 256 and
+    up to 32 columns."""
     for draft, hq, kv, tiles, columns in ((1, 8, "bf16", 1, 32), (8, 8, "bf16", 1, 32), (9, 8, "bf16", 1, 64), (17, 8, "f32", 1, 128),
                                           (64, 8, "bf16", 2, 128), (64, 16, "bf16", 4, 128)):
         shape = _shape(kv, hq=hq)
         plan, workspace = aug.aug_tree_plan_size(shape, _batch(max_draft=draft))
         whole = 4 * 2 * tiles
         assert plan == 64 + 32 * (1024 + whole) + 32 * whole
-        assert workspace == (1024 + whole) * columns * 130 * 4
+        assert workspace == 16 + (1024 + whole) * columns * 130 * 4
+        for blocks, split in ((1, False), (8, False), (9, columns > 32), (16, columns > 32)):
+            got = aug.aug_tree_plan_size(shape, _batch(max_draft=draft, max_blocks=blocks))
+            assert got == ((plan, workspace) if split else (64 + 32 * (1024 + whole), 16)), blocks
     plan, workspace = aug.aug_tree_plan_size(_shape(), _batch(num_reqs=4096, max_draft=1))
-    assert plan == 64 + 32 * (1024 + 8192) + 32 * 1024 and workspace == 2048 * 32 * 130 * 4
+    assert plan == 64 + 32 * (1024 + 8192) + 32 * 1024 and workspace == 16 + 2048 * 32 * 130 * 4
 
 
 @pytest.mark.parametrize("kw,status", [
