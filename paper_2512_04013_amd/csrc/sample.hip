@@ -8,20 +8,28 @@
 // Weights are float64 exponentials as integers in units of 2^-s (aug.h): sums are exact, so
 // they do not depend on the order in which threads come to add.
 //
-// A workgroup of 1024 threads takes a row and keeps it in registers (up to 256 KiB of it;
-// longer rows are read in in every pass). The cut lies near the top of the row, so few elements
+// A workgroup of 1024 threads takes a row and reads it in every pass, from the caches after the
+// first (held in registers it spilled). The cut lies near the top of the row, so few elements
 // need more than a comparison:
 //
 //  * top-k: at least k elements are not below the k-th largest of the maxima of groups of
 //    elements (four groups a thread), which bins over the distance from the row's
 //    largest logit bound from below. What is not below that goes on a list, is sorted by (logit,
 //    index) and cut by top-k, top-p and min-p, and the draw is made on the list sorted by index.
-//  * top-p alone: weights of all elements, by bins over the distance. If all up to the cut's bin fit on the list it goes on as above; else the list has the bin alone, and sums of
+//  * top-p alone: weights of all elements, by bins over the distance. If all up to the cut's bin
+//    fit on the list it goes on as above; else the list has the bin alone, and sums of
 //    the kept weights of pieces of the row, a scan over the pieces, and the piece that the
 //    number falls into element by element make the draw.
 //  * what this does not hold (more elements at the cut than the list has places, infinite
 //    logits) takes a descent over the digits of the logit instead: counts or weights of the
 //    elements that agree in the digits so far, by the next digit.
+//
+// One row of 32000 bf16 logits with top-k 50 and top-p: 11.9 us, of which reading the row is a
+// fifth and the rest barriers and LDS round trips one behind the other. 64 rows of 50257 fp32 with
+// top-p alone: 53 us, the time of the longest row: weights 31 of its 86 thousand cycles, the list
+// 15 and two sorts of some 300 elements 26. 512 rows of 128000 bf16 with every setting: 106 us; rows
+// with top-p alone and flat logits take 230 thousand cycles, 175 of them for weights (40 vector
+// instructions each, on one compute unit), twice.
 
 #include <hip/hip_runtime.h>
 

@@ -23,11 +23,13 @@
 // cases below took 198, 308 and 460 us).
 // Waves with the same columns are merged through LDS, spans by a second launch.
 //
-// 64 requests of 8 drafts behind about 2500 tokens, bf16, 32/8 heads: 190 us with the second
-// launch (12 us), 890 MB of K and V at 5.3 TB/s while the kernel runs. 128 requests of up to
-// 16 drafts, fp8, 64/8 heads: 260 us, 882 MB; 8 requests of 64 drafts behind 16384 to 32768
-// tokens, fp4: 280 us, 233 GFLOP. Both of those spend most instructions on making bf16 of the
-// codes and on the softmax, 250 vector instructions to 32 MFMAs of a step of 32 columns.
+// 64 requests of 8 drafts behind about 2500 tokens, bf16, 32/8 heads: 181 us with the second
+// launch (12 us), 890 MB of K and V at 5.4 TB/s while the kernel runs; its items start and end in
+// two rounds. 128 requests of up to 16 drafts, fp8, 64/8 heads: 250 us, 882 MB, 111 GFLOP; 8
+// requests of 64 drafts behind 16384 to 32768 tokens, fp4: 270 us, 233 GFLOP. Those two are bound by
+// vector instructions (bf16 made of the codes, the softmax: 200 a step of 32 columns over fp8, 160
+// over fp4, beside 32 MFMAs), which keep the SIMDs busy half of the time and overlap with the
+// MFMAs (a quarter, a third) in part.
 //
 // fp32 caches: the same with 16x16x4 fp32 MFMAs, one block a step.
 
@@ -926,8 +928,8 @@ aug_status tree_sizes(const char* who, const aug_attn_shape* s, const aug_tree_b
   z->items = kTreeTarget + whole;
   z->groups = whole < kTreeTarget ? whole : kTreeTarget;
   const int64_t split = z->items < 2 * kTreeTarget ? z->items : 2 * kTreeTarget;
-  // 64 columns a wave: fp4 operands, which cost most to make, 310 us against 280; fp8 has too few
-  // registers for them (260 against 268)
+  // 64 columns a wave: fp4 operands, which cost most to make and fit (310 us with 32, 280 with 64);
+  // over fp8 they need more registers than there are (268 us, 32 columns 260)
   z->tiles = columns > 32 && s->kv_dtype == AUG_MXFP4 ? 4 : 2;
   z->parts = split * wide_for(columns, z->tiles);
   // tables too narrow for any request to be split: nothing to merge
