@@ -50,7 +50,8 @@ constexpr int kPlanThreads = 1024;
 struct TreeHeader {                    // 64 bytes
   int32_t num_items;
   int32_t num_groups;
-  int32_t reserved[14];
+  int32_t hkv, group, tiles;           // what it was made for
+  int32_t reserved[11];
 };
 struct TreeItem {                      // 32 bytes
   int32_t req;
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
     part += s > 1 ? columns * q.wide * s : 0;
     group += s > 1 ? columns : 0;
   }
-  if (tid == 0) *reinterpret_cast<TreeHeader*>(a.plan) = TreeHeader{num_items, num_groups, {}};
+  if (tid == 0) *reinterpret_cast<TreeHeader*>(a.plan) = TreeHeader{num_items, num_groups, a.hkv, a.group, a.tiles, {}};
   __syncthreads();
   TreeItem* out = reinterpret_cast<TreeItem*>(a.plan + sizeof(TreeHeader));
   TreeGroup* group_out = reinterpret_cast<TreeGroup*>(out + a.items);
@@ -463,6 +464,15 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it,
   }
 }
 
+// Items and groups of the plan; none where it was made for other heads or tiles, whose items lie
+// outside this launch's arrays.
+__device__ __forceinline__ int2 tree_counts(const TreeArgs& a, int tiles) {
+  typedef int32_t words_t __attribute__((ext_vector_type(8)));
+  const words_t h = load_uniform(reinterpret_cast<const words_t*>(a.plan));
+  const bool mine = h[2] == a.hkv && h[3] == 1 << a.group_log2 && h[4] == tiles;
+  return mine ? int2{h[0], h[1]} : int2{0, 0};
+}
+
 __device__ __forceinline__ TreeItem load_tree_item(const TreeItem* p) {
   typedef int32_t words_t __attribute__((ext_vector_type(8)));
   const words_t raw = load_uniform(reinterpret_cast<const words_t*>(p));
@@ -501,7 +511,7 @@ __global__ __launch_bounds__(kThreads, T == 4 || (KVT == KV_BF16 && D == 128) ? 
   constexpr int kQuery = 8 * KS * 64;                  // 16-byte query operands
   constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
   __shared__ __align__(16) char lds[kLds];
-  const int items = load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items);
+  const int items = tree_counts(a, T).x;
   const TreeItem it = load_tree_item(reinterpret_cast<const TreeItem*>(a.plan + sizeof(TreeHeader)) + blockIdx.x);
   if (static_cast<int>(blockIdx.x) >= items) return;
   const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -731,7 +741,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel_f32(TreeArgs a) {
   constexpr int kQuery = kTreeWaves * T * KS * 64;
   constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
   __shared__ __align__(16) char lds[kLds];
-  if (static_cast<int>(blockIdx.x) >= load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_items)) return;
+  if (static_cast<int>(blockIdx.x) >= tree_counts(a, 2).x) return;
   const TreeItem it = load_tree_item(reinterpret_cast<const TreeItem*>(a.plan + sizeof(TreeHeader)) + blockIdx.x);
   const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -850,7 +860,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel_f32(TreeArgs a) {
 template <int D, int T, bool F32>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeArgs a) {
   constexpr int N = D / 16, U = 8;                      // spans whose loads are on their way at once
-  const int groups = load_uniform(&reinterpret_cast<const TreeHeader*>(a.plan)->num_groups);
+  const int groups = tree_counts(a, T).y;
   const TreeGroup* all = reinterpret_cast<const TreeGroup*>(a.plan + sizeof(TreeHeader) + a.items * sizeof(TreeItem));
   for (int at = blockIdx.x; at < a.max_groups * a.merge_tiles; at += gridDim.x) {
     const int t = at % a.merge_tiles;

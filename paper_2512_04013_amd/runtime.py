@@ -277,6 +277,8 @@ class TreeAttention:
                              f"{kv.k_cache.device}")
         self.shape, self.kv, self.tables = shape, kv, tables
         self._index = kv._device
+        self._check_pool(kv)
+        self._planned = False
         t = tables
         self._batch = aug_tree_batch(t.max_reqs, t.max_rows, t.max_blocks, t.max_draft, t.q_start.data_ptr(), t.kv_len.data_ptr(),
                                      t.block_table.data_ptr(), t.seen.data_ptr())
@@ -292,6 +294,12 @@ class TreeAttention:
         """Enqueue the work list of the tables as they are then."""
         with _on(self._index):
             aug_tree_plan(self.shape, self._batch, self.plan_dev, stream=stream)
+        self._planned = True
+
+    def _check_pool(self, kv):
+        for field in ("kv_dtype", "num_kv_heads", "head_dim"):
+            if getattr(kv.shape, field) != getattr(self.shape, field):
+                raise ValueError(f"a pool of {field} {getattr(kv.shape, field)}, the attention has {getattr(self.shape, field)}")
 
     def run(self, q: torch.Tensor, out: torch.Tensor = None, stream=None, kv: PagedKV = None):
         """Enqueue the attention of ``q`` ([max_rows][H_q][D], contiguous) into ``out``
@@ -302,6 +310,10 @@ class TreeAttention:
         out = self.out if out is None else out
         if kv.num_pool_blocks != self.kv.num_pool_blocks or kv._device != self._index:
             raise ValueError(f"a pool of {kv.num_pool_blocks} blocks, planned for {self.kv.num_pool_blocks}")
+        if kv is not self.kv:
+            self._check_pool(kv)
+        if not self._planned:
+            raise ValueError("no step has been planned")
         for name, t in (("q", q), ("out", out)):
             if t.shape != self._rows or t.dtype != self._dtype or not t.is_contiguous() or t.get_device() != self._index:
                 raise ValueError(f"{name}: contiguous {self._dtype} of shape {self._rows} on {self.tables.device}, got {t.dtype} "

@@ -256,6 +256,32 @@ def test_refused_requests_and_empty_ones():
             c.att.run(**bad)
 
 
+def test_plans_of_something_else():
+    """No step planned yet, a pool of another format, and plans of other heads or formats: nothing is read or written by them."""
+    import paper_2512_04013_amd as aug
+    from paper_2512_04013_amd import runtime as rt
+    c, other = (Case((16, 2, 128, kv), [40, 3], [700, 90], seed=1) for kv in ("bf16", "fp4"))
+    with pytest.raises(ValueError):
+        c.att.run(c.q.nan_to_num())
+    with pytest.raises(ValueError):
+        rt.TreeAttention(c.shape, other.kv, c.t)
+    for x in (c, other):
+        x.check("its own plan")
+    with pytest.raises(ValueError):
+        c.att.run(c.q.nan_to_num(), kv=other.kv)
+    heads = Case((8, 4, 128, "bf16"), [40, 3], [700, 90], seed=1)
+    heads.check("other heads")
+    for mine, plan in ((c, other), (other, c), (c, heads), (heads, c)):
+        att, t = mine.att, mine.t
+        att.out.fill_(7.0)
+        big = torch.empty(max(mine.att.plan_dev.numel(), plan.att.plan_dev.numel()), dtype=torch.uint8, device="cuda")
+        big[:plan.att.plan_dev.numel()] = plan.att.plan_dev
+        aug.aug_attn_tree(mine.shape, att._batch, big, mine.q.nan_to_num(), mine.kv.k_cache, mine.kv.v_cache, mine.kv.k_scale, mine.kv.v_scale,
+                          mine.kv.num_pool_blocks, att.out, att.workspace)
+        torch.cuda.synchronize()
+        assert (att.out == 7.0).all()
+
+
 @pytest.mark.parametrize("reqs", [1500, 4096])
 def test_many_requests(reqs):
     """More requests than the plan has threads, up to the most that it takes, of every length."""
