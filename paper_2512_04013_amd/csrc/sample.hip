@@ -15,21 +15,21 @@
 //  * top-k: at least k elements are not below the k-th largest of the maxima of groups of
 //    elements (four groups a thread), which bins over the distance from the row's
 //    largest logit bound from below. What is not below that goes on a list, is sorted by (logit,
-//    index) and cut by top-k, top-p and min-p, and the draw is made on the list sorted by index.
+//    index) and cut by top-k, top-p and min-p, and the draw is made on sums of the list by index.
 //  * top-p alone: weights of all elements, by bins over the distance. If all up to the cut's bin
-//    fit on the list it goes on as above; else the list has the bin alone, and sums of
+//    fit on the list only those of that bin are sorted; else the list has the bin alone, and sums of
 //    the kept weights of pieces of the row, a scan over the pieces, and the piece that the
 //    number falls into element by element make the draw.
 //  * what this does not hold (more elements at the cut than the list has places, infinite
 //    logits) takes a descent over the digits of the logit instead: counts or weights of the
 //    elements that agree in the digits so far, by the next digit.
 //
-// One row of 32000 bf16 logits with top-k 50 and top-p: 11.9 us, of which reading the row is a
+// One row of 32000 bf16 logits with top-k 50 and top-p: 10 us, of which reading the row is a
 // fifth and the rest barriers and LDS round trips one behind the other. 64 rows of 50257 fp32 with
-// top-p alone: 53 us, the time of the longest row: weights 31 of its 86 thousand cycles, the list
-// 15 and two sorts of some 300 elements 26. 512 rows of 128000 bf16 with every setting: 106 us; rows
-// with top-p alone and flat logits take 230 thousand cycles, 175 of them for weights (40 vector
-// instructions each, on one compute unit), twice.
+// top-p alone: 35 us, the time of the longest row: weights 31 of its 60 thousand cycles, the list
+// 15. 512 rows of 128000 bf16 with every setting: 103 us; rows with top-p alone and flat
+// logits take 230 thousand cycles, 175 of them for weights (40 vector instructions each, on one
+// compute unit), twice.
 
 #include <hip/hip_runtime.h>
 
@@ -45,6 +45,7 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kDigits = 256;
 constexpr int kBins = 2 * kThreads;
+constexpr int kBinBits = 11;
 constexpr int kList = 2 * kThreads;
 // pieces of a row: what one wave reads at once, at most (2^20 + 3) / 4 words of fp32
 constexpr int kPieces = ((1 << 20) / 4 / kThreads + 1) * kWaves;
@@ -589,29 +590,83 @@ __device__ __forceinline__ void write_token(const Rows& a, int row, int index, f
   if (a.probs) a.probs[row] = static_cast<float>(weight(x) * weight.unit / static_cast<double>(all));
 }
 
-// The draw among the first `keep` elements of the list, which cut_list left.
-__device__ __forceinline__ void draw_from_list(const Rows& a, int row, int keep, u64 floor, double uniform, const Weight& weight, Lds& s,
-                                               const u64 (&place)[2], const u64 (&w)[2]) {
-  // by rising index: ~index above the position, which finds the weight again
-  u64 v[2];
+// The draw among two elements of each thread, of which those with a weight v are kept: sums of
+// the weights by the index's upper eleven bits, and then by its lower ones in the bin that the number falls
+// into (a sort by index and a scan took three times as long).
+__device__ __forceinline__ void draw_by_index(const Rows& a, int row, double uniform, const Weight& weight, Lds& s, const u64 (&place)[2],
+                                              const u64 (&v)[2]) {
+  const int t = threadIdx.x, bits = 32 - __clz(a.vocab), shift = max(bits - kBinBits, 0);
+  const auto find = [&](auto part, auto bin_of, double share, u64 target, u64* before) {
+    __syncthreads();
+    s.mass[2 * t] = s.mass[2 * t + 1] = 0;
+    __syncthreads();
+    times<2>([&](auto i) {
+      const int bin = bin_of(index_at(place[i]));
+      if (v[i] && bin >= 0) atomicAdd(&s.mass[bin], v[i]);
+    });
+    __syncthreads();
+    const u64 w0 = s.mass[2 * t], w1 = s.mass[2 * t + 1];
+    u64 all;
+    const u64 upto = block_upto<part>(w0 + w1, s, &all);
+    if (part == 0) target = draw_of(share, all);
+    if (upto > target && upto - w0 - w1 <= target) {
+      const bool second = upto - w1 <= target;
+      s.found = 2 * t + second;
+      s.found_before = upto - w1 - (second ? 0 : w0);
+    }
+    __syncthreads();
+    *before = s.found_before;
+    return std::pair<u64, u64>{all, target};
+  };
+  u64 before;
+  const auto [all, target] = find(std::integral_constant<int, 0>{}, [&](int index) { return index >> shift; }, uniform, 0, &before);
+  int index = s.found;
+  if (shift > 0) {
+    const int upper = index;
+    u64 unused;
+    find(std::integral_constant<int, 1>{}, [&](int x) { return x >> shift == upper ? x & ((1 << shift) - 1) : -1; }, 0.0, target - before, &unused);
+    index = (upper << shift) + s.found;
+  }
   times<2>([&](auto i) {
-    const int pos = list_pos(i);
-    v[i] = 0;
-    if (pos >= keep) return;
-    v[i] = (place[i] << 32) | static_cast<uint32_t>(pos);
-    s.mass[pos] = w[i] >= floor ? w[i] : 0;
-    s.count[pos] = __float_as_uint(logit_at(place[i]));
+    if (v[i] && index_at(place[i]) == index) write_token(a, row, index, logit_at(place[i]), all, weight);
   });
-  sort_list(keep, v, s);
-  __syncthreads();
-  u64 x[2], upto[2], all;
-  times<2>([&](auto i) { x[i] = list_pos(i) < keep ? s.mass[static_cast<uint32_t>(v[i])] : 0; });
-  list_upto<0>(x[0], x[1], s, upto, &all);
-  const u64 target = draw_of(uniform, all);
-  times<2>([&](auto i) {
-    if (upto[i] > target && upto[i] - x[i] <= target)
-      write_token(a, row, index_at(v[i] >> 32), __uint_as_float(s.count[static_cast<uint32_t>(v[i])]), all, weight);
+}
+
+// A value of each lane, largest first: bitonic.
+__device__ __forceinline__ u64 sort_wave(u64 v) {
+  const int lane = threadIdx.x & 63;
+  times<6>([&](auto r) {
+    times<r + 1>([&](auto g) {
+      constexpr int run = 2 << r, gap = run >> (g + 1);
+      const u64 other = (static_cast<u64>(lane_xor<gap>(static_cast<uint32_t>(v >> 32))) << 32) | lane_xor<gap>(static_cast<uint32_t>(v));
+      v = pick(v, other, ((lane & gap) == 0) == ((lane & run) == 0));
+    });
   });
+  return v;
+}
+// Cut and draw of a list of up to 64 elements by the first wave, with no barrier: sorted, cut, sorted by
+// index. 32000 logits with top-k 50: 11.9 us with the way below, 10.2 with this one.
+__device__ __forceinline__ void finish_wave(const Rows& a, int row, int n, const Cut& cut, u64 floor, double uniform, const Weight& weight, Lds& s) {
+  const int lane = threadIdx.x;
+  if (lane >= 64) return;
+  const u64 place = sort_wave(lane < n ? s.list[lane] : 0);
+  const float x = logit_at(place);
+  const u64 w = place ? weight.fixed(x) : 0;
+  int keep = min(n, cut.k);
+  if (cut.p < 1.f) {
+    const u64 v = lane < keep ? w : 0, upto = wave_upto(v);
+    const u64 target = cut.target ? cut.target : share_of(cut.p, lane_of(upto, 63));
+    const u64 reached = __ballot(upto >= target && upto - v < target);      // the first sum that reaches it
+    if (reached) keep = min(keep, static_cast<int>(__ffsll(reached)));
+  }
+  // by rising index: ~index above the lane that has the weight
+  const u64 by_index = sort_wave(lane < keep ? (place << 32) | static_cast<uint32_t>(lane) : 0);
+  const int from = static_cast<int>(by_index & 63);
+  const u64 kept = __shfl(lane < keep && w >= floor ? w : 0, from);
+  const float logit = __shfl(x, from);
+  const u64 v = lane < keep ? kept : 0, upto = wave_upto(v);
+  const u64 all = lane_of(upto, 63), target = draw_of(uniform, all);
+  if (upto > target && upto - v <= target) write_token(a, row, index_at(by_index >> 32), logit, all, weight);
 }
 
 // Cut and draw of a list of up to 128 elements without sorting it: eight threads an element
@@ -695,12 +750,15 @@ __device__ __forceinline__ int list_from(const R& in, float low, Lds& s) {
 // The list of n elements cut, and the draw from it.
 __device__ __forceinline__ void finish_list(const Rows& a, int row, int n, const Cut& cut, u64 floor, double uniform, const Weight& weight,
                                             Lds& s) {
-  if (n <= 128) {
+  if (n <= 64) {
+    finish_wave(a, row, n, cut, floor, uniform, weight, s);
+  } else if (n <= 128) {
     finish_short(a, row, n, cut, floor, uniform, weight, s);
   } else {
     u64 place[2], w[2];
     const int keep = cut_list(n, cut, weight, s, place, w);
-    draw_from_list(a, row, keep, floor, uniform, weight, s, place, w);
+    times<2>([&](auto i) { w[i] = list_pos(i) < keep && w[i] >= floor ? w[i] : 0; });
+    draw_by_index(a, row, uniform, weight, s, place, w);
   }
 }
 
@@ -794,11 +852,39 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
   if (count_before + in_bin <= kList) {
     // all up to the bin's end
     cut.skip = 0;
+    const u64 before = s.found_before;
+    if (tid == 0) s.tie = 0;
+    __syncthreads();
     in.from(weight.low(bin), [&](int index, float x) {
-      if (weight.bin(x) <= bin) put(index, x, s);
+      const int b = weight.bin(x);
+      if (b > bin) return;
+      put(index, x, s);
+      if (b < bin) return;
+      const int at = atomicAdd(&s.tie, 1);
+      if (at < 64) s.piece[at] = place_of(x, index);
     });
     __syncthreads();
-    finish_list(a, row, min(s.listed, kList), cut, floor, uniform, weight, s);
+    const int n = min(s.listed, kList);
+    if (n <= 64 || in_bin > 64) {
+      finish_list(a, row, n, cut, floor, uniform, weight, s);
+      return Fast::kDrawn;
+    }
+    // the cut lies in the bin: its elements alone are sorted, by the first wave
+    if (tid < 64) {
+      const u64 place = sort_wave(tid < static_cast<int>(in_bin) ? s.piece[tid] : 0);
+      const u64 w = place ? weight.fixed(logit_at(place)) : 0, sum = before + wave_upto(w);
+      const int first = __ffsll(__ballot(sum >= cut.target && place)) - 1;
+      const u64 end = lane_of(place, first < 0 ? static_cast<int>(in_bin) - 1 : first);
+      if (tid == 0) s.other_before = end;
+    }
+    __syncthreads();
+    const u64 end = s.other_before;
+    u64 place[2], w[2];
+    times<2>([&](auto i) {
+      place[i] = list_pos(i) < n ? s.list[list_pos(i)] : 0;
+      w[i] = place[i] >= end ? weight.fixed_from(logit_at(place[i]), floor) : 0;
+    });
+    draw_by_index(a, row, uniform, weight, s, place, w);
     return Fast::kDrawn;
   }
   if (in_bin > kList) return Fast::kNot;
