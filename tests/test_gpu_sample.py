@@ -198,3 +198,36 @@ def test_refusals_and_nothing():
             rt.sample(**{"logits": x, "uniform": u, **bad})
     tokens, probs = rt.sample(x[:0], u[:0])
     assert tokens.shape == probs.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("spread", [0.0, 0.03, 3.0])
+def test_lists_of_every_size(dtype, spread):
+    """Few elements far above the rest, as many as one wave sorts, one more, ..., more than any list holds; equal ones, ones
+    within a bin or two, and spread out; cut by number, by weight and by both."""
+    rng = random.Random(1)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    vocab, sizes = 40000, [1, 2, 63, 64, 65, 100, 127, 128, 129, 255, 257, 300, 1000, 2047, 2048, 2049, 5000]
+    x = torch.randn(len(sizes), vocab, generator=gen, device="cuda") - 30
+    for r, n in enumerate(sizes):
+        at = torch.randperm(vocab, generator=gen, device="cuda")[:n]
+        x[r, at] = 5 + spread * torch.rand(n, generator=gen, device="cuda")
+    x = x.to(dtype)
+    ks = [dict(top_k=n) for n in sizes] + [dict(top_k=n, top_p=0.8) for n in sizes] + [dict(top_k=2 * n, top_p=0.8, min_p=0.3) for n in sizes]
+    ps = [dict(top_k=0, top_p=p) for p in (0.05, 0.5, 0.93, 0.999999) for _ in sizes] + [dict(top_k=0, top_p=0.9, min_p=0.6) for _ in sizes]
+    settings = [{"temperature": 1.0, "top_k": 0, "top_p": 1.0, "min_p": 0.0, **s} for s in ks + ps]
+    rows = x.repeat(len(settings) // len(sizes), 1)
+    u = [rng.random() for _ in settings]
+    host, near = rows.float().cpu().numpy(), 0
+    tokens, probs = _run(rows, u, settings)
+    margin = vocab * 2.0 ** -46 + 2.0 ** -50
+    for r, s in enumerate(settings):
+        s = {k: float(np.float32(v)) if k != "top_k" else v for k, v in s.items()}
+        token, prob, safe = sampling.draw(host[r], float(np.float32(u[r])), **s)
+        if safe <= margin:
+            near += 1           # equal weights: top_p of n of them may lie at a border, as 0.5 of 64 does
+            continue
+        assert tokens[r] == token, (r, s, tokens[r], token, safe)
+        assert abs(probs[r] - prob) <= prob * (2.0 ** -24 + margin + 2.0 ** -49), (r, s, probs[r], prob)
+    say(f"  {near} of {len(settings)} at a border")
+    assert near <= len(settings) // (4 if spread == 0.0 else 50)
