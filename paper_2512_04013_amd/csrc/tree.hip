@@ -150,10 +150,11 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
   // items (1104 for two rounds of 512 took a third round: 460 us against 406).
   int32_t span = kTreeMinSpan;
   const auto length_of = [&](const Req& q) {
-    const int s = max(static_cast<int>((static_cast<int64_t>(q.units) * q.wide + span - 1) / span), 1);
-    return max((q.units + s - 1) / s, 1);
+    // (units * wide is up to 2^19, span up to 2^21)
+    const uint32_t s = max(static_cast<uint32_t>(q.units * q.wide + span - 1) / static_cast<uint32_t>(span), 1u);
+    return max(static_cast<int>((q.units + s - 1) / s), 1);
   };
-  const auto spans_of = [&](const Req& q) { const int l = length_of(q); return max((q.units + l - 1) / l, 1); };
+  const auto spans_of = [&](const Req& q) { const uint32_t l = length_of(q); return max(static_cast<int>((q.units + l - 1) / l), 1); };
   {
     unsigned long long work = 0, total;
     for (int r = r0; r < r1; ++r) {
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
       work += static_cast<unsigned long long>(q.units) * q.tiles * q.wide * a.hkv;
     }
     sum_before(work, waves64, &total);
-    const int64_t even = (total + kTreeTarget - 1) / kTreeTarget;
+    // (no request is longer than 2^19)
+    const int64_t even = min(static_cast<int64_t>((total + kTreeTarget - 1) / kTreeTarget), int64_t{1} << 20);
     span = max(span, static_cast<int32_t>(even));
     const int32_t most = 2 * span;
     for (int i = 0; i < 4; ++i) {
@@ -179,7 +181,9 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
   // 302 against 267, of lengths that differ). 16 classes of length (keys x wide), in each the requests' order.
   constexpr int kClasses = 16, kWaves = kPlanThreads / 64;
   const int lane = tid & 63, wave = tid >> 6, rounds = (n + kPlanThreads - 1) / kPlanThreads;
-  const auto class_of = [&](const Req& q) { return kClasses - 1 - static_cast<int>(static_cast<int64_t>(min(length_of(q) * q.wide, span)) * (kClasses - 1) / span); };
+  const auto class_of = [&](const Req& q) {
+    return kClasses - 1 - static_cast<int>(static_cast<uint32_t>(min(length_of(q) * q.wide, span)) * (kClasses - 1) / static_cast<uint32_t>(span));
+  };
   for (int k = 0; k < rounds; ++k) {
     const int r = k * kPlanThreads + tid;
     const int mine = r < n ? class_of(request(r)) : -1;
