@@ -766,8 +766,8 @@ __device__ __forceinline__ void finish_list(const Rows& a, int row, int n, const
 enum class Fast { kNot, kDrawn, kPieces };     // nothing done; done; pieces summed, `last` the end of what is kept
 
 template <typename R>
-__device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, const float (&maxima)[4], const Weight& weight, int k, float p, double floor,
-                          double uniform, Lds& s, u64* last) {
+__device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, const float (&maxima)[4], const Weight& weight, int k,
+                                          float p, u64 floor, double uniform, Lds& s, u64* last) {
   const int tid = threadIdx.x;
   Cut cut{kList, 0, 0, p};
   if (in.vocab <= kList) {

@@ -174,7 +174,8 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
       }
       sum_before(items, waves, &all);
       if (all <= kTreeTarget || span >= most) break;
-      span = static_cast<int32_t>(min(static_cast<int64_t>(most), max(static_cast<int64_t>(span) + 1, static_cast<int64_t>(span) * (all + kTreeTarget) / (2 * kTreeTarget))));
+      const int64_t longer = static_cast<int64_t>(span) * (all + kTreeTarget) / (2 * kTreeTarget);
+      span = static_cast<int32_t>(min(static_cast<int64_t>(most), max(static_cast<int64_t>(span) + 1, longer)));
     }
   }
   // Requests with the longest items first: those behind fill the gaps at the end (198 us against 182,
