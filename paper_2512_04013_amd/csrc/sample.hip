@@ -156,12 +156,10 @@ struct Weight {
   }
 };
 
-// The largest of three, without the compiler's quieting of what may be signalling NaNs: a
-// signalling NaN makes the result NaN, a quiet one is passed over.
-__device__ __forceinline__ float max3_raw(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+// The largest of three, NaN where one of them is, quiet or signalling (v_maximum3_f32). v_max3_f32 will not
+// do: it makes a quiet NaN of a signalling one, and the next passes over that and over all that was gathered before.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(a, __builtin_elementwise_maximum(b, c));
 }
 
 // A row in 16-byte words, of which the first and last may be parts of one: thread t takes
@@ -210,10 +208,11 @@ struct Row {
       }
     });
   }
+  // NaN if `top` or an element is
   __device__ static __forceinline__ float largest(const uint4& w, float top) {
     float x[VEC];
     values(w, x);
-    times<VEC / 2>([&](auto i) { top = max3_raw(top, x[2 * i], x[2 * i + 1]); });
+    times<VEC / 2>([&](auto i) { top = max3(top, x[2 * i], x[2 * i + 1]); });
     return top;
   }
   // f(turn, word, part) of every word of the thread, four at a time, so that their loads are
@@ -242,7 +241,7 @@ struct Row {
   template <typename F>
   __device__ __forceinline__ void from(float low, F&& f) const {
     by_words([&](int turn, const uint4& u, auto) {
-      if (!__any(largest(u, -INFINITY) >= low)) return;
+      if (!__any(!(largest(u, -INFINITY) < low))) return;      // (words with NaN are looked through)
       float x[VEC];
       values(u, x);
       const int index = first(turn * kThreads + static_cast<int>(threadIdx.x));
@@ -280,7 +279,7 @@ struct Row {
     times<4>([&](auto g) { top[g] = -INFINITY; });
     by_words([&](int, const uint4& u, auto part) { top[part] = largest(u, top[part]); });
     if (top[0] != top[0] || top[1] != top[1] || top[2] != top[2] || top[3] != top[3]) {
-      // signalling NaNs: all in one group, carefully
+      // NaN: all in one group, one by one
       float t = -INFINITY;
 #pragma nounroll
       for (int turn = 0; turn < turns; ++turn) {
