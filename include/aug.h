@@ -675,9 +675,9 @@ aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batc
  * NULL: 1 and all. probs (may be NULL) receives the token's share of what is kept.
  *
  * Which side of a border a number falls on decides tokens, so weights are computed in
- * float64 and summed exactly as integers, multiples of 2^-s with s = min(51, 62 -
- * ceil(log2 vocab)) (a weight below 2^-(s+1) is none): equal inputs give equal tokens, and sums
- * that differ by more than some 2^-s are told apart. */
+ * float64 (off by less than 2^-51) and summed exactly as integers, multiples of 2^-s with s = min(51, 62 -
+ * ceil(log2 vocab)) (a weight below 2^-(s+1) is none): equal inputs give equal tokens, and a weight enters a sum, or
+ * meets min-p, off by less than 2^-51 + 2^-(s+1). */
 typedef struct {
   int32_t rows;
   int32_t vocab;               /* 1 to 2^20 */

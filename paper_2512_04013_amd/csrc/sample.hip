@@ -91,10 +91,12 @@ __device__ __forceinline__ float logit_at(u64 place) {
 }
 __device__ __forceinline__ int index_at(u64 place) { return static_cast<int>(~static_cast<uint32_t>(place)); }
 
-// exp((x - top) / temperature) for x <= top, off by less than 2^-46: with a = (x - top) log2(e) /
-// temperature and m = 32 a rounded, 2^a = 2^(m >> 5) 2^((m & 31) / 32) 2^f with |f| <= 1 / 64, from a
-// table of 2^(j / 32) and the Taylor series of e^(f ln 2) up to its fifth power (the rest is below
-// 2^-48). Adding 1.5 * 2^52 rounds to an integer and leaves it in the low word. The table is
+// exp((x - top) / temperature) for x <= top, off by less than 2^-51 (the largest weight is 1): with
+// a = (x - top) log2(e) / temperature and m = 32 a rounded, 2^a = 2^(m >> 5) 2^((m & 31) / 32) 2^f with
+// |f| <= 1 / 64, from a table of 2^(j / 32) and the Taylor series of e^(f ln 2) up to its sixth power. That
+// one (2^-48.7 at most) is economized: with t = 64 f and Chebyshev's T6, t^6 is (48 t^4 - 18 t^2 + 1 + T6(t)) / 32,
+// so all but 2^-52.7 of it goes into the coefficients of the fourth power and the second, for no
+// instruction. Adding 1.5 * 2^52 rounds to an integer and leaves it in the low word. The table is
 // 256 bytes of LDS, every bank once, so that its reads never wait for one another (128
 // entries, with a shorter series, took twice as long), and -m is the element's bin below.
 constexpr int kPowers = 32;
@@ -116,10 +118,10 @@ struct Weight {
     const u64 p = powers[*m & (kPowers - 1)];
     const int hi = static_cast<int>(p >> 32) + (((*m >> 5) + up) << 20);
     *power = __longlong_as_double(static_cast<long long>((static_cast<u64>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(p)));
-    constexpr double c = 0.69314718055994530942;
-    double e = fma(f, c * c * c * c * c / 120.0, c * c * c * c / 24.0);
+    constexpr double c = 0.69314718055994530942, sixth = c * c * c * c * c * c / 720.0;
+    double e = fma(f, c * c * c * c * c / 120.0, c * c * c * c / 24.0 + sixth * (48.0 / 32.0 / (64.0 * 64.0)));
     e = fma(e, f, c * c * c / 6.0);
-    e = fma(e, f, c * c / 2.0);
+    e = fma(e, f, c * c / 2.0 - sixth * (18.0 / 32.0 / (64.0 * 64.0 * 64.0 * 64.0)));
     e = fma(e, f, c);
     return fma(e, f, 1.0);
   }
