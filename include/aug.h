@@ -487,7 +487,9 @@ typedef enum { AUG_STEP_OK = 0, AUG_STEP_NO_BLOCKS = 1, AUG_STEP_INVALID = 2 } a
  *                   the request for its row j
  *   seen[row]       bit j: row j of the request is the row itself or an ancestor
  *   scratch         AUG_STEP_SCRATCH_BYTES, zero before the first call; a call leaves it
- *                   zero. Calls that overlap need one each */
+ *                   zero. Calls that overlap need one each
+ * ctx_len may be kv_len (a decode's next context is this step's length, 0 if it was refused). No other
+ * array that is only read overlaps one that is written, and those overlap nothing. */
 #define AUG_STEP_SCRATCH_BYTES 16
 typedef struct {
   int32_t num_reqs;
@@ -527,8 +529,8 @@ typedef struct {
  * Entries of block_table beyond a request's blocks, places of free_ids above its top
  * and rows behind the last are left as they were, except that blocks which came back
  * stand above the top where they were taken again at once. One launch (none for no requests).
- * Errors: AUG_ERR_INVALID (NULL pointers, sizes), AUG_ERR_UNSUPPORTED (more requests or
- * blocks), AUG_ERR_HIP (launch). */
+ * Errors: AUG_ERR_INVALID (NULL pointers, sizes, an array that is read overlaps one that is
+ * written), AUG_ERR_UNSUPPORTED (more requests or blocks), AUG_ERR_HIP (launch). */
 aug_status aug_step_tables(const aug_step_tables_args* args, void* stream);
 
 /* Rotary positions. Pair i of the first rotary_dim dims of a head, (x, y), becomes

@@ -11,8 +11,8 @@
 // One launch: every workgroup makes all sums for itself (12 bytes a request, from L2) and
 // then takes its share of the blocks that come back, of those that are taken, and of the
 // rows; whose a block or row is, is looked up in the sums. What the sums were made from
-// (held, free_count) is overwritten by the workgroup that finishes last, when all
-// others have read it.
+// (held, free_count, and kv_len, which may be the array of context lengths) is overwritten by the
+// workgroup that finishes last, when all others have read it.
 //
 // Bound by the chain of loads: lengths, sums, table or stack, stores. 64 requests of 8 drafts:
 // 6.1 us; 2000 of up to 32, 11.3 (with a workgroup a request, its rows behind its blocks: 42).
@@ -196,7 +196,6 @@ __global__ __launch_bounds__(THREADS) void tables_kernel(aug_step_tables_args a)
     const Request q = load_request(a, r);
     const aug_step_state st = outcome(r, q);
     a.q_start[r] = static_cast<int32_t>(start[r]);
-    a.kv_len[r] = st == AUG_STEP_OK ? q.ctx + q.rows : 0;
     a.state[r] = st;
   }
   if (thread == 0) a.q_start[n] = rows_total;
@@ -259,7 +258,9 @@ __global__ __launch_bounds__(THREADS) void tables_kernel(aug_step_tables_args a)
   if (!last) return;
   for (int r = tid; r < n; r += THREADS) {
     const Request q = load_request(a, r);
-    if (outcome(r, q) == AUG_STEP_OK) a.held[r] = q.need;
+    const bool ok = outcome(r, q) == AUG_STEP_OK;
+    a.kv_len[r] = ok ? q.ctx + q.rows : 0;
+    if (ok) a.held[r] = q.need;
   }
   if (tid == 0) *a.free_count = static_cast<int32_t>(avail - taken);
 }
@@ -271,6 +272,17 @@ void launch(const aug_step_tables_args& t, hipStream_t st) {
   const int64_t groups = (threads + THREADS - 1) / THREADS;
   const uint32_t lds = (3u * t.num_reqs + 1) * sizeof(uint32_t);
   hipLaunchKernelGGL((tables_kernel<THREADS>), dim3(static_cast<uint32_t>(groups < 256 ? groups : 256)), dim3(THREADS), lds, st, t);
+}
+
+// An array of the call, in bytes.
+struct Span {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(const Span& x, const Span& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return a && b && a < b + static_cast<uint64_t>(y.bytes) && b < a + static_cast<uint64_t>(x.bytes);
 }
 
 }  // namespace
@@ -295,6 +307,18 @@ extern "C" aug_status aug_step_tables(const aug_step_tables_args* t, void* strea
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   if (t->max_rows > 0 && (!t->positions || !t->slots || (t->max_draft > 0 && !t->seen)))
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
+  const int64_t reqs = t->num_reqs, rows = t->max_rows;
+  const Span read[] = {{"ctx_len", t->ctx_len, 4 * reqs}, {"q_len", t->q_len, 4 * reqs}, {"parents", t->parents, 4 * rows}};
+  const Span written[] = {{"block_table", t->block_table, 4 * reqs * t->max_blocks}, {"held", t->held, 4 * reqs},
+                          {"free_ids", t->free_ids, int64_t{4} * t->num_pool_blocks}, {"free_count", t->free_count, 4},
+                          {"q_start", t->q_start, 4 * (reqs + 1)}, {"kv_len", t->kv_len, 4 * reqs}, {"state", t->state, 4 * reqs},
+                          {"positions", t->positions, 4 * rows}, {"slots", t->slots, 8 * rows}, {"seen", t->seen, 8 * rows},
+                          {"scratch", t->scratch, AUG_STEP_SCRATCH_BYTES}};
+  for (const Span& r : read)
+    for (const Span& w : written) {
+      const bool same = &r == read && w.p == t->kv_len && r.p == w.p;      // kv_len is written behind the last read
+      if (overlap(r, w) && !same) return aug::fail(AUG_ERR_INVALID, "%s: %s overlaps %s", who, r.name, w.name);
+    }
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (t->num_reqs <= kFew) launch<kFew / kEach>(*t, st);
   else launch<AUG_STEP_MAX_REQS / kEach>(*t, st);

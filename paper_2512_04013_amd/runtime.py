@@ -251,7 +251,9 @@ class StepTables:
         tokens in the cache (int32 [max_reqs]); ``parents`` (int32 [max_rows]): the row of
         the same request that each draft follows, -1 for a root; None: every row follows
         the one before. Blocks that requests no longer need are free again, new ones are
-        taken. ``state`` says which requests were refused."""
+        taken. ``state`` says which requests were refused. ``ctx_len`` may be the tables' own
+        ``kv_len`` (plain decoding: 0 for a request that was refused, whose blocks then come
+        back); otherwise what is given here overlaps none of the tables."""
         index = self._index
         _check_vector(ctx_len, "ctx_len", self.max_reqs, torch.int32, index)
         _check_vector(q_len, "q_len", self.max_reqs, torch.int32, index)
