@@ -46,7 +46,9 @@ def _allocating_on(stream, device):
 
 def _on(index: int):
     """Context in which ``index`` is torch's current device: the library's calls
-    are made for the current one."""
+    are made for the current one. Host memory (-1) is refused: no kernel reads it."""
+    if index < 0:
+        raise ValueError("tensors in host memory: this call needs them on a GPU")
     return contextlib.nullcontext() if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
