@@ -477,8 +477,11 @@ def aug_rope_init(rotary_dim: int, interleaved: bool = False, base: float = 1000
 
 
 def _rows_arg(t):
-    """Address and row stride (elements) of rows [rows][heads][dim] whose heads lie together."""
-    return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+    """Address and row stride (elements) of rows [rows][heads][dim] whose heads lie together. One row
+    has no next one, whatever its tensor's stride says (a transposed view has a head's)."""
+    if t is None:
+        return None, 0
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
 def aug_rope_rows(shape: aug_attn_shape, rope: aug_rope, positions, q, k, q_out, k_out, stream=None):
