@@ -644,8 +644,8 @@ aug_status aug_tree_plan_size(const aug_attn_shape* shape, const aug_tree_batch*
 aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batch, void* plan_dev, size_t plan_bytes,
                          void* stream);
 
-/* The attention of a planned step (a plan of other heads, or of a shape that takes the columns
- * otherwise, counts as empty: nothing is written). Device memory: q and out [max_rows][num_q_heads]
+/* The attention of a planned step (a plan of other heads, of a shape that takes the columns
+ * otherwise, or of a batch of other sizes counts as empty: nothing is written). Device memory: q and out [max_rows][num_q_heads]
  * [head_dim], of which rows from q_start[num_reqs] on, and those of a request beyond
  * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out too);
  * workspace 16-byte aligned, its contents do not matter. The caches' tokens 0 .. kv_len - 1

@@ -50,8 +50,10 @@ constexpr int kPlanThreads = 1024;
 struct TreeHeader {                    // 64 bytes
   int32_t num_items;
   int32_t num_groups;
-  int32_t hkv, group, tiles;           // what it was made for
-  int32_t reserved[11];
+  int32_t hkv, group, tiles;           // what it was made for: heads,
+  int32_t max_rows, max_blocks;        // and the batch
+  int32_t reqs_drafts;                 // num_reqs and 2^16 max_draft
+  int32_t reserved[8];
 };
 struct TreeItem {                      // 32 bytes
   int32_t req;
@@ -72,6 +74,9 @@ struct TreeGroup {                     // 32 bytes: one item's columns over all 
   int32_t reserved[3];
 };
 static_assert(sizeof(TreeHeader) == 64 && sizeof(TreeItem) == 32 && sizeof(TreeGroup) == 32, "plan layout");
+
+// num_reqs is up to 4096 and max_draft up to 64.
+__host__ __device__ constexpr int32_t reqs_drafts_of(int num_reqs, int max_draft) { return num_reqs | (max_draft << 16); }
 
 // What follows from a shape and the limits of a batch, on the host.
 struct TreeSizes {
@@ -237,7 +242,9 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreePlanArgs a)
     part += s > 1 ? columns * q.wide * s : 0;
     group += s > 1 ? columns : 0;
   }
-  if (tid == 0) *reinterpret_cast<TreeHeader*>(a.plan) = TreeHeader{num_items, num_groups, a.hkv, a.group, a.tiles, {}};
+  if (tid == 0)
+    *reinterpret_cast<TreeHeader*>(a.plan) = TreeHeader{num_items,  num_groups,   a.hkv, a.group, a.tiles,
+                                                        a.max_rows, a.max_blocks, reqs_drafts_of(n, a.max_draft), {}};
   __syncthreads();
   TreeItem* out = reinterpret_cast<TreeItem*>(a.plan + sizeof(TreeHeader));
   TreeGroup* group_out = reinterpret_cast<TreeGroup*>(out + a.items);
@@ -286,6 +293,7 @@ struct TreeArgs {
   float* partials;
   int64_t items;
   int32_t max_blocks, num_pool_blocks, hq, hkv;
+  int32_t max_rows, reqs_drafts;
   int32_t group_log2;
   int32_t max_groups, merge_tiles;     // tiles of a group, at most
   float scale_log2;
@@ -469,12 +477,13 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, const TreeItem& it,
   }
 }
 
-// Items and groups of the plan; none where it was made for other heads or tiles, whose items lie
-// outside this launch's arrays.
+// Items and groups of the plan; none where it was made for other heads, tiles or sizes of the batch, whose
+// items lie outside this launch's arrays.
 __device__ __forceinline__ int2 tree_counts(const TreeArgs& a, int tiles) {
   typedef int32_t words_t __attribute__((ext_vector_type(8)));
   const words_t h = load_uniform(reinterpret_cast<const words_t*>(a.plan));
-  const bool mine = h[2] == a.hkv && h[3] == 1 << a.group_log2 && h[4] == tiles;
+  const bool mine = h[2] == a.hkv && h[3] == 1 << a.group_log2 && h[4] == tiles && h[5] == a.max_rows && h[6] == a.max_blocks &&
+                    h[7] == a.reqs_drafts;
   return mine ? int2{h[0], h[1]} : int2{0, 0};
 }
 
@@ -1039,6 +1048,8 @@ extern "C" aug_status aug_attn_tree(const aug_attn_shape* s, const aug_tree_batc
   a.merge_tiles = z.merge_tiles;
   a.max_groups = static_cast<int32_t>(z.groups);
   a.max_blocks = b->max_blocks;
+  a.max_rows = b->max_rows;
+  a.reqs_drafts = reqs_drafts_of(b->num_reqs, b->max_draft);
   a.num_pool_blocks = num_pool_blocks;
   a.hq = s->num_q_heads;
   a.hkv = s->num_kv_heads;

@@ -268,6 +268,9 @@ class StepTables:
             aug_step_tables(a, stream=_current_stream(index) if stream is None else stream)
 
 
+_PLAN_HEADER_BYTES = 64
+
+
 class TreeAttention:
     """Attention of a step's drafts over a paged cache, from ``StepTables``: ``plan``
     once a step, ``run`` once a layer. Its work list, workspace and output belong to it:
@@ -288,6 +291,7 @@ class TreeAttention:
                                      t.block_table.data_ptr(), t.seen.data_ptr())
         plan_bytes, workspace_bytes = aug_tree_plan_size(shape, self._batch)
         self.plan_dev = torch.empty(plan_bytes, dtype=torch.uint8, device=t.device)
+        self.plan_dev[:_PLAN_HEADER_BYTES].zero_()       # an empty plan, where plan() has only been captured so far
         self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=t.device)
         self._rows = (t.max_rows, shape.num_q_heads, shape.head_dim)
         self._dtype = torch.float32 if shape.q_dtype == AUG_F32 else torch.bfloat16
