@@ -593,10 +593,12 @@ aug_status aug_rope_rows(const aug_attn_shape* shape, const aug_rope* rope, cons
  * follows. rope NULL: nothing is rotated (positions and q are NULL): an append by slots,
  * which with aug_kv_read also moves rows within a cache, as after drafts that were not accepted.
  * Caches, scales, rounding and encodings as for aug_kv_append, from the rotated float32
- * values (rounded once). The slots of one call are distinct. fp8 caches: rows that
- * follow one another in the call and in a block (each slot one more than the one before)
- * share the growth of its scale, from the scale's old value unless the first of them is slot 0;
- * the rows of one block must follow one another. Strides and alignment as for aug_rope_rows;
+ * values (rounded once). The slots of one call are distinct. fp8 caches: the rows of one
+ * block must follow one another in the call, in any order of slots (rows of slots outside
+ * the pool may stand between), and share the growth of its scale: from its old value, or where slot 0
+ * is among them anew, which ends whatever else the block held. Where the scale grows, the codes
+ * of the other slots below the highest of these are encoded anew; those of the slots above it stay
+ * as they are, since later tokens than the new ones count as gone. Strides and alignment as for aug_rope_rows;
  * q_out may be q, and nothing else overlaps. live_rows (device, or NULL): how many of the rows
  * there are, the others are passed over: a captured step passes its largest number of rows and
  * q_start + num_reqs of aug_step_tables, since the slots behind a step's last row are those of

@@ -133,7 +133,8 @@ class PagedKV:
         ``positions`` (int32) where a ``rope`` is given. With ``q`` its rows are
         rotated too, into ``q_out`` (may be ``q``; allocated on ``stream`` if None),
         which is returned. Without a rope and with what ``read`` returns, rows move
-        to other slots. ``live_rows`` (int32 [1], such as ``StepTables.live_rows``): how
+        to other slots. In an fp8 pool, whose blocks share a scale, the rows of a block
+        follow one another, and what its slots above them held is lost. ``live_rows`` (int32 [1], such as ``StepTables.live_rows``): how
         many of the rows there are; those behind are passed over."""
         n, (hkv, dim), index = len(slots), self._row, self._device
         _check_vector(slots, "slots", n, torch.int64, index)
