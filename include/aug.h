@@ -676,7 +676,8 @@ aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batc
  * and with it exceeds uniform[r] (in [0, 1)) times their whole sum. temperature 0 (below, or NaN): the
  * first token of the order. A row without a logit above -infinity gives -1.
  * Arrays are device memory, one entry a row; temperature, top_k, top_p and min_p may be
- * NULL: 1 and all. probs (may be NULL) receives the token's share of what is kept.
+ * NULL: 1 and all. probs (may be NULL) receives the token's share of what is kept. tokens and
+ * probs overlap neither each other nor what is read.
  *
  * Which side of a border a number falls on decides tokens, so weights are computed in
  * float64 (off by less than 2^-51) and summed exactly as integers, multiples of 2^-s with s = min(51, 62 -
@@ -699,7 +700,7 @@ typedef struct {
 } aug_sample_args;
 
 /* One launch (none for no rows); no workspace.
- * Errors: AUG_ERR_INVALID (NULL or misaligned pointers, sizes, dtype, reserved),
+ * Errors: AUG_ERR_INVALID (NULL or misaligned pointers, sizes, dtype, reserved, overlaps),
  * AUG_ERR_UNSUPPORTED (vocab above 2^20), AUG_ERR_HIP (launch). */
 aug_status aug_sample(const aug_sample_args* args, void* stream);
 

@@ -37,6 +37,7 @@
 #include <utility>
 
 #include "aug.h"
+#include "checks.h"
 #include "status.h"
 
 namespace {
@@ -1065,6 +1066,16 @@ extern "C" aug_status aug_sample(const aug_sample_args* g, void* stream) {
   if (!g->logits || !g->uniform || !g->tokens) return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   if (reinterpret_cast<uintptr_t>(g->logits) & (g->dtype == AUG_F32 ? 3 : 1))
     return aug::fail(AUG_ERR_INVALID, "%s: logits must be aligned to their elements", who);
+  // (a row's workgroup reads other rows' settings, and runs beside those that write)
+  const int64_t n = g->rows, eb = g->dtype == AUG_F32 ? 4 : 2, most = int64_t{1} << 58;
+  const int64_t reach = n - 1 <= most / g->stride ? (n - 1) * g->stride + g->vocab : most;
+  const aug::Span read[] = {{"logits", g->logits, reach * eb}, {"uniform", g->uniform, 4 * n}, {"temperature", g->temperature, 4 * n},
+                            {"top_k", g->top_k, 4 * n}, {"top_p", g->top_p, 4 * n}, {"min_p", g->min_p, 4 * n}};
+  const aug::Span tokens{"tokens", g->tokens, 4 * n}, probs{"probs", g->probs, 4 * n};
+  if (aug::overlap(tokens, probs)) return aug::fail(AUG_ERR_INVALID, "%s: tokens overlap probs", who);
+  for (const aug::Span& r : read)
+    if (aug::overlap(r, tokens) || aug::overlap(r, probs))
+      return aug::fail(AUG_ERR_INVALID, "%s: tokens or probs overlap %s", who, r.name);
   int bits = 0;
   while ((1 << bits) < g->vocab) ++bits;
   const Rows a{g->logits, g->stride, g->vocab, 62 - bits < 51 ? 62 - bits : 51, g->uniform, g->temperature, g->top_k, g->top_p,

@@ -22,6 +22,7 @@
 #include <cstdint>
 
 #include "aug.h"
+#include "checks.h"
 #include "plan_format.h"
 #include "status.h"
 
@@ -274,17 +275,6 @@ void launch(const aug_step_tables_args& t, hipStream_t st) {
   hipLaunchKernelGGL((tables_kernel<THREADS>), dim3(static_cast<uint32_t>(groups < 256 ? groups : 256)), dim3(THREADS), lds, st, t);
 }
 
-// An array of the call, in bytes.
-struct Span {
-  const char* name;
-  const void* p;
-  int64_t bytes;
-};
-bool overlap(const Span& x, const Span& y) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
-  return a && b && a < b + static_cast<uint64_t>(y.bytes) && b < a + static_cast<uint64_t>(x.bytes);
-}
-
 }  // namespace
 
 extern "C" aug_status aug_step_tables(const aug_step_tables_args* t, void* stream) {
@@ -308,16 +298,16 @@ extern "C" aug_status aug_step_tables(const aug_step_tables_args* t, void* strea
   if (t->max_rows > 0 && (!t->positions || !t->slots || (t->max_draft > 0 && !t->seen)))
     return aug::fail(AUG_ERR_INVALID, "%s: NULL device pointer", who);
   const int64_t reqs = t->num_reqs, rows = t->max_rows;
-  const Span read[] = {{"ctx_len", t->ctx_len, 4 * reqs}, {"q_len", t->q_len, 4 * reqs}, {"parents", t->parents, 4 * rows}};
-  const Span written[] = {{"block_table", t->block_table, 4 * reqs * t->max_blocks}, {"held", t->held, 4 * reqs},
+  const aug::Span read[] = {{"ctx_len", t->ctx_len, 4 * reqs}, {"q_len", t->q_len, 4 * reqs}, {"parents", t->parents, 4 * rows}};
+  const aug::Span written[] = {{"block_table", t->block_table, 4 * reqs * t->max_blocks}, {"held", t->held, 4 * reqs},
                           {"free_ids", t->free_ids, int64_t{4} * t->num_pool_blocks}, {"free_count", t->free_count, 4},
                           {"q_start", t->q_start, 4 * (reqs + 1)}, {"kv_len", t->kv_len, 4 * reqs}, {"state", t->state, 4 * reqs},
                           {"positions", t->positions, 4 * rows}, {"slots", t->slots, 8 * rows}, {"seen", t->seen, 8 * rows},
                           {"scratch", t->scratch, AUG_STEP_SCRATCH_BYTES}};
-  for (const Span& r : read)
-    for (const Span& w : written) {
+  for (const aug::Span& r : read)
+    for (const aug::Span& w : written) {
       const bool same = &r == read && w.p == t->kv_len && r.p == w.p;      // kv_len is written behind the last read
-      if (overlap(r, w) && !same) return aug::fail(AUG_ERR_INVALID, "%s: %s overlaps %s", who, r.name, w.name);
+      if (aug::overlap(r, w) && !same) return aug::fail(AUG_ERR_INVALID, "%s: %s overlaps %s", who, r.name, w.name);
     }
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (t->num_reqs <= kFew) launch<kFew / kEach>(*t, st);
