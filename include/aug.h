@@ -649,7 +649,8 @@ aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batc
 /* The attention of a planned step (a plan of other heads, of a shape that takes the columns
  * otherwise, or of a batch of other sizes counts as empty: nothing is written). Device memory: q and out [max_rows][num_q_heads]
  * [head_dim], of which rows from q_start[num_reqs] on, and those of a request beyond
- * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out too);
+ * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out too); out may
+ * be q, and overlaps nothing else;
  * workspace 16-byte aligned, its contents do not matter. The caches' tokens 0 .. kv_len - 1
  * of a request are finite where some row of it sees them; anything may stand elsewhere. Keys of
  * block ids outside the pool count for nothing. Sums and softmax statistics are fp32;
@@ -658,7 +659,7 @@ aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batc
  * Two launches, one where max_blocks are too few for any request to be split (none for no
  * requests or rows).
  * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers,
- * missing scales), AUG_ERR_NO_SPACE (workspace_bytes), AUG_ERR_HIP (launch). */
+ * missing scales, q and out that overlap in part), AUG_ERR_NO_SPACE (workspace_bytes), AUG_ERR_HIP (launch). */
 aug_status aug_attn_tree(const aug_attn_shape* shape, const aug_tree_batch* batch, const void* plan_dev, const void* q,
                          const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                          int32_t num_pool_blocks, void* out, void* workspace, size_t workspace_bytes, void* stream);

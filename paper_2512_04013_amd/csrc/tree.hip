@@ -1033,6 +1033,10 @@ extern "C" aug_status aug_attn_tree(const aug_attn_shape* s, const aug_tree_batc
     return aug::fail(AUG_ERR_INVALID, "%s: plan, rows, caches and workspace must be 16-byte aligned", who);
   if (!workspace || workspace_bytes < static_cast<size_t>(z.workspace_bytes))
     return aug::fail(AUG_ERR_NO_SPACE, "%s: workspace %zu < %lld bytes", who, workspace_bytes, (long long)z.workspace_bytes);
+  // out may be q: a column's queries are read by the one item that has it, or by its spans, before it is written
+  const int64_t bytes = static_cast<int64_t>(b->max_rows) * s->num_q_heads * s->head_dim * (s->q_dtype == AUG_F32 ? 4 : 2);
+  if (q != out && aug::overlap({"q", q, bytes}, {"out", out, bytes}))
+    return aug::fail(AUG_ERR_INVALID, "%s: q and out overlap and are not the same", who);
   TreeArgs a{};
   a.plan = static_cast<const char*>(plan_dev);
   a.q = q;

@@ -312,7 +312,7 @@ class TreeAttention:
 
     def run(self, q: torch.Tensor, out: torch.Tensor = None, stream=None, kv: PagedKV = None):
         """Enqueue the attention of ``q`` ([max_rows][H_q][D], contiguous) into ``out``
-        (the object's own by default), over ``kv`` (another layer's pool of the same
+        (the object's own by default; ``q`` itself will do), over ``kv`` (another layer's pool of the same
         size, or the planned one). Rows that see no key become zeros; rows behind the
         step's last are left as they were."""
         kv = self.kv if kv is None else kv
