@@ -654,8 +654,8 @@ aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batc
  * workspace 16-byte aligned, its contents do not matter. The caches' tokens 0 .. kv_len - 1
  * of a request are finite where some row of it sees them; anything may stand elsewhere. Keys of
  * block ids outside the pool count for nothing. Sums and softmax statistics are fp32;
- * over every cache but F32 each probability is taken as bf16 (off by at most 2^-8 of it, in the row's sum as
- * in its products). Calls that overlap need a workspace each; equal inputs give equal bits.
+ * over bf16 caches each probability is multiplied to 16 bits (off by at most 2^-16 of it), over fp8 and
+ * MXFP4 caches it is taken as bf16 (at most 2^-8, in the row's sum as in its products). Calls that overlap need a workspace each; equal inputs give equal bits.
  * Two launches, one where max_blocks are too few for any request to be split (none for no
  * requests or rows).
  * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers,

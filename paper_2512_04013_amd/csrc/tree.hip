@@ -522,6 +522,7 @@ __global__ __launch_bounds__(kThreads, T == 4 || (KVT == KV_BF16 && D == 128) ? 
   using KV = TreeKv<KVT, D>;
   constexpr int KS = D / 32, NB = D / 16;
   constexpr bool FP8 = KVT == KV_FP8;
+  constexpr bool PAIRS = KVT == KV_BF16;               // probabilities as two bf16
   constexpr int kQuery = 8 * KS * 64;                  // 16-byte query operands
   constexpr int kLds = kQuery * 16 > tree_merge_floats(D) * 4 ? kQuery * 16 : tree_merge_floats(D) * 4;
   __shared__ __align__(16) char lds[kLds];
@@ -689,16 +690,32 @@ __global__ __launch_bounds__(kThreads, T == 4 || (KVT == KV_BF16 && D == 128) ? 
 #pragma unroll
         for (int r = 0; r < 8; ++r) sacc[t][r >> 2][r & 3] = (hidden >> (8 * t + r)) & 1 ? 0.f : sacc[t][r >> 2][r & 3];
     }
-    bf16x8_t pop[N];
+    // Probabilities become operands. Over bf16 caches each is two bf16, the second what the first leaves (2^-16 together):
+    // the results' own rounding is then all that shows, and its products hide behind the loads (64 requests of 8 drafts,
+    // 183 us with and without; 8 of 64 drafts, 64/8 heads, 1218 for 1202; at most, 16 of 64 drafts with heads of 64, 181
+    // for 159). Over codes, which are off by 2^-4 and more themselves, each is one (2^-8): two take 282 us for 258 (fp8)
+    // and 403 for 279 (4 bits).
+    bf16x8_t pop[N], rest[N];
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       uint32_t pp[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) pp[r] = pack_bf16(sacc[t][r >> 1][2 * (r & 1)], sacc[t][r >> 1][2 * (r & 1) + 1]);
-      // exactly the packed probabilities
-      const float s0 = dot2_bf16(pp[1], kBf16PairOne, dot2_bf16(pp[0], kBf16PairOne, 0.f));
-      const float s1 = dot2_bf16(pp[3], kBf16PairOne, dot2_bf16(pp[2], kBf16PairOne, 0.f));
-      l_run[t] = FP8 ? fmaf(s0, vinv[0], fmaf(s1, vinv[1], l_run[t])) : l_run[t] + (s0 + s1);
+      if constexpr (PAIRS) {
+        uint32_t w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          w[r] = pack_bf16(sacc[t][r >> 1][2 * (r & 1)] - __uint_as_float(pp[r] << 16),
+                           sacc[t][r >> 1][2 * (r & 1) + 1] - __uint_as_float(pp[r] & 0xFFFF0000u));
+        rest[t] = as_bf16x8(uint4{w[0], w[1], w[2], w[3]});
+        l_run[t] += ((sacc[t][0][0] + sacc[t][0][1]) + (sacc[t][0][2] + sacc[t][0][3])) +
+                    ((sacc[t][1][0] + sacc[t][1][1]) + (sacc[t][1][2] + sacc[t][1][3]));
+      } else {
+        // exactly the packed probabilities
+        const float s0 = dot2_bf16(pp[1], kBf16PairOne, dot2_bf16(pp[0], kBf16PairOne, 0.f));
+        const float s1 = dot2_bf16(pp[3], kBf16PairOne, dot2_bf16(pp[2], kBf16PairOne, 0.f));
+        l_run[t] = FP8 ? fmaf(s0, vinv[0], fmaf(s1, vinv[1], l_run[t])) : l_run[t] + (s0 + s1);
+      }
       pop[t] = as_bf16x8(uint4{pp[0], pp[1], pp[2], pp[3]});
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -710,6 +727,10 @@ __global__ __launch_bounds__(kThreads, T == 4 || (KVT == KV_BF16 && D == 128) ? 
       for (int t = 0; t < N; ++t) {
         oacc[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pop[t], oacc[t][2 * i], 0, 0, 0);
         oacc[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), pop[t], oacc[t][2 * i + 1], 0, 0, 0);
+        if constexpr (PAIRS) {
+          oacc[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), rest[t], oacc[t][2 * i], 0, 0, 0);
+          oacc[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), rest[t], oacc[t][2 * i + 1], 0, 0, 0);
+        }
       }
     }
     __builtin_amdgcn_sched_barrier(0);
