@@ -647,15 +647,16 @@ aug_status aug_tree_plan(const aug_attn_shape* shape, const aug_tree_batch* batc
                          void* stream);
 
 /* The attention of a planned step (a plan of other heads, of a shape that takes the columns
- * otherwise, or of a batch of other sizes counts as empty: nothing is written). Device memory: q and out [max_rows][num_q_heads]
- * [head_dim], of which rows from q_start[num_reqs] on, and those of a request beyond
- * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out too); out may
- * be q, and overlaps nothing else;
+ * otherwise, or of a batch of other sizes counts as empty: nothing is written). Device memory: q and out
+ * [max_rows][num_q_heads][head_dim], of which rows from q_start[num_reqs] on, and those of a request beyond
+ * max_draft, are left alone; caches and scales as for aug_attn_mixed, 16-byte aligned (q and out
+ * too); out may be q, and overlaps nothing else;
  * workspace 16-byte aligned, its contents do not matter. The caches' tokens 0 .. kv_len - 1
  * of a request are finite where some row of it sees them; anything may stand elsewhere. Keys of
  * block ids outside the pool count for nothing. Sums and softmax statistics are fp32;
- * over bf16 caches each probability is multiplied to 16 bits (off by at most 2^-16 of it), over fp8 and
- * MXFP4 caches it is taken as bf16 (at most 2^-8, in the row's sum as in its products). Calls that overlap need a workspace each; equal inputs give equal bits.
+ * over bf16 caches each probability is multiplied to 16 bits (off by at most 2^-16 of it), over
+ * fp8 and MXFP4 caches it is taken as bf16 (at most 2^-8, in the row's sum as in its products).
+ * Calls that overlap need a workspace each; equal inputs give equal bits.
  * Two launches, one where max_blocks are too few for any request to be split (none for no
  * requests or rows).
  * Errors: those of aug_tree_plan_size, AUG_ERR_INVALID (NULL or misaligned pointers,

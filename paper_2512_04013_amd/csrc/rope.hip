@@ -20,8 +20,8 @@
 // way at once, which leaves four waves a SIMD beside the fp8 part (four groups: 10 us more
 // below; rows and blocks in launches of their own, as much together). 8115 rows of 64/8
 // heads of 128 into an fp8 cache: 98 us, 316 MB; the rows alone take 57 us and the blocks 33,
-// as much instructions (angles, quotients, codes) as traffic. 1001 rows of 8 + 2 fp32 heads
-// in and out: 10 us.
+// as much instructions (angles, quotients, codes) as traffic; into a 4-bit cache 68 us, a bf16 one 75.
+// 4004 rows of 8 + 2 fp32 heads in and out: 10 us.
 
 #include <hip/hip_runtime.h>
 

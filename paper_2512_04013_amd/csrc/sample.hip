@@ -26,10 +26,11 @@
 //
 // One row of 32000 bf16 logits with top-k 50 and top-p: 10 us, of which reading the row is a
 // fifth and the rest barriers and LDS round trips one behind the other. 64 rows of 50257 fp32 with
-// top-p alone: 35 us, the time of the longest row: weights 31 of its 60 thousand cycles, the list
-// 15. 512 rows of 128000 bf16 with every setting: 103 us; rows with top-p alone and flat
-// logits take 230 thousand cycles, 175 of them for weights (40 vector instructions each, on one
-// compute unit), twice.
+// top-p alone: 31 to 47 us by the logits, the time of the longest row; 9 of them for the largest logit, 17 for
+// weights and the draw, as rows with a temperature alone need them (26 us), the rest for the list. 512 rows of
+// 128000 bf16 with every setting: 103 us, bound by rows without top-k and their weights (40 vector instructions
+// each, on one compute unit; a temperature alone 100 us, the largest logits 41). Digit by digit, 64 rows of 50257 take
+// from 126 us (a temperature of 2^41) to 497 (equal logits with top-p, whose sums meet in one bin).
 
 #include <hip/hip_runtime.h>
 
@@ -282,7 +283,7 @@ struct Row {
     times<4>([&](auto g) { top[g] = -INFINITY; });
     by_words([&](int, const uint4& u, auto part) { top[part] = largest(u, top[part]); });
     if (top[0] != top[0] || top[1] != top[1] || top[2] != top[2] || top[3] != top[3]) {
-      // NaN: all in one group, one by one
+      // NaN: all in one group, one by one (64 rows of 50257 with fifty each: 17 us, without 13)
       float t = -INFINITY;
 #pragma nounroll
       for (int turn = 0; turn < turns; ++turn) {
@@ -919,7 +920,8 @@ __device__ __forceinline__ Fast fast_draw(const Rows& a, int row, const R& in, c
 
 // The row of a workgroup. More rows than there are compute units start one after another, and those
 // that compute something for every element (no top-k) take up to five times as long as the others: they
-// go first (512 rows of 128000, a third of them such: 140 us in the order they come).
+// go first (512 rows of 128000, a third of them such: 140 us in the order they come). Each thread looks at one
+// row, so more than 1024 start as they come (1024 rows of 32000: 88 us, 1025: 93).
 __device__ __forceinline__ int row_of_block(const Rows& a, Lds& s) {
   const int b = blockIdx.x, rows = gridDim.x;
   if (rows <= 256 || rows > kThreads || !a.top_k) return b;

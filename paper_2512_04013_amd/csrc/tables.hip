@@ -15,7 +15,7 @@
 // workgroup that finishes last, when all others have read it.
 //
 // Bound by the chain of loads: lengths, sums, table or stack, stores. 64 requests of 8 drafts:
-// 6.1 us; 2000 of up to 32, 11.3 (with a workgroup a request, its rows behind its blocks: 42).
+// 6.3 us; 2000 of up to 32, 11.7 (with a workgroup a request, its rows behind its blocks: 42).
 
 #include <hip/hip_runtime.h>
 
